@@ -104,6 +104,7 @@ extern "C" {
 #define CORTEX_ST_BAD_LINEARIZATION 4 /* forward was handed an inconsistent linearization */
 #define CORTEX_ST_INPUT_RANGE 5      /* an input index outside [-1, rows of the input table) */
 #define CORTEX_ST_EPOCH_WRAP 6       /* the forward workspace has served 2^32 - 1 launches: zero it */
+#define CORTEX_ST_SEQ_OFFSETS 7      /* sequence offsets that do not rise from 0 to the token count */
 
 /* Cells (Sec. 7.1, Table "Models and datasets"). */
 #define CORTEX_TREE_RNN 0            /* h = tanh(W [h_l; h_r] + b); leaf h = x */
@@ -302,6 +303,172 @@ size_t cortex_dag_infer_workspace_bytes(int32_t N, int32_t K, int32_t H);
 int cortex_dag_infer(int32_t H, const int32_t *d_children, const cortex_lin_t *lin, const float *d_x,
                      const float *d_W, const float *d_U, const float *d_b, float *d_h, int32_t *d_status,
                      void *d_ws, size_t ws_bytes, void *stream);
+
+/* ---- sequences -------------------------------------------------------------
+ *
+ * Operators of a recurrent sequence model: the third kind of structure (Sec. 3
+ * names sequences, trees and DAGs) and what a model over sequences needs beside
+ * the recurrence.  They serve: a prompt form takes whole sequences, a step form
+ * one new token of every running sequence; there is no backward pass, as there
+ * is none for the tree cells.
+ *
+ * - The prompts of a batch are one flat array of num_tokens rows; sequence i is
+ *   rows [seq_offsets[i], seq_offsets[i+1]).  Offsets rise from 0 to num_tokens;
+ *   a sequence may have no token.  Others set CORTEX_ST_SEQ_OFFSETS.
+ * - The states of running sequences are rows of a pool; state_index[i] is
+ *   sequence i's row, -1 for none (it starts from zero and its state is not
+ *   kept), NULL for row i.  An index outside [-1, state_rows) sets
+ *   CORTEX_ST_INPUT_RANGE.  No two sequences of a call may share a row.
+ *   state_in NULL starts every sequence from zero, state_out NULL keeps no
+ *   state; the two may be the same array (an update in place).  A sequence
+ *   without a token copies its state (zeros if it has none).  Rows of the pool
+ *   that no sequence names are not written.
+ * - x, y and their like are rows of a fixed stride: the _ld members count
+ *   elements and are at least the row's length, so the columns of a packed
+ *   projection are passed as they are.  Any stride and alignment (of the
+ *   element type) is accepted; rows that start at 16-byte boundaries take
+ *   wider loads.  Outputs overlap no input.
+ * - dtype is the type of activations (and of the convolution's state, which
+ *   holds inputs).  Weights, decays and scan states are float32, and all sums
+ *   are float32 whatever the type, rounded to nearest even once at the store.
+ * - A call with nothing to do (no sequence) enqueues nothing and returns
+ *   CORTEX_OK.  Results are deterministic.
+ */
+#define CORTEX_F32 0
+#define CORTEX_BF16 1
+
+/*
+ * Causal depthwise convolution over time, width W = 2..4:
+ *   y[t, c] = act(bias[c] + sum_k weight[c, k] x[t - W + 1 + k, c])
+ * within a sequence; the W - 1 inputs before its first token come from its
+ * state (zeros without one).  The state is the last W - 1 inputs, oldest first.
+ */
+typedef struct {
+  int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16 */
+  int32_t num_seqs;           /* S */
+  int32_t num_tokens;         /* T; the step form takes one token per sequence: T = S */
+  int32_t channels;           /* C */
+  int32_t width;              /* W, 2..4 */
+  int32_t silu;               /* act(v) = v / (1 + exp(-v)) if non-zero, else v */
+  int32_t state_rows;         /* rows of the pools */
+  const int32_t *seq_offsets; /* [S+1] (not read by the step form) */
+  const int32_t *state_index; /* [S] or NULL */
+  const void *x;              /* [T, C], row stride x_ld */
+  int64_t x_ld;
+  const float *weight;        /* [C, W] */
+  const float *bias;          /* [C] or NULL */
+  const void *state_in;       /* [state_rows, W-1, C] of dtype, or NULL */
+  void *state_out;            /* likewise */
+  void *y;                    /* [T, C], row stride y_ld */
+  int64_t y_ld;
+} cortex_conv_t;
+
+int cortex_conv_forward(const cortex_conv_t *args, int32_t *d_status, void *stream);
+int cortex_conv_step(const cortex_conv_t *args, int32_t *d_status, void *stream);
+
+/*
+ * Selective state space scan.  Channel d of group g keeps a state h[d, 0..N-1]
+ * and at every token
+ *   dt = softplus(dt_raw + dt_bias)           (softplus only if asked for)
+ *   h[d, n] = exp(dt A) h[d, n] + dt x[d] B[g, n]
+ *   y[d]    = (sum_n C[g, n] h[d, n] + skip x[d]) * silu(z[d])
+ * Group g is channels [g D/G, (g+1) D/G).  Two layouts of the decays:
+ *   head_dim == 0   per channel: A [D, N], dt [T, D], skip and dt_bias [D];
+ *                   N = 8, 16, 32 or 64
+ *   head_dim = P    per head of P consecutive channels: A [D/P], dt [T, D/P],
+ *                   skip and dt_bias [D/P]; N = 16, 32, 64 or 128, P a multiple
+ *                   of 16 up to 256 that divides D/G
+ * Other sizes return CORTEX_E_INVAL, and so do states that do not start at a
+ * 16-byte boundary.
+ */
+typedef struct {
+  int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: x, z, dt, B, C, y */
+  int32_t num_seqs;           /* S */
+  int32_t num_tokens;         /* T; step form: T = S */
+  int32_t channels;           /* D */
+  int32_t head_dim;           /* P, or 0 for decays per channel */
+  int32_t groups;             /* G */
+  int32_t state_size;         /* N */
+  int32_t softplus;
+  int32_t state_rows;
+  const int32_t *seq_offsets; /* [S+1] (not read by the step form) */
+  const int32_t *state_index; /* [S] or NULL */
+  const void *x;              /* [T, D] */
+  const void *z;              /* [T, D] or NULL: no gate */
+  const void *dt;             /* [T, D] or [T, D/P] */
+  const void *B;              /* [T, G, N]: row stride B_ld, groups N apart */
+  const void *C;              /* likewise */
+  int64_t x_ld, z_ld, dt_ld, B_ld, C_ld;
+  const float *A;
+  const float *skip;          /* or NULL */
+  const float *dt_bias;       /* or NULL */
+  const float *state_in;      /* [state_rows, D, N] float32, or NULL */
+  float *state_out;           /* likewise */
+  void *y;                    /* [T, D] */
+  int64_t y_ld;
+} cortex_scan_t;
+
+/* Workspace bytes of cortex_scan_forward (0 if invalid); it need not be zeroed. */
+size_t cortex_scan_workspace_bytes(int32_t num_tokens, int32_t num_seqs, int32_t channels, int32_t state_size,
+                                   int32_t head_dim);
+int cortex_scan_forward(const cortex_scan_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream);
+int cortex_scan_step(const cortex_scan_t *args, int32_t *d_status, void *stream);
+
+/*
+ * The last layer's output made ready for the choice of the next token, for every
+ * row b over the vocabulary [0, V):
+ *   v = logits[b, i]
+ *   v = v > 0 ? v / repetition[b] : v * repetition[b]   if i is in the row's history
+ *   v = v - frequency[b] * n,  v = v - presence[b] if n > 0
+ *                              (n: how often i occurs in the history from prompt_len[b] on)
+ *   v = v + the row's bias for i                        (if i is listed twice: the later entry's)
+ *   v = -infinity unless the row's mask allows i
+ * in float32, each operation rounded on its own.
+ *   out     v, rounded to dtype; may be logits itself
+ *   token   the index of the largest v (before that rounding), the lowest of
+ *           equals; a NaN counts as the largest; -1 if every v is -infinity, as where
+ *           the mask leaves nothing
+ *   lse     log sum_i exp(v) (-infinity if every v is)
+ * Each output may be NULL.  A masked entry's logit is never used, whatever it
+ * holds.  A row of the mask is ceil(V / 32) words, bit i % 32 of word i / 32 set
+ * where i is allowed; mask_index[b] = -1 is a row without a mask.
+ * A token outside [0, V), a length outside [0, history_cap] (the prompt's: outside
+ * [0, the history's]), a mask index outside [-1, mask_rows) or bias offsets that
+ * do not rise from 0 to num_biases set CORTEX_ST_INPUT_RANGE.
+ */
+typedef struct {
+  int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: logits and out */
+  int32_t rows;               /* R */
+  int32_t vocab;              /* V */
+  int32_t history_cap;        /* columns of history that may be read */
+  int32_t num_biases;
+  int32_t mask_rows;
+  const void *logits;         /* [R, V], row stride logits_ld */
+  int64_t logits_ld;
+  const int32_t *history;     /* [R, history_cap], row stride history_ld, or NULL: none */
+  int64_t history_ld;
+  const int32_t *history_len; /* [R] */
+  const int32_t *prompt_len;  /* [R], or NULL: 0 */
+  const float *repetition;    /* [R], or NULL: 1 */
+  const float *frequency;     /* [R], or NULL: 0 */
+  const float *presence;      /* [R], or NULL: 0 */
+  const int32_t *bias_offsets; /* [R+1], or NULL: no biases */
+  const int32_t *bias_tokens; /* [num_biases] */
+  const float *bias_values;   /* [num_biases] */
+  const uint32_t *mask;       /* [mask_rows, ceil(V/32)], row stride mask_ld, or NULL: none */
+  int64_t mask_ld;
+  const int32_t *mask_index;  /* [R], or NULL: row b */
+  void *out;                  /* [R, V], row stride out_ld, or NULL */
+  int64_t out_ld;
+  int32_t *token;             /* [R] or NULL */
+  float *lse;                 /* [R] or NULL */
+} cortex_logits_t;
+
+/* Workspace bytes of cortex_logits_process (0 if invalid).  It must be zeroed
+ * before its first use, and again after a call that ended with a non-zero
+ * status; a call leaves it ready for the next of any size that fits it. */
+size_t cortex_logits_workspace_bytes(int32_t rows, int32_t vocab);
+int cortex_logits_process(const cortex_logits_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream);
 
 /* ---- tuning and diagnostics ---------------------------------------------- */
 

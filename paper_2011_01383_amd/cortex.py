@@ -31,6 +31,10 @@ CORTEX_ST_BARRIER_TIMEOUT = 3
 CORTEX_ST_BAD_LINEARIZATION = 4
 CORTEX_ST_INPUT_RANGE = 5
 CORTEX_ST_EPOCH_WRAP = 6
+CORTEX_ST_SEQ_OFFSETS = 7
+
+CORTEX_F32 = 0
+CORTEX_BF16 = 1
 
 CORTEX_TREE_RNN = 0
 CORTEX_NARY_TREELSTM = 1
@@ -61,6 +65,8 @@ EXPORTED = [
     "cortex_last_grid", "cortex_version",
     "cortex_probe_mfma_sink_floats", "cortex_probe_mfma_flops", "cortex_probe_mfma",
     "cortex_probe_levels_workspace_bytes", "cortex_probe_levels",
+    "cortex_conv_forward", "cortex_conv_step", "cortex_scan_workspace_bytes", "cortex_scan_forward",
+    "cortex_scan_step", "cortex_logits_workspace_bytes", "cortex_logits_process",
 ]
 
 
@@ -74,6 +80,33 @@ class cortex_lin_t(ctypes.Structure):
 class cortex_weights_t(ctypes.Structure):
     _fields_ = [("W", ctypes.c_void_p), ("U", ctypes.c_void_p), ("b", ctypes.c_void_p),
                 ("W_M", ctypes.c_void_p)]
+
+
+def _fields(text: str):
+    """(name, ctype) pairs from "i name ..." groups: i int32, l int64, p pointer."""
+    kinds = {"i": ctypes.c_int32, "l": ctypes.c_int64, "p": ctypes.c_void_p}
+    out = []
+    for group in text.split(";"):
+        kind, *names = group.split()
+        out += [(n, kinds[kind]) for n in names]
+    return out
+
+
+class cortex_conv_t(ctypes.Structure):
+    _fields_ = _fields("i dtype num_seqs num_tokens channels width silu state_rows; p seq_offsets state_index x; l x_ld;"
+                       "p weight bias state_in state_out y; l y_ld")
+
+
+class cortex_scan_t(ctypes.Structure):
+    _fields_ = _fields("i dtype num_seqs num_tokens channels head_dim groups state_size softplus state_rows;"
+                       "p seq_offsets state_index x z dt B C; l x_ld z_ld dt_ld B_ld C_ld;"
+                       "p A skip dt_bias state_in state_out y; l y_ld")
+
+
+class cortex_logits_t(ctypes.Structure):
+    _fields_ = _fields("i dtype rows vocab history_cap num_biases mask_rows; p logits; l logits_ld; p history;"
+                       "l history_ld; p history_len prompt_len repetition frequency presence bias_offsets bias_tokens"
+                       " bias_values mask; l mask_ld; p mask_index out; l out_ld; p token lse")
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -127,6 +160,20 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.cortex_probe_levels_workspace_bytes.restype = SZ
     lib.cortex_probe_levels.argtypes = [I32, I32, I32, P, P, SZ, P]
     lib.cortex_probe_levels.restype = ctypes.c_int
+    lib.cortex_conv_forward.argtypes = [ctypes.POINTER(cortex_conv_t), P, P]
+    lib.cortex_conv_forward.restype = ctypes.c_int
+    lib.cortex_conv_step.argtypes = [ctypes.POINTER(cortex_conv_t), P, P]
+    lib.cortex_conv_step.restype = ctypes.c_int
+    lib.cortex_scan_workspace_bytes.argtypes = [I32, I32, I32, I32, I32]
+    lib.cortex_scan_workspace_bytes.restype = SZ
+    lib.cortex_scan_forward.argtypes = [ctypes.POINTER(cortex_scan_t), P, P, SZ, P]
+    lib.cortex_scan_forward.restype = ctypes.c_int
+    lib.cortex_scan_step.argtypes = [ctypes.POINTER(cortex_scan_t), P, P]
+    lib.cortex_scan_step.restype = ctypes.c_int
+    lib.cortex_logits_workspace_bytes.argtypes = [I32, I32]
+    lib.cortex_logits_workspace_bytes.restype = SZ
+    lib.cortex_logits_process.argtypes = [ctypes.POINTER(cortex_logits_t), P, P, SZ, P]
+    lib.cortex_logits_process.restype = ctypes.c_int
     lib.cortex_version.argtypes = []
     lib.cortex_version.restype = ctypes.c_char_p
     _lib = lib
@@ -360,6 +407,235 @@ def cortex_probe_levels(mode: int, grid: int, levels: int, status: torch.Tensor,
     _need(ws, "ws", None, 1)
     return load().cortex_probe_levels(mode, grid, levels, _ptr(status), _ptr(ws), ws.numel() * ws.element_size(),
                                       _stream(stream))
+
+
+# ---- sequences ------------------------------------------------------------------
+
+_DTYPES = {torch.float32: CORTEX_F32, torch.bfloat16: CORTEX_BF16}
+
+
+def _rows(t, name: str, dtype, rows: int, cols: int) -> int:
+    """A [rows, cols] tensor whose rows are whole and may be apart (the columns
+    of a wider array): its row stride."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError("%s is required" % name if t is None else
+                         "%s must be a torch.Tensor, got %s" % (name, type(t).__name__))
+    if t.dtype != dtype:
+        raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError("%s must be [%d, %d], got %s" % (name, rows, cols, list(t.shape)))
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError("%s must have contiguous rows" % name)
+    if rows < 2:
+        ld = max(ld, cols)             # one row: its stride is never used
+    elif ld < cols:
+        raise ValueError("%s must have rows that do not overlap" % name)
+    return ld
+
+
+def _on_device(*pairs) -> None:
+    for t, name in pairs:
+        if t is not None and not t.is_cuda:
+            raise ValueError("%s must be in device memory" % name)
+
+
+def _shape2(t, name: str):
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError("%s must be a 2-dimensional torch.Tensor" % name)
+    if t.dtype not in _DTYPES:
+        raise ValueError("%s must be torch.float32 or torch.bfloat16, got %s" % (name, t.dtype))
+    return t.shape
+
+
+def _state_specs(state_in, state_out, state_index, S: int, dtype, tail: tuple):
+    """Rows of the state pools and what they have to hold."""
+    pools = [t for t in (state_in, state_out) if t is not None]
+    for t in pools:
+        if not isinstance(t, torch.Tensor) or t.dim() != 3 or tuple(t.shape[1:]) != tail or t.shape[0] != pools[0].shape[0]:
+            raise ValueError("state_in and state_out must be [rows, %d, %d], with the same rows" % tail)
+    rows = pools[0].shape[0] if pools else 0
+    if pools and state_index is None and rows < S:
+        raise ValueError("the states have %d rows, %d sequences need as many" % (rows, S))
+    n = rows * tail[0] * tail[1]
+    return rows, [(state_in, "state_in", dtype, n, True), (state_out, "state_out", dtype, n, True),
+                  (state_index, "state_index", torch.int32, S, True)]
+
+
+def _conv(step: bool, x, weight, offsets, y, bias, silu, state_in, state_out, state_index, status, stream) -> int:
+    T, C = _shape2(x, "x")
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 2 or weight.shape[0] != C:
+        raise ValueError("weight must be [%d, W]" % C)
+    W, f32, i32 = weight.shape[1], torch.float32, torch.int32
+    if step:
+        S = T
+        specs = []
+    else:
+        if not isinstance(offsets, torch.Tensor) or offsets.numel() < 1:
+            raise ValueError("offsets must be a torch.Tensor of S + 1 elements")
+        S = offsets.numel() - 1
+        specs = [(offsets, "offsets", i32, S + 1, False)]
+    rows, state = _state_specs(state_in, state_out, state_index, S, x.dtype, (W - 1, C))
+    x_ld, y_ld = _rows(x, "x", x.dtype, T, C), _rows(y, "y", x.dtype, T, C)
+    _need_all(specs + state + [(weight, "weight", f32, C * W, False), (bias, "bias", f32, C, True),
+                               (status, "status", i32, 1, False)])
+    _on_device((x, "x"), (y, "y"))
+    args = cortex_conv_t(_DTYPES[x.dtype], S, T, C, W, int(bool(silu)), rows, _ptr(offsets), _ptr(state_index), _ptr(x),
+                         x_ld, _ptr(weight), _ptr(bias), _ptr(state_in), _ptr(state_out), _ptr(y), y_ld)
+    lib = load()
+    call = lib.cortex_conv_step if step else lib.cortex_conv_forward
+    return call(ctypes.byref(args), _ptr(status), _stream(stream))
+
+
+def cortex_conv_forward(x: torch.Tensor, weight: torch.Tensor, offsets: torch.Tensor, y: torch.Tensor, *, bias=None,
+                        silu: bool = True, state_in=None, state_out=None, state_index=None,
+                        status: torch.Tensor = None, stream=None) -> int:
+    """x, y [T, C]; weight [C, W]; offsets [S + 1]; states [rows, W - 1, C]."""
+    return _conv(False, x, weight, offsets, y, bias, silu, state_in, state_out, state_index, status, stream)
+
+
+def cortex_conv_step(x: torch.Tensor, weight: torch.Tensor, y: torch.Tensor, *, bias=None, silu: bool = True,
+                     state_in=None, state_out=None, state_index=None, status: torch.Tensor = None, stream=None) -> int:
+    """One token of each of S sequences: x, y [S, C]."""
+    return _conv(True, x, weight, None, y, bias, silu, state_in, state_out, state_index, status, stream)
+
+
+def _group_rows(t, name: str, dtype, T: int):
+    """A [T, G, N] tensor with the groups of a row side by side: G, N and its row stride."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise ValueError("%s must be a [T, G, N] torch.Tensor" % name)
+    if t.dtype != dtype:
+        raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    rows, G, N = t.shape
+    if rows != T:
+        raise ValueError("%s must have %d rows, got %d" % (name, T, rows))
+    ld, between, inner = t.stride()
+    if (inner != 1 and N > 1) or (between != N and G > 1):
+        raise ValueError("%s must have contiguous rows" % name)
+    if rows < 2:
+        ld = max(ld, G * N)
+    elif ld < G * N:
+        raise ValueError("%s must have rows that do not overlap" % name)
+    return G, N, ld
+
+
+def _scan(step: bool, x, dt, A, B, C, offsets, y, skip, z, dt_bias, softplus, state_in, state_out, state_index, status,
+          ws, stream) -> int:
+    T, D = _shape2(x, "x")
+    typ, f32, i32 = x.dtype, torch.float32, torch.int32
+    if not isinstance(A, torch.Tensor) or A.dim() not in (1, 2):
+        raise ValueError("A must be [D, N] (decays per channel) or [heads] (decays per head)")
+    G, N, B_ld = _group_rows(B, "B", typ, T)
+    G2, N2, C_ld = _group_rows(C, "C", typ, T)
+    if (G, N) != (G2, N2):
+        raise ValueError("B and C must have the same groups and state size")
+    H = A.shape[0]
+    if A.dim() == 2:
+        if H != D or A.shape[1] != N:
+            raise ValueError("A must be [%d, %d], got %s" % (D, N, list(A.shape)))
+        P = 0
+    else:
+        if H < 1 or D % H:
+            raise ValueError("A must hold a divisor of %d heads, got %d" % (D, H))
+        P = D // H
+    if step:
+        S = T
+        specs = []
+    else:
+        if not isinstance(offsets, torch.Tensor) or offsets.numel() < 1:
+            raise ValueError("offsets must be a torch.Tensor of S + 1 elements")
+        S = offsets.numel() - 1
+        specs = [(offsets, "offsets", i32, S + 1, False), (ws, "ws", None, 1, False)]
+    rows, state = _state_specs(state_in, state_out, state_index, S, f32, (D, N))
+    x_ld, y_ld, dt_ld = _rows(x, "x", typ, T, D), _rows(y, "y", typ, T, D), _rows(dt, "dt", typ, T, H)
+    z_ld = 0 if z is None else _rows(z, "z", typ, T, D)
+    _need_all(specs + state + [(A, "A", f32, A.numel(), False), (skip, "D", f32, H, True),
+                               (dt_bias, "dt_bias", f32, H, True), (status, "status", i32, 1, False)])
+    _on_device((x, "x"), (dt, "dt"), (B, "B"), (C, "C"), (z, "z"), (y, "y"))
+    args = cortex_scan_t(_DTYPES[typ], S, T, D, P, G, N, int(bool(softplus)), rows, _ptr(offsets), _ptr(state_index),
+                         _ptr(x), _ptr(z), _ptr(dt), _ptr(B), _ptr(C), x_ld, z_ld, dt_ld, B_ld, C_ld, _ptr(A), _ptr(skip),
+                         _ptr(dt_bias), _ptr(state_in), _ptr(state_out), _ptr(y), y_ld)
+    lib = load()
+    if step:
+        return lib.cortex_scan_step(ctypes.byref(args), _ptr(status), _stream(stream))
+    return lib.cortex_scan_forward(ctypes.byref(args), _ptr(status), _ptr(ws), ws.numel() * ws.element_size(),
+                                   _stream(stream))
+
+
+def cortex_scan_workspace_bytes(T: int, S: int, D: int, N: int, head_dim: int = 0) -> int:
+    return load().cortex_scan_workspace_bytes(T, S, D, N, head_dim)
+
+
+def cortex_scan_forward(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor,
+                        offsets: torch.Tensor, y: torch.Tensor, *, D=None, z=None, dt_bias=None, softplus: bool = True,
+                        state_in=None, state_out=None, state_index=None, status: torch.Tensor = None,
+                        ws: torch.Tensor = None, stream=None) -> int:
+    """x, y, z [T, D]; B, C [T, G, N]; A [D, N] with dt [T, D], or A [heads] with
+    dt [T, heads]; the skip D and dt_bias like dt's rows; states [rows, D, N]."""
+    return _scan(False, x, dt, A, B, C, offsets, y, D, z, dt_bias, softplus, state_in, state_out, state_index, status, ws,
+                 stream)
+
+
+def cortex_scan_step(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, B: torch.Tensor, C: torch.Tensor,
+                     y: torch.Tensor, *, D=None, z=None, dt_bias=None, softplus: bool = True, state_in=None,
+                     state_out=None, state_index=None, status: torch.Tensor = None, stream=None) -> int:
+    """One token of each of S sequences: x, y, z [S, D], dt and B, C likewise."""
+    return _scan(True, x, dt, A, B, C, None, y, D, z, dt_bias, softplus, state_in, state_out, state_index, status, None,
+                 stream)
+
+
+def cortex_logits_workspace_bytes(rows: int, vocab: int) -> int:
+    return load().cortex_logits_workspace_bytes(rows, vocab)
+
+
+def cortex_logits_process(logits: torch.Tensor, *, out=None, token=None, lse=None, history=None, history_len=None,
+                          prompt_len=None, repetition=None, frequency=None, presence=None, bias_offsets=None,
+                          bias_tokens=None, bias_values=None, mask=None, mask_index=None, status: torch.Tensor = None,
+                          ws: torch.Tensor = None, stream=None) -> int:
+    """logits, out [R, V]; history [R, columns]; mask [states, ceil(V / 32)] of int32 words."""
+    R, V = _shape2(logits, "logits")
+    f32, i32 = torch.float32, torch.int32
+    if out is None and token is None and lse is None:
+        raise ValueError("out, token or lse is required")
+    specs = [(token, "token", i32, R, True), (lse, "lse", f32, R, True), (status, "status", i32, 1, False),
+             (ws, "ws", None, 1, False)]
+    cap = history_ld = biases = states = mask_ld = 0
+    if history is not None:
+        if not isinstance(history, torch.Tensor) or history.dim() != 2:
+            raise ValueError("history must be a 2-dimensional torch.Tensor")
+        cap = history.shape[1]
+        history_ld = _rows(history, "history", i32, R, cap)
+        specs += [(history_len, "history_len", i32, R, False), (prompt_len, "prompt_len", i32, R, True),
+                  (repetition, "repetition", f32, R, True), (frequency, "frequency", f32, R, True),
+                  (presence, "presence", f32, R, True)]
+    elif any(t is not None for t in (history_len, prompt_len, repetition, frequency, presence)):
+        raise ValueError("history is required with its lengths and penalties")
+    if bias_offsets is not None:
+        biases = 0 if bias_tokens is None else bias_tokens.numel()
+        specs += [(bias_offsets, "bias_offsets", i32, R + 1, False), (bias_tokens, "bias_tokens", i32, 0, False),
+                  (bias_values, "bias_values", f32, biases, False)]
+    elif bias_tokens is not None or bias_values is not None:
+        raise ValueError("bias_offsets is required with the biases")
+    if mask is not None:
+        if not isinstance(mask, torch.Tensor) or mask.dim() != 2:
+            raise ValueError("mask must be a 2-dimensional torch.Tensor")
+        states = mask.shape[0]
+        mask_ld = _rows(mask, "mask", i32, states, (V + 31) // 32)
+        specs.append((mask_index, "mask_index", i32, R, True))
+        if mask_index is None and states < R:
+            raise ValueError("mask has %d rows, %d rows of logits need as many" % (states, R))
+    elif mask_index is not None:
+        raise ValueError("mask is required with mask_index")
+    logits_ld = _rows(logits, "logits", logits.dtype, R, V)
+    out_ld = 0 if out is None else _rows(out, "out", logits.dtype, R, V)
+    _need_all(specs)
+    _on_device((logits, "logits"), (out, "out"), (history, "history"), (mask, "mask"))
+    args = cortex_logits_t(_DTYPES[logits.dtype], R, V, cap, biases, states, _ptr(logits), logits_ld, _ptr(history),
+                           history_ld, _ptr(history_len), _ptr(prompt_len), _ptr(repetition), _ptr(frequency),
+                           _ptr(presence), _ptr(bias_offsets), _ptr(bias_tokens), _ptr(bias_values), _ptr(mask), mask_ld,
+                           _ptr(mask_index), _ptr(out), out_ld, _ptr(token), _ptr(lse))
+    return load().cortex_logits_process(ctypes.byref(args), _ptr(status), _ptr(ws), ws.numel() * ws.element_size(),
+                                        _stream(stream))
 
 
 def cortex_version() -> str:

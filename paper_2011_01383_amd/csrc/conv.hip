@@ -1,0 +1,138 @@
+// Causal depthwise convolution over time, for prompts and for single tokens.
+//
+// A thread owns V neighbouring channels (16 bytes of them, or one where rows do
+// not start at 16-byte boundaries) and slides a window of W inputs down a chunk
+// of kConvChunk tokens, so an input is loaded once per chunk, the W - 1 before
+// the chunk aside.
+// The bytes of x and y bound it: 2 W + 4 operations per element loaded and stored.
+#include "sequence.hpp"
+
+namespace cortex {
+
+constexpr int kConvChunk = 32;
+constexpr int kConvThreads = 64;
+
+template <typename T, int W, int V, bool STEP>
+__global__ void __launch_bounds__(kConvThreads) conv_kernel(cortex_conv_t a, int32_t *status) {
+  if (load_status(status) != 0) return;
+  const int slot = (int)blockIdx.x;
+  Chunk c;
+  if constexpr (STEP) {
+    c.seq = c.first = c.begin = slot;
+    c.last = c.end = slot + 1;
+  } else {
+    if (blockIdx.y == 0) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, slot, status);
+    c = find_chunk(a.seq_offsets, a.num_seqs, a.num_tokens, kConvChunk, slot);
+    if (c.seq < 0) return;
+  }
+  const int ch = ((int)blockIdx.y * kConvThreads + (int)threadIdx.x) * V;
+  const bool starts = c.begin == c.first;
+  int row = -1;
+  if (starts && (a.state_in || a.state_out)) {
+    row = state_row(a.state_index, c.seq, a.state_rows, status);
+    if (row < -1) return;
+  }
+  if (ch >= a.channels) return;
+
+  float w[W][V], bias[V], win[W][V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    bias[i] = a.bias ? a.bias[ch + i] : 0.0f;
+#pragma unroll
+    for (int k = 0; k < W; ++k) w[k][i] = a.weight[(int64_t)(ch + i) * W + k];
+  }
+  const T *x = (const T *)a.x + ch;
+  T *y = (T *)a.y + ch;
+  const int64_t state_at = (int64_t)row * (W - 1) * a.channels + ch;
+  // the W - 1 inputs before the chunk: win[1..W-1]
+#pragma unroll
+  for (int k = 1; k < W; ++k) {
+    const int t = c.begin - W + k;
+    if (t >= c.first) {
+      Pack<T, V>::load(x + (int64_t)t * a.x_ld, win[k]);
+    } else if (row >= 0 && a.state_in) {
+      // only a sequence's first chunk has no earlier tokens: Q >= W - 1
+      Pack<T, V>::load((const T *)a.state_in + state_at + (int64_t)(k - 1) * a.channels, win[k]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) win[k][i] = 0.0f;
+    }
+  }
+  if (starts && row >= 0 && a.state_out) {
+    // The sequence's last W - 1 inputs.  The old state is in win already, so the
+    // pool may be updated in place.
+    const int len = c.last - c.first;
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k) {
+      const int j = len - (W - 1) + k;
+      float v[V];
+      if (j >= 0) {
+        Pack<T, V>::load(x + (int64_t)(c.first + j) * a.x_ld, v);
+      } else {
+#pragma unroll
+        for (int m = 1; m < W; ++m)
+          if (m == W + j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = win[m][i];
+      }
+      Pack<T, V>::store((T *)a.state_out + state_at + (int64_t)k * a.channels, v);
+    }
+  }
+  for (int t = c.begin; t < c.end; ++t) {
+#pragma unroll
+    for (int k = 0; k + 1 < W; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) win[k][i] = win[k + 1][i];
+    Pack<T, V>::load(x + (int64_t)t * a.x_ld, win[W - 1]);
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      v[i] = bias[i];
+#pragma unroll
+      for (int k = 0; k < W; ++k) v[i] = __builtin_fmaf(w[k][i], win[k][i], v[i]);
+      if (a.silu) v[i] = silu(v[i]);
+    }
+    Pack<T, V>::store(y + (int64_t)t * a.y_ld, v);
+  }
+}
+
+template <typename T, int W, int V, bool STEP>
+int launch_conv(const cortex_conv_t &a, int32_t *status, void *stream) {
+  const int64_t slots = STEP ? a.num_seqs : chunk_slots(a.num_tokens, a.num_seqs, kConvChunk);
+  const int tiles = (a.channels / V + kConvThreads - 1) / kConvThreads;
+  conv_kernel<T, W, V, STEP><<<dim3((unsigned)slots, tiles), kConvThreads, 0, (hipStream_t)stream>>>(a, status);
+  return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+}
+
+template <typename T, bool STEP> int launch_conv_typed(const cortex_conv_t &a, int32_t *status, void *stream) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const bool wide = a.channels % V == 0 && a.x_ld % V == 0 && a.y_ld % V == 0 && aligned16(a.x) && aligned16(a.y) &&
+                    aligned16(a.state_in) && aligned16(a.state_out);
+  if (a.width == 2) return wide ? launch_conv<T, 2, V, STEP>(a, status, stream) : launch_conv<T, 2, 1, STEP>(a, status, stream);
+  if (a.width == 3) return wide ? launch_conv<T, 3, V, STEP>(a, status, stream) : launch_conv<T, 3, 1, STEP>(a, status, stream);
+  return wide ? launch_conv<T, 4, V, STEP>(a, status, stream) : launch_conv<T, 4, 1, STEP>(a, status, stream);
+}
+
+static int conv_entry(const cortex_conv_t *a, bool step, int32_t *status, void *stream) {
+  if (!a || !status) return CORTEX_E_INVAL;
+  if (bad_batch(a->dtype, a->num_seqs, a->num_tokens, a->channels, a->state_rows, a->state_index,
+                a->state_in || a->state_out))
+    return CORTEX_E_INVAL;
+  if (a->width < 2 || a->width > 4) return CORTEX_E_INVAL;
+  if (step ? a->num_tokens != a->num_seqs : !a->seq_offsets) return CORTEX_E_INVAL;
+  if (!a->weight || a->x_ld < a->channels || a->y_ld < a->channels) return CORTEX_E_INVAL;
+  if (a->num_tokens > 0 && (!a->x || !a->y)) return CORTEX_E_INVAL;
+  if (a->num_seqs == 0) return a->num_tokens == 0 ? CORTEX_OK : CORTEX_E_INVAL;
+  if (a->dtype == CORTEX_BF16)
+    return step ? launch_conv_typed<bf16_t, true>(*a, status, stream) : launch_conv_typed<bf16_t, false>(*a, status, stream);
+  return step ? launch_conv_typed<float, true>(*a, status, stream) : launch_conv_typed<float, false>(*a, status, stream);
+}
+
+}  // namespace cortex
+
+extern "C" int cortex_conv_forward(const cortex_conv_t *args, int32_t *d_status, void *stream) {
+  return cortex::conv_entry(args, false, d_status, stream);
+}
+extern "C" int cortex_conv_step(const cortex_conv_t *args, int32_t *d_status, void *stream) {
+  return cortex::conv_entry(args, true, d_status, stream);
+}

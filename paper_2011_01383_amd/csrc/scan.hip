@@ -1,0 +1,275 @@
+// Selective state space scan, for prompts and for single tokens.
+#include "sequence.hpp"
+
+namespace cortex {
+
+constexpr int kScanWave = 64;
+
+// N consecutive floats (N a multiple of 4, 16-byte aligned).
+template <int N> __device__ __forceinline__ void load_floats(const float *p, float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const float4 q = *(const float4 *)(p + i);
+    v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
+  }
+}
+template <int N> __device__ __forceinline__ void store_floats(float *p, const float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) *(float4 *)(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+}
+
+__device__ __forceinline__ float step_size(const cortex_scan_t &a, float raw, float bias) {
+  const float v = raw + bias;
+  return a.softplus ? softplus(v) : v;
+}
+
+// ---------------------------------------------------------------------------
+// Decays per channel, prompts: a lane is a channel and keeps its N states.
+// ---------------------------------------------------------------------------
+template <typename T, int N>
+__global__ void __launch_bounds__(kScanWave) channel_scan_kernel(cortex_scan_t a, int32_t *status) {
+  if (load_status(status) != 0) return;
+  const int seq = (int)blockIdx.x, g = (int)blockIdx.z;
+  if (blockIdx.y == 0 && g == 0) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, seq, status);
+  const int first = a.seq_offsets[seq], last = a.seq_offsets[seq + 1];
+  if (first < 0 || last < first || last > a.num_tokens) return;
+  const int row = a.state_in || a.state_out ? state_row(a.state_index, seq, a.state_rows, status) : -1;
+  if (row < -1) return;
+  const int per_group = a.channels / a.groups;
+  const int in_group = (int)blockIdx.y * kScanWave + (int)threadIdx.x;
+  if (in_group >= per_group) return;
+  const int d = g * per_group + in_group;
+
+  float h[N], A2[N];
+  const int64_t state_at = ((int64_t)row * a.channels + d) * N;
+  if (row >= 0 && a.state_in) {
+    load_floats<N>(a.state_in + state_at, h);
+  } else {
+#pragma unroll
+    for (int n = 0; n < N; ++n) h[n] = 0.0f;
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) A2[n] = a.A[(int64_t)d * N + n] * kLog2e;
+  const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f, skip = a.skip ? a.skip[d] : 0.0f;
+  for (int64_t t = first; t < last; ++t) {
+    const float x = to_float<T>(((const T *)a.x)[t * a.x_ld + d]);
+    const float dt = step_size(a, to_float<T>(((const T *)a.dt)[t * a.dt_ld + d]), bias);
+    const float u = dt * x;
+    const T *B = (const T *)a.B + t * a.B_ld + g * N, *C = (const T *)a.C + t * a.C_ld + g * N;
+    float y = skip * x;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      h[n] = __builtin_fmaf(h[n], fast_exp2(dt * A2[n]), u * to_float<T>(B[n]));
+      y = __builtin_fmaf(h[n], to_float<T>(C[n]), y);
+    }
+    if (a.z) y *= silu(to_float<T>(((const T *)a.z)[t * a.z_ld + d]));
+    ((T *)a.y)[t * a.y_ld + d] = from_float<T>(y);
+  }
+  if (row >= 0 && a.state_out) store_floats<N>(a.state_out + state_at, h);
+}
+
+// ---------------------------------------------------------------------------
+// Decays per head, prompts: 16 lanes share a channel, each with N / 16 states.
+// ---------------------------------------------------------------------------
+constexpr int kHeadThreads = 256;
+
+__device__ __forceinline__ float sum16(float v) {
+#pragma unroll
+  for (int m = 1; m < 16; m <<= 1) v += __shfl_xor(v, m);
+  return v;
+}
+
+template <typename T, int N>
+__global__ void __launch_bounds__(kHeadThreads) head_scan_kernel(cortex_scan_t a, int32_t *status) {
+  constexpr int M = N / 16;
+  if (load_status(status) != 0) return;
+  const int seq = (int)blockIdx.x;
+  if (blockIdx.y == 0) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, seq, status);
+  const int first = a.seq_offsets[seq], last = a.seq_offsets[seq + 1];
+  if (first < 0 || last < first || last > a.num_tokens) return;
+  const int row = a.state_in || a.state_out ? state_row(a.state_index, seq, a.state_rows, status) : -1;
+  if (row < -1) return;
+  const int part = (int)(threadIdx.x & 15);
+  const int d = (int)blockIdx.y * 16 + (int)(threadIdx.x >> 4);
+  const int head = d / a.head_dim, g = d / (a.channels / a.groups);
+
+  float h[M];
+  const int64_t state_at = ((int64_t)row * a.channels + d) * N + part * M;
+#pragma unroll
+  for (int n = 0; n < M; ++n) h[n] = row >= 0 && a.state_in ? a.state_in[state_at + n] : 0.0f;
+  const float A2 = a.A[head] * kLog2e;
+  const float bias = a.dt_bias ? a.dt_bias[head] : 0.0f, skip = a.skip ? a.skip[head] : 0.0f;
+  for (int64_t t = first; t < last; ++t) {
+    const float x = to_float<T>(((const T *)a.x)[t * a.x_ld + d]);
+    const float dt = step_size(a, to_float<T>(((const T *)a.dt)[t * a.dt_ld + head]), bias);
+    const float u = dt * x, decay = fast_exp2(dt * A2);
+    const T *B = (const T *)a.B + t * a.B_ld + g * N + part * M, *C = (const T *)a.C + t * a.C_ld + g * N + part * M;
+    float y = 0.0f;
+#pragma unroll
+    for (int n = 0; n < M; ++n) {
+      h[n] = __builtin_fmaf(h[n], decay, u * to_float<T>(B[n]));
+      y = __builtin_fmaf(h[n], to_float<T>(C[n]), y);
+    }
+    y = sum16(y) + skip * x;
+    if (part == 0) {
+      if (a.z) y *= silu(to_float<T>(((const T *)a.z)[t * a.z_ld + d]));
+      ((T *)a.y)[t * a.y_ld + d] = from_float<T>(y);
+    }
+  }
+  if (row >= 0 && a.state_out)
+#pragma unroll
+    for (int n = 0; n < M; ++n) a.state_out[state_at + n] = h[n];
+}
+
+// ---------------------------------------------------------------------------
+// One token.  N / 4 lanes share a channel, each with four neighbouring states,
+// so a wave reads and writes whole lines of the state, which bounds it: 8 bytes
+// a state entry against 5 operations.
+// ---------------------------------------------------------------------------
+constexpr int kStepThreads = 256;
+
+template <typename T, int N, bool HEAD>
+__global__ void __launch_bounds__(kStepThreads) scan_step_kernel(cortex_scan_t a, int32_t *status) {
+  constexpr int L = N / 4;                       // lanes per channel
+  if (load_status(status) != 0) return;
+  const int b = (int)blockIdx.x;
+  const int row = a.state_in || a.state_out ? state_row(a.state_index, b, a.state_rows, status) : -1;
+  if (row < -1) return;
+  const int part = (int)(threadIdx.x % L);
+  const int d = (int)blockIdx.y * (kStepThreads / L) + (int)(threadIdx.x / L);
+  if (d >= a.channels) return;                   // the same for all lanes of a channel
+  const int g = d / (a.channels / a.groups), k = HEAD ? d / a.head_dim : d;
+  const int64_t state_at = ((int64_t)row * a.channels + d) * N + part * 4;
+  float h[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (row >= 0 && a.state_in) load_floats<4>(a.state_in + state_at, h);
+  const float x = to_float<T>(((const T *)a.x)[b * a.x_ld + d]);
+  const float dt = step_size(a, to_float<T>(((const T *)a.dt)[b * a.dt_ld + k]), a.dt_bias ? a.dt_bias[k] : 0.0f);
+  const float u = dt * x;
+  const T *B = (const T *)a.B + b * a.B_ld + g * N + part * 4, *C = (const T *)a.C + b * a.C_ld + g * N + part * 4;
+  float y = 0.0f;
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    const float A = HEAD ? a.A[k] : a.A[(int64_t)d * N + part * 4 + n];
+    h[n] = __builtin_fmaf(h[n], fast_exp2(dt * (A * kLog2e)), u * to_float<T>(B[n]));
+    y = __builtin_fmaf(h[n], to_float<T>(C[n]), y);
+  }
+  if (row >= 0 && a.state_out) store_floats<4>(a.state_out + state_at, h);
+#pragma unroll
+  for (int m = 1; m < L; m <<= 1) y += __shfl_xor(y, m);
+  if (part == 0) {
+    if (a.skip) y = __builtin_fmaf(a.skip[k], x, y);
+    if (a.z) y *= silu(to_float<T>(((const T *)a.z)[b * a.z_ld + d]));
+    ((T *)a.y)[b * a.y_ld + d] = from_float<T>(y);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+template <typename T, int N> int launch_channel(const cortex_scan_t &a, int32_t *status, void *stream) {
+  const int per_group = a.channels / a.groups;
+  channel_scan_kernel<T, N><<<dim3(a.num_seqs, (per_group + kScanWave - 1) / kScanWave, a.groups), kScanWave, 0,
+                              (hipStream_t)stream>>>(a, status);
+  return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+}
+
+template <typename T, int N> int launch_head(const cortex_scan_t &a, int32_t *status, void *stream) {
+  head_scan_kernel<T, N><<<dim3(a.num_seqs, a.channels / 16), kHeadThreads, 0, (hipStream_t)stream>>>(a, status);
+  return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+}
+
+template <typename T, int N, bool HEAD> int launch_step(const cortex_scan_t &a, int32_t *status, void *stream) {
+  constexpr int per_block = kStepThreads / (N / 4);
+  scan_step_kernel<T, N, HEAD><<<dim3(a.num_seqs, (a.channels + per_block - 1) / per_block), kStepThreads, 0,
+                                 (hipStream_t)stream>>>(a, status);
+  return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+}
+
+static bool bad_scan_size(int32_t channels, int32_t groups, int32_t state_size, int32_t head_dim) {
+  const int N = state_size;
+  if (channels < 1 || groups < 1 || channels % groups) return true;
+  if (head_dim == 0) return N != 8 && N != 16 && N != 32 && N != 64;
+  if (head_dim < 16 || head_dim > 256 || head_dim % 16 || (channels / groups) % head_dim) return true;
+  return N != 16 && N != 32 && N != 64 && N != 128;
+}
+
+static int check_scan(const cortex_scan_t *a, bool step, int32_t *status) {
+  if (!a || !status) return CORTEX_E_INVAL;
+  if (bad_batch(a->dtype, a->num_seqs, a->num_tokens, a->channels, a->state_rows, a->state_index,
+                a->state_in || a->state_out))
+    return CORTEX_E_INVAL;
+  if (bad_scan_size(a->channels, a->groups, a->state_size, a->head_dim) || a->groups > 65535) return CORTEX_E_INVAL;
+  if (step ? a->num_tokens != a->num_seqs : !a->seq_offsets) return CORTEX_E_INVAL;
+  const int64_t dts = a->head_dim ? a->channels / a->head_dim : a->channels;
+  const int64_t bc = (int64_t)a->groups * a->state_size;
+  if (a->x_ld < a->channels || a->y_ld < a->channels || a->dt_ld < dts || a->B_ld < bc || a->C_ld < bc ||
+      (a->z && a->z_ld < a->channels))
+    return CORTEX_E_INVAL;
+  if (!a->A || !aligned16(a->state_in) || !aligned16(a->state_out)) return CORTEX_E_INVAL;
+  if (a->num_tokens > 0 && (!a->x || !a->dt || !a->B || !a->C || !a->y)) return CORTEX_E_INVAL;
+  if (a->num_seqs == 0 && a->num_tokens != 0) return CORTEX_E_INVAL;
+  return CORTEX_OK;
+}
+
+template <typename T> int scan_forward_typed(const cortex_scan_t &a, int32_t *status, void *stream) {
+  if (a.head_dim == 0) {
+    switch (a.state_size) {
+      case 8: return launch_channel<T, 8>(a, status, stream);
+      case 16: return launch_channel<T, 16>(a, status, stream);
+      case 32: return launch_channel<T, 32>(a, status, stream);
+      default: return launch_channel<T, 64>(a, status, stream);
+    }
+  }
+  switch (a.state_size) {
+    case 16: return launch_head<T, 16>(a, status, stream);
+    case 32: return launch_head<T, 32>(a, status, stream);
+    case 64: return launch_head<T, 64>(a, status, stream);
+    default: return launch_head<T, 128>(a, status, stream);
+  }
+}
+
+template <typename T> int scan_step_typed(const cortex_scan_t &a, int32_t *status, void *stream) {
+  if (a.head_dim == 0) {
+    switch (a.state_size) {
+      case 8: return launch_step<T, 8, false>(a, status, stream);
+      case 16: return launch_step<T, 16, false>(a, status, stream);
+      case 32: return launch_step<T, 32, false>(a, status, stream);
+      default: return launch_step<T, 64, false>(a, status, stream);
+    }
+  }
+  switch (a.state_size) {
+    case 16: return launch_step<T, 16, true>(a, status, stream);
+    case 32: return launch_step<T, 32, true>(a, status, stream);
+    case 64: return launch_step<T, 64, true>(a, status, stream);
+    default: return launch_step<T, 128, true>(a, status, stream);
+  }
+}
+
+}  // namespace cortex
+
+using namespace cortex;
+
+extern "C" size_t cortex_scan_workspace_bytes(int32_t num_tokens, int32_t num_seqs, int32_t channels, int32_t state_size,
+                                              int32_t head_dim) {
+  if (num_tokens < 0 || num_seqs < 0 || bad_scan_size(channels, 1, state_size, head_dim)) return 0;
+  return 256;
+}
+
+extern "C" int cortex_scan_forward(const cortex_scan_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream) {
+  const int rc = check_scan(args, false, d_status);
+  if (rc != CORTEX_OK) return rc;
+  if (args->num_seqs == 0) return CORTEX_OK;
+  if (!d_ws) return CORTEX_E_INVAL;
+  if (ws_bytes < cortex_scan_workspace_bytes(args->num_tokens, args->num_seqs, args->channels, args->state_size, args->head_dim))
+    return CORTEX_E_WORKSPACE;
+  return args->dtype == CORTEX_BF16 ? scan_forward_typed<bf16_t>(*args, d_status, stream)
+                                    : scan_forward_typed<float>(*args, d_status, stream);
+}
+
+extern "C" int cortex_scan_step(const cortex_scan_t *args, int32_t *d_status, void *stream) {
+  const int rc = check_scan(args, true, d_status);
+  if (rc != CORTEX_OK) return rc;
+  if (args->num_seqs == 0) return CORTEX_OK;
+  return args->dtype == CORTEX_BF16 ? scan_step_typed<bf16_t>(*args, d_status, stream)
+                                    : scan_step_typed<float>(*args, d_status, stream);
+}
