@@ -24,48 +24,186 @@ __device__ __forceinline__ float step_size(const cortex_scan_t &a, float raw, fl
 }
 
 // ---------------------------------------------------------------------------
-// Decays per channel, prompts: a lane is a channel and keeps its N states.
+// Splitting a prompt over its length.  The recurrence of a state entry is
+// linear, h <- a h + b, so a segment of tokens acts on the state that enters it
+// as h <- (product of its a) h + (its result from a zero state); the product of
+// exp(dt A) is exp(A sum dt).  Three launches: every segment's result and step
+// sum from zero (part 1), the states that enter the segments, one after another
+// (enter_kernel), then the outputs from those (part 2).  With enough sequences
+// and channels to fill the GPU, or no sequence longer than a segment, one
+// launch walks each sequence whole (part 0): half the arithmetic.
 // ---------------------------------------------------------------------------
-template <typename T, int N>
-__global__ void __launch_bounds__(kScanWave) channel_scan_kernel(cortex_scan_t a, int32_t *status) {
+struct SegmentScratch {
+  float *state;      // [slots, D, N]: a segment's result from zero, then the state that enters it
+  float *steps;      // [slots, channels or heads]: its sum of dt
+};
+
+// One thread per state entry walks its sequence's segments.
+template <bool HEAD>
+__global__ void __launch_bounds__(256) enter_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w, int Q) {
+  constexpr int U = 8;                           // segments loaded ahead of the chain through them
   if (load_status(status) != 0) return;
-  const int seq = (int)blockIdx.x, g = (int)blockIdx.z;
-  if (blockIdx.y == 0 && g == 0) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, seq, status);
+  const int seq = (int)blockIdx.x;
   const int first = a.seq_offsets[seq], last = a.seq_offsets[seq + 1];
   if (first < 0 || last < first || last > a.num_tokens) return;
   const int row = a.state_in || a.state_out ? state_row(a.state_index, seq, a.state_rows, status) : -1;
   if (row < -1) return;
+  const int64_t per_slot = (int64_t)a.channels * a.state_size;
+  const int64_t e = (int64_t)blockIdx.y * 256 + threadIdx.x;
+  if (e >= per_slot) return;
+  const int d = (int)(e / a.state_size), k = HEAD ? d / a.head_dim : d;
+  const int rates = HEAD ? a.channels / a.head_dim : a.channels;
+  const float A2 = a.A[HEAD ? k : e] * kLog2e;
+  float h = row >= 0 && a.state_in ? a.state_in[row * per_slot + e] : 0.0f;
+  const int count = (last - first + Q - 1) / Q;
+  const int64_t slot0 = first / Q + seq;
+  float *st = w.state + slot0 * per_slot + e;
+  const float *sd = w.steps + slot0 * rates + k;
+  for (int c = 0; c < count; c += U) {
+    float r[U], f[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int j = c + i < count ? c + i : count - 1;
+      r[i] = st[j * per_slot];
+      f[i] = fast_exp2(A2 * sd[(int64_t)j * rates]);
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (c + i < count) {
+        st[(c + i) * per_slot] = h;
+        h = __builtin_fmaf(h, f[i], r[i]);
+      }
+  }
+  if (row >= 0 && a.state_out) a.state_out[row * per_slot + e] = h;
+}
+
+// ---------------------------------------------------------------------------
+// Decays per channel, prompts: a lane is a channel and keeps its N states in
+// registers.  The exponentials bound it: N of them and 4 N products and sums
+// for every channel and token.  B and C of kTile tokens are the same for the
+// whole wave: it keeps them in LDS as floats and reads them by broadcast.  What
+// the next kAhead tokens (of B and C: the next tile) need is loaded while these
+// are worked on.
+// ---------------------------------------------------------------------------
+constexpr int kAhead = 4, kTile = 16;
+
+template <typename T, int N, int PART>
+__global__ void __launch_bounds__(kScanWave) channel_scan_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w, int Q) {
+  if (load_status(status) != 0) return;
+  const int slot = (int)blockIdx.x, g = (int)blockIdx.z;
+  const bool checks = blockIdx.y == 0 && g == 0;
+  int seq, begin, end;
+  if constexpr (PART == 0) {
+    seq = slot;
+    if (checks) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, seq, status);
+    begin = a.seq_offsets[seq];
+    end = a.seq_offsets[seq + 1];
+    if (begin < 0 || end < begin || end > a.num_tokens) return;
+  } else {
+    if (PART == 1 && checks) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, slot, status);
+    const Chunk c = find_chunk(a.seq_offsets, a.num_seqs, a.num_tokens, Q, slot);
+    if (c.seq < 0 || c.begin == c.end) return;
+    seq = c.seq;
+    begin = c.begin;
+    end = c.end;
+  }
+  int row = -1;
+  if (PART == 0 && (a.state_in || a.state_out)) {
+    row = state_row(a.state_index, seq, a.state_rows, status);
+    if (row < -1) return;
+  }
   const int per_group = a.channels / a.groups;
-  const int in_group = (int)blockIdx.y * kScanWave + (int)threadIdx.x;
-  if (in_group >= per_group) return;
-  const int d = g * per_group + in_group;
+  const int lane = (int)threadIdx.x, tile0 = (int)blockIdx.y * kScanWave;
+  const bool active = tile0 + lane < per_group;
+  // lanes past the group's last channel repeat it and store nothing
+  const int d = g * per_group + (active ? tile0 + lane : per_group - 1);
 
   float h[N], A2[N];
-  const int64_t state_at = ((int64_t)row * a.channels + d) * N;
-  if (row >= 0 && a.state_in) {
-    load_floats<N>(a.state_in + state_at, h);
-  } else {
+  const int64_t state_at = ((int64_t)(PART == 0 ? row : slot) * a.channels + d) * N;
+  if (PART == 2) load_floats<N>(w.state + state_at, h);
+  else if (PART == 0 && row >= 0 && a.state_in) load_floats<N>(a.state_in + state_at, h);
+  else
 #pragma unroll
     for (int n = 0; n < N; ++n) h[n] = 0.0f;
-  }
 #pragma unroll
   for (int n = 0; n < N; ++n) A2[n] = a.A[(int64_t)d * N + n] * kLog2e;
   const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f, skip = a.skip ? a.skip[d] : 0.0f;
-  for (int64_t t = first; t < last; ++t) {
-    const float x = to_float<T>(((const T *)a.x)[t * a.x_ld + d]);
-    const float dt = step_size(a, to_float<T>(((const T *)a.dt)[t * a.dt_ld + d]), bias);
-    const float u = dt * x;
-    const T *B = (const T *)a.B + t * a.B_ld + g * N, *C = (const T *)a.C + t * a.C_ld + g * N;
-    float y = skip * x;
+  const T *xs = (const T *)a.x + d, *ds = (const T *)a.dt + d, *zs = (const T *)a.z + d;
+  T *ys = (T *)a.y + d;
+  const T *Bs = (const T *)a.B + g * N, *Cs = (const T *)a.C + g * N;
+  const bool gate = a.z != nullptr;
+  float steps = 0.0f;
+
+  constexpr int kShared = PART == 1 ? N : 2 * N;              // B, and C after it
+  constexpr int kStage = kTile * kShared / kScanWave;
+  __shared__ float shared_bc[kTile][kShared];
+  T x0[kAhead], d0[kAhead], z0[kAhead], bc0[kStage];
+  auto fetch = [&](int t0) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      h[n] = __builtin_fmaf(h[n], fast_exp2(dt * A2[n]), u * to_float<T>(B[n]));
-      y = __builtin_fmaf(h[n], to_float<T>(C[n]), y);
+    for (int i = 0; i < kAhead; ++i) {
+      const int64_t t = t0 + i < end ? t0 + i : end - 1;
+      x0[i] = xs[t * a.x_ld];
+      d0[i] = ds[t * a.dt_ld];
+      if (PART != 1 && gate) z0[i] = zs[t * a.z_ld];
     }
-    if (a.z) y *= silu(to_float<T>(((const T *)a.z)[t * a.z_ld + d]));
-    ((T *)a.y)[t * a.y_ld + d] = from_float<T>(y);
+  };
+  auto fetch_bc = [&](int t0) {
+#pragma unroll
+    for (int i = 0; i < kStage; ++i) {
+      const int e = i * kScanWave + lane, k = e % kShared;
+      const int64_t t = t0 + e / kShared < end ? t0 + e / kShared : end - 1;
+      bc0[i] = k < N ? Bs[t * a.B_ld + k] : Cs[t * a.C_ld + k - N];
+    }
+  };
+  if (begin < end) {
+    fetch(begin);
+    fetch_bc(begin);
   }
-  if (row >= 0 && a.state_out) store_floats<N>(a.state_out + state_at, h);
+  for (int tile = begin; tile < end; tile += kTile) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kStage; ++i) (&shared_bc[0][0])[i * kScanWave + lane] = to_float<T>(bc0[i]);
+    __syncthreads();
+    if (tile + kTile < end) fetch_bc(tile + kTile);
+    const int stop = end - tile < kTile ? end : tile + kTile;
+#pragma unroll 1
+    for (int t0 = tile; t0 < stop; t0 += kAhead) {
+      float x[kAhead], dt[kAhead], z[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        x[i] = to_float<T>(x0[i]);
+        dt[i] = step_size(a, to_float<T>(d0[i]), bias);
+        z[i] = to_float<T>(z0[i]);
+      }
+      if (t0 + kAhead < end) fetch(t0 + kAhead);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int64_t t = t0 + i;
+        if (t < stop) {
+          const float u = dt[i] * x[i];
+          const float *B = shared_bc[t - tile], *C = B + N;
+          float y = skip * x[i];
+#pragma unroll
+          for (int n = 0; n < N; ++n) {
+            h[n] = __builtin_fmaf(h[n], fast_exp2(dt[i] * A2[n]), u * B[n]);
+            if (PART != 1) y = __builtin_fmaf(h[n], C[n], y);
+          }
+          if (PART == 1) {
+            steps += dt[i];
+          } else if (active) {
+            if (gate) y *= silu(z[i]);
+            ys[t * a.y_ld] = from_float<T>(y);
+          }
+        }
+      }
+    }
+  }
+  if (!active) return;
+  if (PART == 1) {
+    store_floats<N>(w.state + state_at, h);
+    w.steps[(int64_t)slot * a.channels + d] = steps;
+  }
+  if (PART == 0 && row >= 0 && a.state_out) store_floats<N>(a.state_out + state_at, h);
 }
 
 // ---------------------------------------------------------------------------
@@ -166,11 +304,49 @@ __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(cortex_scan_t a
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-template <typename T, int N> int launch_channel(const cortex_scan_t &a, int32_t *status, void *stream) {
-  const int per_group = a.channels / a.groups;
-  channel_scan_kernel<T, N><<<dim3(a.num_seqs, (per_group + kScanWave - 1) / kScanWave, a.groups), kScanWave, 0,
-                              (hipStream_t)stream>>>(a, status);
-  return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+// Tokens of a segment, 0 for one launch over whole sequences.  A wave of the
+// channel scan is bound by its arithmetic, so the split, which doubles that,
+// pays until every SIMD of the GPU (1,024) has a wave without it; segments are
+// as long as leaves kFillWaves waves, and no shorter than 32 tokens, where the
+// states between them would be most of the bytes.
+constexpr int64_t kFillWaves = 4096;
+static int segment_tokens(int64_t T, int64_t S, int64_t D, int head_dim) {
+  if (head_dim) return 0;
+  const int64_t tiles = (D + kScanWave - 1) / kScanWave;
+  if (S * tiles >= 1024) return 0;
+  int Q = 256;
+  while (Q > 32 && T / Q * tiles < kFillWaves) Q /= 2;
+  return T <= Q ? 0 : Q;
+}
+
+static SegmentScratch scratch_of(const cortex_scan_t &a, int Q, void *ws) {
+  SegmentScratch w = {nullptr, nullptr};
+  if (Q) {
+    w.state = (float *)ws;
+    w.steps = w.state + (size_t)chunk_slots(a.num_tokens, a.num_seqs, Q) * a.channels * a.state_size;
+  }
+  return w;
+}
+
+static bool launched() { return hipGetLastError() == hipSuccess; }
+
+template <typename T, int N> int launch_channel(const cortex_scan_t &a, int32_t *status, void *ws, void *stream) {
+  const int Q = segment_tokens(a.num_tokens, a.num_seqs, a.channels, 0);
+  const SegmentScratch w = scratch_of(a, Q, ws);
+  const unsigned tiles = (a.channels / a.groups + kScanWave - 1) / kScanWave;
+  const hipStream_t st = (hipStream_t)stream;
+  if (!Q) {
+    channel_scan_kernel<T, N, 0><<<dim3(a.num_seqs, tiles, a.groups), kScanWave, 0, st>>>(a, status, w, 0);
+    return launched() ? CORTEX_OK : CORTEX_E_HIP;
+  }
+  const unsigned slots = (unsigned)chunk_slots(a.num_tokens, a.num_seqs, Q);
+  const unsigned entries = (unsigned)(((int64_t)a.channels * N + 255) / 256);
+  channel_scan_kernel<T, N, 1><<<dim3(slots, tiles, a.groups), kScanWave, 0, st>>>(a, status, w, Q);
+  if (!launched()) return CORTEX_E_HIP;
+  enter_kernel<false><<<dim3(a.num_seqs, entries), 256, 0, st>>>(a, status, w, Q);
+  if (!launched()) return CORTEX_E_HIP;
+  channel_scan_kernel<T, N, 2><<<dim3(slots, tiles, a.groups), kScanWave, 0, st>>>(a, status, w, Q);
+  return launched() ? CORTEX_OK : CORTEX_E_HIP;
 }
 
 template <typename T, int N> int launch_head(const cortex_scan_t &a, int32_t *status, void *stream) {
@@ -211,13 +387,13 @@ static int check_scan(const cortex_scan_t *a, bool step, int32_t *status) {
   return CORTEX_OK;
 }
 
-template <typename T> int scan_forward_typed(const cortex_scan_t &a, int32_t *status, void *stream) {
+template <typename T> int scan_forward_typed(const cortex_scan_t &a, int32_t *status, void *ws, void *stream) {
   if (a.head_dim == 0) {
     switch (a.state_size) {
-      case 8: return launch_channel<T, 8>(a, status, stream);
-      case 16: return launch_channel<T, 16>(a, status, stream);
-      case 32: return launch_channel<T, 32>(a, status, stream);
-      default: return launch_channel<T, 64>(a, status, stream);
+      case 8: return launch_channel<T, 8>(a, status, ws, stream);
+      case 16: return launch_channel<T, 16>(a, status, ws, stream);
+      case 32: return launch_channel<T, 32>(a, status, ws, stream);
+      default: return launch_channel<T, 64>(a, status, ws, stream);
     }
   }
   switch (a.state_size) {
@@ -252,7 +428,9 @@ using namespace cortex;
 extern "C" size_t cortex_scan_workspace_bytes(int32_t num_tokens, int32_t num_seqs, int32_t channels, int32_t state_size,
                                               int32_t head_dim) {
   if (num_tokens < 0 || num_seqs < 0 || bad_scan_size(channels, 1, state_size, head_dim)) return 0;
-  return 256;
+  const int Q = segment_tokens(num_tokens, num_seqs, channels, head_dim);
+  if (!Q) return 256;
+  return (size_t)chunk_slots(num_tokens, num_seqs, Q) * channels * (state_size + 1) * sizeof(float);
 }
 
 extern "C" int cortex_scan_forward(const cortex_scan_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream) {
@@ -262,8 +440,8 @@ extern "C" int cortex_scan_forward(const cortex_scan_t *args, int32_t *d_status,
   if (!d_ws) return CORTEX_E_INVAL;
   if (ws_bytes < cortex_scan_workspace_bytes(args->num_tokens, args->num_seqs, args->channels, args->state_size, args->head_dim))
     return CORTEX_E_WORKSPACE;
-  return args->dtype == CORTEX_BF16 ? scan_forward_typed<bf16_t>(*args, d_status, stream)
-                                    : scan_forward_typed<float>(*args, d_status, stream);
+  return args->dtype == CORTEX_BF16 ? scan_forward_typed<bf16_t>(*args, d_status, d_ws, stream)
+                                    : scan_forward_typed<float>(*args, d_status, d_ws, stream);
 }
 
 extern "C" int cortex_scan_step(const cortex_scan_t *args, int32_t *d_status, void *stream) {
