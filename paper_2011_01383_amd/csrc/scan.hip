@@ -1,4 +1,5 @@
 // Selective state space scan, for prompts and for single tokens.
+#include "scan_head.hpp"
 #include "sequence.hpp"
 
 namespace cortex {
@@ -18,11 +19,6 @@ template <int N> __device__ __forceinline__ void store_floats(float *p, const fl
   for (int i = 0; i < N; i += 4) *(float4 *)(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
 }
 
-__device__ __forceinline__ float step_size(const cortex_scan_t &a, float raw, float bias) {
-  const float v = raw + bias;
-  return a.softplus ? softplus(v) : v;
-}
-
 // ---------------------------------------------------------------------------
 // Splitting a prompt over its length.  The recurrence of a state entry is
 // linear, h <- a h + b, so a segment of tokens acts on the state that enters it
@@ -33,23 +29,18 @@ __device__ __forceinline__ float step_size(const cortex_scan_t &a, float raw, fl
 // and channels to fill the GPU, or no sequence longer than a segment, one
 // launch walks each sequence whole (part 0): half the arithmetic.
 // ---------------------------------------------------------------------------
-struct SegmentScratch {
-  float *state;      // [slots, D, N]: a segment's result from zero, then the state that enters it
-  float *steps;      // [slots, channels or heads]: its sum of dt
-};
-
 // One thread per state entry walks its sequence's segments.
 template <bool HEAD>
 __global__ void __launch_bounds__(256) enter_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w, int Q) {
   constexpr int U = 8;                           // segments loaded ahead of the chain through them
   if (load_status(status) != 0) return;
-  const int seq = (int)blockIdx.x;
+  const int seq = (int)blockIdx.y;
   const int first = a.seq_offsets[seq], last = a.seq_offsets[seq + 1];
   if (first < 0 || last < first || last > a.num_tokens) return;
   const int row = a.state_in || a.state_out ? state_row(a.state_index, seq, a.state_rows, status) : -1;
   if (row < -1) return;
   const int64_t per_slot = (int64_t)a.channels * a.state_size;
-  const int64_t e = (int64_t)blockIdx.y * 256 + threadIdx.x;
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (e >= per_slot) return;
   const int d = (int)(e / a.state_size), k = HEAD ? d / a.head_dim : d;
   const int rates = HEAD ? a.channels / a.head_dim : a.channels;
@@ -209,8 +200,6 @@ __global__ void __launch_bounds__(kScanWave) channel_scan_kernel(cortex_scan_t a
 // ---------------------------------------------------------------------------
 // Decays per head, prompts: 16 lanes share a channel, each with N / 16 states.
 // ---------------------------------------------------------------------------
-constexpr int kHeadThreads = 256;
-
 __device__ __forceinline__ float sum16(float v) {
 #pragma unroll
   for (int m = 1; m < 16; m <<= 1) v += __shfl_xor(v, m);
@@ -311,7 +300,13 @@ __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(cortex_scan_t a
 // states between them would be most of the bytes.
 constexpr int64_t kFillWaves = 4096;
 static int segment_tokens(int64_t T, int64_t S, int64_t D, int head_dim) {
-  if (head_dim) return 0;
+  if (head_dim) {
+    const int64_t groups = D / head_dim * ((head_dim + 63) / 64);
+    if (S * groups >= 512) return 0;
+    int Q = 2048;
+    while (Q > 128 && T / Q * groups < 1024) Q /= 2;
+    return T <= Q ? 0 : Q;
+  }
   const int64_t tiles = (D + kScanWave - 1) / kScanWave;
   if (S * tiles >= 1024) return 0;
   int Q = 256;
@@ -343,13 +338,35 @@ template <typename T, int N> int launch_channel(const cortex_scan_t &a, int32_t 
   const unsigned entries = (unsigned)(((int64_t)a.channels * N + 255) / 256);
   channel_scan_kernel<T, N, 1><<<dim3(slots, tiles, a.groups), kScanWave, 0, st>>>(a, status, w, Q);
   if (!launched()) return CORTEX_E_HIP;
-  enter_kernel<false><<<dim3(a.num_seqs, entries), 256, 0, st>>>(a, status, w, Q);
+  enter_kernel<false><<<dim3(entries, a.num_seqs), 256, 0, st>>>(a, status, w, Q);
   if (!launched()) return CORTEX_E_HIP;
   channel_scan_kernel<T, N, 2><<<dim3(slots, tiles, a.groups), kScanWave, 0, st>>>(a, status, w, Q);
   return launched() ? CORTEX_OK : CORTEX_E_HIP;
 }
 
-template <typename T, int N> int launch_head(const cortex_scan_t &a, int32_t *status, void *stream) {
+template <int N> int launch_head_mfma(const cortex_scan_t &a, int32_t *status, void *ws, void *stream) {
+  const int Q = segment_tokens(a.num_tokens, a.num_seqs, a.channels, a.head_dim);
+  const SegmentScratch w = scratch_of(a, Q, ws);
+  const unsigned groups = a.channels / a.head_dim * ((a.head_dim + 63) / 64);
+  const int wide = (a.x_ld % 8 == 0 && aligned16(a.x) ? 1 : 0) | (a.B_ld % 8 == 0 && aligned16(a.B) ? 2 : 0) |
+                   (a.C_ld % 8 == 0 && aligned16(a.C) ? 4 : 0);
+  const hipStream_t st = (hipStream_t)stream;
+  if (!Q) {
+    head_mfma_kernel<N, 0><<<dim3(a.num_seqs, groups), kHeadThreads, 0, st>>>(a, status, w, 0, wide);
+    return launched() ? CORTEX_OK : CORTEX_E_HIP;
+  }
+  const unsigned slots = (unsigned)chunk_slots(a.num_tokens, a.num_seqs, Q);
+  const unsigned entries = (unsigned)(((int64_t)a.channels * N + 255) / 256);
+  head_mfma_kernel<N, 1><<<dim3(slots, groups), kHeadThreads, 0, st>>>(a, status, w, Q, wide);
+  if (!launched()) return CORTEX_E_HIP;
+  enter_kernel<true><<<dim3(entries, a.num_seqs), 256, 0, st>>>(a, status, w, Q);
+  if (!launched()) return CORTEX_E_HIP;
+  head_mfma_kernel<N, 2><<<dim3(slots, groups), kHeadThreads, 0, st>>>(a, status, w, Q, wide);
+  return launched() ? CORTEX_OK : CORTEX_E_HIP;
+}
+
+template <typename T, int N> int launch_head(const cortex_scan_t &a, int32_t *status, void *ws, void *stream) {
+  if constexpr (sizeof(T) == 2) return launch_head_mfma<N>(a, status, ws, stream);
   head_scan_kernel<T, N><<<dim3(a.num_seqs, a.channels / 16), kHeadThreads, 0, (hipStream_t)stream>>>(a, status);
   return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
 }
@@ -397,10 +414,10 @@ template <typename T> int scan_forward_typed(const cortex_scan_t &a, int32_t *st
     }
   }
   switch (a.state_size) {
-    case 16: return launch_head<T, 16>(a, status, stream);
-    case 32: return launch_head<T, 32>(a, status, stream);
-    case 64: return launch_head<T, 64>(a, status, stream);
-    default: return launch_head<T, 128>(a, status, stream);
+    case 16: return launch_head<T, 16>(a, status, ws, stream);
+    case 32: return launch_head<T, 32>(a, status, ws, stream);
+    case 64: return launch_head<T, 64>(a, status, ws, stream);
+    default: return launch_head<T, 128>(a, status, ws, stream);
   }
 }
 

@@ -68,6 +68,11 @@ __device__ __forceinline__ float softplus(float v) {
   return v != v ? v : r;      // fmax drops a NaN
 }
 
+__device__ __forceinline__ float step_size(const cortex_scan_t &a, float raw, float bias) {
+  const float v = raw + bias;
+  return a.softplus ? softplus(v) : v;
+}
+
 // ---------------------------------------------------------------------------
 // Chunks.  Sequence i is cut into chunks of Q tokens from its own first token
 // on.  Its chunks take the slots from off[i] / Q + i on: that is at least as
@@ -140,13 +145,22 @@ __device__ __forceinline__ int state_row(const int32_t *index, int i, int rows, 
   return r;
 }
 
+// Between the launches of a prompt that is split over its length (scan.hip).
+struct SegmentScratch {
+  float *state;      // [slots, D, N]: a segment's result from zero, then the state that enters it
+  float *steps;      // [slots, channels or heads]: its sum of dt
+};
+
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+// Grids count tiles of channels in 16 bits.
+constexpr int32_t kMaxChannels = 1 << 18;
 
 // Host checks that the prompt and step forms share: sizes of the batch.
 inline bool bad_batch(int32_t dtype, int32_t S, int32_t T, int32_t channels, int32_t state_rows, const int32_t *index,
                       bool has_state) {
   if (dtype != CORTEX_F32 && dtype != CORTEX_BF16) return true;
-  if (S < 0 || T < 0 || channels < 1 || channels > (1 << 20) || state_rows < 0) return true;
+  if (S < 0 || T < 0 || channels < 1 || channels > kMaxChannels || state_rows < 0) return true;
   // slots of chunks are counted in 32 bits
   if ((int64_t)S + T > 0x7fff0000) return true;
   return has_state && !index && state_rows < S;

@@ -211,3 +211,24 @@ def test_deterministic_and_on_another_stream(P):
         C.check(p.call(state_out=o, stream=s))
         torch.cuda.synchronize()
         assert torch.equal(p.d["y"], y) and torch.equal(o, out)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("P", [0, 64])
+@pytest.mark.parametrize("what", ["x", "B", "dt", "C"])
+def test_a_token_reaches_no_earlier_one(what, P, dtype):
+    """An infinity or NaN at one token leaves the tokens before it as they were; in x it stays in its channel."""
+    need_gpu()
+    p = Scan(9, [150], 64, 16, 1, P, dtype=dtype)
+    y, _ = run(p, "clean")
+    y = y.clone()
+    for at, v in ((100, float("inf")), (37, float("nan")), (0, float("-inf"))):
+        p.upload()
+        p.d[what][at, ..., 3 if what == "x" else slice(None)] = v
+        C.check(p.call())
+        torch.cuda.synchronize()
+        assert torch.equal(p.d["y"][:at], y[:at]), at
+        if what == "x":
+            others = [c for c in range(64) if c != 3]
+            assert torch.equal(p.d["y"][:, others], y[:, others]), at
+            assert not bool(torch.isfinite(p.d["y"][at:, 3]).any()), at
