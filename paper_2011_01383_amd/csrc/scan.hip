@@ -1,5 +1,6 @@
 // Selective state space scan, for prompts and for single tokens.
 #include "scan_head.hpp"
+#include "scan_head32.hpp"
 #include "sequence.hpp"
 
 namespace cortex {
@@ -198,57 +199,6 @@ __global__ void __launch_bounds__(kScanWave) channel_scan_kernel(cortex_scan_t a
 }
 
 // ---------------------------------------------------------------------------
-// Decays per head, prompts: 16 lanes share a channel, each with N / 16 states.
-// ---------------------------------------------------------------------------
-__device__ __forceinline__ float sum16(float v) {
-#pragma unroll
-  for (int m = 1; m < 16; m <<= 1) v += __shfl_xor(v, m);
-  return v;
-}
-
-template <typename T, int N>
-__global__ void __launch_bounds__(kHeadThreads) head_scan_kernel(cortex_scan_t a, int32_t *status) {
-  constexpr int M = N / 16;
-  if (load_status(status) != 0) return;
-  const int seq = (int)blockIdx.x;
-  if (blockIdx.y == 0) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, seq, status);
-  const int first = a.seq_offsets[seq], last = a.seq_offsets[seq + 1];
-  if (first < 0 || last < first || last > a.num_tokens) return;
-  const int row = a.state_in || a.state_out ? state_row(a.state_index, seq, a.state_rows, status) : -1;
-  if (row < -1) return;
-  const int part = (int)(threadIdx.x & 15);
-  const int d = (int)blockIdx.y * 16 + (int)(threadIdx.x >> 4);
-  const int head = d / a.head_dim, g = d / (a.channels / a.groups);
-
-  float h[M];
-  const int64_t state_at = ((int64_t)row * a.channels + d) * N + part * M;
-#pragma unroll
-  for (int n = 0; n < M; ++n) h[n] = row >= 0 && a.state_in ? a.state_in[state_at + n] : 0.0f;
-  const float A2 = a.A[head] * kLog2e;
-  const float bias = a.dt_bias ? a.dt_bias[head] : 0.0f, skip = a.skip ? a.skip[head] : 0.0f;
-  for (int64_t t = first; t < last; ++t) {
-    const float x = to_float<T>(((const T *)a.x)[t * a.x_ld + d]);
-    const float dt = step_size(a, to_float<T>(((const T *)a.dt)[t * a.dt_ld + head]), bias);
-    const float u = dt * x, decay = fast_exp2(dt * A2);
-    const T *B = (const T *)a.B + t * a.B_ld + g * N + part * M, *C = (const T *)a.C + t * a.C_ld + g * N + part * M;
-    float y = 0.0f;
-#pragma unroll
-    for (int n = 0; n < M; ++n) {
-      h[n] = __builtin_fmaf(h[n], decay, u * to_float<T>(B[n]));
-      y = __builtin_fmaf(h[n], to_float<T>(C[n]), y);
-    }
-    y = sum16(y) + skip * x;
-    if (part == 0) {
-      if (a.z) y *= silu(to_float<T>(((const T *)a.z)[t * a.z_ld + d]));
-      ((T *)a.y)[t * a.y_ld + d] = from_float<T>(y);
-    }
-  }
-  if (row >= 0 && a.state_out)
-#pragma unroll
-    for (int n = 0; n < M; ++n) a.state_out[state_at + n] = h[n];
-}
-
-// ---------------------------------------------------------------------------
 // One token.  N / 4 lanes share a channel, each with four neighbouring states,
 // so a wave reads and writes whole lines of the state, which bounds it: 8 bytes
 // a state entry against 5 operations.
@@ -344,31 +294,32 @@ template <typename T, int N> int launch_channel(const cortex_scan_t &a, int32_t 
   return launched() ? CORTEX_OK : CORTEX_E_HIP;
 }
 
-template <int N> int launch_head_mfma(const cortex_scan_t &a, int32_t *status, void *ws, void *stream) {
+template <typename T, int N, int PART>
+void launch_head_part(const cortex_scan_t &a, int32_t *status, const SegmentScratch &w, int Q, dim3 grid, int wide, hipStream_t st) {
+  if constexpr (sizeof(T) == 2) head_mfma_kernel<N, PART><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q, wide);
+  else head_mfma32_kernel<N, PART><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q, wide);
+}
+
+template <typename T, int N> int launch_head(const cortex_scan_t &a, int32_t *status, void *ws, void *stream) {
+  constexpr int V = 16 / (int)sizeof(T);
   const int Q = segment_tokens(a.num_tokens, a.num_seqs, a.channels, a.head_dim);
   const SegmentScratch w = scratch_of(a, Q, ws);
   const unsigned groups = a.channels / a.head_dim * ((a.head_dim + 63) / 64);
-  const int wide = (a.x_ld % 8 == 0 && aligned16(a.x) ? 1 : 0) | (a.B_ld % 8 == 0 && aligned16(a.B) ? 2 : 0) |
-                   (a.C_ld % 8 == 0 && aligned16(a.C) ? 4 : 0);
+  const int wide = (a.x_ld % V == 0 && aligned16(a.x) ? 1 : 0) | (a.B_ld % V == 0 && aligned16(a.B) ? 2 : 0) |
+                   (a.C_ld % V == 0 && aligned16(a.C) ? 4 : 0);
   const hipStream_t st = (hipStream_t)stream;
   if (!Q) {
-    head_mfma_kernel<N, 0><<<dim3(a.num_seqs, groups), kHeadThreads, 0, st>>>(a, status, w, 0, wide);
+    launch_head_part<T, N, 0>(a, status, w, 0, dim3(a.num_seqs, groups), wide, st);
     return launched() ? CORTEX_OK : CORTEX_E_HIP;
   }
   const unsigned slots = (unsigned)chunk_slots(a.num_tokens, a.num_seqs, Q);
   const unsigned entries = (unsigned)(((int64_t)a.channels * N + 255) / 256);
-  head_mfma_kernel<N, 1><<<dim3(slots, groups), kHeadThreads, 0, st>>>(a, status, w, Q, wide);
+  launch_head_part<T, N, 1>(a, status, w, Q, dim3(slots, groups), wide, st);
   if (!launched()) return CORTEX_E_HIP;
   enter_kernel<true><<<dim3(entries, a.num_seqs), 256, 0, st>>>(a, status, w, Q);
   if (!launched()) return CORTEX_E_HIP;
-  head_mfma_kernel<N, 2><<<dim3(slots, groups), kHeadThreads, 0, st>>>(a, status, w, Q, wide);
+  launch_head_part<T, N, 2>(a, status, w, Q, dim3(slots, groups), wide, st);
   return launched() ? CORTEX_OK : CORTEX_E_HIP;
-}
-
-template <typename T, int N> int launch_head(const cortex_scan_t &a, int32_t *status, void *ws, void *stream) {
-  if constexpr (sizeof(T) == 2) return launch_head_mfma<N>(a, status, ws, stream);
-  head_scan_kernel<T, N><<<dim3(a.num_seqs, a.channels / 16), kHeadThreads, 0, (hipStream_t)stream>>>(a, status);
-  return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
 }
 
 template <typename T, int N, bool HEAD> int launch_step(const cortex_scan_t &a, int32_t *status, void *stream) {
