@@ -253,8 +253,8 @@ static int segment_tokens(int64_t T, int64_t S, int64_t D, int head_dim) {
   if (head_dim) {
     const int64_t groups = D / head_dim * ((head_dim + 63) / 64);
     if (S * groups >= 512) return 0;
-    int Q = 2048;
-    while (Q > 128 && T / Q * groups < 1024) Q /= 2;
+    int Q = 1024;
+    while (Q > 64 && T / Q * groups < 1024) Q /= 2;
     return T <= Q ? 0 : Q;
   }
   const int64_t tiles = (D + kScanWave - 1) / kScanWave;
@@ -295,31 +295,34 @@ template <typename T, int N> int launch_channel(const cortex_scan_t &a, int32_t 
 }
 
 template <typename T, int N, int PART>
-void launch_head_part(const cortex_scan_t &a, int32_t *status, const SegmentScratch &w, int Q, dim3 grid, int wide, hipStream_t st) {
-  if constexpr (sizeof(T) == 2) head_mfma_kernel<N, PART><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q, wide);
-  else head_mfma32_kernel<N, PART><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q, wide);
+int launch_head_part(const cortex_scan_t &a, int32_t *status, const SegmentScratch &w, int Q, unsigned slots, hipStream_t st) {
+  constexpr int V = 16 / (int)sizeof(T);         // elements of 16 bytes
+  auto rows16 = [](const void *p, int64_t ld) { return aligned16(p) && ld % V == 0; };
+  const bool wide = rows16(a.x, a.x_ld) && rows16(a.B, a.B_ld) && rows16(a.C, a.C_ld) && rows16(a.z, a.z ? a.z_ld : 0) &&
+                    rows16(a.y, a.y_ld);
+  const dim3 grid(slots, a.channels / a.head_dim * ((a.head_dim + 63) / 64));
+  if constexpr (sizeof(T) == 2) {
+    if (wide) head_mfma_kernel<N, PART, true><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q);
+    else head_mfma_kernel<N, PART, false><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q);
+  } else {
+    if (wide) head_mfma32_kernel<N, PART, true><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q);
+    else head_mfma32_kernel<N, PART, false><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q);
+  }
+  return launched() ? CORTEX_OK : CORTEX_E_HIP;
 }
 
 template <typename T, int N> int launch_head(const cortex_scan_t &a, int32_t *status, void *ws, void *stream) {
-  constexpr int V = 16 / (int)sizeof(T);
   const int Q = segment_tokens(a.num_tokens, a.num_seqs, a.channels, a.head_dim);
   const SegmentScratch w = scratch_of(a, Q, ws);
-  const unsigned groups = a.channels / a.head_dim * ((a.head_dim + 63) / 64);
-  const int wide = (a.x_ld % V == 0 && aligned16(a.x) ? 1 : 0) | (a.B_ld % V == 0 && aligned16(a.B) ? 2 : 0) |
-                   (a.C_ld % V == 0 && aligned16(a.C) ? 4 : 0);
   const hipStream_t st = (hipStream_t)stream;
-  if (!Q) {
-    launch_head_part<T, N, 0>(a, status, w, 0, dim3(a.num_seqs, groups), wide, st);
-    return launched() ? CORTEX_OK : CORTEX_E_HIP;
-  }
+  if (!Q) return launch_head_part<T, N, 0>(a, status, w, 0, a.num_seqs, st);
   const unsigned slots = (unsigned)chunk_slots(a.num_tokens, a.num_seqs, Q);
   const unsigned entries = (unsigned)(((int64_t)a.channels * N + 255) / 256);
-  launch_head_part<T, N, 1>(a, status, w, Q, dim3(slots, groups), wide, st);
-  if (!launched()) return CORTEX_E_HIP;
+  const int rc = launch_head_part<T, N, 1>(a, status, w, Q, slots, st);
+  if (rc != CORTEX_OK) return rc;
   enter_kernel<true><<<dim3(entries, a.num_seqs), 256, 0, st>>>(a, status, w, Q);
   if (!launched()) return CORTEX_E_HIP;
-  launch_head_part<T, N, 2>(a, status, w, Q, dim3(slots, groups), wide, st);
-  return launched() ? CORTEX_OK : CORTEX_E_HIP;
+  return launch_head_part<T, N, 2>(a, status, w, Q, slots, st);
 }
 
 template <typename T, int N, bool HEAD> int launch_step(const cortex_scan_t &a, int32_t *status, void *stream) {

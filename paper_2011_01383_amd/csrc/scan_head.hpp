@@ -23,8 +23,16 @@
 // over keeps position 8 q + 4 a + r for element 16 a + 4 q + r of each 32: a
 // result then is an operand of the next product as it stands.  The scores are
 // computed as B C^T (columns t) and the state as [N, channels], so neither is
-// ever transposed; B and x are, on their way into LDS.
+// ever transposed; B and x are, on their way into LDS.  y has channels as rows,
+// so a lane loads z and stores y four channels at a time.
+//
+// What it does per sub-chunk and wave at N = 128: 102 products (1,632 cycles of
+// a SIMD's matrix unit), about 60 16-byte reads of LDS.  The skip connection is
+// the scores' diagonal.  Step sizes and their sums are made a sub-chunk ahead by
+// one wave, beside the others' products.
 #pragma once
+
+#include <type_traits>
 
 #include "sequence.hpp"
 
@@ -60,27 +68,67 @@ __device__ __forceinline__ bf16x8v pack8(const __bf16 (&p)[8]) {
   return bf16x8v{p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]};
 }
 
-// LDS of one workgroup.  The scores take the place of B's rows once those are read.
+// Rows of W elements that are read 16 bytes a lane down neighbouring rows: the
+// 16-byte pieces of a row are exchanged by its number, so that eight lanes' reads
+// fall into different banks without padding (which would leave room for one
+// workgroup a CU instead of two).
+template <int W> __device__ __forceinline__ int swizzled(int row, int pos) {
+  const int f = W >= 64 ? (row ^ row >> 3) & 7 : row >> 2 & 3;
+  return row * W + (((pos >> 3) ^ f) << 3 | (pos & 7));
+}
+
+// Step sizes of a sub-chunk: dt_s, c_s, exp(c_s), exp(c_63 - c_s) dt_s, exp(c_63).
+struct HeadSteps {
+  float dt[kSub], cum[kSub], grow[kSub], weight[kSub], decay;
+};
+
 template <int N> struct HeadLds {
   static constexpr int NP = N < 32 ? 32 : N;      // the products over N take 32 at a time; what is past N is 0
-  static constexpr int kRow = NP + 8;             // rows 16 bytes longer: 8 lanes' 16-byte reads cover all banks
-  static constexpr int kTok = kSub + 8;
-  union {
-    unsigned short B[kSub][kRow];                 // [s][n position]
-    unsigned short M[2][kSub][kTok];              // scores, two planes: [t][s position]
-  };
-  unsigned short C[kSub][kRow];                   // [t][n position]
+  static constexpr int kTok = kSub + 8;           // rows 16 bytes longer, for the same purpose
+  unsigned short B[kSub * NP];                    // [s][n position]
+  unsigned short C[kSub * NP];                    // [t][n position]
+  unsigned short M[2][kSub * kSub];               // scores, two planes: [t][s position]
   unsigned short BT[N][kTok];                     // [n][s position]
   unsigned short xT[64][kTok];                    // [channel][s position]
-  float dt[kSub], cum[kSub], grow[kSub], weight[kSub];   // dt_s, c_t, exp(c_t), exp(c_63 - c_s) dt_s
-  float decay;                                    // exp(c_63)
+  HeadSteps steps[2];
 };
+
+// Inclusive sum over the lanes of a wave.
+__device__ __forceinline__ float lane_sums(float v) {
+  auto shifted = [](float x, auto ctrl, auto rows) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value,
+                                                                 decltype(rows)::value, 0xf, false));
+  };
+  typedef std::integral_constant<int, 0xf> All;
+  v += shifted(v, std::integral_constant<int, 0x111>{}, All{});      // from 1, 2, 4, 8 lanes below in a row of 16
+  v += shifted(v, std::integral_constant<int, 0x112>{}, All{});
+  v += shifted(v, std::integral_constant<int, 0x114>{}, All{});
+  v += shifted(v, std::integral_constant<int, 0x118>{}, All{});
+  v += shifted(v, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // lane 15 to the row above
+  v += shifted(v, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // lane 31 to the upper half
+  return v;
+}
+
+// A lane is a token.  The state's weights come from a sum from the end: those
+// near the end, which count most, are sums of few terms.  Returns the sum of dt.
+__device__ __forceinline__ float put_steps(HeadSteps &to, int lane, float dt, float A2) {
+  const float up = lane_sums(dt * A2);
+  const float rev = __shfl(dt, 63 - lane);
+  const float down = lane_sums(rev * A2);         // of tokens 63 - lane and on
+  const float after = __shfl_up(down, 1);
+  to.dt[lane] = dt;
+  to.cum[lane] = up;
+  to.grow[lane] = fast_exp2(up);
+  to.weight[63 - lane] = fast_exp2(lane == 0 ? 0.0f : after) * rev;
+  if (lane == 63) to.decay = fast_exp2(down);
+  return __shfl(lane_sums(dt), 63);
+}
 
 __device__ __forceinline__ bf16x8v lds8(const unsigned short *p) { return __builtin_bit_cast(bf16x8v, *(const u32x4v *)p); }
 
-// Eight elements of a row, as one load where the address allows it.
-__device__ __forceinline__ u32x4v load8(const bf16_t *p, bool wide) {
-  if (wide) return *(const u32x4v *)p;
+// Eight elements of a row: one load where every row starts at a 16-byte boundary.
+template <bool WIDE> __device__ __forceinline__ u32x4v load8(const bf16_t *p) {
+  if constexpr (WIDE) return *(const u32x4v *)p;
   const unsigned short *s = (const unsigned short *)p;
   u32x4v r;
 #pragma unroll
@@ -96,9 +144,8 @@ __device__ __forceinline__ unsigned int pair_of(const u32x4v &a, const u32x4v &b
 
 // PART as for the channel scan: 0 whole sequences, 1 a segment's state from
 // zero, 2 outputs from the state that enters it.
-template <int N, int PART>
-__global__ void __launch_bounds__(kHeadThreads, 2) head_mfma_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w,
-                                                                    int Q, int wide) {
+template <int N, int PART, bool WIDE>
+__global__ void __launch_bounds__(kHeadThreads, 2) head_mfma_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w, int Q) {
   typedef HeadLds<N> Lds;
   constexpr int NT = N / 16, NB = Lds::NP / 32;
   constexpr int OL = N / 8 < 4 ? N / 8 : 4;                       // octets of a row that neighbouring lanes take
@@ -143,151 +190,135 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma_kernel(cortex_scan_
   const float A2 = a.A[head] * kLog2e, bias = a.dt_bias ? a.dt_bias[head] : 0.0f, skip = a.skip ? a.skip[head] : 0.0f;
   const bf16_t *xs = (const bf16_t *)a.x + head * P + p0, *ds = (const bf16_t *)a.dt + head;
   const bf16_t *Bs = (const bf16_t *)a.B + g * N, *Cs = (const bf16_t *)a.C + g * N;
-  const bf16_t *zs = a.z ? (const bf16_t *)a.z + d : nullptr;
-  bf16_t *ys = (bf16_t *)a.y + d;
+  const int ch = head * P + (works ? pw : 0) + q * 4;             // the lane's four channels of y and z
+  const bf16_t *zs = a.z ? (const bf16_t *)a.z + ch : nullptr;
+  bf16_t *ys = (bf16_t *)a.y + ch;
   float steps = 0.0f;
 
-  // What the next sub-chunk needs, loaded while this one is worked on.  Tokens
-  // past the segment's end are zeros, with no step.
+  // What the next sub-chunk needs, loaded while this one is worked on.  The loads
+  // are unconditional, so that nothing waits for one of them: tokens past the
+  // segment's end repeat the last one, and are made zeros when they are stored.
   u32x4v xr[2], br[kItems][2], cr[kItems][2];
   float raw = 0.0f;
   const u32x4v none = {0, 0, 0, 0};
+  const int xo = (tid & 3) | (tid >> 7) << 2, xp = 2 * (tid >> 2 & 31);
+  auto item_octet = [&](int i) { return tid % OL + (i * kHeadThreads + tid) / (OL * 32) * OL; };
+  auto item_token = [&](int i) { return 2 * ((i * kHeadThreads + tid) / OL % 32); };
   auto fetch = [&](int t0) {
-    const int xo = tid & 3 | tid >> 7 << 2, xp = tid >> 2 & 31;
+    const bf16_t *px = xs + (p0 + xo * 8 < P ? xo * 8 : 0);
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const int64_t t = t0 + 2 * xp + r;
-      xr[r] = t < end && p0 + xo * 8 < P ? load8(xs + t * a.x_ld + xo * 8, wide & 1) : none;
-    }
+    for (int r = 0; r < 2; ++r) xr[r] = load8<WIDE>(px + (int64_t)min(t0 + xp + r, end - 1) * a.x_ld);
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-      const int id = i * kHeadThreads + tid, o = id % OL + id / (OL * 32) * OL, sp = id / OL % 32;
+      const int o = min(item_octet(i), N / 8 - 1);
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        const int64_t t = t0 + 2 * sp + r;
-        const bool in = t < end && o < N / 8;
-        br[i][r] = in ? load8(Bs + t * a.B_ld + o * 8, wide & 2) : none;
-        if (PART != 1) cr[i][r] = in ? load8(Cs + t * a.C_ld + o * 8, wide & 4) : none;
+        const int64_t t = min(t0 + item_token(i) + r, end - 1);
+        br[i][r] = load8<WIDE>(Bs + t * a.B_ld + o * 8);
+        if (PART != 1) cr[i][r] = load8<WIDE>(Cs + t * a.C_ld + o * 8);
       }
     }
-    raw = t0 + lane < end ? to_float<bf16_t>(ds[(int64_t)(t0 + lane) * a.dt_ld]) : 0.0f;
+    if (wave == 3) raw = to_float<bf16_t>(ds[(int64_t)min(t0 + lane, end - 1) * a.dt_ld]);
   };
   // Rows of eight state entries (octet o) in k order: two halves of 8 bytes.
-  auto put_row = [&](unsigned short *to, int o, const u32x4v &v) {
-    const int e = o * 8;
-    *(uint2 *)(to + k_position(e)) = make_uint2(v[0], v[1]);
-    *(uint2 *)(to + k_position(e + 4)) = make_uint2(v[2], v[3]);
+  auto put_row = [&](unsigned short *to, int row, int o, const u32x4v &v) {
+    *(uint2 *)(to + swizzled<Lds::NP>(row, k_position(o * 8))) = make_uint2(v[0], v[1]);
+    *(uint2 *)(to + swizzled<Lds::NP>(row, k_position(o * 8 + 4))) = make_uint2(v[2], v[3]);
   };
   if constexpr (N < 32)
     for (int i = tid; i < kSub * (Lds::NP - N) / 4; i += kHeadThreads) {
       const int s = i / ((Lds::NP - N) / 4), e = N + i % ((Lds::NP - N) / 4) * 4;
-      *(uint2 *)&lds.C[s][k_position(e)] = make_uint2(0, 0);
+      *(uint2 *)&lds.B[swizzled<Lds::NP>(s, k_position(e))] = make_uint2(0, 0);
+      *(uint2 *)&lds.C[swizzled<Lds::NP>(s, k_position(e))] = make_uint2(0, 0);
     }
+  // the tiles above the diagonal that a product over 32 tokens reaches: (0,1) and (2,3)
+  if (PART != 1) {
+    const int t = (tid >> 7) * 32 + (tid & 15), s = (tid >> 7) * 32 + 16 + (tid >> 4 & 3) * 4;
+    *(uint2 *)&lds.M[tid >> 6 & 1][swizzled<kSub>(t, k_position(s))] = make_uint2(0, 0);
+  }
 
-  if (begin < end) fetch(begin);
+  if (begin < end) {
+    fetch(begin);
+    if (wave == 3) steps += put_steps(lds.steps[0], lane, begin + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
+  }
+  int buf = 0;
 #pragma unroll 1
-  for (int t0 = begin; t0 < end; t0 += kSub) {
+  for (int t0 = begin; t0 < end; t0 += kSub, buf ^= 1) {
     __syncthreads();                             // everyone is done with the last sub-chunk's LDS
-    {
-      const int xo = tid & 3 | tid >> 7 << 2, xp = k_position(2 * (tid >> 2 & 31));
+    if (t0 + kSub > end) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) *(unsigned int *)&lds.xT[xo * 8 + i][xp] = pair_of(xr[0], xr[1], i);
+      for (int r = 0; r < 2; ++r) {
+        if (t0 + xp + r >= end) xr[r] = none;
+#pragma unroll
+        for (int i = 0; i < kItems; ++i)
+          if (t0 + item_token(i) + r >= end) {
+            br[i][r] = none;
+            if (PART != 1) cr[i][r] = none;
+          }
+      }
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) *(unsigned int *)&lds.xT[xo * 8 + i][k_position(xp)] = pair_of(xr[0], xr[1], i);
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-      const int id = i * kHeadThreads + tid, o = id % OL + id / (OL * 32) * OL, s = id / OL % 32 * 2;
+      const int o = item_octet(i), s = item_token(i);
       if (o < N / 8) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) *(unsigned int *)&lds.BT[o * 8 + k][k_position(s)] = pair_of(br[i][0], br[i][1], k);
         if (PART != 1) {
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
-            put_row(lds.B[s + r], o, br[i][r]);
-            put_row(lds.C[s + r], o, cr[i][r]);
+            put_row(lds.B, s + r, o, br[i][r]);
+            put_row(lds.C, s + r, o, cr[i][r]);
           }
         }
-      }
-    }
-    if constexpr (PART != 1 && N < 32)                     // the scores were here
-      for (int i = tid; i < kSub * (Lds::NP - N) / 4; i += kHeadThreads) {
-        const int s = i / ((Lds::NP - N) / 4), e = N + i % ((Lds::NP - N) / 4) * 4;
-        *(uint2 *)&lds.B[s][k_position(e)] = make_uint2(0, 0);
-      }
-    if (wave == 0) {
-      // a lane is a token.  The weights of the state come from a sum from the
-      // end: those near the end, which count most, are sums of few terms
-      const float dt = t0 + lane < end ? step_size(a, raw, bias) : 0.0f;
-      const float la = dt * A2;
-      float up = la, down = la;
-#pragma unroll
-      for (int m = 1; m < 64; m <<= 1) {
-        const float u = __shfl_up(up, m), v = __shfl_down(down, m);
-        if (lane >= m) up += u;
-        if (lane + m < 64) down += v;
-      }
-      const float after = __shfl_down(down, 1);
-      lds.dt[lane] = dt;
-      lds.cum[lane] = up;
-      lds.grow[lane] = fast_exp2(up);
-      lds.weight[lane] = fast_exp2(lane == 63 ? 0.0f : after) * dt;
-      if (lane == 0) lds.decay = fast_exp2(down);
-      if (PART == 1) {
-        float sum = dt;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
-        steps += sum;
       }
     }
     __syncthreads();
     if (t0 + kSub < end) fetch(t0 + kSub);
+    const HeadSteps &st = lds.steps[buf];
 
     if constexpr (PART != 1) {
-      bf16_t zr[4][4];
+      uint2 zr[4];
       if (zs && works)
 #pragma unroll
-        for (int ti = 0; ti < 4; ++ti)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int64_t t = t0 + ti * 16 + q * 4 + i;
-            zr[ti][i] = t < end ? zs[t * a.z_ld] : (bf16_t)0.0f;
+        for (int ti = 0; ti < 4; ++ti) {
+          const bf16_t *p = zs + (int64_t)min(t0 + ti * 16 + l16, end - 1) * a.z_ld;
+          if constexpr (WIDE) {
+            zr[ti] = *(const uint2 *)p;
+          } else {
+            const unsigned short *e = (const unsigned short *)p;
+            zr[ti] = make_uint2(e[0] | (unsigned int)e[1] << 16, e[2] | (unsigned int)e[3] << 16);
           }
-      // Scores: 10 tiles of 16 x 16 on and below the diagonal, and the two above it that a
-      // product over 32 tokens reaches: three a wave.
-      u16x4 m0[3], m1[3];
+        }
+      // Scores: 10 tiles of 16 x 16 on and below the diagonal, three or two a wave.
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
-        const int id = wave + 4 * k;
-        // (0,0) (1,0) (1,1) (2,0) (2,1) (2,2) (3,0) (3,1) (3,2) (3,3), then (0,1) (2,3)
-        const int ti = id < 1 ? 0 : id < 3 ? 1 : id < 6 ? 2 : id < 10 ? 3 : id == 10 ? 0 : 2;
-        const int si = id < 10 ? id - ti * (ti + 1) / 2 : id == 10 ? 1 : 3;
-        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+        const int id = wave + 4 * k;             // (0,0) (1,0) (1,1) (2,0) (2,1) (2,2) (3,0) (3,1) (3,2) (3,3)
+        const int ti = id < 1 ? 0 : id < 3 ? 1 : id < 6 ? 2 : 3, si = id - ti * (ti + 1) / 2;
         if (id < 10) {
+          f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
           for (int m = 0; m < NB; ++m)
-            acc = mfma_bf16x32(lds8(&lds.B[si * 16 + l16][m * 32 + q * 8]), lds8(&lds.C[ti * 16 + l16][m * 32 + q * 8]), acc);
+            acc = mfma_bf16x32(lds8(&lds.B[swizzled<Lds::NP>(si * 16 + l16, m * 32 + q * 8)]),
+                               lds8(&lds.C[swizzled<Lds::NP>(ti * 16 + l16, m * 32 + q * 8)]), acc);
           const int t = ti * 16 + l16, s = si * 16 + q * 4;
-          const float ct = lds.cum[t];
-          const f32x4 cs = *(const f32x4 *)&lds.cum[s], dt = *(const f32x4 *)&lds.dt[s];
+          const float ct = st.cum[t];
+          const f32x4 cs = *(const f32x4 *)&st.cum[s], dt = *(const f32x4 *)&st.dt[s];
+          float v[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[i] = s + i <= t ? acc[i] * (fast_exp2(ct - cs[i]) * dt[i]) : 0.0f;
+          for (int i = 0; i < 4; ++i) {
+            v[i] = s + i <= t ? acc[i] * (fast_exp2(ct - cs[i]) * dt[i]) : 0.0f;
+            if (s + i == t) v[i] += skip;
+          }
+          __bf16 b[4];
+          plane(v, b);
+          *(u16x4 *)&lds.M[0][swizzled<kSub>(t, k_position(s))] = __builtin_bit_cast(u16x4, b);
+          plane(v, b);
+          *(u16x4 *)&lds.M[1][swizzled<kSub>(t, k_position(s))] = __builtin_bit_cast(u16x4, b);
         }
-        float v[4] = {acc[0], acc[1], acc[2], acc[3]};
-        __bf16 b[4];
-        plane(v, b);
-        m0[k] = __builtin_bit_cast(u16x4, b);
-        plane(v, b);
-        m1[k] = __builtin_bit_cast(u16x4, b);
       }
-      __syncthreads();                           // B's rows are read
-#pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        const int id = wave + 4 * k;
-        const int ti = id < 1 ? 0 : id < 3 ? 1 : id < 6 ? 2 : id < 10 ? 3 : id == 10 ? 0 : 2;
-        const int si = id < 10 ? id - ti * (ti + 1) / 2 : id == 10 ? 1 : 3;
-        *(u16x4 *)&lds.M[0][ti * 16 + l16][k_position(si * 16 + q * 4)] = m0[k];
-        *(u16x4 *)&lds.M[1][ti * 16 + l16][k_position(si * 16 + q * 4)] = m1[k];
-      }
-      // From the state: rows t, columns channels.
+      // From the state: rows channels, columns t.
       f32x4 y[4];
 #pragma unroll
       for (int ti = 0; ti < 4; ++ti) y[ti] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -307,17 +338,13 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma_kernel(cortex_scan_
           const bf16x8v lo = pack8(b);
 #pragma unroll
           for (int ti = 0; ti < 4; ++ti) {
-            const bf16x8v c = lds8(&lds.C[ti * 16 + l16][m * 32 + q * 8]);
-            y[ti] = mfma_bf16x32(c, lo, y[ti]);
-            y[ti] = mfma_bf16x32(c, hi, y[ti]);
+            const bf16x8v c = lds8(&lds.C[swizzled<Lds::NP>(ti * 16 + l16, m * 32 + q * 8)]);
+            y[ti] = mfma_bf16x32(lo, c, y[ti]);
+            y[ti] = mfma_bf16x32(hi, c, y[ti]);
           }
         }
 #pragma unroll
-        for (int ti = 0; ti < 4; ++ti) {
-          const f32x4 e = *(const f32x4 *)&lds.grow[ti * 16 + q * 4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) y[ti][i] *= e[i];
-        }
+        for (int ti = 0; ti < 4; ++ti) y[ti] *= st.grow[ti * 16 + l16];
       }
       __syncthreads();                           // the scores are there
       if (works) {
@@ -332,8 +359,10 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma_kernel(cortex_scan_
         }
         // The products with the zeros above the diagonal would carry such an input to the tokens
         // before it.  It is left out of them, and its channel's tokens from its own on become NaN.
-        int first_odd = kSub;
-        if (__any(odd != 0)) {
+        const bool any_odd = __any(odd != 0);
+        int first_odd[4] = {kSub, kSub, kSub, kSub};
+        if (any_odd) {
+          int first = kSub;
 #pragma unroll
           for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -341,43 +370,54 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma_kernel(cortex_scan_
               const float v = (float)x[kb][j];
               if (!(__builtin_fabsf(v) < __builtin_inff())) {
                 const int s = kb * 32 + (j < 4 ? 0 : 12) + q * 4 + j;
-                first_odd = s < first_odd ? s : first_odd;
+                first = s < first ? s : first;
                 x[kb][j] = (__bf16)0.0f;
               }
             }
-          first_odd = min(first_odd, __shfl_xor(first_odd, 16));
-          first_odd = min(first_odd, __shfl_xor(first_odd, 32));
+          first = min(first, __shfl_xor(first, 16));
+          first = min(first, __shfl_xor(first, 32));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) first_odd[i] = __shfl(first, q * 4 + i);
         }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int ti = 2 * kb; ti < 4; ++ti) {
-            y[ti] = mfma_bf16x32(lds8(&lds.M[1][ti * 16 + l16][kb * 32 + q * 8]), x[kb], y[ti]);
-            y[ti] = mfma_bf16x32(lds8(&lds.M[0][ti * 16 + l16][kb * 32 + q * 8]), x[kb], y[ti]);
-          }
+          for (int ti = 0; ti < 4; ++ti)
+            if (ti >= 2 * kb) {
+              y[ti] = mfma_bf16x32(x[kb], lds8(&lds.M[1][swizzled<kSub>(ti * 16 + l16, kb * 32 + q * 8)]), y[ti]);
+              y[ti] = mfma_bf16x32(x[kb], lds8(&lds.M[0][swizzled<kSub>(ti * 16 + l16, kb * 32 + q * 8)]), y[ti]);
+            }
 #pragma unroll
         for (int ti = 0; ti < 4; ++ti) {
-          const u16x4 xv = *(const u16x4 *)&lds.xT[wave * 16 + l16][k_position(ti * 16 + q * 4)];
+          const int t = t0 + ti * 16 + l16;
+          float v[4] = {y[ti][0], y[ti][1], y[ti][2], y[ti][3]};
+          if (any_odd)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int64_t t = t0 + ti * 16 + q * 4 + i;
-            const unsigned short xb = xv[i];
-            float v = __builtin_fmaf(skip, to_float<bf16_t>(__builtin_bit_cast(bf16_t, xb)), y[ti][i]);
-            if (ti * 16 + q * 4 + i >= first_odd) v = __builtin_nanf("");
-            if (zs) v *= silu(to_float<bf16_t>(zr[ti][i]));
-            if (t < end) ys[t * a.y_ld] = from_float<bf16_t>(v);
+            for (int i = 0; i < 4; ++i) v[i] = ti * 16 + l16 >= first_odd[i] ? __builtin_nanf("") : v[i];
+          if (zs) {
+            v[0] *= silu(__builtin_bit_cast(float, zr[ti].x << 16));
+            v[1] *= silu(__builtin_bit_cast(float, zr[ti].x & 0xffff0000u));
+            v[2] *= silu(__builtin_bit_cast(float, zr[ti].y << 16));
+            v[3] *= silu(__builtin_bit_cast(float, zr[ti].y & 0xffff0000u));
+          }
+          if (t < end) {
+            bf16_t *p = ys + (int64_t)t * a.y_ld;
+            if constexpr (WIDE) Pack<bf16_t, 4>::store(p, v);
+            else
+#pragma unroll
+              for (int i = 0; i < 4; ++i) p[i] = from_float<bf16_t>(v[i]);
           }
         }
       }
     }
     if (works) {
-      const float decay = lds.decay;
+      const float decay = st.decay;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) h[nt] *= decay;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
         const bf16x8v x = lds8(&lds.xT[wave * 16 + l16][kb * 32 + q * 8]);
-        const f32x4 w0 = *(const f32x4 *)&lds.weight[kb * 32 + q * 4], w1 = *(const f32x4 *)&lds.weight[kb * 32 + 16 + q * 4];
+        const f32x4 w0 = *(const f32x4 *)&st.weight[kb * 32 + q * 4], w1 = *(const f32x4 *)&st.weight[kb * 32 + 16 + q * 4];
         float v[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -400,8 +440,10 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma_kernel(cortex_scan_
         }
       }
     }
+    if (wave == 3 && t0 + kSub < end)
+      steps += put_steps(lds.steps[buf ^ 1], lane, t0 + kSub + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
   }
-  if (PART == 1 && tid == 0 && p0 == 0) w.steps[(int64_t)slot * heads + head] = steps;
+  if (PART == 1 && tid == 192 && p0 == 0) w.steps[(int64_t)slot * heads + head] = steps;
   float *h_out = PART == 1 ? w.state + ((int64_t)slot * a.channels + d) * N
                            : PART == 0 && row >= 0 && a.state_out ? a.state_out + ((int64_t)row * a.channels + d) * N : nullptr;
   if (works && h_out)

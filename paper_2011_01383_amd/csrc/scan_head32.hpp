@@ -17,22 +17,41 @@ namespace cortex {
 
 constexpr int kSub32 = 32;
 
+struct HeadSteps32 {
+  float dt[kSub32], cum[kSub32], grow[kSub32], weight[kSub32], decay;
+};
+
 template <int N> struct HeadLds32 {
   float B[kSub32][N + 4];        // rows 16 bytes longer: see the bf16 form
   float C[kSub32][N + 4];
   float x[kSub32][64 + 4];
   float M[kSub32][kSub32 + 4];   // scores [t][s]
-  float dt[kSub32], cum[kSub32], grow[kSub32], weight[kSub32];
-  float decay;
+  HeadSteps32 steps[2];
 };
 
-__device__ __forceinline__ float4 load4f(const float *p, bool wide) {
-  return wide ? *(const float4 *)p : make_float4(p[0], p[1], p[2], p[3]);
+// As put_steps, over 32 tokens; the lanes above them hold a step of 0.
+__device__ __forceinline__ float put_steps32(HeadSteps32 &to, int lane, float dt, float A2) {
+  const float up = lane_sums(dt * A2);
+  const float rev = __shfl(dt, 31 - lane & 63);
+  const float down = lane_sums(lane < 32 ? rev * A2 : 0.0f);
+  const float after = __shfl_up(down, 1);
+  if (lane < 32) {
+    to.dt[lane] = dt;
+    to.cum[lane] = up;
+    to.grow[lane] = fast_exp2(up);
+    to.weight[31 - lane] = fast_exp2(lane == 0 ? 0.0f : after) * rev;
+  }
+  if (lane == 31) to.decay = fast_exp2(down);
+  return __shfl(lane_sums(dt), 63);
 }
 
-template <int N, int PART>
-__global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w,
-                                                                      int Q, int wide) {
+template <bool WIDE> __device__ __forceinline__ float4 load4f(const float *p) {
+  if constexpr (WIDE) return *(const float4 *)p;
+  return make_float4(p[0], p[1], p[2], p[3]);
+}
+
+template <int N, int PART, bool WIDE>
+__global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w, int Q) {
   constexpr int NT = N / 16, kItems = (N / 4 * kSub32 + kHeadThreads - 1) / kHeadThreads;
   __shared__ HeadLds32<N> lds;
   if (load_status(status) != 0) return;
@@ -74,75 +93,58 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
   const float A2 = a.A[head] * kLog2e, bias = a.dt_bias ? a.dt_bias[head] : 0.0f, skip = a.skip ? a.skip[head] : 0.0f;
   const float *xs = (const float *)a.x + head * P + p0, *ds = (const float *)a.dt + head;
   const float *Bs = (const float *)a.B + g * N, *Cs = (const float *)a.C + g * N;
-  const float *zs = a.z ? (const float *)a.z + d : nullptr;
-  float *ys = (float *)a.y + d;
+  const int ch = head * P + (works ? pw : 0) + q * 4;
+  const float *zs = a.z ? (const float *)a.z + ch : nullptr;
+  float *ys = (float *)a.y + ch;
   float steps = 0.0f;
 
   const float4 none = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   float4 xr[2], br[kItems], cr[kItems];
   float raw = 0.0f;
-  auto fetch = [&](int t0) {
+  auto fetch = [&](int t0) {                      // as in the bf16 form
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int id = i * kHeadThreads + tid, c = id % 16 * 4;
-      const int64_t t = t0 + id / 16;
-      xr[i] = t < end && p0 + c < P ? load4f(xs + t * a.x_ld + c, wide & 1) : none;
+      const int id = i * kHeadThreads + tid, c = p0 + id % 16 * 4 < P ? id % 16 * 4 : 0;
+      xr[i] = load4f<WIDE>(xs + (int64_t)min(t0 + id / 16, end - 1) * a.x_ld + c);
     }
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
       const int id = i * kHeadThreads + tid, c = id % (N / 4) * 4;
-      const int64_t t = t0 + id / (N / 4);
-      const bool in = t < end && id < N / 4 * kSub32;
-      br[i] = in ? load4f(Bs + t * a.B_ld + c, wide & 2) : none;
-      if (PART != 1) cr[i] = in ? load4f(Cs + t * a.C_ld + c, wide & 4) : none;
+      const int64_t t = min(t0 + id / (N / 4), end - 1);
+      br[i] = load4f<WIDE>(Bs + t * a.B_ld + c);
+      if (PART != 1) cr[i] = load4f<WIDE>(Cs + t * a.C_ld + c);
     }
-    raw = lane < kSub32 && t0 + lane < end ? ds[(int64_t)(t0 + lane) * a.dt_ld] : 0.0f;
+    if (wave == 3) raw = ds[(int64_t)min(t0 + lane, end - 1) * a.dt_ld];
+  };
+  auto next_steps = [&](int t0, int buf) {
+    steps += put_steps32(lds.steps[buf], lane, lane < kSub32 && t0 + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
   };
 
-  if (begin < end) fetch(begin);
+  if (begin < end) {
+    fetch(begin);
+    if (wave == 3) next_steps(begin, 0);
+  }
+  int buf = 0;
 #pragma unroll 1
-  for (int t0 = begin; t0 < end; t0 += kSub32) {
+  for (int t0 = begin; t0 < end; t0 += kSub32, buf ^= 1) {
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int id = i * kHeadThreads + tid;
-      *(float4 *)&lds.x[id / 16][id % 16 * 4] = xr[i];
+      *(float4 *)&lds.x[id / 16][id % 16 * 4] = t0 + id / 16 < end ? xr[i] : none;
     }
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
       const int id = i * kHeadThreads + tid;
+      const bool in = t0 + id / (N / 4) < end;
       if (id < N / 4 * kSub32) {
-        *(float4 *)&lds.B[id / (N / 4)][id % (N / 4) * 4] = br[i];
-        if (PART != 1) *(float4 *)&lds.C[id / (N / 4)][id % (N / 4) * 4] = cr[i];
-      }
-    }
-    if (wave == 0) {
-      const float dt = lane < kSub32 && t0 + lane < end ? step_size(a, raw, bias) : 0.0f;
-      const float la = dt * A2;
-      float up = la, down = la;                  // from the start, and from the end: see the bf16 form
-#pragma unroll
-      for (int m = 1; m < kSub32; m <<= 1) {
-        const float u = __shfl_up(up, m), v = __shfl_down(down, m);
-        if (lane >= m) up += u;
-        if (lane + m < kSub32) down += v;
-      }
-      const float after = __shfl_down(down, 1);
-      if (lane < kSub32) {
-        lds.dt[lane] = dt;
-        lds.cum[lane] = up;
-        lds.grow[lane] = fast_exp2(up);
-        lds.weight[lane] = fast_exp2(lane == kSub32 - 1 ? 0.0f : after) * dt;
-      }
-      if (lane == 0) lds.decay = fast_exp2(down);
-      if (PART == 1) {
-        float sum = dt;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
-        steps += sum;
+        *(float4 *)&lds.B[id / (N / 4)][id % (N / 4) * 4] = in ? br[i] : none;
+        if (PART != 1) *(float4 *)&lds.C[id / (N / 4)][id % (N / 4) * 4] = in ? cr[i] : none;
       }
     }
     __syncthreads();
     if (t0 + kSub32 < end) fetch(t0 + kSub32);
+    const HeadSteps32 &st = lds.steps[buf];
 
     // the wave's channels of x, by sixteen tokens: k = 4 q + i
     float x[2][4];
@@ -152,15 +154,10 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
       for (int i = 0; i < 4; ++i) x[si][i] = lds.x[si * 16 + q * 4 + i][wave * 16 + l16];
 
     if constexpr (PART != 1) {
-      float zr[2][4];
+      float4 zr[2];
       if (zs && works)
 #pragma unroll
-        for (int ti = 0; ti < 2; ++ti)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int64_t t = t0 + ti * 16 + q * 4 + i;
-            zr[ti][i] = t < end ? zs[t * a.z_ld] : 0.0f;
-          }
+        for (int ti = 0; ti < 2; ++ti) zr[ti] = load4f<WIDE>(zs + (int64_t)min(t0 + ti * 16 + l16, end - 1) * a.z_ld);
       if (wave < 3) {                            // tiles (0,0) (1,0) (1,1) of the scores
         const int ti = wave > 0, si = wave > 1;
         f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -168,10 +165,13 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
         for (int m = 0; m < NT; ++m)
           acc = mfma_k16(*(const float4 *)&lds.B[si * 16 + l16][m * 16 + q * 4], *(const float4 *)&lds.C[ti * 16 + l16][m * 16 + q * 4], acc);
         const int t = ti * 16 + l16, s = si * 16 + q * 4;
-        const float ct = lds.cum[t];
-        const f32x4 cs = *(const f32x4 *)&lds.cum[s], dt = *(const f32x4 *)&lds.dt[s];
+        const float ct = st.cum[t];
+        const f32x4 cs = *(const f32x4 *)&st.cum[s], dt = *(const f32x4 *)&st.dt[s];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] = s + i <= t ? acc[i] * (fast_exp2(ct - cs[i]) * dt[i]) : 0.0f;
+        for (int i = 0; i < 4; ++i) {
+          acc[i] = s + i <= t ? acc[i] * (fast_exp2(ct - cs[i]) * dt[i]) : 0.0f;
+          if (s + i == t) acc[i] += skip;
+        }
         *(f32x4 *)&lds.M[t][s] = acc;
       }
       f32x4 y[2];
@@ -182,10 +182,10 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
         for (int nt = 0; nt < NT; ++nt) {
           const float4 hv = make_float4(h[nt][0], h[nt][1], h[nt][2], h[nt][3]);
 #pragma unroll
-          for (int ti = 0; ti < 2; ++ti) y[ti] = mfma_k16(*(const float4 *)&lds.C[ti * 16 + l16][nt * 16 + q * 4], hv, y[ti]);
+          for (int ti = 0; ti < 2; ++ti) y[ti] = mfma_k16(hv, *(const float4 *)&lds.C[ti * 16 + l16][nt * 16 + q * 4], y[ti]);
         }
 #pragma unroll
-        for (int ti = 0; ti < 2; ++ti) y[ti] *= *(const f32x4 *)&lds.grow[ti * 16 + q * 4];
+        for (int ti = 0; ti < 2; ++ti) y[ti] *= st.grow[ti * 16 + l16];
       }
       __syncthreads();                           // the scores are there
       if (works) {
@@ -206,28 +206,42 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
 #pragma unroll
         for (int si = 0; si < 2; ++si)
 #pragma unroll
-          for (int ti = si; ti < 2; ++ti)
-            y[ti] = mfma_k16(*(const float4 *)&lds.M[ti * 16 + l16][si * 16 + q * 4],
-                             make_float4(xf[si][0], xf[si][1], xf[si][2], xf[si][3]), y[ti]);
-#pragma unroll
-        for (int ti = 0; ti < 2; ++ti)
+          for (int ti = 0; ti < 2; ++ti)
+            if (ti >= si)
+              y[ti] = mfma_k16(make_float4(xf[si][0], xf[si][1], xf[si][2], xf[si][3]),
+                               *(const float4 *)&lds.M[ti * 16 + l16][si * 16 + q * 4], y[ti]);
+        if (__any(first_odd < kSub32)) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int64_t t = t0 + ti * 16 + q * 4 + i;
-            float v = __builtin_fmaf(skip, x[ti][i], y[ti][i]);
-            if (ti * 16 + q * 4 + i >= first_odd) v = __builtin_nanf("");
-            if (zs) v *= silu(zr[ti][i]);
-            if (t < end) ys[t * a.y_ld] = v;
+            const int odd = __shfl(first_odd, q * 4 + i);
+#pragma unroll
+            for (int ti = 0; ti < 2; ++ti)
+              if (ti * 16 + l16 >= odd) y[ti][i] = __builtin_nanf("");
           }
+        }
+#pragma unroll
+        for (int ti = 0; ti < 2; ++ti) {
+          const int t = t0 + ti * 16 + l16;
+          float4 v = make_float4(y[ti][0], y[ti][1], y[ti][2], y[ti][3]);
+          if (zs) v = make_float4(v.x * silu(zr[ti].x), v.y * silu(zr[ti].y), v.z * silu(zr[ti].z), v.w * silu(zr[ti].w));
+          if (t < end) {
+            float *p = ys + (int64_t)t * a.y_ld;
+            if constexpr (WIDE) {
+              *(float4 *)p = v;
+            } else {
+              p[0] = v.x; p[1] = v.y; p[2] = v.z; p[3] = v.w;
+            }
+          }
+        }
       }
     }
     if (works) {
-      const float decay = lds.decay;
+      const float decay = st.decay;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) h[nt] *= decay;
 #pragma unroll
       for (int si = 0; si < 2; ++si) {
-        const f32x4 ws = *(const f32x4 *)&lds.weight[si * 16 + q * 4];
+        const f32x4 ws = *(const f32x4 *)&st.weight[si * 16 + q * 4];
         const float4 xw = make_float4(x[si][0] * ws[0], x[si][1] * ws[1], x[si][2] * ws[2], x[si][3] * ws[3]);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -236,8 +250,9 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
         }
       }
     }
+    if (wave == 3 && t0 + kSub32 < end) next_steps(t0 + kSub32, buf ^ 1);
   }
-  if (PART == 1 && tid == 0 && p0 == 0) w.steps[(int64_t)slot * heads + head] = steps;
+  if (PART == 1 && tid == 192 && p0 == 0) w.steps[(int64_t)slot * heads + head] = steps;
   float *h_out = PART == 1 ? w.state + ((int64_t)slot * a.channels + d) * N
                            : PART == 0 && row >= 0 && a.state_out ? a.state_out + ((int64_t)row * a.channels + d) * N : nullptr;
   if (works && h_out)
