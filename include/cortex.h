@@ -433,9 +433,9 @@ int cortex_scan_step(const cortex_scan_t *args, int32_t *d_status, void *stream)
  * Each output may be NULL.  A masked entry's logit is never used, whatever it
  * holds.  A row of the mask is ceil(V / 32) words, bit i % 32 of word i / 32 set
  * where i is allowed; mask_index[b] = -1 is a row without a mask.
- * A token outside [0, V), a length outside [0, history_cap] (the prompt's: outside
- * [0, the history's]), a mask index outside [-1, mask_rows) or bias offsets that
- * do not rise from 0 to num_biases set CORTEX_ST_INPUT_RANGE.
+ * A row has at most 65,535 biases.  A token outside [0, V), a length outside [0, history_cap] (the prompt's: outside
+ * [0, the history's]), a mask index outside [-1, mask_rows) bias offsets that do
+ * not rise from 0 to num_biases or too many of them set CORTEX_ST_INPUT_RANGE.
  */
 typedef struct {
   int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: logits and out */

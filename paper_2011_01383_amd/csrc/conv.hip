@@ -14,7 +14,7 @@ constexpr int kConvThreads = 64;
 
 template <typename T, int W, int V, bool STEP>
 __global__ void __launch_bounds__(kConvThreads) conv_kernel(cortex_conv_t a, int32_t *status) {
-  if (load_status(status) != 0) return;
+  if (entry_status(status) != 0) return;
   const int slot = (int)blockIdx.x;
   Chunk c;
   if constexpr (STEP) {

@@ -2,20 +2,32 @@
 // penalties from the text so far, biases, the grammar's mask, the greedy token
 // and the normaliser, in one pass over the logits.
 //
-// A workgroup takes one tile of one row's vocabulary.  It first counts the
-// row's history and biases that fall into the tile, in LDS with integer
-// atomics (their order does not matter), then reads each logit once.  The
+// A workgroup takes one tile of one row's vocabulary: eight or sixteen logits a
+// thread, loaded first.  While they are on their way it counts the row's history and
+// biases that fall into the tile, in LDS with integer atomics (their order does
+// not matter), and marks the touched places in a bitmap; the many that are not
+// touched are only masked.  The bytes of the logits, in and out, bound it.  The
 // workgroup that ends a row last joins the tiles' maxima and sums, in tile
 // order, so a call's result does not depend on which one that is.
 #include "sequence.hpp"
 
 namespace cortex {
 
-constexpr int kLogitsThreads = 256;
-constexpr int kLogitsTile = 4096;
+constexpr int kSmallThreads = 256, kSmallTile = 2048, kLargeThreads = 1024, kLargeTile = 16384;
+constexpr int kMaxBiases = 65535;                    // of a row
 constexpr int kLogitsMaxRows = 65535;
 constexpr size_t kLogitsCounterBytes = 256 * 1024;   // one arrival counter a row, at a fixed place for calls of every size
-constexpr uint32_t kSeen = 0x80000000u;              // in the prompt; the bits below count the row's own output
+
+// One entry per logit of a tile: how often the row's own output holds it, and in
+// the highest bit whether its prompt does.  16 bits while no history is longer
+// than they count.
+template <typename E> struct Counts {
+  static constexpr uint32_t kSeen = 1u << (8 * sizeof(E) - 1);
+  static constexpr int kPer = 4 / (int)sizeof(E);
+  static __device__ __forceinline__ uint32_t *word(uint32_t *t, int i) { return t + i / kPer; }
+  static __device__ __forceinline__ int shift(int i) { return i % kPer * 8 * (int)sizeof(E); }
+  static __device__ __forceinline__ uint32_t get(const uint32_t *t, int i) { return ((const E *)t)[i]; }
+};
 
 struct LogitsPart {
   float top;       // the tile's largest value (NaN if it holds one)
@@ -33,15 +45,13 @@ __device__ __forceinline__ bool chosen(float v, int i, float w, int j) {
 }
 
 // Joins two parts of a row.  Parts with nothing allowed have top = -infinity, sum = 0.
-__device__ __forceinline__ LogitsPart join(const LogitsPart &p, const LogitsPart &q) {
-  LogitsPart r = chosen(p.top, p.at, q.top, q.at) ? p : q;
-  if (p.at < 0) r = q;
-  if (q.at < 0) r = p;
-  if (p.at < 0 || q.at < 0) return r;
-  const float a = p.top == r.top ? 1.0f : fast_exp2((p.top - r.top) * kLog2e);
-  const float b = q.top == r.top ? 1.0f : fast_exp2((q.top - r.top) * kLog2e);
-  r.sum = p.sum * a + q.sum * b;
-  return r;
+// Member by member: a choice between the structs would go through memory.
+__device__ __forceinline__ LogitsPart join(const LogitsPart p, const LogitsPart q) {
+  const bool first = q.at < 0 || (p.at >= 0 && chosen(p.top, p.at, q.top, q.at));
+  const float top = first ? p.top : q.top;
+  const float a = p.top == top ? 1.0f : fast_exp2((p.top - top) * kLog2e);
+  const float b = q.top == top ? 1.0f : fast_exp2((q.top - top) * kLog2e);
+  return LogitsPart{top, first ? p.at : q.at, p.sum * a + q.sum * b, 0.0f};
 }
 
 struct RowRules {
@@ -49,27 +59,68 @@ struct RowRules {
 };
 
 // Each operation rounded on its own, in the order the header gives.
-__device__ __forceinline__ float apply_rules(float v, uint32_t count, const RowRules &r) {
+__device__ __forceinline__ float apply_rules(float v, uint32_t n, const RowRules &r) {
 #pragma clang fp contract(off)
   v = v > 0.0f ? v / r.repetition : v * r.repetition;
-  const uint32_t n = count & ~kSeen;
   const float f = r.frequency * (float)n;
   v = v - f;
   if (n) v = v - r.presence;
   return v;
 }
 
-template <typename T, int V>
-__global__ void __launch_bounds__(kLogitsThreads) logits_kernel(cortex_logits_t a, int32_t *status, uint32_t *counters,
-                                                                LogitsPart *parts) {
-  __shared__ uint32_t count[kLogitsTile];
-  __shared__ uint32_t bias[kLogitsTile];      // 1 + the entry of the row's biases
-  __shared__ LogitsPart wave_part[kLogitsThreads / 64];
-  if (load_status(status) != 0) return;
-  const int tid = (int)threadIdx.x, row = (int)blockIdx.y, tiles = (int)gridDim.x;
-  const int v0 = (int)blockIdx.x * kLogitsTile;
-  const int width = a.vocab - v0 < kLogitsTile ? a.vocab - v0 : kLogitsTile;
+__device__ __forceinline__ LogitsPart join_lanes(LogitsPart p, int lane) {
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const LogitsPart q = {__shfl_xor(p.top, s), __shfl_xor(p.at, s), __shfl_xor(p.sum, s), 0.0f};
+    // both lanes of a pair add in the same order
+    const bool upper = lane & s;
+    const LogitsPart lo = {upper ? q.top : p.top, upper ? q.at : p.at, upper ? q.sum : p.sum, 0.0f};
+    const LogitsPart hi = {upper ? p.top : q.top, upper ? p.at : q.at, upper ? p.sum : q.sum, 0.0f};
+    p = join(lo, hi);
+  }
+  return p;
+}
 
+// Adds the values v[0..V) at index `at` and on to a part, one by one.
+template <int V> __device__ void add_values(LogitsPart &part, const float (&v)[V], int at) {
+#pragma unroll
+  for (int k = 0; k < V; ++k)
+    if (v[k] != -__builtin_inff()) part = join(part, LogitsPart{v[k], at + k, v[k] != v[k] ? v[k] : 1.0f, 0.0f});
+}
+
+template <typename T, typename E, int THREADS, int kTile, bool WIDE>
+__global__ void __launch_bounds__(THREADS) logits_kernel(cortex_logits_t a, int32_t *status, uint32_t *counters,
+                                                         LogitsPart *parts) {
+  constexpr int V = 16 / (int)sizeof(T), NV = kTile / THREADS / V;
+  typedef Counts<E> Count;
+  typedef Counts<uint16_t> Entry;
+  extern __shared__ uint32_t table[];            // [kTile] counts, then [kTile] of 16 bits: 1 + the entry of the row's biases
+  __shared__ uint32_t touched[kTile / 32];
+  __shared__ LogitsPart wave_part[THREADS / 64];
+  __shared__ float wave_top[THREADS / 64], wave_sums[THREADS / 64];
+  __shared__ int first_at;
+  const int failed = entry_status(status);        // looked at once the first loads are on their way
+  const int tid = (int)threadIdx.x, lane = tid & 63, row = (int)blockIdx.y, tiles = (int)gridDim.x;
+  const int v0 = (int)blockIdx.x * kTile;
+  const int width = a.vocab - v0 < kTile ? a.vocab - v0 : kTile;
+  const T *src = (const T *)a.logits + (int64_t)row * a.logits_ld + v0;
+  T *dst = a.out ? (T *)a.out + (int64_t)row * a.out_ld + v0 : nullptr;
+
+  // V logits from i on; what is past the row's end repeats its last
+  typedef T vec __attribute__((ext_vector_type(V)));
+  vec raw[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int i = (j * THREADS + tid) * V;
+    if (WIDE && i + V <= width) {
+      raw[j] = *(const vec *)(src + i);
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k) raw[j][k] = src[i + k < width ? i + k : width - 1];
+    }
+  }
+
+  if (failed != 0) return;
   int len = 0, prompt = 0, bias0 = 0, bias1 = 0, m = -1;
   bool broken = false;
   if (a.history_len) {
@@ -80,7 +131,7 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_kernel(cortex_logits_t 
   if (a.bias_offsets) {
     bias0 = a.bias_offsets[row];
     bias1 = a.bias_offsets[row + 1];
-    if (bias0 < 0 || bias1 < bias0 || bias1 > a.num_biases || (row == 0 && bias0 != 0) ||
+    if (bias0 < 0 || bias1 < bias0 || bias1 > a.num_biases || bias1 - bias0 > kMaxBiases || (row == 0 && bias0 != 0) ||
         (row == a.rows - 1 && bias1 != a.num_biases))
       broken = true;
   }
@@ -92,23 +143,48 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_kernel(cortex_logits_t 
     if (tid == 0) raise_status(status, CORTEX_ST_INPUT_RANGE);
     return;
   }
-  for (int i = tid; i < width; i += kLogitsThreads) count[i] = bias[i] = 0;
+  // the mask's words for the thread's values: V divides 32
+  uint32_t open[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int i = (j * THREADS + tid) * V;
+    open[j] = ~0u;
+    if (m >= 0 && i < width) open[j] = a.mask[(int64_t)m * a.mask_ld + (v0 + i) / 32] >> (i % 32);
+    if (i + V > width) open[j] &= i < width ? (1u << (width - i)) - 1u : 0u;
+  }
+  uint32_t *count = table, *bias = table + kTile / Count::kPer;
+  const int words = kTile / Count::kPer + (a.bias_offsets ? kTile / Entry::kPer : 0);
+  const u32x4 zeros = {0, 0, 0, 0};
+  for (int k = tid * 4; k < words; k += THREADS * 4) *(u32x4 *)&table[k] = zeros;
+  if (tid < kTile / 32) touched[tid] = 0;
+  if (tid == 0) first_at = 0x7fffffff;
   __syncthreads();
   bool outside = false;
-  for (int j = tid; j < len; j += kLogitsThreads) {
-    const int tok = a.history[(int64_t)row * a.history_ld + j];
+  const int32_t *text = a.history + (int64_t)row * a.history_ld;
+#pragma unroll 4
+  for (int j = tid; j < len; j += THREADS) {
+    const int tok = text[j], i = tok - v0;
     outside |= tok < 0 || tok >= a.vocab;
-    const int i = tok - v0;
     if (tok >= v0 && i < width) {
-      if (j < prompt) atomicOr(&count[i], kSeen);
-      else atomicAdd(&count[i], 1u);
+      atomicOr(&touched[i / 32], 1u << (i % 32));
+      if (j < prompt) atomicOr(Count::word(count, i), Count::kSeen << Count::shift(i));
+      else atomicAdd(Count::word(count, i), 1u << Count::shift(i));
     }
   }
-  for (int j = bias0 + tid; j < bias1; j += kLogitsThreads) {
-    const int tok = a.bias_tokens[j];
+  for (int j = bias0 + tid; j < bias1; j += THREADS) {
+    const int tok = a.bias_tokens[j], i = tok - v0;
     outside |= tok < 0 || tok >= a.vocab;
-    const int i = tok - v0;
-    if (tok >= v0 && i < width) atomicMax(&bias[i], (uint32_t)(j - bias0) + 1u);
+    if (tok >= v0 && i < width) {
+      atomicOr(&touched[i / 32], 1u << (i % 32));
+      // the largest entry; another lane's change of the word starts it over
+      const uint32_t entry = (uint32_t)(j - bias0) + 1u;
+      uint32_t *w = Entry::word(bias, i), was = *w;
+      while ((was >> Entry::shift(i) & 0xffffu) < entry) {
+        const uint32_t found = atomicCAS(w, was, (was & ~(0xffffu << Entry::shift(i))) | entry << Entry::shift(i));
+        if (found == was) break;
+        was = found;
+      }
+    }
   }
   if (outside) raise_status(status, CORTEX_ST_INPUT_RANGE);
   __syncthreads();
@@ -117,81 +193,135 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_kernel(cortex_logits_t 
   rules.repetition = a.repetition ? a.repetition[row] : 1.0f;
   rules.frequency = a.frequency ? a.frequency[row] : 0.0f;
   rules.presence = a.presence ? a.presence[row] : 0.0f;
-  const T *src = (const T *)a.logits + (int64_t)row * a.logits_ld + v0;
-  T *dst = a.out ? (T *)a.out + (int64_t)row * a.out_ld + v0 : nullptr;
-  const uint32_t *mask = m >= 0 ? a.mask + (int64_t)m * a.mask_ld + v0 / 32 : nullptr;
-
-  LogitsPart part = {-__builtin_inff(), -1, 0.0f, 0.0f};
-  for (int i = tid * V; i < width; i += kLogitsThreads * V) {
-    const int n = width - i < V ? width - i : V;
-    float v[V];
-    if (n == V) Pack<T, V>::load(src + i, v);
-    else
+  // the values at i .. i + V - 1, -infinity past the row's end
+  auto values = [&](int i, const vec &r, uint32_t allowed, float (&v)[V]) {
+    const uint32_t changed = touched[i / 32] >> (i % 32) & ((1u << V) - 1u);
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[k] = k < n ? to_float<T>(src[i + k]) : 0.0f;
-    const uint32_t allowed = mask ? mask[i / 32] >> (i % 32) : ~0u;
-    float top = -__builtin_inff();
-    int at = -1;
+    for (int k = 0; k < V; ++k) v[k] = to_float<T>(r[k]);
+    if (changed)
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (changed >> k & 1) {
+          const uint32_t c = Count::get(count, i + k), e = a.bias_offsets ? Entry::get(bias, i + k) : 0u;
+          if (c) v[k] = apply_rules(v[k], c & ~Count::kSeen, rules);
+          if (e) v[k] += a.bias_values[bias0 + (int)e - 1];
+        }
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      if (k < n) {
-        const uint32_t c = count[i + k], b = bias[i + k];
-        if (c) v[k] = apply_rules(v[k], c, rules);
-        if (b) v[k] += a.bias_values[bias0 + (int)b - 1];
-      }
-      if (k >= n || !(allowed >> k & 1)) v[k] = -__builtin_inff();
-      if (v[k] != -__builtin_inff() && (at < 0 || chosen(v[k], v0 + i + k, top, at))) {
-        top = v[k];
-        at = v0 + i + k;
-      }
+      const unsigned int keep = (unsigned int)((int)(allowed << (31 - k)) >> 31);
+      v[k] = __builtin_bit_cast(float, (__builtin_bit_cast(unsigned int, v[k]) & keep) | (0xff800000u & ~keep));
     }
-    if (dst) {
-      if (n == V) Pack<T, V>::store(dst + i, v);
-      else
-#pragma unroll
-        for (int k = 0; k < V; ++k)
-          if (k < n) dst[i + k] = from_float<T>(v[k]);
-    }
-    if (at >= 0) {
-      LogitsPart q = {top, at, 0.0f, 0.0f};
-#pragma unroll
-      for (int k = 0; k < V; ++k) q.sum += v[k] == top ? 1.0f : fast_exp2((v[k] - top) * kLog2e);
-      part = join(part, q);
-    }
-  }
-  auto from_lane = [](const LogitsPart &p, int mask_) {
-    return LogitsPart{__shfl_xor(p.top, mask_), __shfl_xor(p.at, mask_), __shfl_xor(p.sum, mask_), 0.0f};
   };
+
+  // Largest value and the sum of exponentials below it.  fmax drops a NaN and
+  // inf - inf makes one: a sum that is not a number sends the workgroup over its
+  // values again, one by one.
+  float top = -__builtin_inff(), sum = 0.0f;
 #pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const LogitsPart q = from_lane(part, s);
-    // both lanes of a pair add in the same order
-    part = (tid & s) ? join(q, part) : join(part, q);
-  }
-  if ((tid & 63) == 0) wave_part[tid / 64] = part;
-  __syncthreads();
-  if (tid != 0 || (!a.token && !a.lse)) return;
-  part = wave_part[0];
-  for (int w = 1; w < kLogitsThreads / 64; ++w) part = join(part, wave_part[w]);
-  if (tiles > 1) {
-    unsigned int *mine = (unsigned int *)(parts + (size_t)row * tiles + blockIdx.x);
-    st_agent(mine, __builtin_bit_cast(unsigned int, part.top));
-    st_agent(mine + 1, (unsigned int)part.at);
-    st_agent(mine + 2, __builtin_bit_cast(unsigned int, part.sum));
-    // the last of the row's workgroups finds the others' parts stored; the
-    // counter wraps to 0 for the next call
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
-    const unsigned int before = __hip_atomic_fetch_add(counters + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (before != (unsigned int)tiles - 1u) return;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-    st_agent(counters + row, 0u);
-    for (int t = 0; t < tiles; ++t) {
-      const unsigned int *p = (const unsigned int *)(parts + (size_t)row * tiles + t);
-      const LogitsPart q = {__builtin_bit_cast(float, ld_agent(p)), (int32_t)ld_agent(p + 1),
-                            __builtin_bit_cast(float, ld_agent(p + 2)), 0.0f};
-      part = t == 0 ? q : join(part, q);
+  for (int j = 0; j < NV; ++j) {
+    const int i = (j * THREADS + tid) * V;
+    if (i < width) {
+      float v[V];
+      values(i, raw[j], open[j], v);
+      if (dst) {
+        if (WIDE && i + V <= width) {
+          Pack<T, V>::store(dst + i, v);
+        } else {
+#pragma unroll
+          for (int k = 0; k < V; ++k)
+            if (i + k < width) dst[i + k] = from_float<T>(v[k]);
+        }
+      }
+      float high = v[0];
+#pragma unroll
+      for (int k = 1; k < V; ++k) high = __builtin_fmaxf(high, v[k]);
+      const float old = top;
+      top = __builtin_fmaxf(top, high);
+      const float base = top == -__builtin_inff() ? 0.0f : top;
+      sum *= fast_exp2((old - base) * kLog2e);
+#pragma unroll
+      for (int k = 0; k < V; ++k) sum += fast_exp2((v[k] - base) * kLog2e);
     }
   }
+  if (!a.token && !a.lse) return;
+  const float wtop = wave_max(top);
+  if (lane == 0) wave_top[tid / 64] = wtop;
+  LogitsPart part = {-__builtin_inff(), -1, 0.0f, 0.0f};
+  if (__syncthreads_or(sum != sum)) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int i = (j * THREADS + tid) * V;
+      if (i < width) {
+        float v[V];
+        values(i, raw[j], open[j], v);
+        add_values(part, v, v0 + i);
+      }
+    }
+    part = join_lanes(part, lane);
+    if (lane == 0) wave_part[tid / 64] = part;
+    __syncthreads();
+    if (tid >= 64) return;
+    part = wave_part[lane % (THREADS / 64)];
+    if (lane >= THREADS / 64) part = LogitsPart{-__builtin_inff(), -1, 0.0f, 0.0f};
+    part = join_lanes(part, lane);
+  } else {
+    float high = wave_top[0];
+#pragma unroll
+    for (int k = 1; k < THREADS / 64; ++k) high = __builtin_fmaxf(high, wave_top[k]);
+    const bool some = high > -__builtin_inff();
+    const float all = wave_sum(some ? sum * fast_exp2((top - high) * kLog2e) : 0.0f);
+    if (lane == 0) wave_sums[tid / 64] = all;
+    if (some && top == high) {                   // few lanes: where it is
+      int at = 0x7fffffff;
+#pragma unroll
+      for (int j = NV - 1; j >= 0; --j) {
+        const int i = (j * THREADS + tid) * V;
+        if (i < width) {
+          float v[V];
+          values(i, raw[j], open[j], v);
+#pragma unroll
+          for (int k = V - 1; k >= 0; --k)
+            if (v[k] == high) at = v0 + i + k;
+        }
+      }
+      atomicMin(&first_at, at);
+    }
+    __syncthreads();
+    if (tid >= 64) return;
+    float total = 0.0f;
+#pragma unroll
+    for (int k = 0; k < THREADS / 64; ++k) total += wave_sums[k];
+    if (some) part = LogitsPart{high, first_at, total, 0.0f};
+  }
+  if (tiles > 1) {
+    unsigned int before = 0;
+    if (lane == 0) {
+      unsigned int *mine = (unsigned int *)(parts + (size_t)row * tiles + blockIdx.x);
+      st_agent(mine, __builtin_bit_cast(unsigned int, part.top));
+      st_agent(mine + 1, (unsigned int)part.at);
+      st_agent(mine + 2, __builtin_bit_cast(unsigned int, part.sum));
+      // The last of the row's workgroups finds the others' parts stored: they went past
+      // the L2 (device scope), and are complete before the arrival.  A device-scope
+      // fence would write back the whole L2, the row's output in it.
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+      wave_stores_complete();
+      before = __hip_atomic_fetch_add(counters + row, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (__builtin_amdgcn_readfirstlane(before) != (unsigned int)tiles - 1u) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+    if (lane == 0) st_agent(counters + row, 0u);   // ready for the next call
+    part = LogitsPart{-__builtin_inff(), -1, 0.0f, 0.0f};
+    for (int t = 0; t < tiles; t += 64) {
+      LogitsPart q = {-__builtin_inff(), -1, 0.0f, 0.0f};
+      if (t + lane < tiles) {
+        const unsigned int *p = (const unsigned int *)(parts + (size_t)row * tiles + t + lane);
+        const unsigned int w0 = ld_agent(p), w1 = ld_agent(p + 1), w2 = ld_agent(p + 2);
+        q = LogitsPart{__builtin_bit_cast(float, w0), (int32_t)w1, __builtin_bit_cast(float, w2), 0.0f};
+      }
+      part = join(part, join_lanes(q, lane));
+    }
+  }
+  if (lane != 0) return;
   if (a.token) a.token[row] = part.at;
   if (a.lse) {
     float l = part.top;                          // -infinity, infinity or NaN as it is
@@ -200,15 +330,34 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_kernel(cortex_logits_t 
   }
 }
 
-template <typename T> int launch_logits(const cortex_logits_t &a, int32_t *status, void *ws, void *stream) {
+// Small tiles while the large ones would leave CUs without a workgroup.  The large
+// ones count a row's history and end with an arrival eight times less often.
+static bool small_tiles(int64_t rows, int64_t vocab) { return rows * ((vocab + kLargeTile - 1) / kLargeTile) < 256; }
+
+template <typename T, typename E, int THREADS, int kTile>
+int launch_logits_tiles(const cortex_logits_t &a, int32_t *status, void *ws, void *stream) {
   constexpr int V = 16 / (int)sizeof(T);
   const bool wide = a.logits_ld % V == 0 && aligned16(a.logits) && (!a.out || (a.out_ld % V == 0 && aligned16(a.out)));
-  const dim3 grid((a.vocab + kLogitsTile - 1) / kLogitsTile, a.rows);
+  const dim3 grid((a.vocab + kTile - 1) / kTile, a.rows);
   uint32_t *counters = (uint32_t *)ws;
   LogitsPart *parts = (LogitsPart *)((char *)ws + kLogitsCounterBytes);
-  if (wide) logits_kernel<T, V><<<grid, kLogitsThreads, 0, (hipStream_t)stream>>>(a, status, counters, parts);
-  else logits_kernel<T, 1><<<grid, kLogitsThreads, 0, (hipStream_t)stream>>>(a, status, counters, parts);
+  const size_t lds = kTile * (sizeof(E) + (a.bias_offsets ? sizeof(uint16_t) : 0));
+  const void *kernel = wide ? (const void *)logits_kernel<T, E, THREADS, kTile, true>
+                            : (const void *)logits_kernel<T, E, THREADS, kTile, false>;
+  if (cached_occupancy(kernel, THREADS, lds) < 1) return CORTEX_E_HIP;   // also admits the LDS size
+  if (wide) logits_kernel<T, E, THREADS, kTile, true><<<grid, THREADS, lds, (hipStream_t)stream>>>(a, status, counters, parts);
+  else logits_kernel<T, E, THREADS, kTile, false><<<grid, THREADS, lds, (hipStream_t)stream>>>(a, status, counters, parts);
   return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+}
+
+template <typename T, typename E> int launch_logits_counts(const cortex_logits_t &a, int32_t *status, void *ws, void *stream) {
+  return small_tiles(a.rows, a.vocab) ? launch_logits_tiles<T, E, kSmallThreads, kSmallTile>(a, status, ws, stream)
+                                      : launch_logits_tiles<T, E, kLargeThreads, kLargeTile>(a, status, ws, stream);
+}
+
+template <typename T> int launch_logits(const cortex_logits_t &a, int32_t *status, void *ws, void *stream) {
+  return a.history_cap < 0x8000 ? launch_logits_counts<T, uint16_t>(a, status, ws, stream)
+                                : launch_logits_counts<T, uint32_t>(a, status, ws, stream);
 }
 
 }  // namespace cortex
@@ -217,7 +366,7 @@ using namespace cortex;
 
 extern "C" size_t cortex_logits_workspace_bytes(int32_t rows, int32_t vocab) {
   if (rows < 0 || rows > kLogitsMaxRows || vocab < 1) return 0;
-  return kLogitsCounterBytes + (size_t)rows * (((size_t)vocab + kLogitsTile - 1) / kLogitsTile) * sizeof(LogitsPart);
+  return kLogitsCounterBytes + (size_t)rows * (((size_t)vocab + kSmallTile - 1) / kSmallTile) * sizeof(LogitsPart);
 }
 
 extern "C" int cortex_logits_process(const cortex_logits_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes,

@@ -34,7 +34,7 @@ template <int N> __device__ __forceinline__ void store_floats(float *p, const fl
 template <bool HEAD>
 __global__ void __launch_bounds__(256) enter_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w, int Q) {
   constexpr int U = 8;                           // segments loaded ahead of the chain through them
-  if (load_status(status) != 0) return;
+  if (entry_status(status) != 0) return;
   const int seq = (int)blockIdx.y;
   const int first = a.seq_offsets[seq], last = a.seq_offsets[seq + 1];
   if (first < 0 || last < first || last > a.num_tokens) return;
@@ -81,7 +81,7 @@ constexpr int kAhead = 4, kTile = 16;
 
 template <typename T, int N, int PART>
 __global__ void __launch_bounds__(kScanWave) channel_scan_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w, int Q) {
-  if (load_status(status) != 0) return;
+  if (entry_status(status) != 0) return;
   const int slot = (int)blockIdx.x, g = (int)blockIdx.z;
   const bool checks = blockIdx.y == 0 && g == 0;
   int seq, begin, end;
@@ -208,7 +208,7 @@ constexpr int kStepThreads = 256;
 template <typename T, int N, bool HEAD>
 __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(cortex_scan_t a, int32_t *status) {
   constexpr int L = N / 4;                       // lanes per channel
-  if (load_status(status) != 0) return;
+  if (entry_status(status) != 0) return;
   const int b = (int)blockIdx.x;
   const int row = a.state_in || a.state_out ? state_row(a.state_index, b, a.state_rows, status) : -1;
   if (row < -1) return;

@@ -32,8 +32,6 @@
 // one wave, beside the others' products.
 #pragma once
 
-#include <type_traits>
-
 #include "sequence.hpp"
 
 namespace cortex {
@@ -93,22 +91,6 @@ template <int N> struct HeadLds {
   HeadSteps steps[2];
 };
 
-// Inclusive sum over the lanes of a wave.
-__device__ __forceinline__ float lane_sums(float v) {
-  auto shifted = [](float x, auto ctrl, auto rows) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value,
-                                                                 decltype(rows)::value, 0xf, false));
-  };
-  typedef std::integral_constant<int, 0xf> All;
-  v += shifted(v, std::integral_constant<int, 0x111>{}, All{});      // from 1, 2, 4, 8 lanes below in a row of 16
-  v += shifted(v, std::integral_constant<int, 0x112>{}, All{});
-  v += shifted(v, std::integral_constant<int, 0x114>{}, All{});
-  v += shifted(v, std::integral_constant<int, 0x118>{}, All{});
-  v += shifted(v, std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // lane 15 to the row above
-  v += shifted(v, std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // lane 31 to the upper half
-  return v;
-}
-
 // A lane is a token.  The state's weights come from a sum from the end: those
 // near the end, which count most, are sums of few terms.  Returns the sum of dt.
 __device__ __forceinline__ float put_steps(HeadSteps &to, int lane, float dt, float A2) {
@@ -121,7 +103,7 @@ __device__ __forceinline__ float put_steps(HeadSteps &to, int lane, float dt, fl
   to.grow[lane] = fast_exp2(up);
   to.weight[63 - lane] = fast_exp2(lane == 0 ? 0.0f : after) * rev;
   if (lane == 63) to.decay = fast_exp2(down);
-  return __shfl(lane_sums(dt), 63);
+  return wave_sum(dt);
 }
 
 __device__ __forceinline__ bf16x8v lds8(const unsigned short *p) { return __builtin_bit_cast(bf16x8v, *(const u32x4v *)p); }
@@ -151,7 +133,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma_kernel(cortex_scan_
   constexpr int OL = N / 8 < 4 ? N / 8 : 4;                       // octets of a row that neighbouring lanes take
   constexpr int kItems = (N / 8 * 32 + kHeadThreads - 1) / kHeadThreads;   // (octet, pair of tokens) per thread
   __shared__ Lds lds;
-  if (load_status(status) != 0) return;
+  if (entry_status(status) != 0) return;
   const int slot = (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int q = lane >> 4, l16 = lane & 15;
   const int P = a.head_dim, blocks = (P + 63) / 64;

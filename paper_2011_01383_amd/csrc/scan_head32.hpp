@@ -42,19 +42,26 @@ __device__ __forceinline__ float put_steps32(HeadSteps32 &to, int lane, float dt
     to.weight[31 - lane] = fast_exp2(lane == 0 ? 0.0f : after) * rev;
   }
   if (lane == 31) to.decay = fast_exp2(down);
-  return __shfl(lane_sums(dt), 63);
+  return wave_sum(dt);
 }
 
-template <bool WIDE> __device__ __forceinline__ float4 load4f(const float *p) {
-  if constexpr (WIDE) return *(const float4 *)p;
-  return make_float4(p[0], p[1], p[2], p[3]);
+template <bool WIDE> __device__ __forceinline__ f32x4 load4f(const float *p) {
+  if constexpr (WIDE) return *(const f32x4 *)p;
+  return f32x4{p[0], p[1], p[2], p[3]};
+}
+
+// Sixteen k: the operands of four products.
+__device__ __forceinline__ f32x4 mfma_k16(f32x4 a, f32x4 b, f32x4 c) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+  return c;
 }
 
 template <int N, int PART, bool WIDE>
 __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w, int Q) {
   constexpr int NT = N / 16, kItems = (N / 4 * kSub32 + kHeadThreads - 1) / kHeadThreads;
   __shared__ HeadLds32<N> lds;
-  if (load_status(status) != 0) return;
+  if (entry_status(status) != 0) return;
   const int slot = (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int q = lane >> 4, l16 = lane & 15;
   const int P = a.head_dim, blocks = (P + 63) / 64;
@@ -98,8 +105,8 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
   float *ys = (float *)a.y + ch;
   float steps = 0.0f;
 
-  const float4 none = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  float4 xr[2], br[kItems], cr[kItems];
+  const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
+  f32x4 xr[2], br[kItems], cr[kItems];
   float raw = 0.0f;
   auto fetch = [&](int t0) {                      // as in the bf16 form
 #pragma unroll
@@ -131,15 +138,15 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int id = i * kHeadThreads + tid;
-      *(float4 *)&lds.x[id / 16][id % 16 * 4] = t0 + id / 16 < end ? xr[i] : none;
+      *(f32x4 *)&lds.x[id / 16][id % 16 * 4] = t0 + id / 16 < end ? xr[i] : none;
     }
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
       const int id = i * kHeadThreads + tid;
       const bool in = t0 + id / (N / 4) < end;
       if (id < N / 4 * kSub32) {
-        *(float4 *)&lds.B[id / (N / 4)][id % (N / 4) * 4] = in ? br[i] : none;
-        if (PART != 1) *(float4 *)&lds.C[id / (N / 4)][id % (N / 4) * 4] = in ? cr[i] : none;
+        *(f32x4 *)&lds.B[id / (N / 4)][id % (N / 4) * 4] = in ? br[i] : none;
+        if (PART != 1) *(f32x4 *)&lds.C[id / (N / 4)][id % (N / 4) * 4] = in ? cr[i] : none;
       }
     }
     __syncthreads();
@@ -154,7 +161,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
       for (int i = 0; i < 4; ++i) x[si][i] = lds.x[si * 16 + q * 4 + i][wave * 16 + l16];
 
     if constexpr (PART != 1) {
-      float4 zr[2];
+      f32x4 zr[2];
       if (zs && works)
 #pragma unroll
         for (int ti = 0; ti < 2; ++ti) zr[ti] = load4f<WIDE>(zs + (int64_t)min(t0 + ti * 16 + l16, end - 1) * a.z_ld);
@@ -163,7 +170,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
         f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int m = 0; m < NT; ++m)
-          acc = mfma_k16(*(const float4 *)&lds.B[si * 16 + l16][m * 16 + q * 4], *(const float4 *)&lds.C[ti * 16 + l16][m * 16 + q * 4], acc);
+          acc = mfma_k16(*(const f32x4 *)&lds.B[si * 16 + l16][m * 16 + q * 4], *(const f32x4 *)&lds.C[ti * 16 + l16][m * 16 + q * 4], acc);
         const int t = ti * 16 + l16, s = si * 16 + q * 4;
         const float ct = st.cum[t];
         const f32x4 cs = *(const f32x4 *)&st.cum[s], dt = *(const f32x4 *)&st.dt[s];
@@ -180,9 +187,8 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
       if (works) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          const float4 hv = make_float4(h[nt][0], h[nt][1], h[nt][2], h[nt][3]);
 #pragma unroll
-          for (int ti = 0; ti < 2; ++ti) y[ti] = mfma_k16(hv, *(const float4 *)&lds.C[ti * 16 + l16][nt * 16 + q * 4], y[ti]);
+          for (int ti = 0; ti < 2; ++ti) y[ti] = mfma_k16(h[nt], *(const f32x4 *)&lds.C[ti * 16 + l16][nt * 16 + q * 4], y[ti]);
         }
 #pragma unroll
         for (int ti = 0; ti < 2; ++ti) y[ti] *= st.grow[ti * 16 + l16];
@@ -208,8 +214,8 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
 #pragma unroll
           for (int ti = 0; ti < 2; ++ti)
             if (ti >= si)
-              y[ti] = mfma_k16(make_float4(xf[si][0], xf[si][1], xf[si][2], xf[si][3]),
-                               *(const float4 *)&lds.M[ti * 16 + l16][si * 16 + q * 4], y[ti]);
+              y[ti] = mfma_k16(f32x4{xf[si][0], xf[si][1], xf[si][2], xf[si][3]},
+                               *(const f32x4 *)&lds.M[ti * 16 + l16][si * 16 + q * 4], y[ti]);
         if (__any(first_odd < kSub32)) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -222,14 +228,16 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
 #pragma unroll
         for (int ti = 0; ti < 2; ++ti) {
           const int t = t0 + ti * 16 + l16;
-          float4 v = make_float4(y[ti][0], y[ti][1], y[ti][2], y[ti][3]);
-          if (zs) v = make_float4(v.x * silu(zr[ti].x), v.y * silu(zr[ti].y), v.z * silu(zr[ti].z), v.w * silu(zr[ti].w));
+          f32x4 v = y[ti];
+          if (zs)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] *= silu(zr[ti][i]);
           if (t < end) {
             float *p = ys + (int64_t)t * a.y_ld;
             if constexpr (WIDE) {
-              *(float4 *)p = v;
+              *(f32x4 *)p = v;
             } else {
-              p[0] = v.x; p[1] = v.y; p[2] = v.z; p[3] = v.w;
+              p[0] = v[0]; p[1] = v[1]; p[2] = v[2]; p[3] = v[3];
             }
           }
         }
@@ -242,11 +250,11 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
 #pragma unroll
       for (int si = 0; si < 2; ++si) {
         const f32x4 ws = *(const f32x4 *)&st.weight[si * 16 + q * 4];
-        const float4 xw = make_float4(x[si][0] * ws[0], x[si][1] * ws[1], x[si][2] * ws[2], x[si][3] * ws[3]);
+        const f32x4 xw = f32x4{x[si][0], x[si][1], x[si][2], x[si][3]} * ws;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           const float *b = &lds.B[si * 16 + q * 4][nt * 16 + l16];
-          h[nt] = mfma_k16(make_float4(b[0], b[N + 4], b[2 * (N + 4)], b[3 * (N + 4)]), xw, h[nt]);
+          h[nt] = mfma_k16(f32x4{b[0], b[N + 4], b[2 * (N + 4)], b[3 * (N + 4)]}, xw, h[nt]);
         }
       }
     }

@@ -38,6 +38,12 @@ template <typename T> struct Pack<T, 1> {
   static __device__ __forceinline__ void store(T *p, const float (&v)[1]) { *p = from_float<T>(v[0]); }
 };
 
+// The status as earlier launches left it, through the caches: these kernels have
+// many waves, and none of them waits for another launch's word.
+__device__ __forceinline__ int entry_status(const int32_t *status) {
+  return __hip_atomic_load(status, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // v_exp_f32: 2^x to one unit in the last place, denormal results flushed to zero.
@@ -71,6 +77,34 @@ __device__ __forceinline__ float softplus(float v) {
 __device__ __forceinline__ float step_size(const cortex_scan_t &a, float raw, float bias) {
   const float v = raw + bias;
   return a.softplus ? softplus(v) : v;
+}
+
+// v of the lane that a data-parallel shift names; `none` in lanes that it leaves out.
+template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ float shifted(float v, float none) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL,
+                                                               ROWS, 0xf, false));
+}
+
+// Inclusive combination over the lanes of a wave, neutral element e: from 1, 2, 4
+// and 8 lanes below in a row of 16, lane 15 to the row above, lane 31 to the upper half.
+template <typename F> __device__ __forceinline__ float lane_prefix(float v, float e, F f) {
+  v = f(v, shifted<0x111>(v, e));
+  v = f(v, shifted<0x112>(v, e));
+  v = f(v, shifted<0x114>(v, e));
+  v = f(v, shifted<0x118>(v, e));
+  v = f(v, shifted<0x142, 0xa>(v, e));
+  v = f(v, shifted<0x143, 0xc>(v, e));
+  return v;
+}
+__device__ __forceinline__ float lane_sums(float v) {
+  return lane_prefix(v, 0.0f, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float last_lane(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+__device__ __forceinline__ float wave_sum(float v) { return last_lane(lane_sums(v)); }
+__device__ __forceinline__ float wave_max(float v) {
+  return last_lane(lane_prefix(v, -__builtin_inff(), [](float a, float b) { return __builtin_fmaxf(a, b); }));
 }
 
 // ---------------------------------------------------------------------------
