@@ -272,7 +272,9 @@ def _check_lin(lin: "Linearization", N: int, K: int) -> None:
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        # the handle that torch.cuda.current_stream() wraps in an object (2.7 us of host time a call)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
     return getattr(stream, "cuda_stream", stream)
 
 
