@@ -300,13 +300,14 @@ int launch_head_part(const cortex_scan_t &a, int32_t *status, const SegmentScrat
   auto rows16 = [](const void *p, int64_t ld) { return aligned16(p) && ld % V == 0; };
   const bool wide = rows16(a.x, a.x_ld) && rows16(a.B, a.B_ld) && rows16(a.C, a.C_ld) && rows16(a.z, a.z ? a.z_ld : 0) &&
                     rows16(a.y, a.y_ld);
-  const dim3 grid(slots, a.channels / a.head_dim * ((a.head_dim + 63) / 64));
+  const int64_t units = (int64_t)slots * (a.channels / a.head_dim) * ((a.head_dim + 63) / 64);
+  const unsigned grid = blocks_of_units(units);
   if constexpr (sizeof(T) == 2) {
-    if (wide) head_mfma_kernel<N, PART, true><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q);
-    else head_mfma_kernel<N, PART, false><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q);
+    if (wide) head_mfma_kernel<N, PART, true><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q, units);
+    else head_mfma_kernel<N, PART, false><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q, units);
   } else {
-    if (wide) head_mfma32_kernel<N, PART, true><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q);
-    else head_mfma32_kernel<N, PART, false><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q);
+    if (wide) head_mfma32_kernel<N, PART, true><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q, units);
+    else head_mfma32_kernel<N, PART, false><<<grid, kHeadThreads, 0, st>>>(a, status, w, Q, units);
   }
   return launched() ? CORTEX_OK : CORTEX_E_HIP;
 }

@@ -1,9 +1,9 @@
 // Prompts of the scan with one decay per head, as matrix products (bf16).
 //
-// Within a sub-chunk of 64 tokens, with c_t = sum_{s <= t} dt_s A and the state
+// Within a sub-chunk of 32 tokens, with c_t = sum_{s <= t} dt_s A and the state
 // h that enters it,
 //   y_t  = sum_{s <= t} (C_t . B_s) exp(c_t - c_s) dt_s x_s  +  exp(c_t) C_t h
-//   h'   = exp(c_63) h + sum_s exp(c_63 - c_s) dt_s x_s B_s
+//   h'   = exp(c_31) h + sum_s exp(c_31 - c_s) dt_s x_s B_s
 // A workgroup takes 64 channels of one head (a wave 16 of them) and walks the
 // sub-chunks of a segment with the state in its accumulators, so no state goes
 // to memory between them.
@@ -19,17 +19,17 @@
 // Layouts.  A 16x16x32 product takes both operands as (index = lane & 15; 8
 // consecutive k from 8 (lane >> 4)) and leaves its result as (column = lane &
 // 15; rows 4 (lane >> 4) + 0..3).  The order of k is free as long as both
-// operands agree, so every array over tokens or state entries that is summed
-// over keeps position 8 q + 4 a + r for element 16 a + 4 q + r of each 32: a
-// result then is an operand of the next product as it stands.  The scores are
-// computed as B C^T (columns t) and the state as [N, channels], so neither is
-// ever transposed; B and x are, on their way into LDS.  y has channels as rows,
-// so a lane loads z and stores y four channels at a time.
+// operands agree: k = 8 q + 4 a + r stands for element 16 a + 4 q + r of each
+// 32, of tokens as of state entries, so a result is an operand of the next
+// product as it stands.  The scores are computed as B C^T (columns t), the state
+// as [N, channels] and y as [channels, t].  B and x are summed over their tokens
+// too: the transposing 8-byte LDS read gives a lane four rows' values of its
+// column, which is the four k of one a.
 //
-// What it does per sub-chunk and wave at N = 128: 102 products (1,632 cycles of
-// a SIMD's matrix unit), about 60 16-byte reads of LDS.  The skip connection is
-// the scores' diagonal.  Step sizes and their sums are made a sub-chunk ahead by
-// one wave, beside the others' products.
+// What it does per sub-chunk and wave at N = 128: 48 products (768 cycles of a
+// SIMD's matrix unit).  The skip connection is the scores' diagonal.  Step sizes
+// and their sums are made a sub-chunk ahead by one wave, beside the others'
+// products.  y goes through LDS, so that z is read and y stored in whole rows.
 #pragma once
 
 #include "sequence.hpp"
@@ -41,7 +41,7 @@ typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4v __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kSub = 64;                 // tokens of a sub-chunk
+constexpr int kSub = 32;                 // tokens of a sub-chunk
 constexpr int kHeadWaves = 4;
 constexpr int kHeadThreads = 64 * kHeadWaves;
 
@@ -66,43 +66,44 @@ __device__ __forceinline__ bf16x8v pack8(const __bf16 (&p)[8]) {
   return bf16x8v{p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]};
 }
 
-// Rows of W elements that are read 16 bytes a lane down neighbouring rows: the
-// 16-byte pieces of a row are exchanged by its number, so that eight lanes' reads
-// fall into different banks without padding (which would leave room for one
-// workgroup a CU instead of two).
+// Rows of W elements: the 16-byte pieces of a row are exchanged by its number, so
+// that reads down neighbouring rows fall into different banks.
 template <int W> __device__ __forceinline__ int swizzled(int row, int pos) {
-  const int f = W >= 64 ? (row ^ row >> 3) & 7 : row >> 2 & 3;
+  constexpr int kPieces = W / 8;
+  const int f = kPieces >= 8 ? row & (kPieces - 1) & 15 : row >> 2 & 3;
   return row * W + (((pos >> 3) ^ f) << 3 | (pos & 7));
 }
 
-// Step sizes of a sub-chunk: dt_s, c_s, exp(c_s), exp(c_63 - c_s) dt_s, exp(c_63).
+// Step sizes of a sub-chunk: dt_s, c_s, exp(c_s), exp(c_31 - c_s) dt_s, exp(c_31).
 struct HeadSteps {
   float dt[kSub], cum[kSub], grow[kSub], weight[kSub], decay;
 };
 
 template <int N> struct HeadLds {
   static constexpr int NP = N < 32 ? 32 : N;      // the products over N take 32 at a time; what is past N is 0
-  static constexpr int kTok = kSub + 8;           // rows 16 bytes longer, for the same purpose
   unsigned short B[kSub * NP];                    // [s][n position]
   unsigned short C[kSub * NP];                    // [t][n position]
+  unsigned short x[kSub * 64];                    // [s][channel]
   unsigned short M[2][kSub * kSub];               // scores, two planes: [t][s position]
-  unsigned short BT[N][kTok];                     // [n][s position]
-  unsigned short xT[64][kTok];                    // [channel][s position]
+  float y[kSub * 64];                             // [t][channel]
   HeadSteps steps[2];
 };
 
-// A lane is a token.  The state's weights come from a sum from the end: those
-// near the end, which count most, are sums of few terms.  Returns the sum of dt.
+// A lane is a token; the lanes above them hold a step of 0.  The state's weights
+// come from a sum from the end: those near the end, which count most, are sums of
+// few terms.  Returns the sum of dt.
 __device__ __forceinline__ float put_steps(HeadSteps &to, int lane, float dt, float A2) {
   const float up = lane_sums(dt * A2);
-  const float rev = __shfl(dt, 63 - lane);
-  const float down = lane_sums(rev * A2);         // of tokens 63 - lane and on
+  const float rev = __shfl(dt, (kSub - 1 - lane) & 63);
+  const float down = lane_sums(lane < kSub ? rev * A2 : 0.0f);    // of tokens 31 - lane and on
   const float after = __shfl_up(down, 1);
-  to.dt[lane] = dt;
-  to.cum[lane] = up;
-  to.grow[lane] = fast_exp2(up);
-  to.weight[63 - lane] = fast_exp2(lane == 0 ? 0.0f : after) * rev;
-  if (lane == 63) to.decay = fast_exp2(down);
+  if (lane < kSub) {
+    to.dt[lane] = dt;
+    to.cum[lane] = up;
+    to.grow[lane] = fast_exp2(up);
+    to.weight[kSub - 1 - lane] = fast_exp2(lane == 0 ? 0.0f : after) * rev;
+  }
+  if (lane == kSub - 1) to.decay = fast_exp2(down);
   return wave_sum(dt);
 }
 
@@ -118,36 +119,51 @@ template <bool WIDE> __device__ __forceinline__ u32x4v load8(const bf16_t *p) {
   return r;
 }
 
-// Two rows of eight elements, of neighbouring tokens: their pairs, one word per element.
-__device__ __forceinline__ unsigned int pair_of(const u32x4v &a, const u32x4v &b, int i) {
-  const unsigned int x = a[i / 2], y = b[i / 2];
-  return i & 1 ? (x >> 16) | (y & 0xffff0000u) : (x & 0xffffu) | y << 16;
+// Four elements of four rows, transposed: lane i of a group of 16 gives the address
+// of row i / 4's elements 4 (i % 4) .. + 3 and gets element i of the four rows.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ s16x4 lds_columns(const unsigned short *p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
 }
+__device__ __forceinline__ bf16x8v join8(s16x4 a, s16x4 b) {
+  return __builtin_bit_cast(bf16x8v, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// Workgroups go to the eight XCDs in turn.  Each XCD takes a run of neighbouring
+// units (slot by slot, a slot's heads together), so that the heads of a group find
+// its B and C in the L2 that they share.
+__device__ __forceinline__ int64_t unit_of_block(int64_t units) {
+  const int64_t per = (units + 7) / 8;
+  return (int64_t)(blockIdx.x % 8) * per + blockIdx.x / 8;
+}
+inline unsigned blocks_of_units(int64_t units) { return (unsigned)((units + 7) / 8 * 8); }
 
 // PART as for the channel scan: 0 whole sequences, 1 a segment's state from
 // zero, 2 outputs from the state that enters it.
 template <int N, int PART, bool WIDE>
-__global__ void __launch_bounds__(kHeadThreads, 2) head_mfma_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w, int Q) {
+__global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w, int Q,
+                                                                    int64_t units) {
   typedef HeadLds<N> Lds;
   constexpr int NT = N / 16, NB = Lds::NP / 32;
-  constexpr int OL = N / 8 < 4 ? N / 8 : 4;                       // octets of a row that neighbouring lanes take
-  constexpr int kItems = (N / 8 * 32 + kHeadThreads - 1) / kHeadThreads;   // (octet, pair of tokens) per thread
+  constexpr int OL = N / 8, kItems = (OL * kSub + kHeadThreads - 1) / kHeadThreads;   // octets of a row; of them all per thread
   __shared__ Lds lds;
   if (entry_status(status) != 0) return;
-  const int slot = (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int q = lane >> 4, l16 = lane & 15;
-  const int P = a.head_dim, blocks = (P + 63) / 64;
-  const int head = (int)blockIdx.y / blocks, p0 = (int)blockIdx.y % blocks * 64;
-  const int heads = a.channels / P, g = head / (heads / a.groups);
+  const int P = a.head_dim, blocks = (P + 63) / 64, heads = a.channels / P;
+  const int64_t unit = unit_of_block(units);
+  if (unit >= units) return;
+  const int slot = (int)(unit / (heads * blocks)), part = (int)(unit % (heads * blocks));
+  const int head = part / blocks, p0 = part % blocks * 64, g = head / (heads / a.groups);
   int seq, begin, end;
   if constexpr (PART == 0) {
     seq = slot;
-    if (blockIdx.y == 0) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, seq, status);
+    if (part == 0) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, seq, status);
     begin = a.seq_offsets[seq];
     end = a.seq_offsets[seq + 1];
     if (begin < 0 || end < begin || end > a.num_tokens) return;
   } else {
-    if (PART == 1 && blockIdx.y == 0) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, slot, status);
+    if (PART == 1 && part == 0) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, slot, status);
     const Chunk c = find_chunk(a.seq_offsets, a.num_seqs, a.num_tokens, Q, slot);
     if (c.seq < 0 || c.begin == c.end) return;
     seq = c.seq;
@@ -172,33 +188,28 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma_kernel(cortex_scan_
   const float A2 = a.A[head] * kLog2e, bias = a.dt_bias ? a.dt_bias[head] : 0.0f, skip = a.skip ? a.skip[head] : 0.0f;
   const bf16_t *xs = (const bf16_t *)a.x + head * P + p0, *ds = (const bf16_t *)a.dt + head;
   const bf16_t *Bs = (const bf16_t *)a.B + g * N, *Cs = (const bf16_t *)a.C + g * N;
-  const int ch = head * P + (works ? pw : 0) + q * 4;             // the lane's four channels of y and z
-  const bf16_t *zs = a.z ? (const bf16_t *)a.z + ch : nullptr;
-  bf16_t *ys = (bf16_t *)a.y + ch;
+  // the thread's eight channels of one token, of x, z and y
+  const int xo = tid % 8 * 8, xt = tid / 8;
+  const bool whole = p0 + xo < P;
+  const int xc = whole ? xo : 0;
+  const bf16_t *zs = a.z ? (const bf16_t *)a.z + head * P + p0 + xc : nullptr;
+  bf16_t *ys = (bf16_t *)a.y + head * P + p0 + xc;
   float steps = 0.0f;
 
   // What the next sub-chunk needs, loaded while this one is worked on.  The loads
   // are unconditional, so that nothing waits for one of them: tokens past the
   // segment's end repeat the last one, and are made zeros when they are stored.
-  u32x4v xr[2], br[kItems][2], cr[kItems][2];
+  u32x4v xr, br[kItems], cr[kItems];
   float raw = 0.0f;
   const u32x4v none = {0, 0, 0, 0};
-  const int xo = (tid & 3) | (tid >> 7) << 2, xp = 2 * (tid >> 2 & 31);
-  auto item_octet = [&](int i) { return tid % OL + (i * kHeadThreads + tid) / (OL * 32) * OL; };
-  auto item_token = [&](int i) { return 2 * ((i * kHeadThreads + tid) / OL % 32); };
   auto fetch = [&](int t0) {
-    const bf16_t *px = xs + (p0 + xo * 8 < P ? xo * 8 : 0);
-#pragma unroll
-    for (int r = 0; r < 2; ++r) xr[r] = load8<WIDE>(px + (int64_t)min(t0 + xp + r, end - 1) * a.x_ld);
+    xr = load8<WIDE>(xs + (int64_t)min(t0 + xt, end - 1) * a.x_ld + xc);
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-      const int o = min(item_octet(i), N / 8 - 1);
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int64_t t = min(t0 + item_token(i) + r, end - 1);
-        br[i][r] = load8<WIDE>(Bs + t * a.B_ld + o * 8);
-        if (PART != 1) cr[i][r] = load8<WIDE>(Cs + t * a.C_ld + o * 8);
-      }
+      const int id = i * kHeadThreads + tid;
+      const int64_t t = min(t0 + id / OL, end - 1);
+      br[i] = load8<WIDE>(Bs + t * a.B_ld + id % OL * 8);
+      if (PART != 1) cr[i] = load8<WIDE>(Cs + t * a.C_ld + id % OL * 8);
     }
     if (wave == 3) raw = to_float<bf16_t>(ds[(int64_t)min(t0 + lane, end - 1) * a.dt_ld]);
   };
@@ -213,97 +224,64 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma_kernel(cortex_scan_
       *(uint2 *)&lds.B[swizzled<Lds::NP>(s, k_position(e))] = make_uint2(0, 0);
       *(uint2 *)&lds.C[swizzled<Lds::NP>(s, k_position(e))] = make_uint2(0, 0);
     }
-  // the tiles above the diagonal that a product over 32 tokens reaches: (0,1) and (2,3)
-  if (PART != 1) {
-    const int t = (tid >> 7) * 32 + (tid & 15), s = (tid >> 7) * 32 + 16 + (tid >> 4 & 3) * 4;
-    *(uint2 *)&lds.M[tid >> 6 & 1][swizzled<kSub>(t, k_position(s))] = make_uint2(0, 0);
-  }
+  // the tile above the diagonal, which a product over 32 tokens reaches
+  if (PART != 1 && tid < 128)
+    *(uint2 *)&lds.M[tid >> 6][swizzled<kSub>(l16, k_position(16 + q * 4))] = make_uint2(0, 0);
 
   if (begin < end) {
     fetch(begin);
-    if (wave == 3) steps += put_steps(lds.steps[0], lane, begin + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
+    if (wave == 3) steps += put_steps(lds.steps[0], lane, lane < kSub && begin + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
   }
   int buf = 0;
 #pragma unroll 1
   for (int t0 = begin; t0 < end; t0 += kSub, buf ^= 1) {
-    __syncthreads();                             // everyone is done with the last sub-chunk's LDS
-    if (t0 + kSub > end) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        if (t0 + xp + r >= end) xr[r] = none;
-#pragma unroll
-        for (int i = 0; i < kItems; ++i)
-          if (t0 + item_token(i) + r >= end) {
-            br[i][r] = none;
-            if (PART != 1) cr[i][r] = none;
-          }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) *(unsigned int *)&lds.xT[xo * 8 + i][k_position(xp)] = pair_of(xr[0], xr[1], i);
+    // Everyone is done with the last sub-chunk's B, C, x and scores: they are read
+    // before its y is exchanged.
+    if (PART == 1) __syncthreads();
+    *(u32x4v *)&lds.x[swizzled<64>(xt, xo)] = t0 + xt < end ? xr : none;
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-      const int o = item_octet(i), s = item_token(i);
-      if (o < N / 8) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) *(unsigned int *)&lds.BT[o * 8 + k][k_position(s)] = pair_of(br[i][0], br[i][1], k);
-        if (PART != 1) {
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            put_row(lds.B, s + r, o, br[i][r]);
-            put_row(lds.C, s + r, o, cr[i][r]);
-          }
-        }
+      const int id = i * kHeadThreads + tid, s = id / OL;
+      if (kItems * kHeadThreads == OL * kSub || s < kSub) {
+        put_row(lds.B, s, id % OL, t0 + s < end ? br[i] : none);
+        if (PART != 1) put_row(lds.C, s, id % OL, t0 + s < end ? cr[i] : none);
       }
     }
     __syncthreads();
     if (t0 + kSub < end) fetch(t0 + kSub);
     const HeadSteps &st = lds.steps[buf];
-
+    // x of the wave's channels, over the tokens
+    const bf16x8v x = join8(lds_columns(&lds.x[swizzled<64>(q * 4 + l16 / 4, wave * 16 + l16 % 4 * 4)]),
+                            lds_columns(&lds.x[swizzled<64>(16 + q * 4 + l16 / 4, wave * 16 + l16 % 4 * 4)]));
+    u32x4v zr = none;
+    f32x4 y[2];
     if constexpr (PART != 1) {
-      uint2 zr[4];
-      if (zs && works)
+      if (zs) zr = load8<WIDE>(zs + (int64_t)min(t0 + xt, end - 1) * a.z_ld);
+      // Scores: the tiles (0,0) (1,0) (1,1) on and below the diagonal, one a wave.
+      if (wave < 3) {
+        const int ti = wave > 0, si = wave > 1;
+        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int ti = 0; ti < 4; ++ti) {
-          const bf16_t *p = zs + (int64_t)min(t0 + ti * 16 + l16, end - 1) * a.z_ld;
-          if constexpr (WIDE) {
-            zr[ti] = *(const uint2 *)p;
-          } else {
-            const unsigned short *e = (const unsigned short *)p;
-            zr[ti] = make_uint2(e[0] | (unsigned int)e[1] << 16, e[2] | (unsigned int)e[3] << 16);
-          }
+        for (int m = 0; m < NB; ++m)
+          acc = mfma_bf16x32(lds8(&lds.B[swizzled<Lds::NP>(si * 16 + l16, m * 32 + q * 8)]),
+                             lds8(&lds.C[swizzled<Lds::NP>(ti * 16 + l16, m * 32 + q * 8)]), acc);
+        const int t = ti * 16 + l16, s = si * 16 + q * 4;
+        const float ct = st.cum[t];
+        const f32x4 cs = *(const f32x4 *)&st.cum[s], dt = *(const f32x4 *)&st.dt[s];
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = s + i <= t ? acc[i] * (fast_exp2(ct - cs[i]) * dt[i]) : 0.0f;
+          if (s + i == t) v[i] += skip;
         }
-      // Scores: 10 tiles of 16 x 16 on and below the diagonal, three or two a wave.
-#pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        const int id = wave + 4 * k;             // (0,0) (1,0) (1,1) (2,0) (2,1) (2,2) (3,0) (3,1) (3,2) (3,3)
-        const int ti = id < 1 ? 0 : id < 3 ? 1 : id < 6 ? 2 : 3, si = id - ti * (ti + 1) / 2;
-        if (id < 10) {
-          f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int m = 0; m < NB; ++m)
-            acc = mfma_bf16x32(lds8(&lds.B[swizzled<Lds::NP>(si * 16 + l16, m * 32 + q * 8)]),
-                               lds8(&lds.C[swizzled<Lds::NP>(ti * 16 + l16, m * 32 + q * 8)]), acc);
-          const int t = ti * 16 + l16, s = si * 16 + q * 4;
-          const float ct = st.cum[t];
-          const f32x4 cs = *(const f32x4 *)&st.cum[s], dt = *(const f32x4 *)&st.dt[s];
-          float v[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            v[i] = s + i <= t ? acc[i] * (fast_exp2(ct - cs[i]) * dt[i]) : 0.0f;
-            if (s + i == t) v[i] += skip;
-          }
-          __bf16 b[4];
-          plane(v, b);
-          *(u16x4 *)&lds.M[0][swizzled<kSub>(t, k_position(s))] = __builtin_bit_cast(u16x4, b);
-          plane(v, b);
-          *(u16x4 *)&lds.M[1][swizzled<kSub>(t, k_position(s))] = __builtin_bit_cast(u16x4, b);
-        }
+        __bf16 b[4];
+        plane(v, b);
+        *(u16x4 *)&lds.M[0][swizzled<kSub>(t, k_position(s))] = __builtin_bit_cast(u16x4, b);
+        plane(v, b);
+        *(u16x4 *)&lds.M[1][swizzled<kSub>(t, k_position(s))] = __builtin_bit_cast(u16x4, b);
       }
       // From the state: rows channels, columns t.
-      f32x4 y[4];
-#pragma unroll
-      for (int ti = 0; ti < 4; ++ti) y[ti] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      y[0] = y[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
       if (works) {
 #pragma unroll
         for (int m = 0; m < NB; ++m) {
@@ -319,111 +297,108 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma_kernel(cortex_scan_
           plane(v, b);
           const bf16x8v lo = pack8(b);
 #pragma unroll
-          for (int ti = 0; ti < 4; ++ti) {
+          for (int ti = 0; ti < 2; ++ti) {
             const bf16x8v c = lds8(&lds.C[swizzled<Lds::NP>(ti * 16 + l16, m * 32 + q * 8)]);
             y[ti] = mfma_bf16x32(lo, c, y[ti]);
             y[ti] = mfma_bf16x32(hi, c, y[ti]);
           }
         }
 #pragma unroll
-        for (int ti = 0; ti < 4; ++ti) y[ti] *= st.grow[ti * 16 + l16];
-      }
-      __syncthreads();                           // the scores are there
-      if (works) {
-        bf16x8v x[2];
-        unsigned int odd = 0;                    // an infinity or NaN: an exponent of all ones
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          x[kb] = lds8(&lds.xT[wave * 16 + l16][kb * 32 + q * 8]);
-          const u32x4v v = __builtin_bit_cast(u32x4v, x[kb]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) odd |= ((v[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-        }
-        // The products with the zeros above the diagonal would carry such an input to the tokens
-        // before it.  It is left out of them, and its channel's tokens from its own on become NaN.
-        const bool any_odd = __any(odd != 0);
-        int first_odd[4] = {kSub, kSub, kSub, kSub};
-        if (any_odd) {
-          int first = kSub;
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float v = (float)x[kb][j];
-              if (!(__builtin_fabsf(v) < __builtin_inff())) {
-                const int s = kb * 32 + (j < 4 ? 0 : 12) + q * 4 + j;
-                first = s < first ? s : first;
-                x[kb][j] = (__bf16)0.0f;
-              }
-            }
-          first = min(first, __shfl_xor(first, 16));
-          first = min(first, __shfl_xor(first, 32));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) first_odd[i] = __shfl(first, q * 4 + i);
-        }
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int ti = 0; ti < 4; ++ti)
-            if (ti >= 2 * kb) {
-              y[ti] = mfma_bf16x32(x[kb], lds8(&lds.M[1][swizzled<kSub>(ti * 16 + l16, kb * 32 + q * 8)]), y[ti]);
-              y[ti] = mfma_bf16x32(x[kb], lds8(&lds.M[0][swizzled<kSub>(ti * 16 + l16, kb * 32 + q * 8)]), y[ti]);
-            }
-#pragma unroll
-        for (int ti = 0; ti < 4; ++ti) {
-          const int t = t0 + ti * 16 + l16;
-          float v[4] = {y[ti][0], y[ti][1], y[ti][2], y[ti][3]};
-          if (any_odd)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = ti * 16 + l16 >= first_odd[i] ? __builtin_nanf("") : v[i];
-          if (zs) {
-            v[0] *= silu(__builtin_bit_cast(float, zr[ti].x << 16));
-            v[1] *= silu(__builtin_bit_cast(float, zr[ti].x & 0xffff0000u));
-            v[2] *= silu(__builtin_bit_cast(float, zr[ti].y << 16));
-            v[3] *= silu(__builtin_bit_cast(float, zr[ti].y & 0xffff0000u));
-          }
-          if (t < end) {
-            bf16_t *p = ys + (int64_t)t * a.y_ld;
-            if constexpr (WIDE) Pack<bf16_t, 4>::store(p, v);
-            else
-#pragma unroll
-              for (int i = 0; i < 4; ++i) p[i] = from_float<bf16_t>(v[i]);
-          }
-        }
+        for (int ti = 0; ti < 2; ++ti) y[ti] *= st.grow[ti * 16 + l16];
       }
     }
+    // The state's update.
     if (works) {
       const float decay = st.decay;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) h[nt] *= decay;
+      const f32x4 w0 = *(const f32x4 *)&st.weight[q * 4], w1 = *(const f32x4 *)&st.weight[16 + q * 4];
+      float v[8];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const bf16x8v x = lds8(&lds.xT[wave * 16 + l16][kb * 32 + q * 8]);
-        const f32x4 w0 = *(const f32x4 *)&st.weight[kb * 32 + q * 4], w1 = *(const f32x4 *)&st.weight[kb * 32 + 16 + q * 4];
-        float v[8];
+      for (int i = 0; i < 4; ++i) {
+        v[i] = (float)x[i] * w0[i];
+        v[4 + i] = (float)x[4 + i] * w1[i];
+      }
+      __bf16 b[8];
+      plane(v, b);
+      const bf16x8v x0 = pack8(b);
+      plane(v, b);
+      const bf16x8v x1 = pack8(b);
+      plane(v, b);
+      const bf16x8v x2 = pack8(b);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[i] = (float)x[i] * w0[i];
-          v[4 + i] = (float)x[4 + i] * w1[i];
-        }
-        __bf16 b[8];
-        plane(v, b);
-        const bf16x8v x0 = pack8(b);
-        plane(v, b);
-        const bf16x8v x1 = pack8(b);
-        plane(v, b);
-        const bf16x8v x2 = pack8(b);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const bf16x8v bt = lds8(&lds.BT[nt * 16 + l16][kb * 32 + q * 8]);
-          h[nt] = mfma_bf16x32(bt, x2, h[nt]);
-          h[nt] = mfma_bf16x32(bt, x1, h[nt]);
-          h[nt] = mfma_bf16x32(bt, x0, h[nt]);
-        }
+      for (int nt = 0; nt < NT; ++nt) {
+        const int n = k_position(nt * 16 + l16 % 4 * 4);
+        const bf16x8v bt = join8(lds_columns(&lds.B[swizzled<Lds::NP>(q * 4 + l16 / 4, n)]),
+                                 lds_columns(&lds.B[swizzled<Lds::NP>(16 + q * 4 + l16 / 4, n)]));
+        h[nt] = mfma_bf16x32(bt, x2, h[nt]);
+        h[nt] = mfma_bf16x32(bt, x1, h[nt]);
+        h[nt] = mfma_bf16x32(bt, x0, h[nt]);
       }
     }
     if (wave == 3 && t0 + kSub < end)
-      steps += put_steps(lds.steps[buf ^ 1], lane, t0 + kSub + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
+      steps += put_steps(lds.steps[buf ^ 1], lane, lane < kSub && t0 + kSub + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
+    if constexpr (PART != 1) {
+      __syncthreads();                           // the scores are there
+      if (works) {
+        // The products with the zeros above the diagonal would carry an infinite or NaN x (an
+        // exponent of all ones) to the tokens before it.  It is left out of them, and its
+        // channel's tokens from its own on become NaN.
+        const u32x4v bits = __builtin_bit_cast(u32x4v, x);
+        bf16x8v xf = x;
+        unsigned int odd = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) odd |= ((bits[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+        const bool any_odd = __any(odd != 0);
+        int first = kSub;
+        if (any_odd) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float v = (float)x[j];
+            if (!(__builtin_fabsf(v) < __builtin_inff())) {
+              const int s = (j < 4 ? 0 : 12) + q * 4 + j;
+              first = s < first ? s : first;
+              xf[j] = (__bf16)0.0f;
+            }
+          }
+          first = min(first, __shfl_xor(first, 16));
+          first = min(first, __shfl_xor(first, 32));
+        }
+#pragma unroll
+        for (int p = 1; p >= 0; --p)
+#pragma unroll
+          for (int ti = 0; ti < 2; ++ti)
+            y[ti] = mfma_bf16x32(xf, lds8(&lds.M[p][swizzled<kSub>(ti * 16 + l16, q * 8)]), y[ti]);
+        if (any_odd)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int from = __shfl(first, q * 4 + i);
+#pragma unroll
+            for (int ti = 0; ti < 2; ++ti)
+              if (ti * 16 + l16 >= from) y[ti][i] = __builtin_nanf("");
+          }
+        // 16-byte pieces of a row exchanged by its number
+#pragma unroll
+        for (int ti = 0; ti < 2; ++ti) *(f32x4 *)&lds.y[(ti * 16 + l16) * 64 + (((wave * 4 + q) ^ l16) << 2)] = y[ti];
+      }
+      __syncthreads();                           // y is there
+      if (whole && t0 + xt < end) {
+        const f32x4 lo = *(const f32x4 *)&lds.y[xt * 64 + (((xo >> 2) ^ (xt & 15)) << 2)];
+        const f32x4 hi = *(const f32x4 *)&lds.y[xt * 64 + (((xo >> 2 | 1) ^ (xt & 15)) << 2)];
+        float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        if (zs)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            v[2 * i] *= silu(__builtin_bit_cast(float, zr[i] << 16));
+            v[2 * i + 1] *= silu(__builtin_bit_cast(float, zr[i] & 0xffff0000u));
+          }
+        bf16_t *p = ys + (int64_t)(t0 + xt) * a.y_ld;
+        if constexpr (WIDE) Pack<bf16_t, 8>::store(p, v);
+        else
+#pragma unroll
+          for (int i = 0; i < 8; ++i) p[i] = from_float<bf16_t>(v[i]);
+      }
+    }
   }
   if (PART == 1 && tid == 192 && p0 == 0) w.steps[(int64_t)slot * heads + head] = steps;
   float *h_out = PART == 1 ? w.state + ((int64_t)slot * a.channels + d) * N

@@ -15,35 +15,13 @@
 
 namespace cortex {
 
-constexpr int kSub32 = 32;
-
-struct HeadSteps32 {
-  float dt[kSub32], cum[kSub32], grow[kSub32], weight[kSub32], decay;
-};
-
 template <int N> struct HeadLds32 {
-  float B[kSub32][N + 4];        // rows 16 bytes longer: see the bf16 form
-  float C[kSub32][N + 4];
-  float x[kSub32][64 + 4];
-  float M[kSub32][kSub32 + 4];   // scores [t][s]
-  HeadSteps32 steps[2];
+  float B[kSub][N + 4];        // rows 16 bytes longer: see the bf16 form
+  float C[kSub][N + 4];
+  float x[kSub][64 + 4];
+  float M[kSub][kSub + 4];   // scores [t][s]
+  HeadSteps steps[2];
 };
-
-// As put_steps, over 32 tokens; the lanes above them hold a step of 0.
-__device__ __forceinline__ float put_steps32(HeadSteps32 &to, int lane, float dt, float A2) {
-  const float up = lane_sums(dt * A2);
-  const float rev = __shfl(dt, 31 - lane & 63);
-  const float down = lane_sums(lane < 32 ? rev * A2 : 0.0f);
-  const float after = __shfl_up(down, 1);
-  if (lane < 32) {
-    to.dt[lane] = dt;
-    to.cum[lane] = up;
-    to.grow[lane] = fast_exp2(up);
-    to.weight[31 - lane] = fast_exp2(lane == 0 ? 0.0f : after) * rev;
-  }
-  if (lane == 31) to.decay = fast_exp2(down);
-  return wave_sum(dt);
-}
 
 template <bool WIDE> __device__ __forceinline__ f32x4 load4f(const float *p) {
   if constexpr (WIDE) return *(const f32x4 *)p;
@@ -58,24 +36,27 @@ __device__ __forceinline__ f32x4 mfma_k16(f32x4 a, f32x4 b, f32x4 c) {
 }
 
 template <int N, int PART, bool WIDE>
-__global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w, int Q) {
-  constexpr int NT = N / 16, kItems = (N / 4 * kSub32 + kHeadThreads - 1) / kHeadThreads;
+__global__ void __launch_bounds__(kHeadThreads, 3) head_mfma32_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w, int Q,
+                                                                    int64_t units) {
+  constexpr int NT = N / 16, kItems = (N / 4 * kSub + kHeadThreads - 1) / kHeadThreads;
   __shared__ HeadLds32<N> lds;
   if (entry_status(status) != 0) return;
-  const int slot = (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int q = lane >> 4, l16 = lane & 15;
-  const int P = a.head_dim, blocks = (P + 63) / 64;
-  const int head = (int)blockIdx.y / blocks, p0 = (int)blockIdx.y % blocks * 64;
-  const int heads = a.channels / P, g = head / (heads / a.groups);
+  const int P = a.head_dim, blocks = (P + 63) / 64, heads = a.channels / P;
+  const int64_t unit = unit_of_block(units);
+  if (unit >= units) return;
+  const int slot = (int)(unit / (heads * blocks)), part = (int)(unit % (heads * blocks));
+  const int head = part / blocks, p0 = part % blocks * 64, g = head / (heads / a.groups);
   int seq, begin, end;
   if constexpr (PART == 0) {
     seq = slot;
-    if (blockIdx.y == 0) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, seq, status);
+    if (part == 0) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, seq, status);
     begin = a.seq_offsets[seq];
     end = a.seq_offsets[seq + 1];
     if (begin < 0 || end < begin || end > a.num_tokens) return;
   } else {
-    if (PART == 1 && blockIdx.y == 0) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, slot, status);
+    if (PART == 1 && part == 0) check_offsets(a.seq_offsets, a.num_seqs, a.num_tokens, slot, status);
     const Chunk c = find_chunk(a.seq_offsets, a.num_seqs, a.num_tokens, Q, slot);
     if (c.seq < 0 || c.begin == c.end) return;
     seq = c.seq;
@@ -124,7 +105,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
     if (wave == 3) raw = ds[(int64_t)min(t0 + lane, end - 1) * a.dt_ld];
   };
   auto next_steps = [&](int t0, int buf) {
-    steps += put_steps32(lds.steps[buf], lane, lane < kSub32 && t0 + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
+    steps += put_steps(lds.steps[buf], lane, lane < kSub && t0 + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
   };
 
   if (begin < end) {
@@ -133,7 +114,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
   }
   int buf = 0;
 #pragma unroll 1
-  for (int t0 = begin; t0 < end; t0 += kSub32, buf ^= 1) {
+  for (int t0 = begin; t0 < end; t0 += kSub, buf ^= 1) {
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -144,14 +125,14 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
     for (int i = 0; i < kItems; ++i) {
       const int id = i * kHeadThreads + tid;
       const bool in = t0 + id / (N / 4) < end;
-      if (id < N / 4 * kSub32) {
+      if (id < N / 4 * kSub) {
         *(f32x4 *)&lds.B[id / (N / 4)][id % (N / 4) * 4] = in ? br[i] : none;
         if (PART != 1) *(f32x4 *)&lds.C[id / (N / 4)][id % (N / 4) * 4] = in ? cr[i] : none;
       }
     }
     __syncthreads();
-    if (t0 + kSub32 < end) fetch(t0 + kSub32);
-    const HeadSteps32 &st = lds.steps[buf];
+    if (t0 + kSub < end) fetch(t0 + kSub);
+    const HeadSteps &st = lds.steps[buf];
 
     // the wave's channels of x, by sixteen tokens: k = 4 q + i
     float x[2][4];
@@ -197,7 +178,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
       if (works) {
         // an infinite or NaN x: as in the bf16 form
         float xf[2][4];
-        int first_odd = kSub32;
+        int first_odd = kSub;
 #pragma unroll
         for (int si = 0; si < 2; ++si)
 #pragma unroll
@@ -216,7 +197,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
             if (ti >= si)
               y[ti] = mfma_k16(f32x4{xf[si][0], xf[si][1], xf[si][2], xf[si][3]},
                                *(const f32x4 *)&lds.M[ti * 16 + l16][si * 16 + q * 4], y[ti]);
-        if (__any(first_odd < kSub32)) {
+        if (__any(first_odd < kSub)) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int odd = __shfl(first_odd, q * 4 + i);
@@ -258,7 +239,7 @@ __global__ void __launch_bounds__(kHeadThreads, 2) head_mfma32_kernel(cortex_sca
         }
       }
     }
-    if (wave == 3 && t0 + kSub32 < end) next_steps(t0 + kSub32, buf ^ 1);
+    if (wave == 3 && t0 + kSub < end) next_steps(t0 + kSub, buf ^ 1);
   }
   if (PART == 1 && tid == 192 && p0 == 0) w.steps[(int64_t)slot * heads + head] = steps;
   float *h_out = PART == 1 ? w.state + ((int64_t)slot * a.channels + d) * N
