@@ -37,8 +37,8 @@
 namespace cortex {
 
 typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
-typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4v __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2v __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kSub = 32;                 // tokens of a sub-chunk
@@ -54,38 +54,52 @@ __device__ __forceinline__ constexpr int k_position(int e) {
   return (e & ~31) | ((e & 12) << 1) | ((e & 16) >> 2) | (e & 3);
 }
 
-// The next bf16 plane of v, which keeps what is left.
-template <int M> __device__ __forceinline__ void plane(float (&v)[M], __bf16 (&p)[M]) {
+// The next bf16 plane of v, two values a word, which keeps what is left.
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+template <int M> __device__ __forceinline__ void plane(float (&v)[M], unsigned int (&p)[M / 2]) {
 #pragma unroll
-  for (int i = 0; i < M; ++i) {
-    p[i] = (__bf16)v[i];
-    v[i] -= (float)p[i];
+  for (int i = 0; i < M / 2; ++i) {
+    p[i] = __builtin_bit_cast(unsigned int, __builtin_convertvector(f32x2{v[2 * i], v[2 * i + 1]}, bf16x2v));
+    v[2 * i] -= __builtin_bit_cast(float, p[i] << 16);
+    v[2 * i + 1] -= __builtin_bit_cast(float, p[i] & 0xffff0000u);
   }
 }
-__device__ __forceinline__ bf16x8v pack8(const __bf16 (&p)[8]) {
-  return bf16x8v{p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]};
+__device__ __forceinline__ bf16x8v pack8(const unsigned int (&p)[4]) {
+  return __builtin_bit_cast(bf16x8v, u32x4v{p[0], p[1], p[2], p[3]});
 }
 
-// Rows of W elements: the 16-byte pieces of a row are exchanged by its number, so
-// that reads down neighbouring rows fall into different banks.
-template <int W> __device__ __forceinline__ int swizzled(int row, int pos) {
-  constexpr int kPieces = W / 8;
-  const int f = kPieces >= 8 ? row & (kPieces - 1) & 15 : row >> 2 & 3;
-  return row * W + (((pos >> 3) ^ f) << 3 | (pos & 7));
-}
+// Rows in LDS.  16-byte reads take one place of sixteen rows and the next of
+// sixteen more; the hardware serves rows 0..3 and 12..15 of one place together with
+// rows 4..11 of the next, and the others so.  A row of 64 elements or more is 64
+// bytes longer, so that four rows start in different banks, and the places of four
+// 16-byte pieces are exchanged by (- row / 4) mod 4, which keeps those sixteen
+// apart.  Of an address only the lane's part is computed; sixteen rows or 32
+// elements further on are constants.
+template <int W> struct Rows {
+  static constexpr int kStride = W >= 64 ? W + 32 : W;
+  static __device__ __forceinline__ int at(int row, int pos) {
+    return row * kStride + (pos & ~31) + ((((pos >> 3) ^ -(row >> 2)) & 3) << 3) + (pos & 7);
+  }
+};
+// Rows of 64 channels, or of 64 floats: pieces exchanged by the row's number.
+__device__ __forceinline__ int channel_at(int row, int ch) { return row * 64 + (((ch >> 3) ^ (row & 7)) << 3) + (ch & 7); }
+__device__ __forceinline__ int float_at(int row, int ch) { return row * 64 + (((ch >> 2) ^ (row & 15)) << 2) + (ch & 3); }
 
 // Step sizes of a sub-chunk: dt_s, c_s, exp(c_s), exp(c_31 - c_s) dt_s, exp(c_31).
-struct HeadSteps {
+struct alignas(16) HeadSteps {
   float dt[kSub], cum[kSub], grow[kSub], weight[kSub], decay;
 };
 
 template <int N> struct HeadLds {
   static constexpr int NP = N < 32 ? 32 : N;      // the products over N take 32 at a time; what is past N is 0
-  unsigned short B[kSub * NP];                    // [s][n position]
-  unsigned short C[kSub * NP];                    // [t][n position]
-  unsigned short x[kSub * 64];                    // [s][channel]
-  unsigned short M[2][kSub * kSub];               // scores, two planes: [t][s position]
-  float y[kSub * 64];                             // [t][channel]
+  typedef Rows<NP> N_;
+  typedef Rows<kSub> T_;
+  alignas(16) unsigned short B[kSub * N_::kStride];           // [s][n position]
+  alignas(16) unsigned short C[kSub * N_::kStride];           // [t][n position]
+  alignas(16) unsigned short x[kSub * 64];                    // [s][channel]
+  alignas(16) unsigned short M[2][kSub * T_::kStride];        // scores, two planes: [t][s position]
+  alignas(16) float y[kSub * 64];                             // [t][channel]
   HeadSteps steps[2];
 };
 
@@ -198,35 +212,40 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
 
   // What the next sub-chunk needs, loaded while this one is worked on.  The loads
   // are unconditional, so that nothing waits for one of them: tokens past the
-  // segment's end repeat the last one, and are made zeros when they are stored.
+  // segment's end repeat its last, and are made zeros when they are stored.
   u32x4v xr, br[kItems], cr[kItems];
   float raw = 0.0f;
   const u32x4v none = {0, 0, 0, 0};
   auto fetch = [&](int t0) {
-    xr = load8<WIDE>(xs + (int64_t)min(t0 + xt, end - 1) * a.x_ld + xc);
+    // rows from the sub-chunk's first, in 32 bits (the host admits no longer rows)
+    const int last = end - 1 - t0;
+    const bool all = last >= kSub - 1;
+    const bf16_t *x0 = xs + (int64_t)t0 * a.x_ld, *B0 = Bs + (int64_t)t0 * a.B_ld, *C0 = Cs + (int64_t)t0 * a.C_ld;
+    const uint32_t x_ld = (uint32_t)a.x_ld, B_ld = (uint32_t)a.B_ld, C_ld = (uint32_t)a.C_ld;
+    xr = load8<WIDE>(x0 + ((all ? xt : min(xt, last)) * x_ld + xc));
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-      const int id = i * kHeadThreads + tid;
-      const int64_t t = min(t0 + id / OL, end - 1);
-      br[i] = load8<WIDE>(Bs + t * a.B_ld + id % OL * 8);
-      if (PART != 1) cr[i] = load8<WIDE>(Cs + t * a.C_ld + id % OL * 8);
+      const int id = i * kHeadThreads + tid, o = id % OL * 8;
+      const uint32_t s = kItems * kHeadThreads == OL * kSub && all ? id / OL : min(id / OL, min(last, kSub - 1));
+      br[i] = load8<WIDE>(B0 + (s * B_ld + o));
+      if (PART != 1) cr[i] = load8<WIDE>(C0 + (s * C_ld + o));
     }
     if (wave == 3) raw = to_float<bf16_t>(ds[(int64_t)min(t0 + lane, end - 1) * a.dt_ld]);
   };
   // Rows of eight state entries (octet o) in k order: two halves of 8 bytes.
   auto put_row = [&](unsigned short *to, int row, int o, const u32x4v &v) {
-    *(uint2 *)(to + swizzled<Lds::NP>(row, k_position(o * 8))) = make_uint2(v[0], v[1]);
-    *(uint2 *)(to + swizzled<Lds::NP>(row, k_position(o * 8 + 4))) = make_uint2(v[2], v[3]);
+    *(u32x2v *)(to + Lds::N_::at(row, k_position(o * 8))) = u32x2v{v[0], v[1]};
+    *(u32x2v *)(to + Lds::N_::at(row, k_position(o * 8 + 4))) = u32x2v{v[2], v[3]};
   };
   if constexpr (N < 32)
     for (int i = tid; i < kSub * (Lds::NP - N) / 4; i += kHeadThreads) {
       const int s = i / ((Lds::NP - N) / 4), e = N + i % ((Lds::NP - N) / 4) * 4;
-      *(uint2 *)&lds.B[swizzled<Lds::NP>(s, k_position(e))] = make_uint2(0, 0);
-      *(uint2 *)&lds.C[swizzled<Lds::NP>(s, k_position(e))] = make_uint2(0, 0);
+      *(u32x2v *)&lds.B[Lds::N_::at(s, k_position(e))] = u32x2v{0, 0};
+      *(u32x2v *)&lds.C[Lds::N_::at(s, k_position(e))] = u32x2v{0, 0};
     }
   // the tile above the diagonal, which a product over 32 tokens reaches
   if (PART != 1 && tid < 128)
-    *(uint2 *)&lds.M[tid >> 6][swizzled<kSub>(l16, k_position(16 + q * 4))] = make_uint2(0, 0);
+    *(u32x2v *)&lds.M[tid >> 6][Lds::T_::at(l16, k_position(16 + q * 4))] = u32x2v{0, 0};
 
   if (begin < end) {
     fetch(begin);
@@ -238,33 +257,39 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
     // Everyone is done with the last sub-chunk's B, C, x and scores: they are read
     // before its y is exchanged.
     if (PART == 1) __syncthreads();
-    *(u32x4v *)&lds.x[swizzled<64>(xt, xo)] = t0 + xt < end ? xr : none;
+    if (t0 + kSub > end) {
+      if (t0 + xt >= end) xr = none;
+#pragma unroll
+      for (int i = 0; i < kItems; ++i)
+        if (t0 + (i * kHeadThreads + tid) / OL >= end) br[i] = cr[i] = none;
+    }
+    *(u32x4v *)&lds.x[channel_at(xt, xo)] = xr;
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
       const int id = i * kHeadThreads + tid, s = id / OL;
       if (kItems * kHeadThreads == OL * kSub || s < kSub) {
-        put_row(lds.B, s, id % OL, t0 + s < end ? br[i] : none);
-        if (PART != 1) put_row(lds.C, s, id % OL, t0 + s < end ? cr[i] : none);
+        put_row(lds.B, s, id % OL, br[i]);
+        if (PART != 1) put_row(lds.C, s, id % OL, cr[i]);
       }
     }
     __syncthreads();
     if (t0 + kSub < end) fetch(t0 + kSub);
     const HeadSteps &st = lds.steps[buf];
     // x of the wave's channels, over the tokens
-    const bf16x8v x = join8(lds_columns(&lds.x[swizzled<64>(q * 4 + l16 / 4, wave * 16 + l16 % 4 * 4)]),
-                            lds_columns(&lds.x[swizzled<64>(16 + q * 4 + l16 / 4, wave * 16 + l16 % 4 * 4)]));
+    const bf16x8v x = join8(lds_columns(&lds.x[channel_at(q * 4 + l16 / 4, wave * 16 + l16 % 4 * 4)]),
+                            lds_columns(&lds.x[channel_at(16 + q * 4 + l16 / 4, wave * 16 + l16 % 4 * 4)]));
     u32x4v zr = none;
     f32x4 y[2];
     if constexpr (PART != 1) {
-      if (zs) zr = load8<WIDE>(zs + (int64_t)min(t0 + xt, end - 1) * a.z_ld);
+      if (zs) zr = load8<WIDE>(zs + (int64_t)t0 * a.z_ld + min(xt, end - 1 - t0) * (uint32_t)a.z_ld);
       // Scores: the tiles (0,0) (1,0) (1,1) on and below the diagonal, one a wave.
       if (wave < 3) {
         const int ti = wave > 0, si = wave > 1;
         f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int m = 0; m < NB; ++m)
-          acc = mfma_bf16x32(lds8(&lds.B[swizzled<Lds::NP>(si * 16 + l16, m * 32 + q * 8)]),
-                             lds8(&lds.C[swizzled<Lds::NP>(ti * 16 + l16, m * 32 + q * 8)]), acc);
+          acc = mfma_bf16x32(lds8(&lds.B[Lds::N_::at(si * 16 + l16, m * 32 + q * 8)]),
+                             lds8(&lds.C[Lds::N_::at(ti * 16 + l16, m * 32 + q * 8)]), acc);
         const int t = ti * 16 + l16, s = si * 16 + q * 4;
         const float ct = st.cum[t];
         const f32x4 cs = *(const f32x4 *)&st.cum[s], dt = *(const f32x4 *)&st.dt[s];
@@ -274,11 +299,11 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
           v[i] = s + i <= t ? acc[i] * (fast_exp2(ct - cs[i]) * dt[i]) : 0.0f;
           if (s + i == t) v[i] += skip;
         }
-        __bf16 b[4];
+        unsigned int b[2];
         plane(v, b);
-        *(u16x4 *)&lds.M[0][swizzled<kSub>(t, k_position(s))] = __builtin_bit_cast(u16x4, b);
+        *(u32x2v *)&lds.M[0][Lds::T_::at(t, k_position(s))] = u32x2v{b[0], b[1]};
         plane(v, b);
-        *(u16x4 *)&lds.M[1][swizzled<kSub>(t, k_position(s))] = __builtin_bit_cast(u16x4, b);
+        *(u32x2v *)&lds.M[1][Lds::T_::at(t, k_position(s))] = u32x2v{b[0], b[1]};
       }
       // From the state: rows channels, columns t.
       y[0] = y[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -291,14 +316,14 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
             v[i] = h[2 * m][i];
             v[4 + i] = 2 * m + 1 < NT ? h[2 * m + 1 < NT ? 2 * m + 1 : 0][i] : 0.0f;
           }
-          __bf16 b[8];
+          unsigned int b[4];
           plane(v, b);
           const bf16x8v hi = pack8(b);
           plane(v, b);
           const bf16x8v lo = pack8(b);
 #pragma unroll
           for (int ti = 0; ti < 2; ++ti) {
-            const bf16x8v c = lds8(&lds.C[swizzled<Lds::NP>(ti * 16 + l16, m * 32 + q * 8)]);
+            const bf16x8v c = lds8(&lds.C[Lds::N_::at(ti * 16 + l16, m * 32 + q * 8)]);
             y[ti] = mfma_bf16x32(lo, c, y[ti]);
             y[ti] = mfma_bf16x32(hi, c, y[ti]);
           }
@@ -319,7 +344,7 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
         v[i] = (float)x[i] * w0[i];
         v[4 + i] = (float)x[4 + i] * w1[i];
       }
-      __bf16 b[8];
+      unsigned int b[4];
       plane(v, b);
       const bf16x8v x0 = pack8(b);
       plane(v, b);
@@ -329,8 +354,8 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int n = k_position(nt * 16 + l16 % 4 * 4);
-        const bf16x8v bt = join8(lds_columns(&lds.B[swizzled<Lds::NP>(q * 4 + l16 / 4, n)]),
-                                 lds_columns(&lds.B[swizzled<Lds::NP>(16 + q * 4 + l16 / 4, n)]));
+        const bf16x8v bt = join8(lds_columns(&lds.B[Lds::N_::at(q * 4 + l16 / 4, n)]),
+                                 lds_columns(&lds.B[Lds::N_::at(16 + q * 4 + l16 / 4, n)]));
         h[nt] = mfma_bf16x32(bt, x2, h[nt]);
         h[nt] = mfma_bf16x32(bt, x1, h[nt]);
         h[nt] = mfma_bf16x32(bt, x0, h[nt]);
@@ -368,7 +393,7 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
         for (int p = 1; p >= 0; --p)
 #pragma unroll
           for (int ti = 0; ti < 2; ++ti)
-            y[ti] = mfma_bf16x32(xf, lds8(&lds.M[p][swizzled<kSub>(ti * 16 + l16, q * 8)]), y[ti]);
+            y[ti] = mfma_bf16x32(xf, lds8(&lds.M[p][Lds::T_::at(ti * 16 + l16, q * 8)]), y[ti]);
         if (any_odd)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -377,14 +402,13 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
             for (int ti = 0; ti < 2; ++ti)
               if (ti * 16 + l16 >= from) y[ti][i] = __builtin_nanf("");
           }
-        // 16-byte pieces of a row exchanged by its number
 #pragma unroll
-        for (int ti = 0; ti < 2; ++ti) *(f32x4 *)&lds.y[(ti * 16 + l16) * 64 + (((wave * 4 + q) ^ l16) << 2)] = y[ti];
+        for (int ti = 0; ti < 2; ++ti) *(f32x4 *)&lds.y[float_at(ti * 16 + l16, wave * 16 + q * 4)] = y[ti];
       }
       __syncthreads();                           // y is there
       if (whole && t0 + xt < end) {
-        const f32x4 lo = *(const f32x4 *)&lds.y[xt * 64 + (((xo >> 2) ^ (xt & 15)) << 2)];
-        const f32x4 hi = *(const f32x4 *)&lds.y[xt * 64 + (((xo >> 2 | 1) ^ (xt & 15)) << 2)];
+        const f32x4 lo = *(const f32x4 *)&lds.y[float_at(xt, xo)];
+        const f32x4 hi = *(const f32x4 *)&lds.y[float_at(xt, xo + 4)];
         float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
         if (zs)
 #pragma unroll
@@ -392,7 +416,7 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
             v[2 * i] *= silu(__builtin_bit_cast(float, zr[i] << 16));
             v[2 * i + 1] *= silu(__builtin_bit_cast(float, zr[i] & 0xffff0000u));
           }
-        bf16_t *p = ys + (int64_t)(t0 + xt) * a.y_ld;
+        bf16_t *p = ys + (int64_t)t0 * a.y_ld + xt * (uint32_t)a.y_ld;
         if constexpr (WIDE) Pack<bf16_t, 8>::store(p, v);
         else
 #pragma unroll

@@ -189,6 +189,8 @@ inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
 // Grids count tiles of channels in 16 bits.
 constexpr int32_t kMaxChannels = 1 << 18;
+// 64 rows of elements stay below 2^31, so that places in a sub-chunk take 32 bits.
+constexpr int64_t kMaxRowStride = 1 << 25;
 
 // Host checks that the prompt and step forms share: sizes of the batch.
 inline bool bad_batch(int32_t dtype, int32_t S, int32_t T, int32_t channels, int32_t state_rows, const int32_t *index,
