@@ -100,24 +100,25 @@ template <int N> struct HeadLds {
   alignas(16) unsigned short x[kSub * 64];                    // [s][channel]
   alignas(16) unsigned short M[2][kSub * T_::kStride];        // scores, two planes: [t][s position]
   alignas(16) float y[kSub * 64];                             // [t][channel]
-  HeadSteps steps[2];
+  HeadSteps steps[4];                             // of this sub-chunk, its neighbour and the next two
+  float sums[kHeadWaves];
 };
 
-// A lane is a token; the lanes above them hold a step of 0.  The state's weights
-// come from a sum from the end: those near the end, which count most, are sums of
-// few terms.  Returns the sum of dt.
-__device__ __forceinline__ float put_steps(HeadSteps &to, int lane, float dt, float A2) {
-  const float up = lane_sums(dt * A2);
-  const float rev = __shfl(dt, (kSub - 1 - lane) & 63);
-  const float down = lane_sums(lane < kSub ? rev * A2 : 0.0f);    // of tokens 31 - lane and on
+// The steps of two sub-chunks, a lane a token.  The state's weights come from a sum
+// from the end: those near the end, which count most, are sums of few terms.
+// Returns the sum of dt over both.
+__device__ __forceinline__ float put_steps(HeadSteps (&to)[4], int pair, int lane, float dt, float A2) {
+  const float up = half_sums(dt * A2);
+  const float rev = __shfl_xor(dt, kSub - 1);
+  const float down = half_sums(rev * A2);         // from token 31 - lane of the half on
   const float after = __shfl_up(down, 1);
-  if (lane < kSub) {
-    to.dt[lane] = dt;
-    to.cum[lane] = up;
-    to.grow[lane] = fast_exp2(up);
-    to.weight[kSub - 1 - lane] = fast_exp2(lane == 0 ? 0.0f : after) * rev;
-  }
-  if (lane == kSub - 1) to.decay = fast_exp2(down);
+  const int i = lane % kSub;
+  HeadSteps &st = to[2 * pair + lane / kSub];
+  st.dt[i] = dt;
+  st.cum[i] = up;
+  st.grow[i] = fast_exp2(up);
+  st.weight[kSub - 1 - i] = fast_exp2(i == 0 ? 0.0f : after) * rev;
+  if (i == kSub - 1) st.decay = fast_exp2(down);
   return wave_sum(dt);
 }
 
@@ -214,7 +215,6 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
   // are unconditional, so that nothing waits for one of them: tokens past the
   // segment's end repeat its last, and are made zeros when they are stored.
   u32x4v xr, br[kItems], cr[kItems];
-  float raw = 0.0f;
   const u32x4v none = {0, 0, 0, 0};
   auto fetch = [&](int t0) {
     // rows from the sub-chunk's first, in 32 bits (the host admits no longer rows)
@@ -230,7 +230,6 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
       br[i] = load8<WIDE>(B0 + (s * B_ld + o));
       if (PART != 1) cr[i] = load8<WIDE>(C0 + (s * C_ld + o));
     }
-    if (wave == 3) raw = to_float<bf16_t>(ds[(int64_t)min(t0 + lane, end - 1) * a.dt_ld]);
   };
   // Rows of eight state entries (octet o) in k order: two halves of 8 bytes.
   auto put_row = [&](unsigned short *to, int row, int o, const u32x4v &v) {
@@ -247,13 +246,18 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
   if (PART != 1 && tid < 128)
     *(u32x2v *)&lds.M[tid >> 6][Lds::T_::at(l16, k_position(16 + q * 4))] = u32x2v{0, 0};
 
+  // Steps are made two sub-chunks ahead for two of them, by the waves in turn.
+  auto raw_step = [&](int t0) { return to_float<bf16_t>(ds[(int64_t)min(t0 + lane, end - 1) * a.dt_ld]); };
+  auto make_steps = [&](int t0, int pair, float raw) {
+    steps += put_steps(lds.steps, pair, lane, t0 + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
+  };
   if (begin < end) {
     fetch(begin);
-    if (wave == 3) steps += put_steps(lds.steps[0], lane, lane < kSub && begin + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
+    if (wave == 3) make_steps(begin, 0, raw_step(begin));
   }
-  int buf = 0;
 #pragma unroll 1
-  for (int t0 = begin; t0 < end; t0 += kSub, buf ^= 1) {
+  for (int t0 = begin, k = 0; t0 < end; t0 += kSub, ++k) {
+    const bool makes = k % 2 == 0 && k / 2 % 4 == wave && t0 + 2 * kSub < end;
     // Everyone is done with the last sub-chunk's B, C, x and scores: they are read
     // before its y is exchanged.
     if (PART == 1) __syncthreads();
@@ -274,7 +278,8 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
     }
     __syncthreads();
     if (t0 + kSub < end) fetch(t0 + kSub);
-    const HeadSteps &st = lds.steps[buf];
+    const float raw = makes ? raw_step(t0 + 2 * kSub) : 0.0f;
+    const HeadSteps &st = lds.steps[k % 4];
     // x of the wave's channels, over the tokens
     const bf16x8v x = join8(lds_columns(&lds.x[channel_at(q * 4 + l16 / 4, wave * 16 + l16 % 4 * 4)]),
                             lds_columns(&lds.x[channel_at(16 + q * 4 + l16 / 4, wave * 16 + l16 % 4 * 4)]));
@@ -361,8 +366,7 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
         h[nt] = mfma_bf16x32(bt, x0, h[nt]);
       }
     }
-    if (wave == 3 && t0 + kSub < end)
-      steps += put_steps(lds.steps[buf ^ 1], lane, lane < kSub && t0 + kSub + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
+    if (makes) make_steps(t0 + 2 * kSub, (k / 2 + 1) % 2, raw);
     if constexpr (PART != 1) {
       __syncthreads();                           // the scores are there
       if (works) {
@@ -424,7 +428,12 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
       }
     }
   }
-  if (PART == 1 && tid == 192 && p0 == 0) w.steps[(int64_t)slot * heads + head] = steps;
+  if (PART == 1) {
+    if (lane == 0) lds.sums[wave] = steps;
+    __syncthreads();
+    if (tid == 0 && p0 == 0)
+      w.steps[(int64_t)slot * heads + head] = (lds.sums[0] + lds.sums[1]) + (lds.sums[2] + lds.sums[3]);
+  }
   float *h_out = PART == 1 ? w.state + ((int64_t)slot * a.channels + d) * N
                            : PART == 0 && row >= 0 && a.state_out ? a.state_out + ((int64_t)row * a.channels + d) * N : nullptr;
   if (works && h_out)

@@ -20,7 +20,8 @@ template <int N> struct HeadLds32 {
   float C[kSub][N + 4];
   float x[kSub][64 + 4];
   float M[kSub][kSub + 4];   // scores [t][s]
-  HeadSteps steps[2];
+  HeadSteps steps[4];
+  float sums[kHeadWaves];
 };
 
 template <bool WIDE> __device__ __forceinline__ f32x4 load4f(const float *p) {
@@ -88,7 +89,6 @@ __global__ void __launch_bounds__(kHeadThreads, 3) head_mfma32_kernel(cortex_sca
 
   const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
   f32x4 xr[2], br[kItems], cr[kItems];
-  float raw = 0.0f;
   auto fetch = [&](int t0) {                      // as in the bf16 form
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -102,19 +102,19 @@ __global__ void __launch_bounds__(kHeadThreads, 3) head_mfma32_kernel(cortex_sca
       br[i] = load4f<WIDE>(Bs + t * a.B_ld + c);
       if (PART != 1) cr[i] = load4f<WIDE>(Cs + t * a.C_ld + c);
     }
-    if (wave == 3) raw = ds[(int64_t)min(t0 + lane, end - 1) * a.dt_ld];
   };
-  auto next_steps = [&](int t0, int buf) {
-    steps += put_steps(lds.steps[buf], lane, lane < kSub && t0 + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
+  auto raw_step = [&](int t0) { return ds[(int64_t)min(t0 + lane, end - 1) * a.dt_ld]; };
+  auto make_steps = [&](int t0, int pair, float raw) {
+    steps += put_steps(lds.steps, pair, lane, t0 + lane < end ? step_size(a, raw, bias) : 0.0f, A2);
   };
 
   if (begin < end) {
     fetch(begin);
-    if (wave == 3) next_steps(begin, 0);
+    if (wave == 3) make_steps(begin, 0, raw_step(begin));
   }
-  int buf = 0;
 #pragma unroll 1
-  for (int t0 = begin; t0 < end; t0 += kSub, buf ^= 1) {
+  for (int t0 = begin, k = 0; t0 < end; t0 += kSub, ++k) {
+    const bool makes = k % 2 == 0 && k / 2 % 4 == wave && t0 + 2 * kSub < end;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -132,7 +132,8 @@ __global__ void __launch_bounds__(kHeadThreads, 3) head_mfma32_kernel(cortex_sca
     }
     __syncthreads();
     if (t0 + kSub < end) fetch(t0 + kSub);
-    const HeadSteps &st = lds.steps[buf];
+    const float raw = makes ? raw_step(t0 + 2 * kSub) : 0.0f;
+    const HeadSteps &st = lds.steps[k % 4];
 
     // the wave's channels of x, by sixteen tokens: k = 4 q + i
     float x[2][4];
@@ -239,9 +240,14 @@ __global__ void __launch_bounds__(kHeadThreads, 3) head_mfma32_kernel(cortex_sca
         }
       }
     }
-    if (wave == 3 && t0 + kSub < end) next_steps(t0 + kSub, buf ^ 1);
+    if (makes) make_steps(t0 + 2 * kSub, (k / 2 + 1) % 2, raw);
   }
-  if (PART == 1 && tid == 192 && p0 == 0) w.steps[(int64_t)slot * heads + head] = steps;
+  if (PART == 1) {
+    if (lane == 0) lds.sums[wave] = steps;
+    __syncthreads();
+    if (tid == 0 && p0 == 0)
+      w.steps[(int64_t)slot * heads + head] = (lds.sums[0] + lds.sums[1]) + (lds.sums[2] + lds.sums[3]);
+  }
   float *h_out = PART == 1 ? w.state + ((int64_t)slot * a.channels + d) * N
                            : PART == 0 && row >= 0 && a.state_out ? a.state_out + ((int64_t)row * a.channels + d) * N : nullptr;
   if (works && h_out)

@@ -87,24 +87,28 @@ template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ float shifted(flo
 
 // Inclusive combination over the lanes of a wave, neutral element e: from 1, 2, 4
 // and 8 lanes below in a row of 16, lane 15 to the row above, lane 31 to the upper half.
-template <typename F> __device__ __forceinline__ float lane_prefix(float v, float e, F f) {
+// HALVES: over each half of the wave.
+template <bool HALVES, typename F> __device__ __forceinline__ float lane_prefix(float v, float e, F f) {
   v = f(v, shifted<0x111>(v, e));
   v = f(v, shifted<0x112>(v, e));
   v = f(v, shifted<0x114>(v, e));
   v = f(v, shifted<0x118>(v, e));
   v = f(v, shifted<0x142, 0xa>(v, e));
-  v = f(v, shifted<0x143, 0xc>(v, e));
+  if (!HALVES) v = f(v, shifted<0x143, 0xc>(v, e));
   return v;
 }
 __device__ __forceinline__ float lane_sums(float v) {
-  return lane_prefix(v, 0.0f, [](float a, float b) { return a + b; });
+  return lane_prefix<false>(v, 0.0f, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float half_sums(float v) {
+  return lane_prefix<true>(v, 0.0f, [](float a, float b) { return a + b; });
 }
 __device__ __forceinline__ float last_lane(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 __device__ __forceinline__ float wave_sum(float v) { return last_lane(lane_sums(v)); }
 __device__ __forceinline__ float wave_max(float v) {
-  return last_lane(lane_prefix(v, -__builtin_inff(), [](float a, float b) { return __builtin_fmaxf(a, b); }));
+  return last_lane(lane_prefix<false>(v, -__builtin_inff(), [](float a, float b) { return __builtin_fmaxf(a, b); }));
 }
 
 // ---------------------------------------------------------------------------
