@@ -243,24 +243,32 @@ __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(cortex_scan_t a
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-// Tokens of a segment, 0 for one launch over whole sequences.  A wave of the
-// channel scan is bound by its arithmetic, so the split, which doubles that,
-// pays until every SIMD of the GPU (1,024) has a wave without it; segments are
-// as long as leaves kFillWaves waves, and no shorter than 32 tokens, where the
-// states between them would be most of the bytes.
-constexpr int64_t kFillWaves = 4096;
-static int segment_tokens(int64_t T, int64_t S, int64_t D, int head_dim) {
+// Tokens of a segment, 0 for one launch over whole sequences.
+//
+// Per channel.  A wave is bound by its arithmetic, so the split, which doubles
+// that, pays until every SIMD of the GPU (1,024) has a wave without it.  Segments
+// are as long as leaves four waves a SIMD (8,192 tokens of 16 sequences and 2,048
+// channels, 32 tokens: 160 us; 128: 202; one launch: 1,190); below half a wave a
+// SIMD they go down to 16 (257 tokens of 512 channels, 24 tokens: 27 us; 32: 33; 64: 55).
+//
+// Per head.  The workgroups that the GPU holds at once (three a CU at N = 128,
+// four below) get a segment each, of at least 64 tokens: 32,768 tokens of 64 heads,
+// 2,752 tokens: 519 us; 1,024: 530; 256: 660; 4,099 float32 tokens of 16 heads,
+// 96 tokens: 48; 64: 56; 256: 69.  From 512 workgroups on one launch is faster
+// (8,192 tokens of 16 sequences and 32 heads: 90 us, split 154 to 200).
+static int segment_tokens(int64_t T, int64_t S, int64_t D, int N, int head_dim) {
   if (head_dim) {
     const int64_t groups = D / head_dim * ((head_dim + 63) / 64);
     if (S * groups >= 512) return 0;
-    int Q = 1024;
-    while (Q > 64 && T / Q * groups < 1024) Q /= 2;
-    return T <= Q ? 0 : Q;
+    const int64_t segments = (N == 128 ? 768 : 1024) / groups;       // 2 at least
+    const int64_t Q = ((T + segments - 1) / segments + 31) / 32 * 32;
+    return T <= 64 ? 0 : Q < 64 ? 64 : (int)Q;
   }
   const int64_t tiles = (D + kScanWave - 1) / kScanWave;
   if (S * tiles >= 1024) return 0;
   int Q = 256;
-  while (Q > 32 && T / Q * tiles < kFillWaves) Q /= 2;
+  while (Q > 32 && T / Q * tiles < 4096) Q /= 2;
+  if (T / Q * tiles < 512) Q = 16;
   return T <= Q ? 0 : Q;
 }
 
@@ -276,7 +284,7 @@ static SegmentScratch scratch_of(const cortex_scan_t &a, int Q, void *ws) {
 static bool launched() { return hipGetLastError() == hipSuccess; }
 
 template <typename T, int N> int launch_channel(const cortex_scan_t &a, int32_t *status, void *ws, void *stream) {
-  const int Q = segment_tokens(a.num_tokens, a.num_seqs, a.channels, 0);
+  const int Q = segment_tokens(a.num_tokens, a.num_seqs, a.channels, N, 0);
   const SegmentScratch w = scratch_of(a, Q, ws);
   const unsigned tiles = (a.channels / a.groups + kScanWave - 1) / kScanWave;
   const hipStream_t st = (hipStream_t)stream;
@@ -313,7 +321,7 @@ int launch_head_part(const cortex_scan_t &a, int32_t *status, const SegmentScrat
 }
 
 template <typename T, int N> int launch_head(const cortex_scan_t &a, int32_t *status, void *ws, void *stream) {
-  const int Q = segment_tokens(a.num_tokens, a.num_seqs, a.channels, a.head_dim);
+  const int Q = segment_tokens(a.num_tokens, a.num_seqs, a.channels, N, a.head_dim);
   const SegmentScratch w = scratch_of(a, Q, ws);
   const hipStream_t st = (hipStream_t)stream;
   if (!Q) return launch_head_part<T, N, 0>(a, status, w, 0, a.num_seqs, st);
@@ -403,7 +411,7 @@ using namespace cortex;
 extern "C" size_t cortex_scan_workspace_bytes(int32_t num_tokens, int32_t num_seqs, int32_t channels, int32_t state_size,
                                               int32_t head_dim) {
   if (num_tokens < 0 || num_seqs < 0 || bad_scan_size(channels, 1, state_size, head_dim)) return 0;
-  const int Q = segment_tokens(num_tokens, num_seqs, channels, head_dim);
+  const int Q = segment_tokens(num_tokens, num_seqs, channels, state_size, head_dim);
   if (!Q) return 256;
   return (size_t)chunk_slots(num_tokens, num_seqs, Q) * channels * (state_size + 1) * sizeof(float);
 }
