@@ -201,42 +201,84 @@ __global__ void __launch_bounds__(kScanWave) channel_scan_kernel(cortex_scan_t a
 // ---------------------------------------------------------------------------
 // One token.  N / 4 lanes share a channel, each with four neighbouring states,
 // so a wave reads and writes whole lines of the state, which bounds it: 8 bytes
-// a state entry against 5 operations.
+// a state entry against 5 operations.  A lane takes U channels of a head, which
+// share B and C, or U rows of a channel, which share its decays; their loads are
+// on their way together.  The new state is stored past the caches (nontemporal:
+// 134 MB of states 70 -> 66 us).  Loads past them pay where the states were not
+// in the 256 MB last-level cache (67 MB: 40 -> 32 us, 134 MB: 70 -> 59, the states
+// of other layers used in between) and cost where they were (134 MB: 48 -> 58,
+// 67 MB: 28 -> 30, 34 MB: 16 -> 19, one layer again and again), so they are taken
+// from 64 MiB on, where a model's layers no longer fit together.
 // ---------------------------------------------------------------------------
 constexpr int kStepThreads = 256;
 
-template <typename T, int N, bool HEAD>
+template <typename T, int N, bool HEAD, int U, bool STREAM>
 __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(cortex_scan_t a, int32_t *status) {
-  constexpr int L = N / 4;                       // lanes per channel
+  constexpr int L = N / 4, kChannels = kStepThreads / L;         // lanes per channel, channels side by side
+  constexpr int UC = HEAD ? U : 1, UR = HEAD ? 1 : U;            // channels and rows of a lane
   if (entry_status(status) != 0) return;
-  const int b = (int)blockIdx.x;
-  const int row = a.state_in || a.state_out ? state_row(a.state_index, b, a.state_rows, status) : -1;
-  if (row < -1) return;
-  const int part = (int)(threadIdx.x % L);
-  const int d = (int)blockIdx.y * (kStepThreads / L) + (int)(threadIdx.x / L);
-  if (d >= a.channels) return;                   // the same for all lanes of a channel
-  const int g = d / (a.channels / a.groups), k = HEAD ? d / a.head_dim : d;
-  const int64_t state_at = ((int64_t)row * a.channels + d) * N + part * 4;
-  float h[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (row >= 0 && a.state_in) load_floats<4>(a.state_in + state_at, h);
-  const float x = to_float<T>(((const T *)a.x)[b * a.x_ld + d]);
-  const float dt = step_size(a, to_float<T>(((const T *)a.dt)[b * a.dt_ld + k]), a.dt_bias ? a.dt_bias[k] : 0.0f);
-  const float u = dt * x;
-  const T *B = (const T *)a.B + b * a.B_ld + g * N + part * 4, *C = (const T *)a.C + b * a.C_ld + g * N + part * 4;
-  float y = 0.0f;
+  const int part = (int)(threadIdx.x % L), c0 = (int)blockIdx.y * kChannels * UC;
+  const int b0 = (int)blockIdx.x * UR;
+  typedef T vec4 __attribute__((ext_vector_type(4)));
+  int row[UR];
 #pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    const float A = HEAD ? a.A[k] : a.A[(int64_t)d * N + part * 4 + n];
-    h[n] = __builtin_fmaf(h[n], fast_exp2(dt * (A * kLog2e)), u * to_float<T>(B[n]));
-    y = __builtin_fmaf(h[n], to_float<T>(C[n]), y);
+  for (int r = 0; r < UR; ++r) {
+    row[r] = -1;
+    if (a.state_in || a.state_out) {
+      row[r] = b0 + r < a.num_seqs ? state_row(a.state_index, b0 + r, a.state_rows, status) : -1;
+      if (row[r] < -1) return;
+    }
   }
-  if (row >= 0 && a.state_out) store_floats<4>(a.state_out + state_at, h);
+  // channel u / UR and row u % UR; past the last it repeats that and stores nothing
+  f32x4 h[U];
+  float x[U], raw[U], z[U];
+  vec4 Bv[U], Cv[U];
+  int d[U], b[U];
 #pragma unroll
-  for (int m = 1; m < L; m <<= 1) y += __shfl_xor(y, m);
-  if (part == 0) {
-    if (a.skip) y = __builtin_fmaf(a.skip[k], x, y);
-    if (a.z) y *= silu(to_float<T>(((const T *)a.z)[b * a.z_ld + d]));
-    ((T *)a.y)[b * a.y_ld + d] = from_float<T>(y);
+  for (int u = 0; u < U; ++u) {
+    d[u] = min(c0 + u / UR * kChannels + (int)(threadIdx.x / L), a.channels - 1);
+    b[u] = min(b0 + u % UR, a.num_seqs - 1);
+    const int slot = row[u % UR];
+    h[u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (slot >= 0 && a.state_in) {
+      const f32x4 *p = (const f32x4 *)(a.state_in + ((int64_t)slot * a.channels + d[u]) * N + part * 4);
+      h[u] = STREAM ? __builtin_nontemporal_load(p) : *p;
+    }
+    const int64_t t = b[u];
+    x[u] = to_float<T>(((const T *)a.x)[t * a.x_ld + d[u]]);
+    raw[u] = to_float<T>(((const T *)a.dt)[t * a.dt_ld + (HEAD ? d[u] / a.head_dim : d[u])]);
+    if (a.z) z[u] = to_float<T>(((const T *)a.z)[t * a.z_ld + d[u]]);
+    const int g = d[u] / (a.channels / a.groups);
+    const T *B = (const T *)a.B + t * a.B_ld + g * N + part * 4, *C = (const T *)a.C + t * a.C_ld + g * N + part * 4;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      Bv[u][n] = B[n];
+      Cv[u][n] = C[n];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int k = HEAD ? d[u] / a.head_dim : d[u];
+    const bool stores = c0 + u / UR * kChannels + (int)(threadIdx.x / L) < a.channels && b0 + u % UR < a.num_seqs;
+    const float dt = step_size(a, raw[u], a.dt_bias ? a.dt_bias[k] : 0.0f);
+    const float w = dt * x[u], decay = HEAD ? fast_exp2(dt * (a.A[k] * kLog2e)) : 0.0f;
+    float y = 0.0f;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const float f = HEAD ? decay : fast_exp2(dt * (a.A[(int64_t)k * N + part * 4 + n] * kLog2e));
+      h[u][n] = __builtin_fmaf(h[u][n], f, w * to_float<T>(Bv[u][n]));
+      y = __builtin_fmaf(h[u][n], to_float<T>(Cv[u][n]), y);
+    }
+    const int slot = row[u % UR];
+    if (slot >= 0 && a.state_out && stores)
+      __builtin_nontemporal_store(h[u], (f32x4 *)(a.state_out + ((int64_t)slot * a.channels + d[u]) * N + part * 4));
+#pragma unroll
+    for (int m = 1; m < L; m <<= 1) y += __shfl_xor(y, m);
+    if (part == 0 && stores) {
+      if (a.skip) y = __builtin_fmaf(a.skip[k], x[u], y);
+      if (a.z) y *= silu(z[u]);
+      ((T *)a.y)[(int64_t)b[u] * a.y_ld + d[u]] = from_float<T>(y);
+    }
   }
 }
 
@@ -334,11 +376,21 @@ template <typename T, int N> int launch_head(const cortex_scan_t &a, int32_t *st
   return launch_head_part<T, N, 2>(a, status, w, Q, slots, st);
 }
 
+template <typename T, int N, bool HEAD, int U, bool STREAM>
+int launch_step_units(const cortex_scan_t &a, int32_t *status, void *stream) {
+  constexpr int kRows = HEAD ? 1 : U, kChannels = kStepThreads / (N / 4) * (HEAD ? U : 1);
+  scan_step_kernel<T, N, HEAD, U, STREAM><<<dim3((a.num_seqs + kRows - 1) / kRows, (a.channels + kChannels - 1) / kChannels),
+                                            kStepThreads, 0, (hipStream_t)stream>>>(a, status);
+  return launched() ? CORTEX_OK : CORTEX_E_HIP;
+}
+
+// Two of a lane's units while that leaves eight waves a SIMD (four: 134 MB of
+// states 76 us, two: 70, eight: 98).
 template <typename T, int N, bool HEAD> int launch_step(const cortex_scan_t &a, int32_t *status, void *stream) {
-  constexpr int per_block = kStepThreads / (N / 4);
-  scan_step_kernel<T, N, HEAD><<<dim3(a.num_seqs, (a.channels + per_block - 1) / per_block), kStepThreads, 0,
-                                 (hipStream_t)stream>>>(a, status);
-  return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+  const int64_t entries = (int64_t)a.num_seqs * a.channels * N;
+  if (entries / 4 / 64 < 2 * 8192) return launch_step_units<T, N, HEAD, 1, false>(a, status, stream);
+  return entries < (16 << 20) ? launch_step_units<T, N, HEAD, 2, false>(a, status, stream)
+                              : launch_step_units<T, N, HEAD, 2, true>(a, status, stream);
 }
 
 static bool bad_scan_size(int32_t channels, int32_t groups, int32_t state_size, int32_t head_dim) {
