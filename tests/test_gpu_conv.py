@@ -144,3 +144,15 @@ def test_another_stream():
     with torch.cuda.stream(s):
         y3, out3 = run(p, False)
     assert torch.equal(y, y2) and torch.equal(out, out2) and torch.equal(y, y3) and torch.equal(out, out3)
+
+
+def test_long_batches():
+    """Enough tokens for the longer chunks, aligned rows and others."""
+    need_gpu()
+    r = np.random.default_rng(1)
+    for ch, left, lens in ((1040, 0, r.integers(0, 900, 24).tolist()), (300, 1, [5000, 0, 1, 15, 16, 17, 2100])):
+        for W in (2, 4):
+            announce("conv, %d tokens of %d channels W %d" % (sum(lens), ch, W))
+            p = make(7, lens, ch, W, "bf16", left)
+            y, out = run(p, False)
+            check(p, y, out, W)

@@ -251,3 +251,42 @@ def test_graph_replays():
         call() if k == 2 else None
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((out, token, lse), want)), k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_rows_of_several_tiles(dtype):
+    need_gpu()
+    for left in (0, 1):
+        c = Case(11, 130, 33001, dtype, cap=200, left=left)
+        c.check(*c.call("same"))
+
+
+def test_long_history():
+    """Histories that are counted in 32 bits, one token often."""
+    need_gpu()
+    for R, V in ((2, 5000), (140, 17000)):
+        c = Case(12, R, V, cap=40000)
+        c.hist[0, :] = 3
+        c.lens[0], c.prompt[0] = 40000, 1000
+        c.check(*c.call())
+    c = Case(13, 2, 5000, cap=32767)                     # the longest in 16 bits
+    c.hist[:] = 4999
+    c.lens[:], c.prompt[:] = 32767, [0, 5]
+    c.check(*c.call())
+
+
+def test_biases_of_one_token():
+    """Every entry names the same token or its neighbour: the last of each counts."""
+    need_gpu()
+    c = Case(14, 2, 5000, history=False, mask=False)
+    c.bias = [[(10 + (k % 2), float(k)) for k in range(1500)], [(4999, 1.0), (4999, -2.0), (0, 4.0)]]
+    c.check(*c.call())
+
+
+def test_too_many_biases():
+    need_gpu()
+    for n, want in ((65535, 0), (65536, C.CORTEX_ST_INPUT_RANGE)):
+        c = Case(15, 1, 70000, history=False, mask=False)
+        c.bias = [[(k, 1.0) for k in range(n)]]
+        c.call()
+        assert int(c.status.item()) == want, n

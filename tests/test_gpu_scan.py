@@ -232,3 +232,47 @@ def test_a_token_reaches_no_earlier_one(what, P, dtype):
             others = [c for c in range(64) if c != 3]
             assert torch.equal(p.d["y"][:, others], y[:, others]), at
             assert not bool(torch.isfinite(p.d["y"][at:, 3]).any()), at
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_sequences(dtype):
+    """Enough sequences that each is walked whole, in one launch."""
+    need_gpu()
+    r = np.random.default_rng(0)
+    run(Scan(1, r.integers(0, 6, 1100).tolist(), 64, 8, 1, dtype=dtype), "channel, 1100 sequences %s" % dtype)
+    run(Scan(2, (r.integers(0, 40, 140) * 3).tolist(), 256, 32, 2, 64, dtype=dtype), "head, 140 sequences %s" % dtype)
+    run(Scan(3, (r.integers(0, 40, 600)).tolist(), 128, 128, 1, 128, dtype=dtype), "head of 128, 600 sequences %s" % dtype)
+
+
+def test_large_pools():
+    """Batches that take two units a lane, and the loads past the caches: odd rows and channels."""
+    need_gpu()
+    run(Scan(1, [1] * 41, 2050, 64, 1, dtype="bf16"), "channel step, 41 x 2050 x 64", True)
+    run(Scan(2, [1] * 17, 2064, 128, 1, 48), "head step, 17 x 2064 x 128", True)
+    run(Scan(3, [1] * 35, 4112, 128, 1, 16, dtype="f32"), "head step, 35 x 4112 x 128", True)
+    run(Scan(4, [1] * 135, 2049, 64, 3, dtype="f32"), "channel step, 135 x 2049 x 64", True)
+
+
+@pytest.mark.parametrize("P", [0, 64])
+def test_rows_far_apart(P):
+    """Rows of a wide array: element offsets beyond 2^31."""
+    need_gpu()
+    T, D, N, ld = 80, 64, 16, 1 << 25
+    p = Scan(6, [T], D, N, 1, P)
+    d = p.upload()
+    wide = torch.empty(T, ld, dtype=torch.bfloat16, device="cuda")
+    at = 0
+    for name in ("x", "z", "dt", "B", "C"):
+        t = d[name]
+        cols = t.flatten(1)
+        v = wide[:, at:at + cols.shape[1]]
+        v.copy_(cols)
+        d[name] = v.unflatten(1, (1, N)) if t.dim() == 3 else v
+        at += 64
+    d["y"] = wide[:, at:at + D]
+    out = torch.full_like(d["state"], 7.0)
+    announce("rows %d elements apart P %d" % (ld, P))
+    C.check(p.call(state_out=out))
+    torch.cuda.synchronize()
+    assert int(d["status"].item()) == 0
+    p.check(d["y"], out, "far rows")
