@@ -91,15 +91,16 @@ struct alignas(16) HeadSteps {
   float dt[kSub], cum[kSub], grow[kSub], weight[kSub], decay;
 };
 
-template <int N> struct HeadLds {
+// Part 1 has no use for what makes y.
+template <int N, bool OUTPUT> struct HeadLds {
   static constexpr int NP = N < 32 ? 32 : N;      // the products over N take 32 at a time; what is past N is 0
   typedef Rows<NP> N_;
   typedef Rows<kSub> T_;
   alignas(16) unsigned short B[kSub * N_::kStride];           // [s][n position]
-  alignas(16) unsigned short C[kSub * N_::kStride];           // [t][n position]
+  alignas(16) unsigned short C[OUTPUT ? kSub * N_::kStride : 8];           // [t][n position]
   alignas(16) unsigned short x[kSub * 64];                    // [s][channel]
-  alignas(16) unsigned short M[2][kSub * T_::kStride];        // scores, two planes: [t][s position]
-  alignas(16) float y[kSub * 64];                             // [t][channel]
+  alignas(16) unsigned short M[2][OUTPUT ? kSub * T_::kStride : 8];        // scores, two planes: [t][s position]
+  alignas(16) float y[OUTPUT ? kSub * 64 : 4];                             // [t][channel]
   HeadSteps steps[4];                             // of this sub-chunk, its neighbour and the next two
   float sums[kHeadWaves];
 };
@@ -158,7 +159,7 @@ inline unsigned blocks_of_units(int64_t units) { return (unsigned)((units + 7) /
 template <int N, int PART, bool WIDE>
 __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kernel(cortex_scan_t a, int32_t *status, SegmentScratch w, int Q,
                                                                     int64_t units) {
-  typedef HeadLds<N> Lds;
+  typedef HeadLds<N, PART != 1> Lds;
   constexpr int NT = N / 16, NB = Lds::NP / 32;
   constexpr int OL = N / 8, kItems = (OL * kSub + kHeadThreads - 1) / kHeadThreads;   // octets of a row; of them all per thread
   __shared__ Lds lds;
@@ -240,7 +241,7 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
     for (int i = tid; i < kSub * (Lds::NP - N) / 4; i += kHeadThreads) {
       const int s = i / ((Lds::NP - N) / 4), e = N + i % ((Lds::NP - N) / 4) * 4;
       *(u32x2v *)&lds.B[Lds::N_::at(s, k_position(e))] = u32x2v{0, 0};
-      *(u32x2v *)&lds.C[Lds::N_::at(s, k_position(e))] = u32x2v{0, 0};
+      if (PART != 1) *(u32x2v *)&lds.C[Lds::N_::at(s, k_position(e))] = u32x2v{0, 0};
     }
   // the tile above the diagonal, which a product over 32 tokens reaches
   if (PART != 1 && tid < 128)
