@@ -194,6 +194,15 @@ def _need(t, name: str, dtype: torch.dtype, min_numel: int, optional: bool = Fal
 def _need_all(specs) -> None:
     """_need over several tensors: every dtype, layout and size first, then
     that each tensor is in device memory."""
+    for t, _, dtype, min_numel, optional in specs:
+        if t is None:
+            if not optional:
+                break
+        elif not (type(t) is torch.Tensor and (dtype is None or t.dtype is dtype) and t.is_contiguous()
+                  and t.numel() >= min_numel and t.is_cuda):
+            break
+    else:
+        return                          # nothing to refuse: the usual call
     for t, name, dtype, min_numel, optional in specs:
         if t is None:
             if optional:

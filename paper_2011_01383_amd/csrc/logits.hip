@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(cortex_logits_t a, int3
   __shared__ LogitsPart wave_part[THREADS / 64];
   __shared__ float wave_top[THREADS / 64], wave_sums[THREADS / 64];
   __shared__ int first_at;
-  const int failed = entry_status(status);        // looked at once the first loads are on their way
+  const int failed = entry_status(status);       // looked at, by all together, at the first barrier
   const int tid = (int)threadIdx.x, lane = tid & 63, row = (int)blockIdx.y, tiles = (int)gridDim.x;
   const int v0 = (int)blockIdx.x * kTile;
   const int width = a.vocab - v0 < kTile ? a.vocab - v0 : kTile;
@@ -120,7 +120,6 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(cortex_logits_t a, int3
     }
   }
 
-  if (failed != 0) return;
   int len = 0, prompt = 0, bias0 = 0, bias1 = 0, m = -1;
   bool broken = false;
   if (a.history_len) {
@@ -158,7 +157,9 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(cortex_logits_t a, int3
   for (int k = tid * 4; k < words; k += THREADS * 4) *(u32x4 *)&table[k] = zeros;
   if (tid < kTile / 32) touched[tid] = 0;
   if (tid == 0) first_at = 0x7fffffff;
-  __syncthreads();
+  // Another workgroup's error may be seen by some waves and not by others.  None goes
+  // on alone: the tables' entries become places in bias_values.
+  if (__syncthreads_or(failed != 0)) return;
   bool outside = false;
   const int32_t *text = a.history + (int64_t)row * a.history_ld;
 #pragma unroll 4
