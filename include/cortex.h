@@ -102,7 +102,8 @@ extern "C" {
 #define CORTEX_ST_CYCLE 2            /* the structure has a cycle (not a DAG) */
 #define CORTEX_ST_BARRIER_TIMEOUT 3  /* a barrier or per-datum wait passed its limit */
 #define CORTEX_ST_BAD_LINEARIZATION 4 /* forward was handed an inconsistent linearization */
-#define CORTEX_ST_INPUT_RANGE 5      /* an input index outside [-1, rows of the input table) */
+#define CORTEX_ST_INPUT_RANGE 5      /* an input index outside [-1, rows of the input table); for the
+                                        sequence operators: an index or length outside its range */
 #define CORTEX_ST_EPOCH_WRAP 6       /* the forward workspace has served 2^32 - 1 launches: zero it */
 #define CORTEX_ST_SEQ_OFFSETS 7      /* sequence offsets that do not rise from 0 to the token count */
 
@@ -432,10 +433,12 @@ int cortex_scan_step(const cortex_scan_t *args, int32_t *d_status, void *stream)
  *   lse     log sum_i exp(v) (-infinity if every v is)
  * Each output may be NULL.  A masked entry's logit is never used, whatever it
  * holds.  A row of the mask is ceil(V / 32) words, bit i % 32 of word i / 32 set
- * where i is allowed; mask_index[b] = -1 is a row without a mask.
- * A row has at most 65,535 biases.  A token outside [0, V), a length outside [0, history_cap] (the prompt's: outside
- * [0, the history's]), a mask index outside [-1, mask_rows) bias offsets that do
- * not rise from 0 to num_biases or too many of them set CORTEX_ST_INPUT_RANGE.
+ * where i is allowed; mask_index[b] = -1 is a row without a mask.  A row has at
+ * most 65,535 biases, a call at most 65,535 rows.
+ * CORTEX_ST_INPUT_RANGE: a token outside [0, V), a history length outside
+ * [0, history_cap], a prompt length outside [0, the row's history length], a mask
+ * index outside [-1, mask_rows), bias offsets that do not rise from 0 to
+ * num_biases, or too many of them in a row.
  */
 typedef struct {
   int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: logits and out */
