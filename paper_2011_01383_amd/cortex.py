@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -85,28 +86,43 @@ class cortex_weights_t(ctypes.Structure):
 def _fields(text: str):
     """(name, ctype) pairs from "i name ..." groups: i int32, l int64, p pointer."""
     kinds = {"i": ctypes.c_int32, "l": ctypes.c_int64, "p": ctypes.c_void_p}
-    out = []
-    for group in text.split(";"):
-        kind, *names = group.split()
-        out += [(n, kinds[kind]) for n in names]
-    return out
+    return [(n, kinds[group.split()[0]]) for group in text.split(";") for n in group.split()[1:]]
+
+
+def _packer(text: str, cls):
+    """The structure's bytes from its members' values in order; a call then costs
+    the host a third of what filling a ctypes structure does."""
+    kinds = {"i": "i", "l": "q", "p": "P"}
+    s = struct.Struct("@" + "".join(kinds[group.split()[0]] * len(group.split()[1:]) for group in text.split(";")))
+    assert s.size == ctypes.sizeof(cls)
+    return s.pack
+
+
+_CONV = ("i dtype num_seqs num_tokens channels width silu state_rows; p seq_offsets state_index x; l x_ld;"
+         "p weight bias state_in state_out y; l y_ld")
+_SCAN = ("i dtype num_seqs num_tokens channels head_dim groups state_size softplus state_rows;"
+         "p seq_offsets state_index x z dt B C; l x_ld z_ld dt_ld B_ld C_ld;"
+         "p A skip dt_bias state_in state_out y; l y_ld")
+_LOGITS = ("i dtype rows vocab history_cap num_biases mask_rows; p logits; l logits_ld; p history; l history_ld;"
+           "p history_len prompt_len repetition frequency presence bias_offsets bias_tokens bias_values mask;"
+           "l mask_ld; p mask_index out; l out_ld; p token lse")
 
 
 class cortex_conv_t(ctypes.Structure):
-    _fields_ = _fields("i dtype num_seqs num_tokens channels width silu state_rows; p seq_offsets state_index x; l x_ld;"
-                       "p weight bias state_in state_out y; l y_ld")
+    _fields_ = _fields(_CONV)
 
 
 class cortex_scan_t(ctypes.Structure):
-    _fields_ = _fields("i dtype num_seqs num_tokens channels head_dim groups state_size softplus state_rows;"
-                       "p seq_offsets state_index x z dt B C; l x_ld z_ld dt_ld B_ld C_ld;"
-                       "p A skip dt_bias state_in state_out y; l y_ld")
+    _fields_ = _fields(_SCAN)
 
 
 class cortex_logits_t(ctypes.Structure):
-    _fields_ = _fields("i dtype rows vocab history_cap num_biases mask_rows; p logits; l logits_ld; p history;"
-                       "l history_ld; p history_len prompt_len repetition frequency presence bias_offsets bias_tokens"
-                       " bias_values mask; l mask_ld; p mask_index out; l out_ld; p token lse")
+    _fields_ = _fields(_LOGITS)
+
+
+_pack_conv = _packer(_CONV, cortex_conv_t)
+_pack_scan = _packer(_SCAN, cortex_scan_t)
+_pack_logits = _packer(_LOGITS, cortex_logits_t)
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -160,19 +176,19 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.cortex_probe_levels_workspace_bytes.restype = SZ
     lib.cortex_probe_levels.argtypes = [I32, I32, I32, P, P, SZ, P]
     lib.cortex_probe_levels.restype = ctypes.c_int
-    lib.cortex_conv_forward.argtypes = [ctypes.POINTER(cortex_conv_t), P, P]
+    lib.cortex_conv_forward.argtypes = [P, P, P]
     lib.cortex_conv_forward.restype = ctypes.c_int
-    lib.cortex_conv_step.argtypes = [ctypes.POINTER(cortex_conv_t), P, P]
+    lib.cortex_conv_step.argtypes = [P, P, P]
     lib.cortex_conv_step.restype = ctypes.c_int
     lib.cortex_scan_workspace_bytes.argtypes = [I32, I32, I32, I32, I32]
     lib.cortex_scan_workspace_bytes.restype = SZ
-    lib.cortex_scan_forward.argtypes = [ctypes.POINTER(cortex_scan_t), P, P, SZ, P]
+    lib.cortex_scan_forward.argtypes = [P, P, P, SZ, P]
     lib.cortex_scan_forward.restype = ctypes.c_int
-    lib.cortex_scan_step.argtypes = [ctypes.POINTER(cortex_scan_t), P, P]
+    lib.cortex_scan_step.argtypes = [P, P, P]
     lib.cortex_scan_step.restype = ctypes.c_int
     lib.cortex_logits_workspace_bytes.argtypes = [I32, I32]
     lib.cortex_logits_workspace_bytes.restype = SZ
-    lib.cortex_logits_process.argtypes = [ctypes.POINTER(cortex_logits_t), P, P, SZ, P]
+    lib.cortex_logits_process.argtypes = [P, P, P, SZ, P]
     lib.cortex_logits_process.restype = ctypes.c_int
     lib.cortex_version.argtypes = []
     lib.cortex_version.restype = ctypes.c_char_p
@@ -283,7 +299,7 @@ def _stream(stream) -> Optional[int]:
     if stream is None:
         # the handle that torch.cuda.current_stream() wraps in an object (2.7 us of host time a call)
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
+        return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch._C._cuda_getDevice())
     return getattr(stream, "cuda_stream", stream)
 
 
@@ -425,30 +441,35 @@ def cortex_probe_levels(mode: int, grid: int, levels: int, status: torch.Tensor,
 _DTYPES = {torch.float32: CORTEX_F32, torch.bfloat16: CORTEX_BF16}
 
 
+def _at(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
 def _rows(t, name: str, dtype, rows: int, cols: int) -> int:
     """A [rows, cols] tensor whose rows are whole and may be apart (the columns
     of a wider array): its row stride."""
     if not isinstance(t, torch.Tensor):
         raise ValueError("%s is required" % name if t is None else
                          "%s must be a torch.Tensor, got %s" % (name, type(t).__name__))
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError("%s must be [%d, %d], got %s" % (name, rows, cols, list(t.shape)))
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != rows or shape[1] != cols:
+        raise ValueError("%s must be [%d, %d], got %s" % (name, rows, cols, list(shape)))
     ld, inner = t.stride()
     if inner != 1 and cols > 1:
         raise ValueError("%s must have contiguous rows" % name)
-    if rows < 2:
-        ld = max(ld, cols)             # one row: its stride is never used
-    elif ld < cols:
-        raise ValueError("%s must have rows that do not overlap" % name)
+    if ld < cols:
+        if rows > 1:
+            raise ValueError("%s must have rows that do not overlap" % name)
+        return cols                    # one row: its stride is never used
     return ld
 
 
-def _on_device(*pairs) -> None:
-    for t, name in pairs:
+def _on_device(names: str, *tensors) -> None:
+    for i, t in enumerate(tensors):
         if t is not None and not t.is_cuda:
-            raise ValueError("%s must be in device memory" % name)
+            raise ValueError("%s must be in device memory" % names.split()[i])
 
 
 def _shape2(t, name: str):
@@ -461,12 +482,17 @@ def _shape2(t, name: str):
 
 def _state_specs(state_in, state_out, state_index, S: int, dtype, tail: tuple):
     """Rows of the state pools and what they have to hold."""
-    pools = [t for t in (state_in, state_out) if t is not None]
-    for t in pools:
-        if not isinstance(t, torch.Tensor) or t.dim() != 3 or tuple(t.shape[1:]) != tail or t.shape[0] != pools[0].shape[0]:
+    rows = -1
+    for t in (state_in,) if state_out is state_in else (state_in, state_out):
+        if t is None:
+            continue
+        shape = t.shape if isinstance(t, torch.Tensor) else ()
+        if len(shape) != 3 or shape[1:] != tail or (rows >= 0 and shape[0] != rows):
             raise ValueError("state_in and state_out must be [rows, %d, %d], with the same rows" % tail)
-    rows = pools[0].shape[0] if pools else 0
-    if pools and state_index is None and rows < S:
+        rows = shape[0]
+    if rows < 0:
+        rows = 0
+    elif state_index is None and rows < S:
         raise ValueError("the states have %d rows, %d sequences need as many" % (rows, S))
     n = rows * tail[0] * tail[1]
     return rows, [(state_in, "state_in", dtype, n, True), (state_out, "state_out", dtype, n, True),
@@ -490,12 +516,12 @@ def _conv(step: bool, x, weight, offsets, y, bias, silu, state_in, state_out, st
     x_ld, y_ld = _rows(x, "x", x.dtype, T, C), _rows(y, "y", x.dtype, T, C)
     _need_all(specs + state + [(weight, "weight", f32, C * W, False), (bias, "bias", f32, C, True),
                                (status, "status", i32, 1, False)])
-    _on_device((x, "x"), (y, "y"))
-    args = cortex_conv_t(_DTYPES[x.dtype], S, T, C, W, int(bool(silu)), rows, _ptr(offsets), _ptr(state_index), _ptr(x),
-                         x_ld, _ptr(weight), _ptr(bias), _ptr(state_in), _ptr(state_out), _ptr(y), y_ld)
+    _on_device("x y", x, y)
+    args = _pack_conv(_DTYPES[x.dtype], S, T, C, W, 1 if silu else 0, rows, _at(offsets), _at(state_index), x.data_ptr(),
+                      x_ld, weight.data_ptr(), _at(bias), _at(state_in), _at(state_out), y.data_ptr(), y_ld)
     lib = load()
     call = lib.cortex_conv_step if step else lib.cortex_conv_forward
-    return call(ctypes.byref(args), _ptr(status), _stream(stream))
+    return call(args, status.data_ptr(), _stream(stream))
 
 
 def cortex_conv_forward(x: torch.Tensor, weight: torch.Tensor, offsets: torch.Tensor, y: torch.Tensor, *, bias=None,
@@ -515,7 +541,7 @@ def _group_rows(t, name: str, dtype, T: int):
     """A [T, G, N] tensor with the groups of a row side by side: G, N and its row stride."""
     if not isinstance(t, torch.Tensor) or t.dim() != 3:
         raise ValueError("%s must be a [T, G, N] torch.Tensor" % name)
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
     rows, G, N = t.shape
     if rows != T:
@@ -523,10 +549,10 @@ def _group_rows(t, name: str, dtype, T: int):
     ld, between, inner = t.stride()
     if (inner != 1 and N > 1) or (between != N and G > 1):
         raise ValueError("%s must have contiguous rows" % name)
-    if rows < 2:
-        ld = max(ld, G * N)
-    elif ld < G * N:
-        raise ValueError("%s must have rows that do not overlap" % name)
+    if ld < G * N:
+        if rows > 1:
+            raise ValueError("%s must have rows that do not overlap" % name)
+        ld = G * N
     return G, N, ld
 
 
@@ -562,14 +588,14 @@ def _scan(step: bool, x, dt, A, B, C, offsets, y, skip, z, dt_bias, softplus, st
     z_ld = 0 if z is None else _rows(z, "z", typ, T, D)
     _need_all(specs + state + [(A, "A", f32, A.numel(), False), (skip, "D", f32, H, True),
                                (dt_bias, "dt_bias", f32, H, True), (status, "status", i32, 1, False)])
-    _on_device((x, "x"), (dt, "dt"), (B, "B"), (C, "C"), (z, "z"), (y, "y"))
-    args = cortex_scan_t(_DTYPES[typ], S, T, D, P, G, N, int(bool(softplus)), rows, _ptr(offsets), _ptr(state_index),
-                         _ptr(x), _ptr(z), _ptr(dt), _ptr(B), _ptr(C), x_ld, z_ld, dt_ld, B_ld, C_ld, _ptr(A), _ptr(skip),
-                         _ptr(dt_bias), _ptr(state_in), _ptr(state_out), _ptr(y), y_ld)
+    _on_device("x dt B C z y", x, dt, B, C, z, y)
+    args = _pack_scan(_DTYPES[typ], S, T, D, P, G, N, 1 if softplus else 0, rows, _at(offsets), _at(state_index),
+                      x.data_ptr(), _at(z), dt.data_ptr(), B.data_ptr(), C.data_ptr(), x_ld, z_ld, dt_ld, B_ld, C_ld,
+                      A.data_ptr(), _at(skip), _at(dt_bias), _at(state_in), _at(state_out), y.data_ptr(), y_ld)
     lib = load()
     if step:
-        return lib.cortex_scan_step(ctypes.byref(args), _ptr(status), _stream(stream))
-    return lib.cortex_scan_forward(ctypes.byref(args), _ptr(status), _ptr(ws), ws.numel() * ws.element_size(),
+        return lib.cortex_scan_step(args, status.data_ptr(), _stream(stream))
+    return lib.cortex_scan_forward(args, status.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(),
                                    _stream(stream))
 
 
@@ -640,12 +666,12 @@ def cortex_logits_process(logits: torch.Tensor, *, out=None, token=None, lse=Non
     logits_ld = _rows(logits, "logits", logits.dtype, R, V)
     out_ld = 0 if out is None else _rows(out, "out", logits.dtype, R, V)
     _need_all(specs)
-    _on_device((logits, "logits"), (out, "out"), (history, "history"), (mask, "mask"))
-    args = cortex_logits_t(_DTYPES[logits.dtype], R, V, cap, biases, states, _ptr(logits), logits_ld, _ptr(history),
-                           history_ld, _ptr(history_len), _ptr(prompt_len), _ptr(repetition), _ptr(frequency),
-                           _ptr(presence), _ptr(bias_offsets), _ptr(bias_tokens), _ptr(bias_values), _ptr(mask), mask_ld,
-                           _ptr(mask_index), _ptr(out), out_ld, _ptr(token), _ptr(lse))
-    return load().cortex_logits_process(ctypes.byref(args), _ptr(status), _ptr(ws), ws.numel() * ws.element_size(),
+    _on_device("logits out history mask", logits, out, history, mask)
+    args = _pack_logits(_DTYPES[logits.dtype], R, V, cap, biases, states, logits.data_ptr(), logits_ld, _at(history),
+                        history_ld, _at(history_len), _at(prompt_len), _at(repetition), _at(frequency), _at(presence),
+                        _at(bias_offsets), _at(bias_tokens), _at(bias_values), _at(mask), mask_ld, _at(mask_index),
+                        _at(out), out_ld, _at(token), _at(lse))
+    return load().cortex_logits_process(args, status.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(),
                                         _stream(stream))
 
 
