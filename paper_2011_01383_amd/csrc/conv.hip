@@ -5,7 +5,7 @@
 // inputs and the W - 1 before them at once, then slides the window down them.
 // The bytes of x and y bound it: 2 W + 4 operations per element loaded and stored.
 // 8,192 tokens of 2,304 bf16 channels: 24 us, 3.2 TB/s of inputs and outputs (a
-// large copy runs at 4.8); 7 rows of single tokens: 3.6 us.  What is left is the
+// large copy runs at 4.8); 7 rows of single tokens: 3.7 us.  What is left is the
 // launch's ramp: every wave loads, then every wave stores (chunks of 8 to 16
 // tokens measure the same).
 #include "sequence.hpp"

@@ -77,10 +77,10 @@ __global__ void __launch_bounds__(256) enter_kernel(cortex_scan_t a, int32_t *st
 // the next kAhead tokens (of B and C: the next tile) need is loaded while these
 // are worked on.
 //
-// 32,768 tokens of 2,048 channels and 16 states, split: 266 us (part 1) + 18 (the
-// states between) + 304 (part 2), 1.3 and 1.7 ns of a SIMD a token and wave of 64:
-// 28 and 32 cycles a state and channel for the exponential (16) and the products,
-// 110 and 170 for the softplus and the gate, which is all that the SIMDs issue.
+// 32,768 tokens of 2,048 channels and 16 states, split: 269 us (part 1) + 18 (the
+// states between) + 310 (part 2), traced.  That is 263 and 303 ns of a SIMD a token
+// and wave, for 100 and 138 vector instructions: about 218 and 292 ns at 1.9 ns each
+// and 3.5 for an exponential, as four waves a SIMD of nothing else take for them.
 // ---------------------------------------------------------------------------
 constexpr int kAhead = 4, kTile = 16;
 

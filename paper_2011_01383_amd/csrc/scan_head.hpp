@@ -31,11 +31,12 @@
 // and their sums are made a sub-chunk ahead by one wave, beside the others'
 // products.  y goes through LDS, so that z is read and y stored in whole rows.
 //
-// 32,768 tokens of 64 heads of 64 channels, N = 128, in segments of 2,752: 165 us
-// (part 1) + 14 + 370 (part 2, 1.7 TB/s of x, z and y).  Nothing alone bounds it:
+// 32,768 tokens of 64 heads of 64 channels, N = 128, in segments of 2,752: 177 us
+// (part 1) + 15 + 405 (part 2, 2.0 TB/s of x, z and y), traced; 500 to 518 as a
+// program calls it.  Nothing alone bounds it:
 // without its loads and stores, or without its products, it takes three quarters
 // of the time; the vector unit (plane splits, gates) is busy half of it, the
-// matrix unit a fifth, LDS two fifths.  12 waves a CU is what its registers allow.
+// matrix unit a fifth, LDS more than a third.  12 waves a CU is what its registers allow.
 #pragma once
 
 #include "sequence.hpp"

@@ -9,7 +9,7 @@
 // moving.  At 64 operations a cycle and SIMD these units bound it (three bf16
 // planes a value, six products at a sixteenth of the time each, would want every
 // value that is read split).  4,099 tokens of 16 heads of 64 channels, N = 64, in
-// segments of 96: 15 + 8 + 28 us.
+// segments of 96: 15 + 9 + 28 us.
 #pragma once
 
 #include "scan_head.hpp"
