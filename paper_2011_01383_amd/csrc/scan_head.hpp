@@ -9,12 +9,14 @@
 // to memory between them.
 //
 // Precision.  x, B and C are bf16 and enter the matrix units as they are.  What
-// is computed on the way is split into bf16 planes (each the rounding of what
-// the ones before it leave): the scaled scores and the state that y reads into
-// two, 16 bits, since y itself is rounded to bf16; the step-weighted x that the
-// state is summed from into three, all 24 bits, since the state stays float32.
-// All sums are float32.  An infinite or NaN x makes its channel NaN from its token
-// on (the token-by-token order might keep an infinity).
+// is computed on the way (the scaled scores, the state that y reads, the
+// step-weighted x that the state is summed from) is float32 and enters as three
+// bf16 planes, eight bits each, which together are the value itself.  So every
+// product is exact, all sums are float32, and y is rounded once, as token by token.
+// (Two planes, 16 bits, would do for y's own rounding, but a y that is a small
+// difference of large terms would lose it: 1e-4 of y instead of 2e-5 off the
+// float32 order.)  An infinite or NaN x or state makes its channel NaN from its
+// token on (the token-by-token order might keep an infinity).
 //
 // Layouts.  A 16x16x32 product takes both operands as (index = lane & 15; 8
 // consecutive k from 8 (lane >> 4)) and leaves its result as (column = lane &
@@ -26,7 +28,7 @@
 // too: the transposing 8-byte LDS read gives a lane four rows' values of its
 // column, which is the four k of one a.
 //
-// What it does per sub-chunk and wave at N = 128: 48 products (768 cycles of a
+// What it does per sub-chunk and wave at N = 128: 58 products (928 cycles of a
 // SIMD's matrix unit).  The skip connection is the scores' diagonal.  Step sizes
 // and their sums are made a sub-chunk ahead by one wave, beside the others'
 // products.  y goes through LDS, so that z is read and y stored in whole rows.
@@ -61,15 +63,16 @@ __device__ __forceinline__ constexpr int k_position(int e) {
   return (e & ~31) | ((e & 12) << 1) | ((e & 16) >> 2) | (e & 3);
 }
 
-// The next bf16 plane of v, two values a word, which keeps what is left.
-typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
+// The next bf16 plane of v, two values a word: its upper halves as they are, so
+// that three planes hold all of it and no finite value becomes an infinity.  v
+// keeps what is left.
 template <int M> __device__ __forceinline__ void plane(float (&v)[M], unsigned int (&p)[M / 2]) {
 #pragma unroll
   for (int i = 0; i < M / 2; ++i) {
-    p[i] = __builtin_bit_cast(unsigned int, __builtin_convertvector(f32x2{v[2 * i], v[2 * i + 1]}, bf16x2v));
-    v[2 * i] -= __builtin_bit_cast(float, p[i] << 16);
-    v[2 * i + 1] -= __builtin_bit_cast(float, p[i] & 0xffff0000u);
+    const unsigned int a = __builtin_bit_cast(unsigned int, v[2 * i]), b = __builtin_bit_cast(unsigned int, v[2 * i + 1]);
+    p[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    v[2 * i] -= __builtin_bit_cast(float, a & 0xffff0000u);
+    v[2 * i + 1] -= __builtin_bit_cast(float, b & 0xffff0000u);
   }
 }
 __device__ __forceinline__ bf16x8v pack8(const unsigned int (&p)[4]) {
@@ -106,7 +109,7 @@ template <int N, bool OUTPUT> struct HeadLds {
   alignas(16) unsigned short B[kSub * N_::kStride];           // [s][n position]
   alignas(16) unsigned short C[OUTPUT ? kSub * N_::kStride : 8];           // [t][n position]
   alignas(16) unsigned short x[kSub * 64];                    // [s][channel]
-  alignas(16) unsigned short M[2][OUTPUT ? kSub * T_::kStride : 8];        // scores, two planes: [t][s position]
+  alignas(16) unsigned short M[3][OUTPUT ? kSub * T_::kStride : 8];        // scores, three planes: [t][s position]
   alignas(16) float y[OUTPUT ? kSub * 64 : 4];                             // [t][channel]
   HeadSteps steps[4];                             // of this sub-chunk, its neighbour and the next two
   float sums[kHeadWaves];
@@ -251,8 +254,8 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
       if (PART != 1) *(u32x2v *)&lds.C[Lds::N_::at(s, k_position(e))] = u32x2v{0, 0};
     }
   // the tile above the diagonal, which a product over 32 tokens reaches
-  if (PART != 1 && tid < 128)
-    *(u32x2v *)&lds.M[tid >> 6][Lds::T_::at(l16, k_position(16 + q * 4))] = u32x2v{0, 0};
+  if (PART != 1 && wave < 3)
+    *(u32x2v *)&lds.M[wave][Lds::T_::at(l16, k_position(16 + q * 4))] = u32x2v{0, 0};
 
   // Steps are made two sub-chunks ahead for two of them, by the waves in turn.
   auto raw_step = [&](int t0) { return to_float<bf16_t>(ds[(int64_t)min(t0 + lane, end - 1) * a.dt_ld]); };
@@ -312,11 +315,12 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
           v[i] = s + i <= t ? acc[i] * (fast_exp2(ct - cs[i]) * dt[i]) : 0.0f;
           if (s + i == t) v[i] += skip;
         }
-        unsigned int b[2];
-        plane(v, b);
-        *(u32x2v *)&lds.M[0][Lds::T_::at(t, k_position(s))] = u32x2v{b[0], b[1]};
-        plane(v, b);
-        *(u32x2v *)&lds.M[1][Lds::T_::at(t, k_position(s))] = u32x2v{b[0], b[1]};
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+          unsigned int b[2];
+          plane(v, b);
+          *(u32x2v *)&lds.M[p][Lds::T_::at(t, k_position(s))] = u32x2v{b[0], b[1]};
+        }
       }
       // From the state: rows channels, columns t.
       y[0] = y[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -331,14 +335,17 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
           }
           unsigned int b[4];
           plane(v, b);
-          const bf16x8v hi = pack8(b);
+          const bf16x8v h0 = pack8(b);
           plane(v, b);
-          const bf16x8v lo = pack8(b);
+          const bf16x8v h1 = pack8(b);
+          plane(v, b);
+          const bf16x8v h2 = pack8(b);
 #pragma unroll
           for (int ti = 0; ti < 2; ++ti) {
             const bf16x8v c = lds8(&lds.C[Lds::N_::at(ti * 16 + l16, m * 32 + q * 8)]);
-            y[ti] = mfma_bf16x32(lo, c, y[ti]);
-            y[ti] = mfma_bf16x32(hi, c, y[ti]);
+            y[ti] = mfma_bf16x32(h2, c, y[ti]);
+            y[ti] = mfma_bf16x32(h1, c, y[ti]);
+            y[ti] = mfma_bf16x32(h0, c, y[ti]);
           }
         }
 #pragma unroll
@@ -402,7 +409,7 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
           first = min(first, __shfl_xor(first, 32));
         }
 #pragma unroll
-        for (int p = 1; p >= 0; --p)
+        for (int p = 2; p >= 0; --p)
 #pragma unroll
           for (int ti = 0; ti < 2; ++ti)
             y[ti] = mfma_bf16x32(xf, lds8(&lds.M[p][Lds::T_::at(ti * 16 + l16, q * 8)]), y[ti]);
