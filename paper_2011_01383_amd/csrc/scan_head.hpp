@@ -96,9 +96,10 @@ template <int W> struct Rows {
 __device__ __forceinline__ int channel_at(int row, int ch) { return row * 64 + (((ch >> 3) ^ (row & 7)) << 3) + (ch & 7); }
 __device__ __forceinline__ int float_at(int row, int ch) { return row * 64 + (((ch >> 2) ^ (row & 15)) << 2) + (ch & 3); }
 
-// Step sizes of a sub-chunk: dt_s, c_s, exp(c_s), exp(c_31 - c_s) dt_s, exp(c_31).
+// Step sizes of a sub-chunk: dt_s, c_s and what its rounding left, exp(c_s),
+// exp(c_31 - c_s) dt_s, exp(c_31).
 struct alignas(16) HeadSteps {
-  float dt[kSub], cum[kSub], grow[kSub], weight[kSub], decay;
+  float dt[kSub], cum[kSub], low[kSub], grow[kSub], weight[kSub], decay;
 };
 
 // Part 1 has no use for what makes y.
@@ -115,11 +116,33 @@ template <int N, bool OUTPUT> struct HeadLds {
   float sums[kHeadWaves];
 };
 
+// A sum of two floats and what its rounding left out of it.
+__device__ __forceinline__ void add_exactly(float &hi, float &lo, float b, float b_lo) {
+#pragma clang fp contract(off) reassociate(off)
+  const float s = hi + b, t = s - hi;
+  lo = (lo + b_lo) + ((hi - (s - t)) + (b - t));
+  hi = s;
+}
+// half_sums with the sums' roundings in `low`.
+__device__ __forceinline__ float half_sums(float v, float &low) {
+  low = 0.0f;
+  add_exactly(v, low, shifted<0x111>(v, 0.0f), shifted<0x111>(low, 0.0f));
+  add_exactly(v, low, shifted<0x112>(v, 0.0f), shifted<0x112>(low, 0.0f));
+  add_exactly(v, low, shifted<0x114>(v, 0.0f), shifted<0x114>(low, 0.0f));
+  add_exactly(v, low, shifted<0x118>(v, 0.0f), shifted<0x118>(low, 0.0f));
+  add_exactly(v, low, shifted<0x142, 0xa>(v, 0.0f), shifted<0x142, 0xa>(low, 0.0f));
+  return v;
+}
+
 // The steps of two sub-chunks, a lane a token.  The state's weights come from a sum
-// from the end: those near the end, which count most, are sums of few terms.
-// Returns the sum of dt over both.
+// from the end: those near the end, which count most, are sums of few terms.  The
+// scores need sums between any two tokens, which are differences of the sums from
+// the start: after one large step those are large themselves, so what their
+// roundings left is kept beside them.  Returns the sum of dt over both.
 __device__ __forceinline__ float put_steps(HeadSteps (&to)[4], int pair, int lane, float dt, float A2) {
-  const float up = half_sums(dt * A2);
+#pragma clang fp contract(off)                    // each product is the same wherever it is added
+  float low;
+  const float up = half_sums(dt * A2, low);
   const float rev = __shfl_xor(dt, kSub - 1);
   const float down = half_sums(rev * A2);         // from token 31 - lane of the half on
   const float after = __shfl_up(down, 1);
@@ -127,10 +150,22 @@ __device__ __forceinline__ float put_steps(HeadSteps (&to)[4], int pair, int lan
   HeadSteps &st = to[2 * pair + lane / kSub];
   st.dt[i] = dt;
   st.cum[i] = up;
+  st.low[i] = low;
   st.grow[i] = fast_exp2(up);
   st.weight[kSub - 1 - i] = fast_exp2(i == 0 ? 0.0f : after) * rev;
   if (i == kSub - 1) st.decay = fast_exp2(down);
   return wave_sum(dt);
+}
+
+// exp(c_t - c_s) dt_s of four tokens s.
+__device__ __forceinline__ f32x4 step_scales(const HeadSteps &st, int t, int s) {
+#pragma clang fp reassociate(off)
+  const float ct = st.cum[t], lt = st.low[t];
+  const f32x4 cs = *(const f32x4 *)&st.cum[s], ls = *(const f32x4 *)&st.low[s], dt = *(const f32x4 *)&st.dt[s];
+  f32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = fast_exp2((ct - cs[i]) + (lt - ls[i])) * dt[i];
+  return r;
 }
 
 __device__ __forceinline__ bf16x8v lds8(const unsigned short *p) { return __builtin_bit_cast(bf16x8v, *(const u32x4v *)p); }
@@ -307,12 +342,11 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
           acc = mfma_bf16x32(lds8(&lds.B[Lds::N_::at(si * 16 + l16, m * 32 + q * 8)]),
                              lds8(&lds.C[Lds::N_::at(ti * 16 + l16, m * 32 + q * 8)]), acc);
         const int t = ti * 16 + l16, s = si * 16 + q * 4;
-        const float ct = st.cum[t];
-        const f32x4 cs = *(const f32x4 *)&st.cum[s], dt = *(const f32x4 *)&st.dt[s];
+        const f32x4 scale = step_scales(st, t, s);
         float v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          v[i] = s + i <= t ? acc[i] * (fast_exp2(ct - cs[i]) * dt[i]) : 0.0f;
+          v[i] = s + i <= t ? acc[i] * scale[i] : 0.0f;
           if (s + i == t) v[i] += skip;
         }
 #pragma unroll

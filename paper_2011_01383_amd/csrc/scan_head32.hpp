@@ -155,11 +155,10 @@ __global__ void __launch_bounds__(kHeadThreads, 3) head_mfma32_kernel(cortex_sca
         for (int m = 0; m < NT; ++m)
           acc = mfma_k16(*(const f32x4 *)&lds.B[si * 16 + l16][m * 16 + q * 4], *(const f32x4 *)&lds.C[ti * 16 + l16][m * 16 + q * 4], acc);
         const int t = ti * 16 + l16, s = si * 16 + q * 4;
-        const float ct = st.cum[t];
-        const f32x4 cs = *(const f32x4 *)&st.cum[s], dt = *(const f32x4 *)&st.dt[s];
+        const f32x4 scale = step_scales(st, t, s);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          acc[i] = s + i <= t ? acc[i] * (fast_exp2(ct - cs[i]) * dt[i]) : 0.0f;
+          acc[i] = s + i <= t ? acc[i] * scale[i] : 0.0f;
           if (s + i == t) acc[i] += skip;
         }
         *(f32x4 *)&lds.M[t][s] = acc;

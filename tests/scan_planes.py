@@ -21,20 +21,33 @@ def held(v, planes):
     return sum_
 
 
-def prefix(e):
-    """Inclusive sums over 32 tokens in the order of the lanes' shifts."""
-    hi = np.array(e, f32)
+def below(v, s):
+    """v of the lane that the shift by s names, 0 where it leaves one out: 1, 2, 4 and 8 stay in a
+    row of 16 lanes, 16 is lane 15 to the upper row."""
+    b = np.zeros_like(v)
+    if s == 16:
+        b[16:] = v[15]
+    else:
+        b[s:16], b[16 + s:] = v[:16 - s], v[16:-s]
+    return b
+
+
+def prefix(e, low=None):
+    """Inclusive sums over 32 tokens in the order of the lanes' shifts; `low`, if given, collects what
+    their roundings left."""
+    hi, lo = np.array(e, f32), np.zeros(SUB, f32)
     for s in (1, 2, 4, 8, 16):
-        b = np.concatenate([np.zeros(s, f32), hi[:-s]])
-        if s == 16:
-            b = np.where(np.arange(SUB) >= 16, hi[15], f32(0)).astype(f32)
-        elif s < 16:
-            b[16:16 + s] = 0                                # the shifts stay in a row of 16 lanes
-        hi = (hi + b).astype(f32)
+        b, b_lo = below(hi, s), below(lo, s)
+        total = (hi + b).astype(f32)
+        t = (total - hi).astype(f32)
+        lo = ((lo + b_lo) + ((hi - (total - t)) + (b - t))).astype(f32)
+        hi = total
+    if low is not None:
+        low[:] = lo
     return hi
 
 
-def head_scan(x, dt, A, B, C, h0, planes_score=3, planes_read=3, planes_add=3):
+def head_scan(x, dt, A, B, C, h0, planes_score=3, planes_read=3, planes_add=3, exact_sums=True):
     """One head, one sequence of whole sub-chunks: x [T, P], dt [T], B and C [T, N], h0 [P, N].
     Returns y and the last state."""
     A2 = f32(f32(A) * f32(1.44269504088896340736))
@@ -44,11 +57,14 @@ def head_scan(x, dt, A, B, C, h0, planes_score=3, planes_read=3, planes_add=3):
         s = slice(t0, t0 + SUB)
         xs, Bs, Cs, d = x[s].astype(f32), B[s].astype(f32), C[s].astype(f32), dt[s].astype(f32)
         e = (d * A2).astype(f32)
-        cum = prefix(e)
+        low = np.zeros(SUB, f32)
+        cum = prefix(e, low)
+        low *= exact_sums
         after = np.concatenate([prefix(e[::-1])[:-1][::-1], [f32(0)]])
         decay = np.exp2(prefix(e[::-1])[-1])
         with np.errstate(over="ignore", invalid="ignore"):
-            score = ((Cs @ Bs.T) * (np.exp2(cum[:, None] - cum[None]) * d)).astype(f32)
+            between = (cum[:, None] - cum[None]) + (low[:, None] - low[None])
+            score = ((Cs @ Bs.T) * (np.exp2(between) * d)).astype(f32)
         score = held(np.where(lower, score, f32(0)), planes_score)
         y[s] = (Cs @ held(h, planes_read).T) * np.exp2(cum)[:, None] + score @ xs
         weighted = held((xs * (np.exp2(after) * d)[:, None]).astype(f32), planes_add)

@@ -159,3 +159,51 @@ def test_whole_outputs(N, dtype):
         assert norm_error(host(out), states) <= WHOLE
         if dtype == "f32":
             assert norm_error(host(d["y"]), ref) <= WHOLE
+
+
+# ---- ordinary tokens after a large step ----
+
+def large_step(dtype, size, N=64, P=32, A=16.0):
+    """Token 40 has a step of `size`, so nothing of the tokens before it is left; the others' are small."""
+    p = Scan(11, [T], 2 * P, N, 1, P, dtype=dtype, z=False, skip=False, bias=False, soft=False, state=False)
+    p.A[:] = -A
+    p.dt[:] = bf16(0.002 + 0.006 * np.random.default_rng(1).random(p.dt.shape))
+    p.dt[40] = bf16(size)
+    p.x[40] = 0                                  # its own input would hide the others'
+    return p
+
+
+@pytest.mark.parametrize("size,wrong", [(20.0, 1.5e-6), (100.0, 1e-5), (1000.0, 1e-4), (20000.0, 2e-3)])
+def test_the_norm_tells_sums_that_lose_small_steps(size, wrong):
+    p = large_step("f32", size)
+    ref = p.reference()[0][:, :32]
+
+    def error(**kw):
+        y, _ = E.head_scan(p.x[:, :32], p.dt[:, 0].astype(np.float32), p.A[0], p.B[:, 0], p.C[:, 0], np.zeros((32, 64)), **kw)
+        return norm_error(y[41:].astype(np.float64), ref[41:])
+
+    assert error() <= WHOLE / 2
+    assert error(exact_sums=False) > wrong
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [20.0, 100.0, 1000.0, 20000.0])
+def test_tokens_after_a_large_step(size, dtype):
+    """As exact as without it.  A bf16 output is off by its store's rounding, 2^-9 at most.  Its float32
+    value is off by some 3e-7, which takes it to the other side of a rounding's tie in 2 * 3e-7 / 2^-8 of
+    the outputs, a few times more where the terms cancel."""
+    need_gpu()
+    for N in (16, 64, 128):
+        announce("a step of %g, %s N %d" % (size, dtype, N))
+        p = large_step(dtype, size, N)
+        d = p.upload()
+        C.check(p.call())
+        torch.cuda.synchronize()
+        assert int(d["status"].item()) == 0
+        ref = p.reference()[0][41:]
+        got = host(d["y"])[41:]
+        assert norm_error(got, ref) <= (WHOLE if dtype == "f32" else 2.0 ** -9)
+        if dtype == "bf16":
+            # the rounded reference itself: few outputs fall on the other side of a tie
+            assert np.mean(got != bf16(ref)) <= 0.002
