@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(256) enter_kernel(cortex_scan_t a, int32_t *st
   if (e >= per_slot) return;
   const int d = (int)(e / a.state_size), k = HEAD ? d / a.head_dim : d;
   const int rates = HEAD ? a.channels / a.head_dim : a.channels;
-  const float A2 = a.A[HEAD ? k : e] * kLog2e;
+  const float A2 = decay_rate(a.A[HEAD ? k : e]);
   float h = row >= 0 && a.state_in ? a.state_in[row * per_slot + e] : 0.0f;
   const int count = (last - first + Q - 1) / Q;
   const int64_t slot0 = first / Q + seq;
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kScanWave) channel_scan_kernel(cortex_scan_t a
 #pragma unroll
     for (int n = 0; n < N; ++n) h[n] = 0.0f;
 #pragma unroll
-  for (int n = 0; n < N; ++n) A2[n] = a.A[(int64_t)d * N + n] * kLog2e;
+  for (int n = 0; n < N; ++n) A2[n] = decay_rate(a.A[(int64_t)d * N + n]);
   const float bias = a.dt_bias ? a.dt_bias[d] : 0.0f, skip = a.skip ? a.skip[d] : 0.0f;
   const T *xs = (const T *)a.x + d, *ds = (const T *)a.dt + d, *zs = (const T *)a.z + d;
   T *ys = (T *)a.y + d;
@@ -268,11 +268,11 @@ __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(cortex_scan_t a
     const int k = HEAD ? d[u] / a.head_dim : d[u];
     const bool stores = c0 + u / UR * kChannels + (int)(threadIdx.x / L) < a.channels && b0 + u % UR < a.num_seqs;
     const float dt = step_size(a, raw[u], a.dt_bias ? a.dt_bias[k] : 0.0f);
-    const float w = dt * x[u], decay = HEAD ? fast_exp2(dt * (a.A[k] * kLog2e)) : 0.0f;
+    const float w = dt * x[u], decay = HEAD ? fast_exp2(dt * decay_rate(a.A[k])) : 0.0f;
     float y = 0.0f;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      const float f = HEAD ? decay : fast_exp2(dt * (a.A[(int64_t)k * N + part * 4 + n] * kLog2e));
+      const float f = HEAD ? decay : fast_exp2(dt * decay_rate(a.A[(int64_t)k * N + part * 4 + n]));
       h[u][n] = __builtin_fmaf(h[u][n], f, w * to_float<T>(Bv[u][n]));
       y = __builtin_fmaf(h[u][n], to_float<T>(Cv[u][n]), y);
     }

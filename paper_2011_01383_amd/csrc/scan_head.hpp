@@ -138,13 +138,16 @@ __device__ __forceinline__ float half_sums(float v, float &low) {
 // from the end: those near the end, which count most, are sums of few terms.  The
 // scores need sums between any two tokens, which are differences of the sums from
 // the start: after one large step those are large themselves, so what their
-// roundings left is kept beside them.  Returns the sum of dt over both.
+// roundings left is kept beside them.  A step's exponent is held to -256, which
+// leaves nothing of the state (the smallest float is 2^-149), so that no sum is
+// infinite and no difference of two a NaN.  Returns the sum of dt over both.
 __device__ __forceinline__ float put_steps(HeadSteps (&to)[4], int pair, int lane, float dt, float A2) {
 #pragma clang fp contract(off)                    // each product is the same wherever it is added
+  const float e = dt * A2, held = e < -256.0f ? -256.0f : e;     // (a NaN stays one)
   float low;
-  const float up = half_sums(dt * A2, low);
+  const float up = half_sums(held, low);
   const float rev = __shfl_xor(dt, kSub - 1);
-  const float down = half_sums(rev * A2);         // from token 31 - lane of the half on
+  const float down = half_sums(__shfl_xor(held, kSub - 1));      // from token 31 - lane of the half on
   const float after = __shfl_up(down, 1);
   const int i = lane % kSub;
   HeadSteps &st = to[2 * pair + lane / kSub];
@@ -246,7 +249,7 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
     h[nt] = works && h_in ? *(const f32x4 *)(h_in + nt * 16 + q * 4) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const float A2 = a.A[head] * kLog2e, bias = a.dt_bias ? a.dt_bias[head] : 0.0f, skip = a.skip ? a.skip[head] : 0.0f;
+  const float A2 = decay_rate(a.A[head]), bias = a.dt_bias ? a.dt_bias[head] : 0.0f, skip = a.skip ? a.skip[head] : 0.0f;
   const bf16_t *xs = (const bf16_t *)a.x + head * P + p0, *ds = (const bf16_t *)a.dt + head;
   const bf16_t *Bs = (const bf16_t *)a.B + g * N, *Cs = (const bf16_t *)a.C + g * N;
   // the thread's eight channels of one token, of x, z and y

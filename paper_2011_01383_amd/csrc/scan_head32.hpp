@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(kHeadThreads, 3) head_mfma32_kernel(cortex_sca
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
     h[nt] = works && h_in ? *(const f32x4 *)(h_in + nt * 16 + q * 4) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const float A2 = a.A[head] * kLog2e, bias = a.dt_bias ? a.dt_bias[head] : 0.0f, skip = a.skip ? a.skip[head] : 0.0f;
+  const float A2 = decay_rate(a.A[head]), bias = a.dt_bias ? a.dt_bias[head] : 0.0f, skip = a.skip ? a.skip[head] : 0.0f;
   const float *xs = (const float *)a.x + head * P + p0, *ds = (const float *)a.dt + head;
   const float *Bs = (const float *)a.B + g * N, *Cs = (const float *)a.C + g * N;
   const int ch = head * P + (works ? pw : 0) + q * 4;

@@ -49,6 +49,14 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // v_exp_f32: 2^x to one unit in the last place, denormal results flushed to zero.
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A decay's rate to the base 2.  Past the float range it stays a number, so that a step
+// of 0, as tokens past a sequence's end have it, keeps the state (0 * infinity would not).
+__device__ __forceinline__ float decay_rate(float A) {
+  constexpr float kLowest = -3.402823466e38f;
+  const float r = A * kLog2e;
+  return r < kLowest ? kLowest : r;              // (a NaN stays one)
+}
+
 // v / (1 + exp(-v)).
 __device__ __forceinline__ float silu(float v) {
   return v * __builtin_amdgcn_rcpf(1.0f + fast_exp2(v * -kLog2e));
