@@ -433,7 +433,8 @@ int cortex_scan_step(const cortex_scan_t *args, int32_t *d_status, void *stream)
  *   lse     log sum_i exp(v) (-infinity if every v is)
  * Each output may be NULL.  A masked entry's logit is never used, whatever it
  * holds.  A row of the mask is ceil(V / 32) words, bit i % 32 of word i / 32 set
- * where i is allowed; mask_index[b] = -1 is a row without a mask.  A row has at
+ * where i is allowed; mask_index[b] = -1 is a row without a mask.  Without mask
+ * there is none for any row, and mask_index and mask_rows are not read.  A row has at
  * most 65,535 biases, a call at most 65,535 rows.
  * CORTEX_ST_INPUT_RANGE: a token outside [0, V), a history length outside
  * [0, history_cap], a prompt length outside [0, the row's history length], a mask

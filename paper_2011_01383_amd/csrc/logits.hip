@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(THREADS) logits_kernel(cortex_logits_t a, int3
         (row == a.rows - 1 && bias1 != a.num_biases))
       broken = true;
   }
-  if (a.mask || a.mask_index) {
+  if (a.mask) {
     m = a.mask_index ? a.mask_index[row] : row;
     if (m < -1 || m >= a.mask_rows) broken = true;
   }
