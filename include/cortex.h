@@ -335,6 +335,10 @@ int cortex_dag_infer(int32_t H, const int32_t *d_children, const cortex_lin_t *l
  * - At most 262,144 channels; the scan's row strides at most 2^25.
  * - A call with nothing to do (no sequence) enqueues nothing and returns
  *   CORTEX_OK.  Results are deterministic.
+ * - A call that finds an error in its own data stops where it is: outputs and
+ *   states of its other sequences are then what they were or what the call
+ *   computes for them, element by element, so a pool that is updated in place
+ *   has to be set anew.
  */
 #define CORTEX_F32 0
 #define CORTEX_BF16 1

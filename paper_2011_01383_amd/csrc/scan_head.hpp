@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
   constexpr int NT = N / 16, NB = Lds::NP / 32;
   constexpr int OL = N / 8, kItems = (OL * kSub + kHeadThreads - 1) / kHeadThreads;   // octets of a row; of them all per thread
   __shared__ Lds lds;
-  if (entry_status(status) != 0) return;
+  const int failed = entry_status(status);
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int q = lane >> 4, l16 = lane & 15;
   const int P = a.head_dim, blocks = (P + 63) / 64, heads = a.channels / P;
@@ -239,6 +239,9 @@ __global__ void __launch_bounds__(kHeadThreads, N == 128 ? 3 : 4) head_mfma_kern
     row = state_row(a.state_index, seq, a.state_rows, status);
     if (row < -1) return;
   }
+  // Another workgroup's error may be seen by some waves and not by others.  None goes on
+  // alone: the others would store what LDS held in its place.
+  if (__syncthreads_or(failed != 0)) return;
   const int pw = p0 + wave * 16;                 // the wave's channels in the head
   const bool works = pw < P;                     // a head of less than 64 channels has none for the last waves
   const int d = head * P + (works ? pw : 0) + l16;

@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(kHeadThreads, 3) head_mfma32_kernel(cortex_sca
                                                                     int64_t units) {
   constexpr int NT = N / 16, kItems = (N / 4 * kSub + kHeadThreads - 1) / kHeadThreads;
   __shared__ HeadLds32<N> lds;
-  if (entry_status(status) != 0) return;
+  const int failed = entry_status(status);
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int q = lane >> 4, l16 = lane & 15;
   const int P = a.head_dim, blocks = (P + 63) / 64, heads = a.channels / P;
@@ -70,6 +70,7 @@ __global__ void __launch_bounds__(kHeadThreads, 3) head_mfma32_kernel(cortex_sca
     row = state_row(a.state_index, seq, a.state_rows, status);
     if (row < -1) return;
   }
+  if (__syncthreads_or(failed != 0)) return;     // all waves or none, as in the bf16 form
   const int pw = p0 + wave * 16;
   const bool works = pw < P;
   const int d = head * P + (works ? pw : 0) + l16;
