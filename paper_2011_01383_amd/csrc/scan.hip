@@ -27,8 +27,8 @@ template <int N> __device__ __forceinline__ void store_floats(float *p, const fl
 // exp(dt A) is exp(A sum dt).  Three launches: every segment's result and step
 // sum from zero (part 1), the states that enter the segments, one after another
 // (enter_kernel), then the outputs from those (part 2).  With enough sequences
-// and channels to fill the GPU, or no sequence longer than a segment, one
-// launch walks each sequence whole (part 0): half the arithmetic.
+// and channels to fill the GPU, or few tokens, one launch walks each sequence
+// whole (part 0): half the arithmetic.
 // ---------------------------------------------------------------------------
 // One thread per state entry walks its sequence's segments.
 template <bool HEAD>
@@ -294,31 +294,54 @@ __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(cortex_scan_t a
 // ---------------------------------------------------------------------------
 // Tokens of a segment, 0 for one launch over whole sequences.
 //
-// Per channel.  A wave is bound by its arithmetic, so the split, which doubles
-// that, pays until every SIMD of the GPU (1,024) has a wave without it.  Segments
-// are as long as leaves four waves a SIMD (8,192 tokens of 16 sequences and 2,048
-// channels, 32 tokens: 160 us; 128: 202; one launch: 1,190); below half a wave a
-// SIMD they go down to 16 (257 tokens of 512 channels, 24 tokens: 27 us; 32: 33; 64: 55).
+// The host knows how many tokens and sequences there are, not how long each is, so
+// a rule can be right for equal lengths, for a ramp of them, or for one long prompt
+// among short ones, not for all.  Times in us, split and in one launch.
 //
-// Per head.  The workgroups that the GPU holds at once (three a CU at N = 128,
-// four below) get a segment each, of at least 64 tokens: 32,768 tokens of 64 heads,
-// 2,752 tokens: 519 us; 1,024: 530; 256: 660; 4,099 float32 tokens of 16 heads,
-// 96 tokens: 48; 64: 56; 256: 69.  From 512 workgroups on one launch is faster
-// (8,192 tokens of 16 sequences and 32 heads: 90 us, split 154 to 200).
+// Per channel.  A wave is bound by its arithmetic, which a split doubles; in one
+// launch the longest sequence is a chain of tokens at 0.45 us each (N = 16).  The
+// switch is where equal lengths lose by the split what a ramp gains, one wave a SIMD
+// (1,024): 8,192 tokens of 2,048 bf16 channels, 24 prompts: equal 167 and 163, ramp
+// 172 and 302; 32: 164 and 124, 177 and 231; 64: 174 and 84, 205 and 156.  With fewer
+// channels and shorter prompts it would be lower (4,096 float32 tokens of 512
+// channels, 64 prompts: 51 and 34, 52 and 62; 100: 61 and 25, 60 and 41), but a long
+// prompt among them would then cost ten times a split.  Up to 36 tokens three
+// launches cost more than any chain (32 tokens: 20 and 17, 48: 20 and 24; N = 64: 44 and
+// 44, 44 and 64).  Segments are as long as leaves four waves a SIMD (8,192 tokens of 16
+// sequences and 2,048 channels, 32 tokens: 160; 128: 202); below half a wave a
+// SIMD they go down to 16 (257 tokens of 512 channels, 24 tokens: 27; 32: 33; 64: 55).
+//
+// Per head.  A unit is 64 channels of a head in one sequence.  In one launch the
+// longest sequence is a chain of sub-chunks at 1.6 to 2.4 us (float32 3.3 to 5.2).  8,192
+// tokens of 32 bf16 heads, N = 128: 8 prompts (256 units): equal 126 and 85, ramp 133
+// and 144, half of the tokens in one prompt 131 and 320; 12 (384): 138 and 77, 145 and
+// 116, 159 and 315; 15 (480): 142 and 65, 145 and 97, 166 and 320; 16,384 tokens of 64
+// heads, 7 prompts (448): 436 and 255, 397 and 380; 4,096 float32 tokens of 16 heads, 24
+// prompts (384): 67 and 37, 70 and 59.  At 400 units the most that either choice loses is
+// about the same.  Short prompts: 192 tokens of one unit 16 and 16, of 32 (N = 128) 24 and
+// 20; 256: 16 and 19, 24 and 25; 64 units: 256: 35 and 25, 512: 43 and 44; 128 units of four
+// sequences, half of the tokens in one: 512: 43 and 25, 1,024: 47 and 45; float32, 16 units:
+// 128: 20 and 18, 192: 21 and 25.  The workgroups that the GPU holds at once (three a CU at
+// N = 128, four below) get a segment each, of at least 64 tokens: 32,768 tokens of 64 heads,
+// 2,752 tokens: 519; 1,024: 530; 256: 660; 4,099 float32 tokens of 16 heads, 96 tokens: 48;
+// 64: 56; 256: 69.
+constexpr int64_t kWholeUnits = 400, kWholeWaves = 1024;   // from these on one launch
 static int segment_tokens(int64_t T, int64_t S, int64_t D, int N, int head_dim) {
+  int64_t Q;
   if (head_dim) {
-    const int64_t groups = D / head_dim * ((head_dim + 63) / 64);
-    if (S * groups >= 512) return 0;
-    const int64_t segments = (N == 128 ? 768 : 1024) / groups;       // 2 at least
-    const int64_t Q = ((T + segments - 1) / segments + 31) / 32 * 32;
-    return T <= 64 ? 0 : Q < 64 ? 64 : (int)Q;
+    const int64_t groups = D / head_dim * ((head_dim + 63) / 64), units = S * groups;
+    if (units >= kWholeUnits || T <= 160 + 2 * units) return 0;
+    const int64_t segments = (N == 128 ? 768 : 1024) / groups;
+    Q = ((T + segments - 1) / segments + 31) / 32 * 32;
+    if (Q < 64) Q = 64;
+  } else {
+    const int64_t tiles = (D + kScanWave - 1) / kScanWave;
+    if (S * tiles >= kWholeWaves || T <= 36) return 0;
+    Q = 256;
+    while (Q > 32 && T / Q * tiles < 4096) Q /= 2;
+    if (T / Q * tiles < 512) Q = 16;
   }
-  const int64_t tiles = (D + kScanWave - 1) / kScanWave;
-  if (S * tiles >= 1024) return 0;
-  int Q = 256;
-  while (Q > 32 && T / Q * tiles < 4096) Q /= 2;
-  if (T / Q * tiles < 512) Q = 16;
-  return T <= Q ? 0 : Q;
+  return T <= Q ? 0 : (int)Q;                    // one segment is not split
 }
 
 static SegmentScratch scratch_of(const cortex_scan_t &a, int Q, void *ws) {

@@ -18,7 +18,7 @@ def bf16(a):
     return torch.from_numpy(np.asarray(a, np.float64)).to(torch.bfloat16).double().numpy()
 
 
-def close_states(N, H, P, seed=0):
+def close_states(N, H, P, seed=0, T=T):
     """y is the difference of two entries of the state that are the same to 15 bits: no inputs, no decay."""
     r = np.random.default_rng(seed)
     D = H * P
@@ -32,7 +32,7 @@ def close_states(N, H, P, seed=0):
     return p
 
 
-def close_scores(N, H, P, seed=0):
+def close_scores(N, H, P, seed=0, T=T):
     """Two neighbouring tokens of every 32 have opposite inputs, and their decays differ in the 14th bit."""
     r = np.random.default_rng(seed)
     D = H * P
