@@ -414,7 +414,8 @@ typedef struct {
   int64_t y_ld;
 } cortex_scan_t;
 
-/* Workspace bytes of cortex_scan_forward (0 if invalid); it need not be zeroed. */
+/* Workspace bytes of cortex_scan_forward for batches of up to num_tokens tokens in
+ * up to num_seqs sequences (0 if invalid); it need not be zeroed. */
 size_t cortex_scan_workspace_bytes(int32_t num_tokens, int32_t num_seqs, int32_t channels, int32_t state_size,
                                    int32_t head_dim);
 int cortex_scan_forward(const cortex_scan_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream);

@@ -3,6 +3,8 @@
 #include "scan_head32.hpp"
 #include "sequence.hpp"
 
+#include <algorithm>
+
 namespace cortex {
 
 constexpr int kScanWave = 64;
@@ -344,6 +346,28 @@ static int segment_tokens(int64_t T, int64_t S, int64_t D, int N, int head_dim) 
   return T <= Q ? 0 : (int)Q;                    // one segment is not split
 }
 
+// A call that does not split has to bring a workspace too, of 256 bytes.
+static size_t scratch_bytes(int64_t slots, int64_t D, int N) {
+  return std::max<size_t>(256, (size_t)slots * D * (N + 1) * sizeof(float));
+}
+
+// The most slots that segment_tokens leads to for up to T tokens in up to S sequences
+// (more of either may mean fewer: longer segments, or one launch).  A batch that is
+// split has less than kWholeUnits / groups sequences.  Per head T / Q is at most T / 64 and
+// at most `segments`.  Per channel Q = 256 gives T / 256; a smaller one was taken since
+// T / 2Q * tiles < 4,096 (for 16: T / 32 * tiles < 512), so T / Q <= 2 * (4,095 / tiles) + 1.
+static int64_t most_slots(int64_t T, int64_t S, int64_t D, int N, int head_dim) {
+  if (head_dim) {
+    const int64_t groups = D / head_dim * ((head_dim + 63) / 64);
+    const int64_t segments = (N == 128 ? 768 : 1024) / groups;
+    if (groups >= kWholeUnits || segments < 2 || T <= 160 + 2 * groups) return 0;
+    return std::min(T / 64, segments) + std::min(S, (kWholeUnits - 1) / groups);
+  }
+  const int64_t tiles = (D + kScanWave - 1) / kScanWave;
+  if (tiles >= kWholeWaves || T <= 36) return 0;
+  return std::min(T / 16, std::max(T / 256, 2 * (4095 / tiles) + 1)) + std::min(S, (kWholeWaves - 1) / tiles);
+}
+
 static SegmentScratch scratch_of(const cortex_scan_t &a, int Q, void *ws) {
   SegmentScratch w = {nullptr, nullptr};
   if (Q) {
@@ -493,9 +517,7 @@ using namespace cortex;
 extern "C" size_t cortex_scan_workspace_bytes(int32_t num_tokens, int32_t num_seqs, int32_t channels, int32_t state_size,
                                               int32_t head_dim) {
   if (num_tokens < 0 || num_seqs < 0 || bad_scan_size(channels, 1, state_size, head_dim)) return 0;
-  const int Q = segment_tokens(num_tokens, num_seqs, channels, state_size, head_dim);
-  if (!Q) return 256;
-  return (size_t)chunk_slots(num_tokens, num_seqs, Q) * channels * (state_size + 1) * sizeof(float);
+  return scratch_bytes(most_slots(num_tokens, num_seqs, channels, state_size, head_dim), channels, state_size);
 }
 
 extern "C" int cortex_scan_forward(const cortex_scan_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream) {
@@ -503,8 +525,9 @@ extern "C" int cortex_scan_forward(const cortex_scan_t *args, int32_t *d_status,
   if (rc != CORTEX_OK) return rc;
   if (args->num_seqs == 0) return CORTEX_OK;
   if (!d_ws) return CORTEX_E_INVAL;
-  if (ws_bytes < cortex_scan_workspace_bytes(args->num_tokens, args->num_seqs, args->channels, args->state_size, args->head_dim))
-    return CORTEX_E_WORKSPACE;
+  const int Q = segment_tokens(args->num_tokens, args->num_seqs, args->channels, args->state_size, args->head_dim);
+  const int64_t slots = Q ? chunk_slots(args->num_tokens, args->num_seqs, Q) : 0;
+  if (ws_bytes < scratch_bytes(slots, args->channels, args->state_size)) return CORTEX_E_WORKSPACE;
   return args->dtype == CORTEX_BF16 ? scan_forward_typed<bf16_t>(*args, d_status, d_ws, stream)
                                     : scan_forward_typed<float>(*args, d_status, d_ws, stream);
 }

@@ -15,7 +15,6 @@ WHOLE_SEQUENCES = 256          # bytes of workspace of a call that does not spli
     (5000, 1, 12800, 128, 32),              # 400 heads: the GPU holds one segment of each
     (100000, 1, 385 * 16, 128, 16),         # 385
     (300, 1, 399 * 64, 64, 64),
-    (8192, 15, 2048, 128, 64), (8192, 16, 2048, 128, 64),
     (96, 1, 2048, 128, 64), (160, 1, 64, 64, 64), (128, 64, 256, 64, 64),
     (32, 1, 512, 16, 0), (36, 4, 64, 64, 0)])
 def test_one_launch(T, S, D, N, P):
@@ -27,6 +26,23 @@ def test_one_launch(T, S, D, N, P):
     (32768, 1, 4096, 128, 64), (4099, 5, 1024, 64, 64), (8192, 8, 2048, 128, 64), (8192, 16, 2048, 16, 0), (257, 1, 512, 16, 0)])
 def test_segments(T, S, D, N, P):
     assert C.cortex_scan_workspace_bytes(T, S, D, N, P) > 2 * D * N * 4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,S,whole", [(8192, 15, True), (8192, 16, True), (8192, 12, False), (8192, 1, False), (224, 1, True),
+                                       (225, 1, False)])
+def test_one_launch_needs_no_workspace(T, S, whole):
+    """32 heads of 64: a call that does not split takes 256 bytes, one that does refuses them."""
+    need_gpu()
+    D, N, H = 2048, 128, 32
+    announce("%d tokens of %d prompts in 256 bytes" % (T, S))
+    z = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device="cuda")
+    off = torch.tensor([T * i // S for i in range(S + 1)], dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    rc = C.cortex_scan_forward(z(T, D), z(T, H), torch.zeros(H, device="cuda"), z(T, 1, N), z(T, 1, N), off, z(T, D),
+                               status=status, ws=C.workspace(WHOLE_SEQUENCES))
+    torch.cuda.synchronize()
+    assert rc == (C.CORTEX_OK if whole else C.CORTEX_E_WORKSPACE) and int(status.item()) == 0
 
 
 @pytest.mark.gpu
