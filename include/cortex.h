@@ -332,6 +332,7 @@ int cortex_dag_infer(int32_t H, const int32_t *d_children, const cortex_lin_t *l
  * - dtype is the type of activations (and of the convolution's state, which
  *   holds inputs).  Weights, decays and scan states are float32, and all sums
  *   are float32 whatever the type, rounded to nearest even once at the store.
+ * - A workspace starts at a 16-byte boundary (others: CORTEX_E_INVAL).
  * - At most 262,144 channels; the scan's row strides at most 2^25.
  * - A call with nothing to do (no sequence) enqueues nothing and returns
  *   CORTEX_OK.  Results are deterministic.

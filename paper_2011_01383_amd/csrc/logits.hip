@@ -375,7 +375,7 @@ extern "C" size_t cortex_logits_workspace_bytes(int32_t rows, int32_t vocab) {
 
 extern "C" int cortex_logits_process(const cortex_logits_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes,
                                      void *stream) {
-  if (!args || !d_status || !d_ws) return CORTEX_E_INVAL;
+  if (!args || !d_status || !d_ws || !aligned16(d_ws)) return CORTEX_E_INVAL;
   const cortex_logits_t &a = *args;
   if ((a.dtype != CORTEX_F32 && a.dtype != CORTEX_BF16) || a.rows < 0 || a.rows > kLogitsMaxRows || a.vocab < 1 ||
       a.vocab > 0x7fff0000)

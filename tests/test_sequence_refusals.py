@@ -1,0 +1,24 @@
+"""More refusals of the sequence operators that need no GPU."""
+import ctypes
+import os
+
+import pytest
+import torch
+
+from paper_2011_01383_amd import cortex as C
+from tests.test_sequence_abi import P8, logits_args, scan_args
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(C.LIB_PATH):
+        from paper_2011_01383_amd import build
+        build.build()
+    return C.load()
+
+
+@pytest.mark.parametrize("off", [1, 2, 4, 8])
+def test_workspaces_start_at_16_bytes(lib, off):
+    """The scan stores 16 bytes at once, the logits count arrivals with atomics."""
+    assert lib.cortex_scan_forward(ctypes.byref(scan_args()), P8, P8 + off, 1 << 40, None) == C.CORTEX_E_INVAL
+    assert lib.cortex_logits_process(ctypes.byref(logits_args()), P8, P8 + off, 1 << 40, None) == C.CORTEX_E_INVAL
