@@ -386,7 +386,8 @@ int cortex_conv_step(const cortex_conv_t *args, int32_t *d_status, void *stream)
  *                   skip and dt_bias [D/P]; N = 16, 32, 64 or 128, P a multiple
  *                   of 16 up to 256 that divides D/G
  * Other sizes return CORTEX_E_INVAL, and so do states that do not start at a
- * 16-byte boundary.
+ * 16-byte boundary, and prompts of 2^24 and more heads of all sequences together
+ * (a head of more than 64 channels counts as several of 64).
  */
 typedef struct {
   int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: x, z, dt, B, C, y */

@@ -524,6 +524,10 @@ extern "C" int cortex_scan_forward(const cortex_scan_t *args, int32_t *d_status,
   const int rc = check_scan(args, false, d_status);
   if (rc != CORTEX_OK) return rc;
   if (args->num_seqs == 0) return CORTEX_OK;
+  // Whole sequences per head are a workgroup a unit, and a grid has less than 2^32 threads.
+  if (args->head_dim && (int64_t)args->num_seqs * (args->channels / args->head_dim) * ((args->head_dim + 63) / 64) >=
+                            (int64_t)1 << 24)
+    return CORTEX_E_INVAL;
   if (!d_ws || !aligned16(d_ws)) return CORTEX_E_INVAL;
   const int Q = segment_tokens(args->num_tokens, args->num_seqs, args->channels, args->state_size, args->head_dim);
   const int64_t slots = Q ? chunk_slots(args->num_tokens, args->num_seqs, Q) : 0;

@@ -22,3 +22,11 @@ def test_workspaces_start_at_16_bytes(lib, off):
     """The scan stores 16 bytes at once, the logits count arrivals with atomics."""
     assert lib.cortex_scan_forward(ctypes.byref(scan_args()), P8, P8 + off, 1 << 40, None) == C.CORTEX_E_INVAL
     assert lib.cortex_logits_process(ctypes.byref(logits_args()), P8, P8 + off, 1 << 40, None) == C.CORTEX_E_INVAL
+
+
+@pytest.mark.parametrize("S,P", [(1 << 25, 64), (1 << 23, 64), (1 << 22, 256), (3 << 28, 16)])
+def test_prompts_of_more_heads_than_a_grid_holds(lib, S, P):
+    """Their number was cut to 32 bits: 2^32 and more of them ran too few workgroups, or none."""
+    D = 2 * P if P < 256 else P
+    a = scan_args(num_seqs=S, num_tokens=64, channels=D, head_dim=P, groups=1, state_rows=S, x_ld=D, y_ld=D, dt_ld=D // P)
+    assert lib.cortex_scan_forward(ctypes.byref(a), P8, P8, 1 << 50, None) == C.CORTEX_E_INVAL
