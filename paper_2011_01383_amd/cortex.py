@@ -648,6 +648,8 @@ def cortex_logits_process(logits: torch.Tensor, *, out=None, token=None, lse=Non
     elif any(t is not None for t in (history_len, prompt_len, repetition, frequency, presence)):
         raise ValueError("history is required with its lengths and penalties")
     if bias_offsets is not None:
+        if bias_tokens is not None and not isinstance(bias_tokens, torch.Tensor):
+            raise ValueError("bias_tokens must be a torch.Tensor, got %s" % type(bias_tokens).__name__)
         biases = 0 if bias_tokens is None else bias_tokens.numel()
         specs += [(bias_offsets, "bias_offsets", i32, R + 1, False), (bias_tokens, "bias_tokens", i32, 0, False),
                   (bias_values, "bias_values", f32, biases, False)]
