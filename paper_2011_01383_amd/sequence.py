@@ -134,6 +134,17 @@ def write_trees(model: SequenceModel, prompts, most: int = 40, repetition: float
     """Continues every prompt (lists of tokens) with one tree in prefix order of at most ``most``
     tokens, greedily under the grammar.  ``opening`` is a bias for another inner node.
     Returns the trees' tokens and their log-probabilities under the masked, penalised logits."""
+    # on the device a token or row out of range would end the process, and an empty prompt
+    # would continue its neighbour's
+    if len(prompts) > model.rows:
+        raise ValueError("%d prompts, the model runs %d at once" % (len(prompts), model.rows))
+    for i, p in enumerate(prompts):
+        if len(p) == 0:
+            raise ValueError("prompt %d is empty" % i)
+        if min(p) < 0 or max(p) >= model.vocab:
+            raise ValueError("prompt %d has a token outside [0, %d)" % (i, model.vocab))
+    if not prompts:
+        return [], np.zeros(0, dtype=np.float32)
     S, dev = len(prompts), model.device
     ints = lambda v: torch.tensor(v, dtype=torch.int32, device=dev)
     full = lambda v: torch.full((S,), float(v), device=dev)
