@@ -106,6 +106,14 @@ class SequenceModel:
             layer.conv_state[slots.long()] = 0
             layer.state[slots.long()] = 0
 
+    def check(self) -> None:
+        """Raises what the calls since the last check reported, and clears it: a status left in
+        place would make every later call a no-op."""
+        code = int(self.status.item())
+        if code != 0:
+            self.status.zero_()
+            raise RuntimeError("device status %d" % code)
+
     def prompt(self, tokens, offsets, slots):
         """Logits after the last token of each prompt (none may be empty)."""
         x = self._run(tokens, slots, offsets)
@@ -182,8 +190,7 @@ def write_trees(model: SequenceModel, prompts, most: int = 40, repetition: float
             # a finished sequence keeps its states: its row of the pools is not named
             logits = model.step(chosen, torch.where(done, -1, slots).to(torch.int32)).contiguous()
     text, ends = history.cpu().numpy(), at.cpu().numpy()
-    if int(model.status.item()) != 0:
-        raise RuntimeError("device status %d" % int(model.status.item()))
+    model.check()
     return [text[i, lens[i]:ends[i]].tolist() for i in range(S)], logprob.cpu().numpy()
 
 

@@ -18,3 +18,18 @@ def test_prompts_are_checked_before_the_device_sees_them():
             Q.write_trees(model, prompts)
     trees, logprob = Q.write_trees(model, [])
     assert trees == [] and logprob.shape == (0,)
+
+
+@pytest.mark.gpu
+def test_a_call_that_failed_does_not_end_the_model():
+    need_gpu()
+    announce("sequence example, status of an earlier call")
+    model = Q.SequenceModel(50, width=64, rows=3)
+    prompts = [[3, 4], [5], [6, 7, 8]]
+    trees, logprob = Q.write_trees(model, prompts, most=9, opening=3.0)
+    # a step of a row that the pools do not have: the recurrences report it
+    model.step(torch.tensor([1], dtype=torch.int32, device="cuda"), torch.tensor([7], dtype=torch.int32, device="cuda"))
+    with pytest.raises(RuntimeError, match="device status %d" % C.CORTEX_ST_INPUT_RANGE):
+        Q.write_trees(model, prompts, most=9, opening=3.0)
+    again, logprob2 = Q.write_trees(model, prompts, most=9, opening=3.0)
+    assert again == trees and np.array_equal(logprob, logprob2)
