@@ -198,21 +198,19 @@ def tree_arrays(trees):
     """Prefix texts as the arrays of a batch: children [N * 2] and the word of every node, -1 inside."""
     children, words = [], []
     for text in trees:
-        pos = 0
-
-        def read() -> int:
-            nonlocal pos
-            v, t = len(words), text[pos]
-            pos += 1
+        open_slots = [None]                     # (node, slot) that the coming subtrees fill, the next one last
+        for pos, t in enumerate(text):
+            if not open_slots:
+                raise ValueError("%d tokens after the tree" % (len(text) - pos))
+            v, slot = len(words), open_slots.pop()
+            if slot is not None:
+                children[slot[0]][slot[1]] = v
             words.append(-1 if t == NODE else t)
             children.append([-1, -1])
             if t == NODE:
-                children[v] = [read(), read()]
-            return v
-
-        read()
-        if pos != len(text):
-            raise ValueError("%d tokens after the tree" % (len(text) - pos))
+                open_slots += [(v, 1), (v, 0)]
+        if open_slots:
+            raise ValueError("a tree of %d tokens lacks %d subtrees" % (len(text), len(open_slots)))
     return np.array(children, dtype=np.int32).reshape(-1), np.array(words, dtype=np.int32)
 
 

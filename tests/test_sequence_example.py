@@ -20,6 +20,27 @@ def test_prompts_are_checked_before_the_device_sees_them():
     assert trees == [] and logprob.shape == (0,)
 
 
+@pytest.mark.parametrize("left", [False, True])
+def test_trees_deeper_than_the_interpreter_recurses(left):
+    """A comb of 20,000 inner nodes, leaning either way."""
+    n = 20000
+    text = [0] * n + [5] * (n + 1) if left else [0, 5] * n + [7]
+    children, words = Q.tree_arrays([text, [9]])
+    assert words.tolist() == [-1 if t == 0 else t for t in text] + [9]
+    children = children.reshape(-1, 2)
+    if left:
+        assert all(children[v].tolist() == [v + 1, 2 * n - v] for v in range(n))
+    else:
+        assert all(children[2 * v].tolist() == [2 * v + 1, 2 * v + 2] for v in range(n))
+    assert (children[words >= 0] == -1).all()
+
+
+def test_texts_that_are_no_tree():
+    for text, what in (([0, 5], "a tree of 2 tokens lacks 1 subtrees"), ([], "a tree of 0 tokens lacks 1"), ([5, 0, 5], "2 tokens after the tree")):
+        with pytest.raises(ValueError, match=what):
+            Q.tree_arrays([text])
+
+
 @pytest.mark.gpu
 def test_a_call_that_failed_does_not_end_the_model():
     need_gpu()
