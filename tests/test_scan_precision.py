@@ -207,3 +207,25 @@ def test_tokens_after_a_large_step(size, dtype):
         if dtype == "bf16":
             # the rounded reference itself: few outputs fall on the other side of a tie
             assert np.mean(got != bf16(ref)) <= 0.002
+
+
+# ---- 16-bit outputs are the rounded float32 ones ----
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", ["channel", "head"])
+@pytest.mark.parametrize("step", [False, True])
+def test_outputs_are_rounded_once(form, step):
+    """Float32 sums are off by some U of their terms' magnitudes, which are some sqrt(N) <= 11 of the sum: 1e-7 * 11 *
+    a few, or 4e-6 of an output; that is on the other side of a tie in 2 * 4e-6 / 2^-8 = 0.2 percent of them.  An operand
+    held to 16 bits, off by 2^-17 of its term, puts 1 to 2 percent there."""
+    need_gpu()
+    shapes = [(130, 16, 1, 0), (128, 64, 2, 0)] if form == "channel" else [(128, 16, 1, 32), (256, 64, 2, 64), (256, 128, 1, 128)]
+    for D, N, G, P in shapes:
+        for lens in ([[1] * 400] if step else [[70, 3, 0, 330], [5] * 1100]):
+            announce("rounded once: %s step %s D %d N %d, %d sequences" % (form, step, D, N, len(lens)))
+            p = Scan(7, lens, D, N, G, P, dtype="bf16")
+            d = p.upload()
+            C.check(p.call(step))
+            torch.cuda.synchronize()
+            assert int(d["status"].item()) == 0
+            assert np.mean(host(d["y"]) != bf16(p.reference()[0])) <= 0.003
