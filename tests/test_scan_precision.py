@@ -215,9 +215,9 @@ def test_tokens_after_a_large_step(size, dtype):
 @pytest.mark.parametrize("form", ["channel", "head"])
 @pytest.mark.parametrize("step", [False, True])
 def test_outputs_are_rounded_once(form, step):
-    """Float32 sums are off by some U of their terms' magnitudes, which are some sqrt(N) <= 11 of the sum: 1e-7 * 11 *
-    a few, or 4e-6 of an output; that is on the other side of a tie in 2 * 4e-6 / 2^-8 = 0.2 percent of them.  An operand
-    held to 16 bits, off by 2^-17 of its term, puts 1 to 2 percent there."""
+    """Float32 sums are off by half a U of their terms' magnitudes on average, and those are some sqrt(N) <= 11 of the
+    sum: some 5e-7 of an output, 1e-6 with the smaller ones among them.  That is on the other side of a rounding's tie in
+    2 * 1e-6 / 2^-8 = 0.05 percent of them.  Operands held to 16 bits put 0.1 to 0.25 percent there."""
     need_gpu()
     shapes = [(130, 16, 1, 0), (128, 64, 2, 0)] if form == "channel" else [(128, 16, 1, 32), (256, 64, 2, 64), (256, 128, 1, 128)]
     for D, N, G, P in shapes:
@@ -228,4 +228,4 @@ def test_outputs_are_rounded_once(form, step):
             C.check(p.call(step))
             torch.cuda.synchronize()
             assert int(d["status"].item()) == 0
-            assert np.mean(host(d["y"]) != bf16(p.reference()[0])) <= 0.003
+            assert np.mean(host(d["y"]) != bf16(p.reference()[0])) <= 0.0005
