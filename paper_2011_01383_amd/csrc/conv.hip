@@ -6,8 +6,9 @@
 // The bytes of x and y bound it: 2 W + 4 operations per element loaded and stored.
 // 8,192 tokens of 2,304 bf16 channels: 24 us, 3.2 TB/s of inputs and outputs (a
 // large copy runs at 4.8); 7 rows of single tokens: 3.7 us.  What is left is the
-// launch's ramp: every wave loads, then every wave stores (chunks of 8 to 16
-// tokens measure the same).
+// shape of the launch: a wave looks up its sequence and pool row, loads its rows
+// and weights, then stores, once, and all waves do so at the same time (chunks of
+// 8 to 16 tokens measure the same).
 #include "sequence.hpp"
 
 namespace cortex {

@@ -79,8 +79,8 @@ __global__ void __launch_bounds__(256) enter_kernel(cortex_scan_t a, int32_t *st
 // the next kAhead tokens (of B and C: the next tile) need is loaded while these
 // are worked on.
 //
-// 32,768 tokens of 2,048 channels and 16 states, split: 269 us (part 1) + 18 (the
-// states between) + 310 (part 2), traced.  That is 263 and 303 ns of a SIMD a token
+// 32,768 tokens of 2,048 channels and 16 states, split: 266 us (part 1) + 19 (the
+// states between) + 309 (part 2), traced.  That is 260 and 302 ns of a SIMD a token
 // and wave, for 100 and 138 vector instructions: about 218 and 292 ns at 1.9 ns each
 // and 3.5 for an exponential, as four waves a SIMD of nothing else take for them.
 // ---------------------------------------------------------------------------
@@ -310,8 +310,10 @@ __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(cortex_scan_t a
 // prompt among them would then cost ten times a split.  Up to 36 tokens three
 // launches cost more than any chain (32 tokens: 20 and 17, 48: 20 and 24; N = 64: 44 and
 // 44, 44 and 64).  Segments are as long as leaves four waves a SIMD (8,192 tokens of 16
-// sequences and 2,048 channels, 32 tokens: 160; 128: 202); below half a wave a
-// SIMD they go down to 16 (257 tokens of 512 channels, 24 tokens: 27; 32: 33; 64: 55).
+// sequences and 2,048 channels, 64 tokens: 158 equal, 169 ramp; 128: 200; 32: 143, 150, but
+// with twice the states between the passes; one sequence of 32,768 tokens, 256: 537; 512: 746;
+// 128: 497); below half a wave a SIMD they go down to 16 (257 tokens of 512 float32
+// channels, 16 tokens: 22; 24: 27; 32: 32; 64: 56).
 //
 // Per head.  A unit is 64 channels of a head in one sequence.  In one launch the
 // longest sequence is a chain of sub-chunks at 1.6 to 2.4 us (float32 3.3 to 5.2).  8,192
@@ -325,8 +327,8 @@ __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(cortex_scan_t a
 // sequences, half of the tokens in one: 512: 43 and 25, 1,024: 47 and 45; float32, 16 units:
 // 128: 20 and 18, 192: 21 and 25.  The workgroups that the GPU holds at once (three a CU at
 // N = 128, four below) get a segment each, of at least 64 tokens: 32,768 tokens of 64 heads,
-// 2,752 tokens: 519; 1,024: 530; 256: 660; 4,099 float32 tokens of 16 heads, 96 tokens: 48;
-// 64: 56; 256: 69.
+// 2,752 tokens: 561; 1,024: 575; 256: 669; 4,099 float32 tokens of 16 heads, 96 tokens: 49;
+// 64: 56; 256: 70.
 constexpr int64_t kWholeUnits = 400, kWholeWaves = 1024;   // from these on one launch
 static int segment_tokens(int64_t T, int64_t S, int64_t D, int N, int head_dim) {
   int64_t Q;

@@ -33,12 +33,13 @@
 // and their sums are made a sub-chunk ahead by one wave, beside the others'
 // products.  y goes through LDS, so that z is read and y stored in whole rows.
 //
-// 32,768 tokens of 64 heads of 64 channels, N = 128, in segments of 2,752: 177 us
-// (part 1) + 15 + 405 (part 2, 2.0 TB/s of x, z and y), traced; 500 to 518 as a
-// program calls it.  Nothing alone bounds it:
-// without its loads and stores, or without its products, it takes three quarters
-// of the time; the vector unit (plane splits, gates) is busy half of it, the
-// matrix unit a fifth, LDS more than a third.  12 waves a CU is what its registers allow.
+// 32,768 tokens of 64 heads of 64 channels, N = 128, in segments of 2,752: 181 us
+// (part 1) + 15 + 447 (part 2, 1.8 TB/s of x, z and y), traced; 538 to 568 as a
+// program calls it, by the GPU.  Nothing alone bounds it: the vector unit (plane
+// splits, gates: 516 instructions a wave and sub-chunk of part 2, products
+// included) is busy half of the time, the matrix unit a fifth, LDS a third; the form
+// with two planes took three quarters of its time without its loads and stores, or
+// without its products.  12 waves a CU is what its registers allow.
 #pragma once
 
 #include "sequence.hpp"

@@ -6,10 +6,11 @@
 // for both operands, so four neighbouring values of a row, or of a result
 // (rows 4 (lane >> 4) + 0..3), are the operands of the four steps as they
 // stand: the state goes from accumulators into the output's products without
-// moving.  At 64 operations a cycle and SIMD these units bound it (three bf16
-// planes a value, six products at a sixteenth of the time each, would want every
-// value that is read split).  4,099 tokens of 16 heads of 64 channels, N = 64, in
-// segments of 96: 15 + 9 + 28 us.
+// moving.  (Three bf16 planes a value, six products at a sixteenth of the time
+// each, would want every value that is read split.)  4,099 tokens of 16 heads of 64
+// channels, N = 64, in segments of 96: 15 + 10 + 29 us.  What bounds it there is the
+// latency of three sub-chunks one after another: these units are busy a third of
+// the time.
 #pragma once
 
 #include "scan_head.hpp"
