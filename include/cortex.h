@@ -385,6 +385,9 @@ int cortex_conv_step(const cortex_conv_t *args, int32_t *d_status, void *stream)
  *   head_dim = P    per head of P consecutive channels: A [D/P], dt [T, D/P],
  *                   skip and dt_bias [D/P]; N = 16, 32, 64 or 128, P a multiple
  *                   of 16 up to 256 that divides D/G
+ * The prompt form multiplies the decays of many tokens at once.  Where states
+ * grow (dt A > 0) until such a product leaves the float range, it gives
+ * infinities or NaN even for a state of 0; decays of any size are fine.
  * Other sizes return CORTEX_E_INVAL, and so do states that do not start at a
  * 16-byte boundary, and prompts of 2^24 and more heads of all sequences together
  * (a head of more than 64 channels counts as several of 64).
