@@ -14,7 +14,7 @@
 // bf16 planes, eight bits each, which together are the value itself.  So every
 // product is exact, all sums are float32, and y is rounded once, as token by token.
 // (Two planes, 16 bits, would do for y's own rounding, but a y that is a small
-// difference of large terms would lose it: 1e-4 of y instead of 2e-5 off the
+// difference of large terms would lose it: 1e-4 of y instead of 2e-5 to 4e-5 off the
 // float32 order.)  An infinite or NaN x or state makes its channel NaN from its
 // token on (the token-by-token order might keep an infinity).
 //
