@@ -467,7 +467,7 @@ static int check_scan(const cortex_scan_t *a, bool step, int32_t *status) {
   const int64_t dts = a->head_dim ? a->channels / a->head_dim : a->channels;
   const int64_t bc = (int64_t)a->groups * a->state_size;
   const int64_t most = kMaxRowStride;
-  if (a->x_ld > most || a->z_ld > most || a->y_ld > most || a->dt_ld > most || a->B_ld > most || a->C_ld > most)
+  if (a->x_ld > most || (a->z && a->z_ld > most) || a->y_ld > most || a->dt_ld > most || a->B_ld > most || a->C_ld > most)
     return CORTEX_E_INVAL;
   if (a->x_ld < a->channels || a->y_ld < a->channels || a->dt_ld < dts || a->B_ld < bc || a->C_ld < bc ||
       (a->z && a->z_ld < a->channels))

@@ -1,4 +1,6 @@
 """The scan at the ends of its types' ranges and of its arguments'."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -29,3 +31,31 @@ def test_decays_that_leave_the_float_range(A, size, P, dtype):
         torch.cuda.synchronize()
         assert int(d["status"].item()) == 0
         p.check(d["y"], out, "A %g" % A)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("z_ld", [-1, 0, 1 << 40])
+def test_no_gate_has_no_stride(z_ld):
+    """z NULL: its stride is not looked at."""
+    need_gpu()
+    announce("no gate, z_ld %d" % z_ld)
+    p = Scan(3, [1, 1, 1], 64, 16, 1, 32, dtype="f32", z=False)
+    d = p.upload()
+    for step in (False, True):
+        C.check(p.call(step))
+        torch.cuda.synchronize()
+        want = d["y"].clone()
+        d["y"].fill_(float("nan"))
+        at = lambda t: None if t is None else t.data_ptr()
+        a = C.cortex_scan_t(dtype=C.CORTEX_F32, num_seqs=3, num_tokens=3, channels=64, head_dim=32, groups=1, state_size=16,
+                            softplus=1, state_rows=3, seq_offsets=at(d["offsets"]), x=at(d["x"]), dt=at(d["dt"]), B=at(d["B"]),
+                            C=at(d["C"]), x_ld=d["x"].stride(0), z_ld=z_ld, dt_ld=d["dt"].stride(0), B_ld=d["B"].stride(0),
+                            C_ld=d["C"].stride(0), A=at(d["A"]), skip=at(d["skip"]), dt_bias=at(d["dt_bias"]),
+                            state_in=at(d["state"]), y=at(d["y"]), y_ld=d["y"].stride(0))
+        lib, status = C.load(), at(d["status"])
+        if step:
+            C.check(lib.cortex_scan_step(ctypes.byref(a), status, None))
+        else:
+            C.check(lib.cortex_scan_forward(ctypes.byref(a), status, at(d["ws"]), d["ws"].numel(), None))
+        torch.cuda.synchronize()
+        assert int(d["status"].item()) == 0 and torch.equal(d["y"], want)
