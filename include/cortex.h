@@ -485,6 +485,149 @@ typedef struct {
 size_t cortex_logits_workspace_bytes(int32_t rows, int32_t vocab);
 int cortex_logits_process(const cortex_logits_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream);
 
+/*
+ * Gated delta rule.  Head h of key head g = h / (heads / key_heads) keeps a state
+ * S [V, K] and at every token
+ *   S <- exp(dt A) S                          dt = softplus(dt_raw + dt_bias) (softplus only if asked for)
+ *   u  = beta (v - S k)                       beta = 1 / (1 + exp(-b)) if asked for, else b
+ *   S <- S + u k^T
+ *   y  = scale S q
+ * K = 32, 64 or 128; V a multiple of 16 up to 256; any number of key heads that
+ * divides the heads; heads V at most 262,144.  A NULL leaves the decay out (dt and
+ * dt_bias are then not read).  Keys of norm at most 1 (cortex_qk_norm) and beta in
+ * [0, 1] keep states bounded; larger ones, and steps dt A > 0, may let them grow past
+ * the float range, where the prompt form may give infinities or NaN earlier than the
+ * token form.  After an infinite or NaN key, update share or step size a head's
+ * outputs and state are no longer finite, after an infinite or NaN value or state entry
+ * those of its row of the state; which of infinity and NaN they are is not said.  No
+ * earlier token is touched, in either form.  Other sizes return CORTEX_E_INVAL, and
+ * so do states that do not start at a 16-byte boundary.
+ */
+typedef struct {
+  int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: q, k, v, b, dt, y */
+  int32_t num_seqs;           /* S */
+  int32_t num_tokens;         /* T; step form: T = S */
+  int32_t heads;              /* H */
+  int32_t key_heads;          /* G, divides H */
+  int32_t key_dim;            /* K */
+  int32_t value_dim;          /* V */
+  int32_t softplus;
+  int32_t sigmoid;
+  int32_t state_rows;
+  float scale;
+  const int32_t *seq_offsets; /* [S+1] (not read by the step form) */
+  const int32_t *state_index; /* [S] or NULL */
+  const void *q;              /* [T, G, K]: row stride q_ld, heads K apart */
+  const void *k;              /* likewise */
+  const void *v;              /* [T, H, V]: row stride v_ld, heads V apart */
+  const void *b;              /* [T, H] */
+  const void *dt;             /* [T, H] */
+  int64_t q_ld, k_ld, v_ld, b_ld, dt_ld;
+  const float *A;             /* [H] or NULL: no decay */
+  const float *dt_bias;       /* [H] or NULL */
+  const float *state_in;      /* [state_rows, H V, K] float32, or NULL */
+  float *state_out;           /* likewise */
+  void *y;                    /* [T, H, V]: row stride y_ld, heads V apart */
+  int64_t y_ld;
+} cortex_delta_t;
+
+/* Workspace bytes of cortex_delta_forward for batches of up to num_tokens tokens in
+ * up to num_seqs sequences (0 if invalid); it need not be zeroed. */
+size_t cortex_delta_workspace_bytes(int32_t num_tokens, int32_t num_seqs, int32_t heads, int32_t key_dim,
+                                    int32_t value_dim);
+int cortex_delta_forward(const cortex_delta_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream);
+int cortex_delta_step(const cortex_delta_t *args, int32_t *d_status, void *stream);
+
+/*
+ * Norms of queries and keys, and their rotation by the token's position.  For
+ * every token and head, with x one head's P elements,
+ *   CORTEX_NORM_RMS   x <- x / sqrt(mean x^2 + eps)
+ *   CORTEX_NORM_L2    x <- x / sqrt(sum x^2 + eps)
+ *   CORTEX_NORM_NONE  x as it is
+ *   x <- x * weight                                           (if given)
+ *   (x[i], x[j]) <- (x[i] cos f - x[j] sin f, x[j] cos f + x[i] sin f)    f = position * freqs[i']
+ * for the R / 2 pairs of the first R elements: i' = i, j = i + R / 2, or neighbours
+ * (i = 2 i', j = 2 i' + 1).  Angles are formed in 64 bits.  All is float32 and
+ * rounded once.  Prompts and single tokens alike: rows are tokens.  P is even, at
+ * most 512; R is even, at most P, 0 for no rotation (positions and freqs are then not
+ * read).  Without keys key_heads is 0.  Outputs may be the inputs themselves.
+ */
+#define CORTEX_NORM_NONE 0
+#define CORTEX_NORM_RMS 1
+#define CORTEX_NORM_L2 2
+typedef struct {
+  int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: q, k and outputs */
+  int32_t num_tokens;         /* T */
+  int32_t heads;              /* H, of q */
+  int32_t key_heads;          /* G, of k, or 0 */
+  int32_t head_dim;           /* P */
+  int32_t rotary_dim;         /* R */
+  int32_t interleaved;        /* pairs: neighbours if non-zero, else halves */
+  int32_t norm;               /* CORTEX_NORM_* */
+  float eps;                  /* at least 0 */
+  const void *q;              /* [T, H, P]: row stride q_ld, heads P apart */
+  const void *k;              /* [T, G, P]: row stride k_ld */
+  int64_t q_ld, k_ld;
+  const float *q_weight;      /* [P] or NULL */
+  const float *k_weight;      /* [P] or NULL */
+  const int32_t *positions;   /* [T] */
+  const float *freqs;         /* [R / 2], radians a position */
+  void *q_out;                /* [T, H, P], row stride q_out_ld */
+  void *k_out;                /* [T, G, P], row stride k_out_ld */
+  int64_t q_out_ld, k_out_ld;
+} cortex_qk_norm_t;
+
+int cortex_qk_norm(const cortex_qk_norm_t *args, int32_t *d_status, void *stream);
+
+/*
+ * Rows to 8 bits: scale[r] = max |x[r]| / 127, q[r, c] = x[r, c] / scale[r] rounded to
+ * the nearest whole number (ties to even), each in float32; a row of zeros has a scale
+ * of 0 and zeros.  A row that holds an infinity or NaN gets a NaN scale and zeros.
+ */
+typedef struct {
+  int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: x */
+  int32_t rows;
+  int32_t columns;            /* at most 131,071 */
+  const void *x;              /* [rows, columns], row stride x_ld */
+  int64_t x_ld;
+  int8_t *q;                  /* [rows, columns], row stride q_ld */
+  int64_t q_ld;
+  float *scale;               /* [rows] */
+} cortex_quant_i8_t;
+
+int cortex_quant_i8(const cortex_quant_i8_t *args, int32_t *d_status, void *stream);
+
+/*
+ * Projection with weights in 8 bits, a scale per token and per channel:
+ *   y[t, n] = (sum_k xq[t, k] w[n, k]) * x_scale[t] * w_scale[n] + bias[n]
+ * Without x_scale, x is of dtype and brought to 8 bits as by cortex_quant_i8; with it,
+ * x holds the 8-bit rows themselves.  The sum is exact (at most 131,071 inputs); it is
+ * then rounded to float32, multiplied by the two scales in turn and added to the bias,
+ * each rounded on its own, and rounded to dtype.  Rows of w start at 16-byte
+ * boundaries and lie w_ld bytes apart, a multiple of 16; what their last 16 bytes hold
+ * past the inputs does not matter, but is read.
+ */
+typedef struct {
+  int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: y, and x without x_scale */
+  int32_t tokens;             /* T */
+  int32_t inputs;             /* K */
+  int32_t outputs;            /* N */
+  const void *x;              /* [T, K] of dtype, or int8 with x_scale; row stride x_ld in elements */
+  int64_t x_ld;
+  const float *x_scale;       /* [T] or NULL */
+  const int8_t *w;            /* [N, K], row stride w_ld */
+  int64_t w_ld;
+  const float *w_scale;       /* [N] */
+  const float *bias;          /* [N] or NULL */
+  void *y;                    /* [T, N], row stride y_ld */
+  int64_t y_ld;
+} cortex_linear_i8_t;
+
+/* Workspace bytes of cortex_linear_i8 for up to `tokens` rows (0 if invalid); it need
+ * not be zeroed. */
+size_t cortex_linear_i8_workspace_bytes(int32_t tokens, int32_t outputs, int32_t inputs);
+int cortex_linear_i8(const cortex_linear_i8_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream);
+
 /* ---- tuning and diagnostics ---------------------------------------------- */
 
 /*

@@ -105,3 +105,64 @@ def logits(v, history=None, history_len=None, prompt_len=None, repetition=None, 
         return v, token, np.inf
     w = v.astype(np.float64)
     return v, token, float(top + np.log(np.exp(w - top).sum()))
+
+
+def delta(q, k, v, b, offsets, dt=None, A=None, dt_bias=None, soft=True, sig=True, scale=1.0, index=None, state=None):
+    """The gated delta rule: y [T, H, V], its magnitude, {pool row: (new state [H V, K], its magnitude [H V, 1])}.
+
+    With |k| <= 1 and beta in [0, 1] a token's map of a state row shrinks (2-norm), so a row's error is at
+    most a times what it was, plus what the token's own roundings add: those are parts of a |S| and of
+    beta (|v| + a |S|).  The magnitude is that sum."""
+    T, H, V = v.shape
+    G, K = k.shape[1:]
+    of = np.arange(H) // (H // G)
+    raw = None if A is None else dt + (0 if dt_bias is None else dt_bias)
+    a = np.ones((T, H)) if A is None else np.exp((softplus(raw) if soft else raw) * A)
+    beta = 1.0 / (1.0 + np.exp(-b)) if sig else b
+    y, mag, new = np.zeros((T, H, V)), np.zeros((T, H, V)), {}
+    for _, i, j, row in rows_of(offsets, index):
+        S = np.zeros((H, V, K)) if row < 0 or state is None else state[row].reshape(H, V, K).copy()
+        m = np.sqrt((S * S).sum(-1))
+        for t in range(i, j):
+            kt, qt = k[t][of], q[t][of]
+            S = S * a[t][:, None, None]
+            old = np.sqrt((S * S).sum(-1))
+            u = beta[t][:, None] * (v[t] - (S * kt[:, None]).sum(-1))
+            S = S + u[..., None] * kt[:, None]
+            m = a[t][:, None] * m + old + np.abs(beta[t])[:, None] * (np.abs(v[t]) + old)
+            y[t] = scale * (S * qt[:, None]).sum(-1)
+            mag[t] = abs(scale) * m * np.sqrt((qt * qt).sum(-1))[:, None]
+        if row >= 0:
+            new[row] = (S.reshape(H * V, K), m.reshape(H * V, 1))
+    return y, mag, new
+
+
+def qk_norm(x, norm, eps, weight=None, positions=None, freqs=None, interleaved=False):
+    """x [T, H, P] normed per head, weighted and rotated; and the sum of the magnitudes behind every output."""
+    P = x.shape[-1]
+    size = 1.0 if norm == "none" else np.sqrt((x * x).sum(-1, keepdims=True) / (P if norm == "rms" else 1) + eps)
+    v = x / size * (1.0 if weight is None else weight)
+    mag = np.abs(v)
+    if freqs is None or len(freqs) == 0:
+        return v, mag
+    R = 2 * len(freqs)
+    f = positions.astype(np.float64)[:, None, None] * freqs
+    i = np.arange(R // 2) * 2 if interleaved else np.arange(R // 2)
+    j = i + 1 if interleaved else i + R // 2
+    out, m = v.copy(), mag.copy()
+    out[..., i] = v[..., i] * np.cos(f) - v[..., j] * np.sin(f)
+    out[..., j] = v[..., j] * np.cos(f) + v[..., i] * np.sin(f)
+    m[..., i] = m[..., j] = mag[..., i] + mag[..., j]
+    return out, m
+
+
+def quant_rows(x):
+    """8-bit rows and their scales, by the float32 roundings that define them (x float32)."""
+    x = x.astype(np.float32)
+    bad = ~np.isfinite(x).all(1)
+    with np.errstate(invalid="ignore", divide="ignore", over="ignore"):
+        scale = np.abs(x).max(1) / np.float32(127)
+        q = np.clip(np.rint(x / scale[:, None]), -127, 127)
+    q[(scale == 0) | bad] = 0
+    scale[bad] = np.nan
+    return q.astype(np.int8), scale

@@ -31,7 +31,7 @@ HIPCC_FLAGS = [
     "-Wno-unused-command-line-argument",
 ]
 SOURCES = ["abi.hip", "linearize.hip", "forward.hip", "probe.hip", "noalloc.hip", "conv.hip", "scan.hip",
-           "logits.hip"]
+           "logits.hip", "delta.hip", "qk_norm.hip", "linear_i8.hip"]
 # packed two-lane fp32 arithmetic, which this library must not contain
 PACKED_FP32 = ("v_pk_add_f32", "v_pk_mul_f32", "v_pk_fma_f32")
 LLVM_BIN = "/opt/rocm/llvm/bin"

@@ -37,6 +37,10 @@ CORTEX_ST_SEQ_OFFSETS = 7
 CORTEX_F32 = 0
 CORTEX_BF16 = 1
 
+CORTEX_NORM_NONE = 0
+CORTEX_NORM_RMS = 1
+CORTEX_NORM_L2 = 2
+
 CORTEX_TREE_RNN = 0
 CORTEX_NARY_TREELSTM = 1
 CORTEX_CHILDSUM_TREELSTM = 2
@@ -68,6 +72,8 @@ EXPORTED = [
     "cortex_probe_levels_workspace_bytes", "cortex_probe_levels",
     "cortex_conv_forward", "cortex_conv_step", "cortex_scan_workspace_bytes", "cortex_scan_forward",
     "cortex_scan_step", "cortex_logits_workspace_bytes", "cortex_logits_process",
+    "cortex_delta_workspace_bytes", "cortex_delta_forward", "cortex_delta_step", "cortex_qk_norm",
+    "cortex_quant_i8", "cortex_linear_i8_workspace_bytes", "cortex_linear_i8",
 ]
 
 
@@ -84,15 +90,15 @@ class cortex_weights_t(ctypes.Structure):
 
 
 def _fields(text: str):
-    """(name, ctype) pairs from "i name ..." groups: i int32, l int64, p pointer."""
-    kinds = {"i": ctypes.c_int32, "l": ctypes.c_int64, "p": ctypes.c_void_p}
+    """(name, ctype) pairs from "i name ..." groups: i int32, f float, l int64, p pointer."""
+    kinds = {"i": ctypes.c_int32, "f": ctypes.c_float, "l": ctypes.c_int64, "p": ctypes.c_void_p}
     return [(n, kinds[group.split()[0]]) for group in text.split(";") for n in group.split()[1:]]
 
 
 def _packer(text: str, cls):
     """The structure's bytes from its members' values in order; a call then costs
     the host a third of what filling a ctypes structure does."""
-    kinds = {"i": "i", "l": "q", "p": "P"}
+    kinds = {"i": "i", "f": "f", "l": "q", "p": "P"}
     s = struct.Struct("@" + "".join(kinds[group.split()[0]] * len(group.split()[1:]) for group in text.split(";")))
     assert s.size == ctypes.sizeof(cls)
     return s.pack
@@ -106,6 +112,13 @@ _SCAN = ("i dtype num_seqs num_tokens channels head_dim groups state_size softpl
 _LOGITS = ("i dtype rows vocab history_cap num_biases mask_rows; p logits; l logits_ld; p history; l history_ld;"
            "p history_len prompt_len repetition frequency presence bias_offsets bias_tokens bias_values mask;"
            "l mask_ld; p mask_index out; l out_ld; p token lse")
+_DELTA = ("i dtype num_seqs num_tokens heads key_heads key_dim value_dim softplus sigmoid state_rows; f scale;"
+          "p seq_offsets state_index q k v b dt; l q_ld k_ld v_ld b_ld dt_ld;"
+          "p A dt_bias state_in state_out y; l y_ld")
+_QK_NORM = ("i dtype num_tokens heads key_heads head_dim rotary_dim interleaved norm; f eps; p q k; l q_ld k_ld;"
+            "p q_weight k_weight positions freqs q_out k_out; l q_out_ld k_out_ld")
+_QUANT = "i dtype rows columns; p x; l x_ld; p q; l q_ld; p scale"
+_LINEAR = "i dtype tokens inputs outputs; p x; l x_ld; p x_scale w; l w_ld; p w_scale bias y; l y_ld"
 
 
 class cortex_conv_t(ctypes.Structure):
@@ -120,9 +133,29 @@ class cortex_logits_t(ctypes.Structure):
     _fields_ = _fields(_LOGITS)
 
 
+class cortex_delta_t(ctypes.Structure):
+    _fields_ = _fields(_DELTA)
+
+
+class cortex_qk_norm_t(ctypes.Structure):
+    _fields_ = _fields(_QK_NORM)
+
+
+class cortex_quant_i8_t(ctypes.Structure):
+    _fields_ = _fields(_QUANT)
+
+
+class cortex_linear_i8_t(ctypes.Structure):
+    _fields_ = _fields(_LINEAR)
+
+
 _pack_conv = _packer(_CONV, cortex_conv_t)
 _pack_scan = _packer(_SCAN, cortex_scan_t)
 _pack_logits = _packer(_LOGITS, cortex_logits_t)
+_pack_delta = _packer(_DELTA, cortex_delta_t)
+_pack_qk_norm = _packer(_QK_NORM, cortex_qk_norm_t)
+_pack_quant = _packer(_QUANT, cortex_quant_i8_t)
+_pack_linear = _packer(_LINEAR, cortex_linear_i8_t)
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -190,6 +223,20 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.cortex_logits_workspace_bytes.restype = SZ
     lib.cortex_logits_process.argtypes = [P, P, P, SZ, P]
     lib.cortex_logits_process.restype = ctypes.c_int
+    lib.cortex_delta_workspace_bytes.argtypes = [I32, I32, I32, I32, I32]
+    lib.cortex_delta_workspace_bytes.restype = SZ
+    lib.cortex_delta_forward.argtypes = [P, P, P, SZ, P]
+    lib.cortex_delta_forward.restype = ctypes.c_int
+    lib.cortex_delta_step.argtypes = [P, P, P]
+    lib.cortex_delta_step.restype = ctypes.c_int
+    lib.cortex_qk_norm.argtypes = [P, P, P]
+    lib.cortex_qk_norm.restype = ctypes.c_int
+    lib.cortex_quant_i8.argtypes = [P, P, P]
+    lib.cortex_quant_i8.restype = ctypes.c_int
+    lib.cortex_linear_i8_workspace_bytes.argtypes = [I32, I32, I32]
+    lib.cortex_linear_i8_workspace_bytes.restype = SZ
+    lib.cortex_linear_i8.argtypes = [P, P, P, SZ, P]
+    lib.cortex_linear_i8.restype = ctypes.c_int
     lib.cortex_version.argtypes = []
     lib.cortex_version.restype = ctypes.c_char_p
     _lib = lib
@@ -675,6 +722,163 @@ def cortex_logits_process(logits: torch.Tensor, *, out=None, token=None, lse=Non
                         _at(out), out_ld, _at(token), _at(lse))
     return load().cortex_logits_process(args, status.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(),
                                         _stream(stream))
+
+
+def _on_current_device(names: str, *tensors) -> None:
+    """The launch goes to the current device, whose memory these have to be."""
+    _on_device(names, *tensors)
+    current = torch.cuda.current_device()
+    for name, t in zip(names.split(), tensors):
+        if t is not None and t.get_device() != current:
+            raise ValueError("%s must be on the current device (%d), got %d" % (name, current, t.get_device()))
+
+
+def _head_rows(t, name: str, dtype, T: int, like=None):
+    """A [T, heads, elements] tensor: heads, elements and its row stride."""
+    H, P, ld = _group_rows(t, name, dtype, T)
+    if like is not None and (H, P) != like:
+        raise ValueError("%s must be [%d, %d, %d], got %s" % (name, T, like[0], like[1], list(t.shape)))
+    return H, P, ld
+
+
+def _number(v, name: str) -> float:
+    if isinstance(v, torch.Tensor) or isinstance(v, str):
+        raise ValueError("%s must be a number, got %s" % (name, type(v).__name__))
+    return float(v)
+
+
+def _delta(step: bool, q, k, v, b, offsets, y, dt, A, dt_bias, softplus, sigmoid, scale, state_in, state_out, state_index,
+           status, ws, stream) -> int:
+    if not isinstance(v, torch.Tensor) or v.dim() != 3 or v.dtype not in _DTYPES:
+        raise ValueError("v must be a [T, H, V] torch.Tensor of torch.float32 or torch.bfloat16")
+    scale = _number(scale, "scale")
+    T, typ, f32, i32 = v.shape[0], v.dtype, torch.float32, torch.int32
+    H, V, v_ld = _head_rows(v, "v", typ, T)
+    G, K, q_ld = _head_rows(q, "q", typ, T)
+    _, _, k_ld = _head_rows(k, "k", typ, T, (G, K))
+    _, _, y_ld = _head_rows(y, "y", typ, T, (H, V))
+    b_ld = _rows(b, "b", typ, T, H)
+    if A is None:
+        if dt is not None or dt_bias is not None:
+            raise ValueError("A is required with dt and dt_bias")
+        dt_ld = 0
+    else:
+        dt_ld = _rows(dt, "dt", typ, T, H)
+    if step:
+        S = T
+        specs = []
+    else:
+        if not isinstance(offsets, torch.Tensor) or offsets.numel() < 1:
+            raise ValueError("offsets must be a torch.Tensor of S + 1 elements")
+        S = offsets.numel() - 1
+        specs = [(offsets, "offsets", i32, S + 1, False), (ws, "ws", None, 1, False)]
+    rows, state = _state_specs(state_in, state_out, state_index, S, f32, (H * V, K))
+    _need_all(specs + state + [(A, "A", f32, H, True), (dt_bias, "dt_bias", f32, H, True), (status, "status", i32, 1, False)])
+    _on_current_device("q k v b dt y offsets ws A dt_bias state_in state_out state_index status", q, k, v, b, dt, y, offsets, ws,
+                       A, dt_bias, state_in, state_out, state_index, status)
+    args = _pack_delta(_DTYPES[typ], S, T, H, G, K, V, 1 if softplus else 0, 1 if sigmoid else 0, rows,
+                       scale, _at(offsets), _at(state_index), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                       b.data_ptr(), _at(dt), q_ld, k_ld, v_ld, b_ld, dt_ld, _at(A), _at(dt_bias), _at(state_in),
+                       _at(state_out), y.data_ptr(), y_ld)
+    lib = load()
+    if step:
+        return lib.cortex_delta_step(args, status.data_ptr(), _stream(stream))
+    return lib.cortex_delta_forward(args, status.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream))
+
+
+def cortex_delta_workspace_bytes(T: int, S: int, H: int, K: int, V: int) -> int:
+    return load().cortex_delta_workspace_bytes(T, S, H, K, V)
+
+
+def cortex_delta_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, b: torch.Tensor, offsets: torch.Tensor,
+                         y: torch.Tensor, *, dt=None, A=None, dt_bias=None, softplus: bool = True, sigmoid: bool = True,
+                         scale: float = 1.0, state_in=None, state_out=None, state_index=None,
+                         status: torch.Tensor = None, ws: torch.Tensor = None, stream=None) -> int:
+    """q, k [T, key heads, K]; v, y [T, H, V]; b, dt [T, H]; A, dt_bias [H]; states [rows, H V, K]."""
+    return _delta(False, q, k, v, b, offsets, y, dt, A, dt_bias, softplus, sigmoid, scale, state_in, state_out, state_index,
+                  status, ws, stream)
+
+
+def cortex_delta_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, b: torch.Tensor, y: torch.Tensor, *, dt=None,
+                      A=None, dt_bias=None, softplus: bool = True, sigmoid: bool = True, scale: float = 1.0, state_in=None,
+                      state_out=None, state_index=None, status: torch.Tensor = None, stream=None) -> int:
+    """One token of each of S sequences: q, k [S, key heads, K] and the others likewise."""
+    return _delta(True, q, k, v, b, None, y, dt, A, dt_bias, softplus, sigmoid, scale, state_in, state_out, state_index,
+                  status, None, stream)
+
+
+def cortex_qk_norm(q: torch.Tensor, q_out: torch.Tensor, *, k=None, k_out=None, norm: int = CORTEX_NORM_RMS,
+                   eps: float = 1e-6, q_weight=None, k_weight=None, positions=None, freqs=None, interleaved: bool = False,
+                   status: torch.Tensor = None, stream=None) -> int:
+    """q, q_out [T, H, P]; k, k_out [T, key heads, P]; weights [P]; positions [T]; freqs [R / 2]."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.dtype not in _DTYPES:
+        raise ValueError("q must be a [T, H, P] torch.Tensor of torch.float32 or torch.bfloat16")
+    eps = _number(eps, "eps")
+    T, typ, f32 = q.shape[0], q.dtype, torch.float32
+    H, P, q_ld = _head_rows(q, "q", typ, T)
+    _, _, qo_ld = _head_rows(q_out, "q_out", typ, T, (H, P))
+    G = k_ld = ko_ld = R = 0
+    if k is not None:
+        G, _, k_ld = _head_rows(k, "k", typ, T)
+        _head_rows(k, "k", typ, T, (G, P))
+        _, _, ko_ld = _head_rows(k_out, "k_out", typ, T, (G, P))
+    elif k_out is not None or k_weight is not None:
+        raise ValueError("k is required with k_out and k_weight")
+    if freqs is not None:
+        if not isinstance(freqs, torch.Tensor):
+            raise ValueError("freqs must be a torch.Tensor, got %s" % type(freqs).__name__)
+        R = 2 * freqs.numel()
+    elif positions is not None:
+        raise ValueError("freqs is required with positions")
+    _need_all([(q_weight, "q_weight", f32, P, True), (k_weight, "k_weight", f32, P, True),
+               (positions, "positions", torch.int32, T, freqs is None), (freqs, "freqs", f32, 0, True),
+               (status, "status", torch.int32, 1, False)])
+    _on_current_device("q q_out k k_out q_weight k_weight positions freqs status", q, q_out, k, k_out, q_weight, k_weight,
+                       positions, freqs, status)
+    args = _pack_qk_norm(_DTYPES[typ], T, H, G, P, R, 1 if interleaved else 0, norm, eps, q.data_ptr(), _at(k),
+                         q_ld, k_ld, _at(q_weight), _at(k_weight), _at(positions), _at(freqs), q_out.data_ptr(), _at(k_out),
+                         qo_ld, ko_ld)
+    return load().cortex_qk_norm(args, status.data_ptr(), _stream(stream))
+
+
+def cortex_quant_i8(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, *, status: torch.Tensor = None,
+                    stream=None) -> int:
+    """x [rows, columns] to q (int8) of the same shape and scale [rows]."""
+    rows, cols = _shape2(x, "x")
+    x_ld, q_ld = _rows(x, "x", x.dtype, rows, cols), _rows(q, "q", torch.int8, rows, cols)
+    _need_all([(scale, "scale", torch.float32, rows, False), (status, "status", torch.int32, 1, False)])
+    _on_current_device("x q scale status", x, q, scale, status)
+    args = _pack_quant(_DTYPES[x.dtype], rows, cols, x.data_ptr(), x_ld, q.data_ptr(), q_ld, scale.data_ptr())
+    return load().cortex_quant_i8(args, status.data_ptr(), _stream(stream))
+
+
+def cortex_linear_i8_workspace_bytes(T: int, N: int, K: int) -> int:
+    return load().cortex_linear_i8_workspace_bytes(T, N, K)
+
+
+def cortex_linear_i8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, y: torch.Tensor, *, x_scale=None, bias=None,
+                     status: torch.Tensor = None, ws: torch.Tensor = None, stream=None) -> int:
+    """x [T, K] of y's type, or int8 with x_scale [T]; w [N, K] int8 in rows that start at
+    16-byte boundaries; w_scale, bias [N]; y [T, N]."""
+    T, N = _shape2(y, "y")
+    f32, i8 = torch.float32, torch.int8
+    if not isinstance(w, torch.Tensor) or w.dim() != 2:
+        raise ValueError("w must be a 2-dimensional torch.Tensor")
+    K = w.shape[1]
+    w_ld = _rows(w, "w", i8, N, K)
+    if N == 1:                         # its stride is never used
+        w_ld = (K + 15) // 16 * 16
+    x_ld, y_ld = _rows(x, "x", y.dtype if x_scale is None else i8, T, K), _rows(y, "y", y.dtype, T, N)
+    if w_ld % 16 or w.data_ptr() % 16:
+        raise ValueError("w must have rows that start at 16-byte boundaries")
+    if N > 0 and w.storage_offset() + (N - 1) * w_ld + (K + 15) // 16 * 16 > w.untyped_storage().nbytes():
+        raise ValueError("w must hold whole pieces of 16 bytes, its last row too")
+    _need_all([(w_scale, "w_scale", f32, N, False), (x_scale, "x_scale", f32, T, True), (bias, "bias", f32, N, True),
+               (status, "status", torch.int32, 1, False), (ws, "ws", None, 1, False)])
+    _on_current_device("x w w_scale y x_scale bias status ws", x, w, w_scale, y, x_scale, bias, status, ws)
+    args = _pack_linear(_DTYPES[y.dtype], T, K, N, x.data_ptr(), x_ld, _at(x_scale), w.data_ptr(), w_ld, w_scale.data_ptr(),
+                        _at(bias), y.data_ptr(), y_ld)
+    return load().cortex_linear_i8(args, status.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream))
 
 
 def cortex_version() -> str:

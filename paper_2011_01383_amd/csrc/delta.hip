@@ -1,0 +1,196 @@
+// The gated delta rule, for prompts and for single tokens.
+//
+//   S <- a S,  u = beta (v - S k),  S <- S + u k^T,  y = scale S q
+//
+// Rows of a head's state (one per value channel) share nothing but k, q, a and
+// beta.  Eight lanes hold a row, four entries of each 32 a lane, so that a row's
+// loads and stores are whole 128-byte pieces; a wave holds sixteen rows.
+#include "sequence.hpp"
+
+namespace cortex {
+
+constexpr int kDeltaWaves = 4;           // tiles of 16 rows in a workgroup, of neighbouring number
+constexpr int kDeltaTile = 16;
+
+// Sum over the eight lanes that share a row.
+__device__ __forceinline__ float row_sum(float v) {
+  v += shifted<0xb1>(v, 0.0f);           // quad_perm: the neighbour
+  v += shifted<0x4e>(v, 0.0f);           // the other pair of four
+  v += shifted<0x141>(v, 0.0f);          // the other four of eight
+  return v;
+}
+
+__device__ __forceinline__ float sigmoid(float v) {
+  return __builtin_amdgcn_rcpf(1.0f + fast_exp2(v * -kLog2e));
+}
+
+// The decay of a token's state and its share of the update.
+struct DeltaGate {
+  float a, beta;
+  __device__ __forceinline__ DeltaGate(const cortex_delta_t &p, float dt, float b, float A2, float bias) {
+    a = 1.0f;
+    if (p.A) {
+      const float v = dt + bias;
+      a = fast_exp2((p.softplus ? softplus(v) : v) * A2);
+    }
+    beta = p.sigmoid ? sigmoid(b) : b;
+  }
+};
+
+// Four consecutive elements.
+template <typename T, bool WIDE> __device__ __forceinline__ void load4(const T *p, float (&v)[4]) {
+  if constexpr (WIDE) Pack<T, 4>::load(p, v);
+  else
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = to_float<T>(p[i]);
+}
+
+template <typename T, int K, bool STEP, bool WIDE>
+__global__ void __launch_bounds__(64 * kDeltaWaves) delta_walk_kernel(cortex_delta_t p, int32_t *status, int64_t units) {
+  constexpr int C = K / 32;
+  if (entry_status(status) != 0) return;
+  const int lane = (int)threadIdx.x & 63, part = lane & 7, row8 = lane >> 3;
+  const int64_t unit = (int64_t)blockIdx.x * kDeltaWaves + (threadIdx.x >> 6);
+  if (unit >= units) return;
+  const int V = p.value_dim, tiles = V / kDeltaTile, per = p.heads * tiles;
+  const int seq = (int)(unit / per), rest = (int)(unit % per), head = rest / tiles;
+  const int v0 = rest % tiles * kDeltaTile + row8, g = head / (p.heads / p.key_heads);
+  int begin = seq, end = seq + 1;
+  if constexpr (!STEP) {
+    if (rest == 0) check_offsets(p.seq_offsets, p.num_seqs, p.num_tokens, seq, status);
+    begin = p.seq_offsets[seq];
+    end = p.seq_offsets[seq + 1];
+    if (begin < 0 || end < begin || end > p.num_tokens) return;
+  }
+  int pool = -1;
+  if (p.state_in || p.state_out) {
+    pool = state_row(p.state_index, seq, p.state_rows, status);
+    if (pool < -1) return;
+  }
+  const int64_t at = (((int64_t)pool * p.heads + head) * V + v0) * K + part * 4;
+  typedef float vec __attribute__((ext_vector_type(4)));
+  vec h[2][C];
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      h[r][c] = p.state_in && pool >= 0 ? *(const vec *)(p.state_in + at + r * 8 * K + c * 32) : vec{0.0f, 0.0f, 0.0f, 0.0f};
+  const float A2 = p.A ? decay_rate(p.A[head]) : 0.0f, bias = p.A && p.dt_bias ? p.dt_bias[head] : 0.0f;
+  const T *qs = (const T *)p.q + g * K + part * 4, *ks = (const T *)p.k + g * K + part * 4;
+  const T *vs = (const T *)p.v + (int64_t)head * V + v0, *bs = (const T *)p.b + head, *ds = (const T *)p.dt + head;
+  T *ys = (T *)p.y + (int64_t)head * V + v0;
+#pragma unroll 1
+  for (int64_t t = begin; t < end; ++t) {
+    float q[C][4], k[C][4], v[2];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      load4<T, WIDE>(qs + t * p.q_ld + c * 32, q[c]);
+      load4<T, WIDE>(ks + t * p.k_ld + c * 32, k[c]);
+    }
+    v[0] = to_float<T>(vs[t * p.v_ld]);
+    v[1] = to_float<T>(vs[t * p.v_ld + 8]);
+    const DeltaGate gate(p, p.A ? to_float<T>(ds[t * p.dt_ld]) : 0.0f, to_float<T>(bs[t * p.b_ld]), A2, bias);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      float dot = 0.0f;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          h[r][c][i] *= gate.a;
+          dot = __builtin_fmaf(h[r][c][i], k[c][i], dot);
+        }
+      const float u = gate.beta * (v[r] - row_sum(dot));
+      float y = 0.0f;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          h[r][c][i] = __builtin_fmaf(u, k[c][i], h[r][c][i]);
+          y = __builtin_fmaf(h[r][c][i], q[c][i], y);
+        }
+      y = row_sum(y) * p.scale;
+      if (part == 0) ys[t * p.y_ld + r * 8] = from_float<T>(y);
+    }
+  }
+  if (p.state_out && pool >= 0)
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int c = 0; c < C; ++c) *(vec *)(p.state_out + at + r * 8 * K + c * 32) = h[r][c];
+}
+
+static bool launched() { return hipGetLastError() == hipSuccess; }
+
+template <typename T, int K, bool STEP> int launch_walk(const cortex_delta_t &a, int32_t *status, void *stream) {
+  const int64_t units = (int64_t)a.num_seqs * a.heads * (a.value_dim / kDeltaTile);
+  const unsigned grid = (unsigned)((units + kDeltaWaves - 1) / kDeltaWaves);
+  constexpr uintptr_t mask = 4 * sizeof(T) - 1;
+  const bool wide = a.q_ld % 4 == 0 && a.k_ld % 4 == 0 && ((uintptr_t)a.q & mask) == 0 && ((uintptr_t)a.k & mask) == 0;
+  if (wide) delta_walk_kernel<T, K, STEP, true><<<grid, 64 * kDeltaWaves, 0, (hipStream_t)stream>>>(a, status, units);
+  else delta_walk_kernel<T, K, STEP, false><<<grid, 64 * kDeltaWaves, 0, (hipStream_t)stream>>>(a, status, units);
+  return launched() ? CORTEX_OK : CORTEX_E_HIP;
+}
+
+template <typename T, bool STEP> int launch_delta(const cortex_delta_t &a, int32_t *status, void *stream) {
+  switch (a.key_dim) {
+    case 32: return launch_walk<T, 32, STEP>(a, status, stream);
+    case 64: return launch_walk<T, 64, STEP>(a, status, stream);
+    default: return launch_walk<T, 128, STEP>(a, status, stream);
+  }
+}
+
+static bool bad_delta_size(int32_t heads, int32_t key_heads, int32_t K, int32_t V) {
+  if (heads < 1 || key_heads < 1 || heads % key_heads) return true;
+  if (V < 16 || V > 256 || V % 16 || (int64_t)heads * V > kMaxChannels) return true;
+  return K != 32 && K != 64 && K != 128;
+}
+
+static int check_delta(const cortex_delta_t *a, bool step, int32_t *status) {
+  if (!a || !status) return CORTEX_E_INVAL;
+  if (bad_delta_size(a->heads, a->key_heads, a->key_dim, a->value_dim)) return CORTEX_E_INVAL;
+  if (bad_batch(a->dtype, a->num_seqs, a->num_tokens, a->heads * a->value_dim, a->state_rows, a->state_index,
+                a->state_in || a->state_out))
+    return CORTEX_E_INVAL;
+  if (step ? a->num_tokens != a->num_seqs : !a->seq_offsets) return CORTEX_E_INVAL;
+  const int64_t qk = (int64_t)a->key_heads * a->key_dim, vy = (int64_t)a->heads * a->value_dim;
+  if (a->q_ld < qk || a->k_ld < qk || a->v_ld < vy || a->y_ld < vy || a->b_ld < a->heads || (a->A && a->dt_ld < a->heads))
+    return CORTEX_E_INVAL;
+  if (a->q_ld > kMaxRowStride || a->k_ld > kMaxRowStride || a->v_ld > kMaxRowStride || a->y_ld > kMaxRowStride ||
+      a->b_ld > kMaxRowStride || (a->A && a->dt_ld > kMaxRowStride))
+    return CORTEX_E_INVAL;
+  if (!aligned16(a->state_in) || !aligned16(a->state_out)) return CORTEX_E_INVAL;
+  if (a->num_tokens > 0 && (!a->q || !a->k || !a->v || !a->b || !a->y || (a->A && !a->dt))) return CORTEX_E_INVAL;
+  if (a->num_seqs == 0 && a->num_tokens != 0) return CORTEX_E_INVAL;
+  // A unit is a wave, four of them a workgroup, and a grid has less than 2^32 threads.
+  if ((int64_t)a->num_seqs * a->heads * (a->value_dim / kDeltaTile) >= (int64_t)1 << 25) return CORTEX_E_INVAL;
+  return CORTEX_OK;
+}
+
+}  // namespace cortex
+
+using namespace cortex;
+
+extern "C" size_t cortex_delta_workspace_bytes(int32_t num_tokens, int32_t num_seqs, int32_t heads, int32_t key_dim,
+                                               int32_t value_dim) {
+  if (num_tokens < 0 || num_seqs < 0 || bad_delta_size(heads, 1, key_dim, value_dim)) return 0;
+  return 16;
+}
+
+extern "C" int cortex_delta_forward(const cortex_delta_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream) {
+  const int rc = check_delta(args, false, d_status);
+  if (rc != CORTEX_OK) return rc;
+  if (args->num_seqs == 0) return CORTEX_OK;
+  if (!d_ws || !aligned16(d_ws)) return CORTEX_E_INVAL;
+  if (ws_bytes < 16) return CORTEX_E_WORKSPACE;
+  return args->dtype == CORTEX_BF16 ? launch_delta<bf16_t, false>(*args, d_status, stream)
+                                    : launch_delta<float, false>(*args, d_status, stream);
+}
+
+extern "C" int cortex_delta_step(const cortex_delta_t *args, int32_t *d_status, void *stream) {
+  const int rc = check_delta(args, true, d_status);
+  if (rc != CORTEX_OK) return rc;
+  if (args->num_seqs == 0) return CORTEX_OK;
+  return args->dtype == CORTEX_BF16 ? launch_delta<bf16_t, true>(*args, d_status, stream)
+                                    : launch_delta<float, true>(*args, d_status, stream);
+}

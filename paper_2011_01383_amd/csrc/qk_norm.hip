@@ -1,0 +1,239 @@
+// Norms of queries and keys per head, their weights and their rotation, in one pass.
+//
+// Every element is read once and written once: the bytes bound it.  A rotation
+// pairs elements R / 2 apart or neighbours, so a lane takes two pieces of 16 bytes
+// whose pairs are all its own, and a head's lanes (a power of two of them, some
+// without work where the head is none) only have to add their squares.  A wave
+// takes heads of one token, 64 / lanes of them at a time, so that a token's cosines
+// and sines are made once by the wave, an angle a lane, and held in registers.
+#include "sequence.hpp"
+
+namespace cortex {
+
+constexpr int kNormWaves = 4;
+constexpr int kMaxHeadDim = 512;
+
+// cos and sin of position * freq, turned into turns and cut to half a turn in 64
+// bits: at position 2^31 the angle is off by 2^-22, at 200,000 by 2^-35.
+__device__ __forceinline__ void angle(int position, float freq, float &c, float &s) {
+  constexpr double kTurn = 0.15915494309189533577;
+  double turns = (double)position * (double)freq * kTurn;
+  turns -= __builtin_rint(turns);
+  sincospif(2.0f * (float)turns, &s, &c);
+}
+
+// Where a token's head begins, in q or in k.
+template <typename T> struct NormRow {
+  const T *in;
+  T *out;
+  const float *weight;
+};
+template <typename T> __device__ __forceinline__ NormRow<T> norm_row(const cortex_qk_norm_t &a, int64_t t, int r) {
+  const int P = a.head_dim;
+  if (r < a.heads)
+    return {(const T *)a.q + t * a.q_ld + (int64_t)r * P, (T *)a.q_out + t * a.q_out_ld + (int64_t)r * P, a.q_weight};
+  r -= a.heads;
+  return {(const T *)a.k + t * a.k_ld + (int64_t)r * P, (T *)a.k_out + t * a.k_out_ld + (int64_t)r * P, a.k_weight};
+}
+
+__device__ __forceinline__ float norm_scale(const cortex_qk_norm_t &a, float squares) {
+  if (a.norm == CORTEX_NORM_NONE) return 1.0f;
+  const float v = (a.norm == CORTEX_NORM_RMS ? squares / (float)a.head_dim : squares) + a.eps;
+  return 1.0f / __builtin_sqrtf(v);
+}
+
+// Sum over 2^k neighbouring lanes, the same in each.
+template <int LANES> __device__ __forceinline__ float lanes_sum(float v) {
+  if (LANES > 1) v += shifted<0xb1>(v, 0.0f);
+  if (LANES > 2) v += shifted<0x4e>(v, 0.0f);
+  if (LANES > 4) v += shifted<0x141>(v, 0.0f);
+  if (LANES > 8) v += shifted<0x140>(v, 0.0f);
+  if (LANES > 16) v += __shfl_xor(v, 16);
+  if (LANES > 32) v += __shfl_xor(v, 32);
+  return v;
+}
+
+// Rows at 16-byte boundaries; LANES lanes a head.  A wave takes the rows (a
+// token's heads, queries then keys) from `first` on, `rows` of them.
+template <typename T, int LANES>
+__global__ void __launch_bounds__(64 * kNormWaves) norm_wide_kernel(cortex_qk_norm_t a, int32_t *status, int splits) {
+  constexpr int V = 16 / (int)sizeof(T);
+  __shared__ float turn[kNormWaves][2][kMaxHeadDim / 2];
+  if (entry_status(status) != 0) return;
+  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+  const int64_t task = (int64_t)blockIdx.x * kNormWaves + wave;
+  const int64_t t = task / splits;
+  if (t >= a.num_tokens) return;
+  const int R = a.rotary_dim, P = a.head_dim, total = a.heads + a.key_heads;
+  const int part = lane % LANES, group = lane / LANES;
+  const bool works = part * 2 * V < P;
+  // the lane's two pieces
+  int lo = part * 2 * V, hi = lo + V;
+  if (!a.interleaved && lo < R) {
+    lo = part * V;
+    hi = R / 2 + lo;
+  }
+  if (!works) lo = hi = 0;
+  const bool turns = works && lo < R;            // halves: all of both pieces; neighbours: as far as R reaches
+  float c[V], s[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    c[i] = 1.0f;
+    s[i] = 0.0f;
+  }
+  if (R) {
+    const int position = a.positions[t];
+    for (int i = lane; i < R / 2; i += 64) angle(position, a.freqs[i], turn[wave][0][i], turn[wave][1][i]);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    if (turns)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int at = a.interleaved ? lo / 2 + i : lo + i;
+        if (at < R / 2) {
+          c[i] = turn[wave][0][at];
+          s[i] = turn[wave][1][at];
+        }
+      }
+  }
+  const int each = (total + splits - 1) / splits, first = (int)(task % splits) * each, last = min(first + each, total);
+  for (int r = first + group; r < last; r += 64 / LANES) {
+    const NormRow<T> row = norm_row<T>(a, t, r);
+    float x[2 * V];
+    {
+      float u[V], w[V];
+      Pack<T, V>::load(row.in + lo, u);
+      Pack<T, V>::load(row.in + hi, w);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        x[i] = u[i];
+        x[V + i] = w[i];
+      }
+    }
+    float squares = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) squares = __builtin_fmaf(x[i], x[i], squares);
+    const float m = norm_scale(a, lanes_sum<LANES>(works ? squares : 0.0f));
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) {
+      x[i] *= m;
+      if (row.weight) x[i] *= row.weight[(i < V ? lo : hi - V) + i];
+    }
+    float y[2][V];
+    if (a.interleaved) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        y[2 * i / V][2 * i % V] = x[2 * i] * c[i] - x[2 * i + 1] * s[i];
+        y[2 * i / V][2 * i % V + 1] = x[2 * i + 1] * c[i] + x[2 * i] * s[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        y[0][i] = x[i] * c[i] - x[V + i] * s[i];
+        y[1][i] = x[V + i] * c[i] + x[i] * s[i];
+      }
+    }
+    if (works) {
+      Pack<T, V>::store(row.out + lo, y[0]);
+      Pack<T, V>::store(row.out + hi, y[1]);
+    }
+  }
+}
+
+// Any alignment and any even sizes: a wave a head, pairs by lane.
+template <typename T>
+__global__ void __launch_bounds__(64 * kNormWaves) norm_pair_kernel(cortex_qk_norm_t a, int32_t *status) {
+  constexpr int N = kMaxHeadDim / 128;
+  if (entry_status(status) != 0) return;
+  const int lane = (int)threadIdx.x & 63;
+  const int total = a.heads + a.key_heads, R = a.rotary_dim, P = a.head_dim;
+  const int64_t task = (int64_t)blockIdx.x * kNormWaves + (threadIdx.x >> 6), t = task / total;
+  if (t >= a.num_tokens) return;
+  const NormRow<T> row = norm_row<T>(a, t, (int)(task % total));
+  float x[N], y[N], squares = 0.0f;
+  int at[N], to[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int pair = n * 64 + lane;
+    const bool halves = !a.interleaved && pair < R / 2;
+    at[n] = halves ? pair : 2 * pair;
+    to[n] = halves ? pair + R / 2 : 2 * pair + 1;
+    x[n] = y[n] = 0.0f;
+    if (pair < P / 2) {
+      x[n] = to_float<T>(row.in[at[n]]);
+      y[n] = to_float<T>(row.in[to[n]]);
+    }
+    squares = __builtin_fmaf(x[n], x[n], __builtin_fmaf(y[n], y[n], squares));
+  }
+  const float m = norm_scale(a, lanes_sum<64>(squares));
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int pair = n * 64 + lane;
+    if (pair >= P / 2) continue;
+    float u = x[n] * m, v = y[n] * m;
+    if (row.weight) {
+      u *= row.weight[at[n]];
+      v *= row.weight[to[n]];
+    }
+    float c = 1.0f, s = 0.0f;
+    if (pair < R / 2) angle(a.positions[t], a.freqs[pair], c, s);
+    row.out[at[n]] = from_float<T>(u * c - v * s);
+    row.out[to[n]] = from_float<T>(v * c + u * s);
+  }
+}
+
+template <typename T, int LANES> int launch_wide(const cortex_qk_norm_t &a, int32_t *status, int splits, void *stream) {
+  const int64_t tasks = (int64_t)a.num_tokens * splits;
+  norm_wide_kernel<T, LANES><<<(unsigned)((tasks + kNormWaves - 1) / kNormWaves), 64 * kNormWaves, 0, (hipStream_t)stream>>>(
+      a, status, splits);
+  return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+}
+
+template <typename T> int launch_norm(const cortex_qk_norm_t &a, int32_t *status, void *stream) {
+  constexpr int V = 16 / (int)sizeof(T);
+  auto rows16 = [](const void *p, int64_t ld) { return aligned16(p) && ld % V == 0; };
+  const bool wide = a.head_dim % (2 * V) == 0 && (a.interleaved || a.rotary_dim % (2 * V) == 0) && rows16(a.q, a.q_ld) &&
+                    rows16(a.q_out, a.q_out_ld) && (!a.key_heads || (rows16(a.k, a.k_ld) && rows16(a.k_out, a.k_out_ld)));
+  const int total = a.heads + a.key_heads;
+  if (!wide) {
+    const int64_t tasks = (int64_t)a.num_tokens * total;
+    norm_pair_kernel<T><<<(unsigned)((tasks + kNormWaves - 1) / kNormWaves), 64 * kNormWaves, 0, (hipStream_t)stream>>>(a, status);
+    return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+  }
+  int lanes = 1;
+  while (lanes * 2 * V < a.head_dim) lanes *= 2;
+  // A token's heads go to several waves while there are fewer than four a SIMD (1,024).
+  const int at_once = 64 / lanes, most = (total + at_once - 1) / at_once;
+  const int64_t want = (4096 + a.num_tokens - 1) / a.num_tokens;
+  const int splits = (int)(want < most ? want : most);
+  switch (lanes) {
+    case 1: return launch_wide<T, 1>(a, status, splits, stream);
+    case 2: return launch_wide<T, 2>(a, status, splits, stream);
+    case 4: return launch_wide<T, 4>(a, status, splits, stream);
+    case 8: return launch_wide<T, 8>(a, status, splits, stream);
+    case 16: return launch_wide<T, 16>(a, status, splits, stream);
+    case 32: return launch_wide<T, 32>(a, status, splits, stream);
+    default: return launch_wide<T, 64>(a, status, splits, stream);
+  }
+}
+
+}  // namespace cortex
+
+extern "C" int cortex_qk_norm(const cortex_qk_norm_t *a, int32_t *status, void *stream) {
+  using namespace cortex;
+  if (!a || !status) return CORTEX_E_INVAL;
+  if (a->dtype != CORTEX_F32 && a->dtype != CORTEX_BF16) return CORTEX_E_INVAL;
+  const int64_t P = a->head_dim;
+  if (a->num_tokens < 0 || a->heads < 1 || a->key_heads < 0 || a->heads > 65536 || a->key_heads > 65536) return CORTEX_E_INVAL;
+  if (P < 2 || P > kMaxHeadDim || P % 2 || a->rotary_dim < 0 || a->rotary_dim > P || a->rotary_dim % 2) return CORTEX_E_INVAL;
+  if (a->norm < CORTEX_NORM_NONE || a->norm > CORTEX_NORM_L2 || !(a->eps >= 0.0f)) return CORTEX_E_INVAL;
+  if (a->q_ld < a->heads * P || a->q_out_ld < a->heads * P) return CORTEX_E_INVAL;
+  if (a->key_heads && (a->k_ld < a->key_heads * P || a->k_out_ld < a->key_heads * P)) return CORTEX_E_INVAL;
+  // four waves a workgroup, at most a wave a token and head, and a grid has less than 2^32 threads
+  if ((int64_t)a->num_tokens * (a->heads + a->key_heads) >= (int64_t)1 << 25) return CORTEX_E_INVAL;
+  if (a->num_tokens == 0) return CORTEX_OK;
+  if (!a->q || !a->q_out || (a->key_heads && (!a->k || !a->k_out)) || (a->rotary_dim && (!a->positions || !a->freqs)))
+    return CORTEX_E_INVAL;
+  return a->dtype == CORTEX_BF16 ? launch_norm<bf16_t>(*a, status, stream) : launch_norm<float>(*a, status, stream);
+}

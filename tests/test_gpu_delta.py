@@ -1,0 +1,220 @@
+"""The gated delta rule against its float64 definition: ragged prompts, single tokens, head layouts, states,
+strides and types; what a NaN may touch; broken batches; streams and graphs."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2011_01383_amd import cortex as C
+from tests.delta_helpers import LENS, Delta, say
+from tests.gpu_helpers import need_gpu
+from tests.sequence_helpers import dev, host
+
+pytestmark = pytest.mark.gpu
+
+
+def run(p, step=False, in_place=False, with_state=True, stream=None):
+    d = p.upload()
+    out = None
+    if with_state and p.state is not None:
+        out = d["state"] if in_place else torch.full_like(d["state"], 7.0)
+    C.check(p.call(step, state_in="state" if with_state else None, state_out=out, stream=stream))
+    torch.cuda.synchronize()
+    assert int(d["status"].item()) == 0
+    return d["y"], out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [32, 64, 128])
+@pytest.mark.parametrize("lens", sorted(LENS))
+def test_prompts(lens, K, dtype):
+    need_gpu()
+    say("delta prompts", lens, K, dtype)
+    p = Delta(1, LENS[lens], 2, 1, K, 32, dtype)
+    y, out = run(p)
+    p.check(y, out, "prompts")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,K,V", [(1, 1, 32, 16), (6, 3, 64, 48), (4, 4, 128, 128), (8, 1, 32, 80), (2, 1, 128, 256), (3, 3, 64, 112)])
+def test_layouts(H, G, K, V, dtype):
+    need_gpu()
+    say("delta layouts", H, G, K, V, dtype)
+    p = Delta(2, [70, 3, 0, 130], H, G, K, V, dtype)
+    y, out = run(p)
+    p.check(y, out, "layouts")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("left", [1, 2, 4, 8, 16])
+def test_strides_and_alignments(left, dtype):
+    need_gpu()
+    say("delta strides", left, dtype)
+    p = Delta(3, [66, 5], 3, 1, 64, 32, dtype, left=left)
+    for step in (False, True):
+        if step:
+            p = Delta(3, [1] * 9, 3, 1, 64, 32, dtype, left=left)
+        y, out = run(p, step)
+        p.check(y, out, "strides")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kw", [dict(decay=False), dict(soft=False), dict(sig=False), dict(bias=False), dict(state=False), dict(lean=3.0),
+                                dict(slow=0.01), dict(slow=30.0), dict(scale=-2.0)], ids=lambda k: "%s-%s" % list(k.items())[0])
+def test_options(kw, dtype):
+    need_gpu()
+    say("delta options", kw, dtype)
+    for step in (False, True):
+        p = Delta(4, [1] * 5 if step else [100, 64, 7], 2, 2, 64, 32, dtype, **kw)
+        y, out = run(p, step)
+        p.check(y, out, "options")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("S,H,G,K,V", [(1, 1, 1, 32, 16), (5, 4, 2, 128, 128), (33, 3, 1, 64, 48), (300, 2, 2, 32, 32), (7, 2, 1, 128, 256)])
+def test_tokens(S, H, G, K, V, dtype):
+    need_gpu()
+    say("delta tokens", S, H, G, K, V, dtype)
+    p = Delta(5, [1] * S, H, G, K, V, dtype)
+    y, out = run(p, True)
+    p.check(y, out, "tokens")
+
+
+@pytest.mark.parametrize("step", [False, True])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_pool_rows(step, in_place):
+    """Rows in any order, two without a row, rows that nobody names."""
+    need_gpu()
+    say("delta pool rows", step, in_place)
+    lens = [1] * 6 if step else [65, 0, 3, 130, 64, 1]
+    index = [4, 7, -1, 0, 2, -1]
+    p = Delta(6, lens, 2, 1, 64, 32, index=index, rows=9)
+    y, out = run(p, step, in_place)
+    new = p.check(y, out, "pool")
+    got = host(out)
+    for row in set(range(9)) - set(new):
+        assert np.array_equal(got[row], p.state[row] if in_place else np.full_like(p.state[row], 7.0)), row
+
+
+def test_prompt_then_tokens_is_one_prompt():
+    """The state that a prompt leaves is the one that its next tokens need."""
+    need_gpu()
+    say("delta prompt then tokens")
+    whole = Delta(7, [70, 70, 70], 4, 2, 128, 64, "f32")
+    y, end = run(whole)
+    d = whole.d
+    state = d["state"].clone()
+    cut = [66, 69, 3]
+    rows = np.concatenate([np.arange(70 * i, 70 * i + c) for i, c in enumerate(cut)])
+    at = torch.from_numpy(rows).cuda()
+    kw = dict(A=d["A"], dt_bias=d["dt_bias"], scale=whole.scale, state_in=state, state_out=state, status=d["status"])
+    part = lambda name, i: d[name][i].contiguous()
+    out = torch.empty_like(y)
+    head = torch.empty(len(rows), 4, 64, device="cuda")
+    C.check(C.cortex_delta_forward(part("q", at), part("k", at), part("v", at), part("b", at), dev(np.cumsum([0] + cut), torch.int32), head,
+                                   dt=part("dt", at), ws=d["ws"], **kw))
+    out[at] = head
+    for j in range(70):
+        live = [i for i in range(3) if cut[i] + j < 70]
+        if not live:
+            break
+        at = torch.tensor([70 * i + cut[i] + j for i in live], device="cuda")
+        one = torch.empty(len(live), 4, 64, device="cuda")
+        C.check(C.cortex_delta_step(part("q", at), part("k", at), part("v", at), part("b", at), one, dt=part("dt", at),
+                                    state_index=torch.tensor(live, dtype=torch.int32, device="cuda"), **kw))
+        out[at] = one
+    whole.check(out, state, "prompt then tokens")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("where", ["v", "k", "q", "b", "dt", "state"])
+def test_what_is_not_finite_stays_behind_its_token(where, bad, dtype):
+    """A value or a state entry reaches its row of the state, a key, share or step size its head, a query its own
+    output; tokens before it and other sequences keep their results."""
+    need_gpu()
+    say("delta not finite", where, bad, dtype)
+    p = Delta(8, [40, 150, 20], 4, 2, 64, 32, dtype)
+    clean, end = (host(v) for v in run(p))
+    t, head, row = 40 + 77, 3, 5                 # in the second sequence's second chunk; head 3 reads key head 1
+    hit = np.zeros(clean.shape, dtype=bool)
+    hit_end = np.zeros(end.shape, dtype=bool).reshape(3, 4, 32, 64)
+    if where == "v":
+        p.v[t, head, row] = bad
+        hit[t:190, head, row] = hit_end[1, head, row] = True
+    elif where == "k":
+        p.k[t, 1, 9] = bad
+        hit[t:190, 2:] = hit_end[1, 2:] = True
+    elif where == "q":
+        p.q[t, 1, 9] = bad
+        hit[t, 2:] = True
+    elif where == "b":
+        p.b[t, head] = bad
+        hit[t:190, head] = hit_end[1, head] = True
+    elif where == "dt":
+        p.dt[t, head] = bad
+        hit[t:190, head] = hit_end[1, head] = True
+    else:
+        p.state[1, head * 32 + row, 3] = bad
+        hit[40:190, head, row] = hit_end[1, head, row] = True
+    got, got_end = (host(v) for v in run(p))
+    hit_end = hit_end.reshape(end.shape)
+    assert np.array_equal(got[~hit], clean[~hit]) and np.array_equal(got_end[~hit_end], end[~hit_end])
+    # an infinite share is one or none, an infinite step forgets the state: finite either way
+    if not (where in ("b", "dt") and np.isinf(bad)):
+        assert not np.isfinite(got[hit]).any() and not np.isfinite(got_end[hit_end].reshape(-1, 64)).all(1).any()
+
+
+@pytest.mark.parametrize("step", [False, True])
+def test_broken_batches(step):
+    need_gpu()
+    say("delta broken batches", step)
+    lens = [1, 1, 1] if step else [70, 3, 64]
+    for index, offsets, want in (([0, 3, 1], None, C.CORTEX_ST_INPUT_RANGE), ([0, -2, 1], None, C.CORTEX_ST_INPUT_RANGE),
+                                 (None, [0, 80, 73, 137], C.CORTEX_ST_SEQ_OFFSETS), (None, [1, 70, 73, 137], C.CORTEX_ST_SEQ_OFFSETS),
+                                 (None, [0, 70, 73, 136], C.CORTEX_ST_SEQ_OFFSETS), (None, [0, -5, 73, 137], C.CORTEX_ST_SEQ_OFFSETS),
+                                 (None, [0, 70, 73, 2 ** 31 - 1], C.CORTEX_ST_SEQ_OFFSETS)):
+        if step and offsets is not None:
+            continue
+        p = Delta(9, lens, 2, 1, 32, 16, index=index)
+        if offsets is not None:
+            p.offsets = np.array(offsets)
+        d = p.upload()
+        out = torch.full_like(d["state"], 7.0)
+        C.check(p.call(step, state_out=out))
+        torch.cuda.synchronize()
+        assert int(d["status"].item()) == want
+        # the next call finds the status and writes nothing
+        d["y"].fill_(5.0)
+        out.fill_(7.0)
+        C.check(p.call(step, state_out=out))
+        torch.cuda.synchronize()
+        assert (host(d["y"]) == 5.0).all() and (host(out) == 7.0).all()
+
+
+def test_same_bits_on_another_stream_and_in_a_graph():
+    need_gpu()
+    say("delta streams and graphs")
+    for step in (False, True):
+        p = Delta(10, [1] * 9 if step else [70, 200, 3], 4, 2, 64, 32)
+        y, out = run(p, step)
+        y, out = y.clone(), out.clone()
+        d = p.d
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        again = torch.empty_like(out)
+        d["y"].zero_()
+        torch.cuda.synchronize()
+        C.check(p.call(step, state_out=again, stream=side))
+        side.synchronize()
+        assert torch.equal(d["y"], y) and torch.equal(again, out)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            C.check(p.call(step, state_out=again))
+        for _ in range(3):
+            d["y"].zero_()
+            again.zero_()
+            d["ws"].fill_(255)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(d["y"], y) and torch.equal(again, out)
+        assert int(d["status"].item()) == 0
