@@ -5,7 +5,7 @@
 // Rows of a head's state (one per value channel) share nothing but k, q, a and
 // beta.  Eight lanes hold a row, four entries of each 32 a lane, so that a row's
 // loads and stores are whole 128-byte pieces; a wave holds sixteen rows.
-#include "sequence.hpp"
+#include "delta_chunk.hpp"
 
 namespace cortex {
 
@@ -20,23 +20,6 @@ __device__ __forceinline__ float row_sum(float v) {
   return v;
 }
 
-__device__ __forceinline__ float sigmoid(float v) {
-  return __builtin_amdgcn_rcpf(1.0f + fast_exp2(v * -kLog2e));
-}
-
-// The decay of a token's state and its share of the update.
-struct DeltaGate {
-  float a, beta;
-  __device__ __forceinline__ DeltaGate(const cortex_delta_t &p, float dt, float b, float A2, float bias) {
-    a = 1.0f;
-    if (p.A) {
-      const float v = dt + bias;
-      a = fast_exp2((p.softplus ? softplus(v) : v) * A2);
-    }
-    beta = p.sigmoid ? sigmoid(b) : b;
-  }
-};
-
 // Four consecutive elements.
 template <typename T, bool WIDE> __device__ __forceinline__ void load4(const T *p, float (&v)[4]) {
   if constexpr (WIDE) Pack<T, 4>::load(p, v);
@@ -45,8 +28,8 @@ template <typename T, bool WIDE> __device__ __forceinline__ void load4(const T *
     for (int i = 0; i < 4; ++i) v[i] = to_float<T>(p[i]);
 }
 
-template <typename T, int K, bool STEP, bool WIDE>
-__global__ void __launch_bounds__(64 * kDeltaWaves) delta_walk_kernel(cortex_delta_t p, int32_t *status, int64_t units) {
+template <typename T, int K, bool WIDE>
+__global__ void __launch_bounds__(64 * kDeltaWaves) delta_step_kernel(cortex_delta_t p, int32_t *status, int64_t units) {
   constexpr int C = K / 32;
   if (entry_status(status) != 0) return;
   const int lane = (int)threadIdx.x & 63, part = lane & 7, row8 = lane >> 3;
@@ -55,13 +38,6 @@ __global__ void __launch_bounds__(64 * kDeltaWaves) delta_walk_kernel(cortex_del
   const int V = p.value_dim, tiles = V / kDeltaTile, per = p.heads * tiles;
   const int seq = (int)(unit / per), rest = (int)(unit % per), head = rest / tiles;
   const int v0 = rest % tiles * kDeltaTile + row8, g = head / (p.heads / p.key_heads);
-  int begin = seq, end = seq + 1;
-  if constexpr (!STEP) {
-    if (rest == 0) check_offsets(p.seq_offsets, p.num_seqs, p.num_tokens, seq, status);
-    begin = p.seq_offsets[seq];
-    end = p.seq_offsets[seq + 1];
-    if (begin < 0 || end < begin || end > p.num_tokens) return;
-  }
   int pool = -1;
   if (p.state_in || p.state_out) {
     pool = state_row(p.state_index, seq, p.state_rows, status);
@@ -75,70 +51,105 @@ __global__ void __launch_bounds__(64 * kDeltaWaves) delta_walk_kernel(cortex_del
 #pragma unroll
     for (int c = 0; c < C; ++c)
       h[r][c] = p.state_in && pool >= 0 ? *(const vec *)(p.state_in + at + r * 8 * K + c * 32) : vec{0.0f, 0.0f, 0.0f, 0.0f};
-  const float A2 = p.A ? decay_rate(p.A[head]) : 0.0f, bias = p.A && p.dt_bias ? p.dt_bias[head] : 0.0f;
   const T *qs = (const T *)p.q + g * K + part * 4, *ks = (const T *)p.k + g * K + part * 4;
-  const T *vs = (const T *)p.v + (int64_t)head * V + v0, *bs = (const T *)p.b + head, *ds = (const T *)p.dt + head;
+  const T *vs = (const T *)p.v + (int64_t)head * V + v0;
   T *ys = (T *)p.y + (int64_t)head * V + v0;
-#pragma unroll 1
-  for (int64_t t = begin; t < end; ++t) {
-    float q[C][4], k[C][4], v[2];
+  const int64_t t = seq;
+  float q[C][4], k[C][4], v[2];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      load4<T, WIDE>(qs + t * p.q_ld + c * 32, q[c]);
-      load4<T, WIDE>(ks + t * p.k_ld + c * 32, k[c]);
-    }
-    v[0] = to_float<T>(vs[t * p.v_ld]);
-    v[1] = to_float<T>(vs[t * p.v_ld + 8]);
-    const DeltaGate gate(p, p.A ? to_float<T>(ds[t * p.dt_ld]) : 0.0f, to_float<T>(bs[t * p.b_ld]), A2, bias);
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      float dot = 0.0f;
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          h[r][c][i] *= gate.a;
-          dot = __builtin_fmaf(h[r][c][i], k[c][i], dot);
-        }
-      const float u = gate.beta * (v[r] - row_sum(dot));
-      float y = 0.0f;
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          h[r][c][i] = __builtin_fmaf(u, k[c][i], h[r][c][i]);
-          y = __builtin_fmaf(h[r][c][i], q[c][i], y);
-        }
-      y = row_sum(y) * p.scale;
-      if (part == 0) ys[t * p.y_ld + r * 8] = from_float<T>(y);
-    }
+  for (int c = 0; c < C; ++c) {
+    load4<T, WIDE>(qs + t * p.q_ld + c * 32, q[c]);
+    load4<T, WIDE>(ks + t * p.k_ld + c * 32, k[c]);
   }
-  if (p.state_out && pool >= 0)
+  v[0] = to_float<T>(vs[t * p.v_ld]);
+  v[1] = to_float<T>(vs[t * p.v_ld + 8]);
+  float a = 1.0f;
+  if (p.A) {
+    const float raw = to_float<T>(((const T *)p.dt)[t * p.dt_ld + head]) + (p.dt_bias ? p.dt_bias[head] : 0.0f);
+    a = fast_exp2((p.softplus ? softplus(raw) : raw) * decay_rate(p.A[head]));
+  }
+  const float b = to_float<T>(((const T *)p.b)[t * p.b_ld + head]), beta = p.sigmoid ? sigmoid(b) : b;
 #pragma unroll
-    for (int r = 0; r < 2; ++r)
+  for (int r = 0; r < 2; ++r) {
+    float dot = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        h[r][c][i] *= a;
+        dot = __builtin_fmaf(h[r][c][i], k[c][i], dot);
+      }
+    const float u = beta * (v[r] - row_sum(dot));
+    float y = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        h[r][c][i] = __builtin_fmaf(u, k[c][i], h[r][c][i]);
+        y = __builtin_fmaf(h[r][c][i], q[c][i], y);
+      }
+    y = row_sum(y) * p.scale;
+    if (part == 0) ys[t * p.y_ld + r * 8] = from_float<T>(y);
+    if (p.state_out && pool >= 0)
 #pragma unroll
       for (int c = 0; c < C; ++c) *(vec *)(p.state_out + at + r * 8 * K + c * 32) = h[r][c];
+  }
 }
 
 static bool launched() { return hipGetLastError() == hipSuccess; }
 
-template <typename T, int K, bool STEP> int launch_walk(const cortex_delta_t &a, int32_t *status, void *stream) {
+template <typename T, int K> int launch_step_of(const cortex_delta_t &a, int32_t *status, void *stream) {
   const int64_t units = (int64_t)a.num_seqs * a.heads * (a.value_dim / kDeltaTile);
   const unsigned grid = (unsigned)((units + kDeltaWaves - 1) / kDeltaWaves);
   constexpr uintptr_t mask = 4 * sizeof(T) - 1;
   const bool wide = a.q_ld % 4 == 0 && a.k_ld % 4 == 0 && ((uintptr_t)a.q & mask) == 0 && ((uintptr_t)a.k & mask) == 0;
-  if (wide) delta_walk_kernel<T, K, STEP, true><<<grid, 64 * kDeltaWaves, 0, (hipStream_t)stream>>>(a, status, units);
-  else delta_walk_kernel<T, K, STEP, false><<<grid, 64 * kDeltaWaves, 0, (hipStream_t)stream>>>(a, status, units);
+  if (wide) delta_step_kernel<T, K, true><<<grid, 64 * kDeltaWaves, 0, (hipStream_t)stream>>>(a, status, units);
+  else delta_step_kernel<T, K, false><<<grid, 64 * kDeltaWaves, 0, (hipStream_t)stream>>>(a, status, units);
   return launched() ? CORTEX_OK : CORTEX_E_HIP;
 }
 
-template <typename T, bool STEP> int launch_delta(const cortex_delta_t &a, int32_t *status, void *stream) {
+template <typename T, int K, int NT, bool WIDE>
+void launch_walk(const cortex_delta_t &a, int32_t *status, const ChunkMap *maps, hipStream_t st) {
+  constexpr int kColumns = 16 * NT * kChunkWaves;
+  const int64_t units = (int64_t)a.num_seqs * a.heads * ((a.value_dim + kColumns - 1) / kColumns);
+  chunk_walk_kernel<T, K, NT, WIDE><<<blocks_of_units(units), kChunkThreads, 0, st>>>(a, status, maps, units);
+}
+
+template <typename T, int K, bool WIDE> int launch_chunks_of(const cortex_delta_t &a, int32_t *status, ChunkMap *maps, void *stream) {
+  const hipStream_t st = (hipStream_t)stream;
+  const int64_t chunks = chunk_slots(a.num_tokens, a.num_seqs, kChunk) * a.heads;
+  chunk_maps_kernel<T, K, WIDE><<<blocks_of_units(chunks), kChunkThreads, 0, st>>>(a, status, maps, chunks);
+  if (!launched()) return CORTEX_E_HIP;
+  const int64_t units = (int64_t)a.num_seqs * a.heads * (a.value_dim / 16);
+  if (units <= 1024) chunk_chain_kernel<T, K, WIDE><<<blocks_of_units(units), 2 * kChunkThreads, 0, st>>>(a, status, maps, units);
+  else if (sizeof(T) == 2 && a.value_dim % 32 == 0) launch_walk<T, K, sizeof(T) == 2 ? 2 : 1, WIDE>(a, status, maps, st);
+  else launch_walk<T, K, 1, WIDE>(a, status, maps, st);
+  return launched() ? CORTEX_OK : CORTEX_E_HIP;
+}
+
+template <typename T, int K> int launch_chunks(const cortex_delta_t &a, int32_t *status, ChunkMap *maps, void *stream) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const bool wide = a.q_ld % V == 0 && a.k_ld % V == 0 && aligned16(a.q) && aligned16(a.k);
+  return wide ? launch_chunks_of<T, K, true>(a, status, maps, stream) : launch_chunks_of<T, K, false>(a, status, maps, stream);
+}
+
+template <typename T> int launch_forward(const cortex_delta_t &a, int32_t *status, void *ws, void *stream) {
   switch (a.key_dim) {
-    case 32: return launch_walk<T, 32, STEP>(a, status, stream);
-    case 64: return launch_walk<T, 64, STEP>(a, status, stream);
-    default: return launch_walk<T, 128, STEP>(a, status, stream);
+    case 32: return launch_chunks<T, 32>(a, status, (ChunkMap *)ws, stream);
+    case 64: return launch_chunks<T, 64>(a, status, (ChunkMap *)ws, stream);
+    default: return launch_chunks<T, 128>(a, status, (ChunkMap *)ws, stream);
   }
 }
+
+template <typename T> int launch_step(const cortex_delta_t &a, int32_t *status, void *stream) {
+  switch (a.key_dim) {
+    case 32: return launch_step_of<T, 32>(a, status, stream);
+    case 64: return launch_step_of<T, 64>(a, status, stream);
+    default: return launch_step_of<T, 128>(a, status, stream);
+  }
+}
+
+static size_t delta_bytes(int64_t T, int64_t S, int64_t heads) { return (size_t)(chunk_slots(T, S, kChunk) * heads) * sizeof(ChunkMap); }
 
 static bool bad_delta_size(int32_t heads, int32_t key_heads, int32_t K, int32_t V) {
   if (heads < 1 || key_heads < 1 || heads % key_heads) return true;
@@ -174,23 +185,25 @@ using namespace cortex;
 extern "C" size_t cortex_delta_workspace_bytes(int32_t num_tokens, int32_t num_seqs, int32_t heads, int32_t key_dim,
                                                int32_t value_dim) {
   if (num_tokens < 0 || num_seqs < 0 || bad_delta_size(heads, 1, key_dim, value_dim)) return 0;
-  return 16;
+  return delta_bytes(num_tokens, num_seqs, heads) + 16;
 }
 
 extern "C" int cortex_delta_forward(const cortex_delta_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream) {
   const int rc = check_delta(args, false, d_status);
   if (rc != CORTEX_OK) return rc;
   if (args->num_seqs == 0) return CORTEX_OK;
+  // a workgroup a chunk and head, and a grid has less than 2^32 threads
+  if (chunk_slots(args->num_tokens, args->num_seqs, kChunk) * args->heads >= (int64_t)1 << 24) return CORTEX_E_INVAL;
   if (!d_ws || !aligned16(d_ws)) return CORTEX_E_INVAL;
-  if (ws_bytes < 16) return CORTEX_E_WORKSPACE;
-  return args->dtype == CORTEX_BF16 ? launch_delta<bf16_t, false>(*args, d_status, stream)
-                                    : launch_delta<float, false>(*args, d_status, stream);
+  if (ws_bytes < delta_bytes(args->num_tokens, args->num_seqs, args->heads)) return CORTEX_E_WORKSPACE;
+  return args->dtype == CORTEX_BF16 ? launch_forward<bf16_t>(*args, d_status, d_ws, stream)
+                                    : launch_forward<float>(*args, d_status, d_ws, stream);
 }
 
 extern "C" int cortex_delta_step(const cortex_delta_t *args, int32_t *d_status, void *stream) {
   const int rc = check_delta(args, true, d_status);
   if (rc != CORTEX_OK) return rc;
   if (args->num_seqs == 0) return CORTEX_OK;
-  return args->dtype == CORTEX_BF16 ? launch_delta<bf16_t, true>(*args, d_status, stream)
-                                    : launch_delta<float, true>(*args, d_status, stream);
+  return args->dtype == CORTEX_BF16 ? launch_step<bf16_t>(*args, d_status, stream)
+                                    : launch_step<float>(*args, d_status, stream);
 }

@@ -62,6 +62,10 @@ __device__ __forceinline__ float silu(float v) {
   return v * __builtin_amdgcn_rcpf(1.0f + fast_exp2(v * -kLog2e));
 }
 
+__device__ __forceinline__ float sigmoid(float v) {
+  return __builtin_amdgcn_rcpf(1.0f + fast_exp2(v * -kLog2e));
+}
+
 // softplus(v) = max(v, 0) + log1p(e), e = exp(-|v|) in (0, 1].  With
 // s = e / (2 + e) <= 1/3, log1p(e) = 2 atanh(s) = 2 s (1 + s^2/3 + s^4/5 + ...);
 // after the s^14 term what is left is below 2^-27 of the sum.  log(1 + e) itself

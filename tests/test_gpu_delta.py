@@ -218,3 +218,16 @@ def test_same_bits_on_another_stream_and_in_a_graph():
             torch.cuda.synchronize()
             assert torch.equal(d["y"], y) and torch.equal(again, out)
         assert int(d["status"].item()) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,K,V", [(8, 4, 64, 64), (4, 4, 128, 128), (40, 8, 32, 16), (12, 3, 64, 48)])
+def test_many_prompts(H, G, K, V, dtype):
+    """More heads of sequences than the GPU takes at once with few columns a workgroup."""
+    need_gpu()
+    say("delta many prompts", H, G, K, V, dtype)
+    r = np.random.default_rng(11)
+    S = 1200 // (H * V // 16) + 20
+    p = Delta(11, [int(n) for n in r.integers(0, 100, S)], H, G, K, V, dtype, index=r.permutation(S).tolist())
+    y, out = run(p)
+    p.check(y, out, "many prompts")
