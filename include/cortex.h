@@ -604,8 +604,8 @@ int cortex_quant_i8(const cortex_quant_i8_t *args, int32_t *d_status, void *stre
  * x holds the 8-bit rows themselves.  The sum is exact (at most 131,071 inputs); it is
  * then rounded to float32, multiplied by the two scales in turn and added to the bias,
  * each rounded on its own, and rounded to dtype.  Rows of w start at 16-byte
- * boundaries and lie w_ld bytes apart, a multiple of 16; what their last 16 bytes hold
- * past the inputs does not matter, but is read.
+ * boundaries and lie w_ld bytes apart, a multiple of 16 up to 2^24; what their last 16
+ * bytes hold past the inputs does not matter, but is read.
  */
 typedef struct {
   int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: y, and x without x_scale */

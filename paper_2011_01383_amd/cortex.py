@@ -726,6 +726,13 @@ def cortex_logits_process(logits: torch.Tensor, *, out=None, token=None, lse=Non
 
 def _on_current_device(names: str, *tensors) -> None:
     """The launch goes to the current device, whose memory these have to be."""
+    device = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            break
+    else:
+        if device >= 0 and device == torch.cuda.current_device():
+            return                      # nothing to refuse: the usual call
     _on_device(names, *tensors)
     current = torch.cuda.current_device()
     for name, t in zip(names.split(), tensors):

@@ -185,7 +185,8 @@ using namespace cortex;
 extern "C" size_t cortex_delta_workspace_bytes(int32_t num_tokens, int32_t num_seqs, int32_t heads, int32_t key_dim,
                                                int32_t value_dim) {
   if (num_tokens < 0 || num_seqs < 0 || bad_delta_size(heads, 1, key_dim, value_dim)) return 0;
-  return delta_bytes(num_tokens, num_seqs, heads) + 16;
+  const size_t bytes = delta_bytes(num_tokens, num_seqs, heads);
+  return bytes ? bytes : 256;
 }
 
 extern "C" int cortex_delta_forward(const cortex_delta_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream) {

@@ -7,7 +7,9 @@
 namespace cortex {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
+constexpr int64_t kMaxRow = 1 << 24;              // 255 rows of bytes stay below 2^32
 constexpr int32_t kMaxInputs = 131071;           // 128 * 128 of each stay below 2^31
 
 // ---------------------------------------------------------------------------
@@ -22,60 +24,120 @@ __device__ __forceinline__ int quant_value(float x, float scale) {
   return (int)__builtin_fminf(__builtin_fmaxf(v, -127.0f), 127.0f);
 }
 
-// `filled`: columns of q that are written, zeros past the row's own.
-template <typename T, bool WIDE>
+// The scale of a row whose largest |x| has these bits, and whether its values are all 0.
+__device__ __forceinline__ float quant_scale(unsigned int top, bool &none) {
+  const bool odd = top >= 0x7f800000u;           // infinities and NaN are the largest
+  const float scale = odd ? __builtin_nanf("") : __builtin_bit_cast(float, top) / 127.0f;
+  none = odd || scale == 0.0f;
+  return scale;
+}
+
+// Eight elements; `n` of them are there, the others 0.
+template <typename T, bool WIDE> __device__ __forceinline__ void load_eight(const T *x, int n, float (&v)[8]) {
+  if (WIDE) {
+    if (n > 0) {
+      Pack<T, 8>::load(x, v);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? to_float<T>(x[i]) : 0.0f;
+  }
+}
+
+__device__ __forceinline__ u32x2 quant_eight(const float (&v)[8], float scale, bool none) {
+  unsigned int b[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b[i / 4] |= (none ? 0u : (unsigned int)quant_value(v[i], scale) & 255u) << (8 * (i % 4));
+  return u32x2{b[0], b[1]};
+}
+
+// |x| as whole numbers keep their order.
+__device__ __forceinline__ unsigned int top_of(const float (&v)[8], unsigned int top) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __builtin_bit_cast(unsigned int, v[i]) & 0x7fffffffu);
+  return top;
+}
+__device__ __forceinline__ unsigned int wave_top(unsigned int top) {
+#pragma unroll
+  for (int m = 32; m; m >>= 1) top = max(top, (unsigned int)__shfl_xor((int)top, m));
+  return top;
+}
+
+// A workgroup a row, which it keeps in registers where it has at most 8 * 256 * KEEP
+// columns, and reads again otherwise.  `filled`: columns of q that are written, zeros past
+// the row's own.  WIDE: rows of x and q in whole eights at their alignment.
+template <typename T, bool WIDE, int KEEP>
 __global__ void __launch_bounds__(kQuantThreads) quant_kernel(cortex_quant_i8_t a, int32_t *status, int filled) {
-  constexpr int V = WIDE ? 8 : 1;
   __shared__ unsigned int most[kQuantThreads / 64];
   if (__syncthreads_or(entry_status(status) != 0)) return;
+  constexpr int kStride = kQuantThreads * 8;
   const int tid = (int)threadIdx.x;
   const int64_t r = blockIdx.x;
   const T *x = (const T *)a.x + r * a.x_ld;
   int8_t *q = a.q + r * a.q_ld;
-  // |x| as whole numbers keep their order; infinities and NaN are the largest
+  float v[KEEP > 0 ? KEEP : 1][8];
   unsigned int top = 0;
-  for (int c = tid * V; c < a.columns; c += kQuantThreads * V) {
-    float v[V];
-    Pack<T, V>::load(x + c, v);
+  if constexpr (KEEP > 0) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) top = max(top, __builtin_bit_cast(unsigned int, v[i]) & 0x7fffffffu);
+    for (int k = 0; k < KEEP; ++k) {
+      const int c = tid * 8 + k * kStride;
+      load_eight<T, WIDE>(x + c, a.columns - c, v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) top = top_of(v[k], top);
+  } else {
+    for (int c = tid * 8; c < a.columns; c += kStride) {
+      load_eight<T, WIDE>(x + c, a.columns - c, v[0]);
+      top = top_of(v[0], top);
+    }
   }
-#pragma unroll
-  for (int m = 32; m; m >>= 1) top = max(top, (unsigned int)__shfl_xor((int)top, m));
+  top = wave_top(top);
   if ((tid & 63) == 0) most[tid >> 6] = top;
   __syncthreads();
-  top = max(max(most[0], most[1]), max(most[2], most[3]));
-  const bool odd = top >= 0x7f800000u;
-  const float scale = odd ? __builtin_nanf("") : __builtin_bit_cast(float, top) / 127.0f;
-  const bool none = odd || scale == 0.0f;
-  for (int c = tid * V; c < filled; c += kQuantThreads * V) {
-    float v[V];
-    int8_t to[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) to[i] = 0;
-    if (c < a.columns) {
-      Pack<T, V>::load(x + c, v);
-#pragma unroll
-      for (int i = 0; i < V; ++i) to[i] = none ? 0 : (int8_t)quant_value(v[i], scale);
-    }
-    if constexpr (WIDE) {
-      typedef int8_t pack __attribute__((ext_vector_type(8)));
-      *(pack *)(q + c) = pack{to[0], to[1], to[2], to[3], to[4], to[5], to[6], to[7]};
+  bool none;
+  const float scale = quant_scale(max(max(most[0], most[1]), max(most[2], most[3])), none);
+  auto put = [&](int c, const float (&u)[8]) {
+    if (c >= filled) return;
+    const u32x2 b = quant_eight(u, scale, none);
+    if (WIDE) {
+      *(u32x2 *)(q + c) = b;
     } else {
-      q[c] = to[0];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (c + i < filled) q[c + i] = (int8_t)(b[i / 4] >> (8 * (i % 4)));
+    }
+  };
+  if constexpr (KEEP > 0) {
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) put(tid * 8 + k * kStride, v[k]);
+  } else {
+    for (int c = tid * 8; c < filled; c += kStride) {
+      load_eight<T, WIDE>(x + c, a.columns - c, v[0]);
+      put(c, v[0]);
     }
   }
   if (tid == 0) a.scale[r] = scale;
 }
 
-template <typename T> int launch_quant(const cortex_quant_i8_t &a, int32_t *status, int filled, void *stream) {
-  constexpr uintptr_t mask = sizeof(T) == 2 ? 15 : 31;
-  const bool wide = a.columns % 8 == 0 && filled % 8 == 0 && a.x_ld % 8 == 0 && a.q_ld % 8 == 0 && ((uintptr_t)a.x & mask) == 0 &&
-                    ((uintptr_t)a.q & 7) == 0;
+template <typename T, bool WIDE> int launch_quant_rows(const cortex_quant_i8_t &a, int32_t *status, int filled, void *stream) {
   const hipStream_t st = (hipStream_t)stream;
-  if (wide) quant_kernel<T, true><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a, status, filled);
-  else quant_kernel<T, false><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a, status, filled);
+  if (filled <= 2048) quant_kernel<T, WIDE, 1><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a, status, filled);
+  else if (filled <= 4096) quant_kernel<T, WIDE, 2><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a, status, filled);
+  else if (filled <= 8192) quant_kernel<T, WIDE, 4><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a, status, filled);
+  else quant_kernel<T, WIDE, 0><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a, status, filled);
   return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+}
+
+template <typename T> bool eights(const void *x, int64_t x_ld, int columns) {
+  return columns % 8 == 0 && x_ld % 8 == 0 && ((uintptr_t)x & (8 * sizeof(T) - 1)) == 0;
+}
+
+template <typename T> int launch_quant(const cortex_quant_i8_t &a, int32_t *status, int filled, void *stream) {
+  const bool wide = eights<T>(a.x, a.x_ld, a.columns) && filled % 8 == 0 && a.q_ld % 8 == 0 && ((uintptr_t)a.q & 7) == 0;
+  return wide ? launch_quant_rows<T, true>(a, status, filled, stream) : launch_quant_rows<T, false>(a, status, filled, stream);
 }
 
 // 8-bit rows of any alignment into rows of whole pieces, zeros at their ends.
@@ -89,8 +151,10 @@ __global__ void __launch_bounds__(256) pad_kernel(const int8_t *x, int64_t x_ld,
 // ---------------------------------------------------------------------------
 // The product
 // ---------------------------------------------------------------------------
-// What a product kernel takes: x in rows of whole 16-byte pieces, zeros past the
-// inputs; `pieces` of them hold inputs.
+constexpr int kDepth = 64;                       // bytes of the inputs at a time
+
+// What a product kernel takes: x in rows of a multiple of kDepth bytes, zeros past the
+// inputs, so that what w holds there does not matter; `pieces` of 16 bytes of a row of w are read.
 struct Product {
   const int8_t *x, *w;
   int64_t x_ld, w_ld, y_ld;
@@ -106,97 +170,245 @@ template <typename T> __device__ __forceinline__ T finish(const Product &a, int 
   return from_float<T>(v);
 }
 
-constexpr int kTile = 128, kDepth = 128;         // channels or tokens of a tile, bytes of the inputs at a time
+// Four neighbouring channels of one token.
+template <typename T> __device__ __forceinline__ void put_four(const Product &a, i32x4 acc, float xs, int t, int n, bool aligned) {
+  T *y = (T *)a.y + (int64_t)t * a.y_ld;
+  if (aligned && n + 3 < a.outputs) {
+    typedef T pack __attribute__((ext_vector_type(4)));
+    pack v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = finish<T>(a, acc[r], xs, n + r);
+    *(pack *)(y + n) = v;
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (n + r < a.outputs) y[n + r] = finish<T>(a, acc[r], xs, n + r);
+  }
+}
 
-// A row of 128 bytes in LDS, its 16-byte pieces exchanged so that the rows and pieces
+// A row of 64 bytes in LDS, its four 16-byte pieces exchanged so that the rows and pieces
 // that the hardware serves together (rows 0-3 and 12-15 of sixteen with rows 4-11 of
 // the next piece) lie in different banks.
-__device__ __forceinline__ int piece_at(int row, int piece) { return row * kDepth + ((piece ^ ((row >> 1) & 7)) << 4); }
+__device__ __forceinline__ int piece_place(int row, int piece) { return piece ^ (-(row >> 2) & 3); }
 
-template <typename T>
-__global__ void __launch_bounds__(256) product_kernel(Product a, const int32_t *status, bool aligned) {
-  __shared__ __attribute__((aligned(16))) int8_t lds[2][2][kTile * kDepth];
+// 16 bytes a lane straight into LDS, lane after lane from `to` on.  The compiler does not
+// see the load: the caller waits for it (copies_done) before the barrier.
+__device__ __forceinline__ void copy_to_lds(const int8_t *base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
+}
+template <int N> __device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory"); }
+
+// Tiles of TN channels and TT tokens by WN x WT waves; BUFFERS stages of kDepth bytes in
+// LDS, all but one of them on their way while one is multiplied.  XCDs take runs of
+// neighbouring tiles, four tiles of tokens by as many of channels as there are.
+template <typename T, int TN, int TT, int WN, int WT, int BUFFERS>
+__global__ void __launch_bounds__(64 * WN * WT) product_kernel(Product a, const int32_t *status, bool aligned, int n_tiles, int t_tiles) {
+  constexpr int kWaves = WN * WT, I = TN / WN / 16, J = TT / WT / 16, kStage = (TN + TT) * kDepth;
+  constexpr int kCopies = (TN + TT) / 16 / kWaves;         // of 16 rows each, per wave and stage
+  __shared__ __attribute__((aligned(1024))) int8_t lds[BUFFERS * kStage];
+  const int64_t total = (int64_t)n_tiles * t_tiles, tile = unit_of_block(total);
+  if (tile >= total) return;
   if (__syncthreads_or(entry_status(status) != 0)) return;
-  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, q = lane >> 4, l16 = lane & 15;
-  const int n0 = (int)blockIdx.x * kTile, t0 = (int)blockIdx.y * kTile;
-  const int wn = wave % 2 * 64, wt = wave / 2 * 64;
-  i32x4 acc[4][4];
+  const int lane = (int)threadIdx.x & 63, q = lane >> 4, l16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int band = (int)(tile / (4 * n_tiles)), rest = (int)(tile % (4 * n_tiles)), tall = min(4, t_tiles - band * 4);
+  const int n0 = rest / tall * TN, t0 = (band * 4 + rest % tall) * TT;
+  const int wn = wave % WN * (TN / WN), wt = wave / WN * (TT / WT);
+  const int8_t *ws = a.w + (int64_t)n0 * a.w_ld, *xs = a.x + (int64_t)t0 * a.x_ld;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t *)lds;
+  // The lane's piece of each copy; a copy is of w or of x alone.
+  uint32_t offset[kCopies];
+  int piece[kCopies];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-  i32x4 wr[4], xr[4];
-  auto fetch = [&](int p0) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int id = i * 256 + tid, row = id / 8, p = p0 + id % 8;
-      wr[i] = xr[i] = i32x4{0, 0, 0, 0};
-      if (p < a.pieces) {
-        wr[i] = *(const i32x4 *)(a.w + (int64_t)min(n0 + row, a.outputs - 1) * a.w_ld + (int64_t)p * 16);
-        xr[i] = *(const i32x4 *)(a.x + (int64_t)min(t0 + row, a.tokens - 1) * a.x_ld + (int64_t)p * 16);
-      }
-    }
-  };
-  auto put = [&](int b) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int id = i * 256 + tid;
-      *(i32x4 *)&lds[b][0][piece_at(id / 8, id % 8)] = wr[i];
-      *(i32x4 *)&lds[b][1][piece_at(id / 8, id % 8)] = xr[i];
-    }
-  };
-  fetch(0);
-  put(0);
-  __syncthreads();
-  int b = 0;
-#pragma unroll 1
-  for (int p0 = 0; p0 < a.pieces; p0 += 8, b ^= 1) {
-    if (p0 + 8 < a.pieces) fetch(p0 + 8);
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      i32x4 w[4], x[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w[i] = *(const i32x4 *)&lds[b][0][piece_at(wn + i * 16 + l16, m * 4 + q)];
-        x[i] = *(const i32x4 *)&lds[b][1][piece_at(wt + i * 16 + l16, m * 4 + q)];
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], x[j], acc[i][j], 0, 0, 0);
-    }
-    if (p0 + 8 < a.pieces) put(b ^ 1);
-    __syncthreads();
+  for (int i = 0; i < kCopies; ++i) {
+    const int row = (wave * kCopies + i) * 16 + lane / 4;
+    piece[i] = piece_place(row, lane % 4);
+    offset[i] = row < TN ? (uint32_t)min(row, a.outputs - 1 - n0) * (uint32_t)a.w_ld
+                         : (uint32_t)min(row - TN, a.tokens - 1 - t0) * (uint32_t)a.x_ld;
   }
+  const int steps = (a.pieces + 3) / 4;
+  auto copy = [&](int step, int buffer) {
+    step = min(step, steps - 1);                 // past the end: once more the last, so that the count of copies on their way is fixed
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+    for (int i = 0; i < kCopies; ++i) {
+      const int first = (wave * kCopies + i) * 16;
+      const bool of_w = first < TN;
+      // what w lacks of the last stage repeats its last piece
+      const uint32_t p = of_w ? (uint32_t)min(step * 4 + piece[i], a.pieces - 1) : (uint32_t)(step * 4 + piece[i]);
+      copy_to_lds(of_w ? ws : xs, offset[i] + p * 16, lds0 + (uint32_t)(buffer * kStage + first * kDepth));
+    }
+  };
+  i32x4 acc[I][J];
+#pragma unroll
+  for (int i = 0; i < I; ++i)
+#pragma unroll
+    for (int j = 0; j < J; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int b = 0; b < BUFFERS - 1; ++b) copy(b, b);
+  i32x4 wf[2][I], xf[2][J];
+  auto read = [&](int buffer, i32x4 (&wr)[I], i32x4 (&xr)[J]) {
+    const int8_t *w = lds + buffer * kStage, *x = w + TN * kDepth;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      const int row = wn + i * 16 + l16;
+      wr[i] = *(const i32x4 *)(w + row * kDepth + piece_place(row, q) * 16);
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int row = wt + j * 16 + l16;
+      xr[j] = *(const i32x4 *)(x + row * kDepth + piece_place(row, q) * 16);
+    }
+  };
+  copies_done<(BUFFERS - 2) * kCopies>();
+  __syncthreads();
+  read(0, wf[0], xf[0]);
+  int buffer = 0;
+  // One stage is multiplied from registers while the next is read from LDS.
+  auto multiply = [&](int step, const i32x4 (&wc)[I], const i32x4 (&xc)[J], i32x4 (&wr)[I], i32x4 (&xr)[J]) {
+    copies_done<(BUFFERS - 3) * kCopies>();
+    __syncthreads();                             // the next stage is there, the one before this is multiplied
+    copy(step + BUFFERS - 1, buffer == 0 ? BUFFERS - 1 : buffer - 1);
+    buffer = buffer == BUFFERS - 1 ? 0 : buffer + 1;
+    read(buffer, wr, xr);
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+      for (int j = 0; j < J; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wc[i], xc[j], acc[i][j], 0, 0, 0);
+  };
+#pragma unroll 1
+  for (int step = 0; step < steps; step += 2) {
+    multiply(step, wf[0], xf[0], wf[1], xf[1]);
+    if (step + 1 < steps) multiply(step + 1, wf[1], xf[1], wf[0], xf[0]);
+  }
+  copies_done<0>();                              // LDS is given back only when nothing is on its way to it
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
     const int t = t0 + wt + j * 16 + l16;
     if (t >= a.tokens) continue;
-    const float xs = a.x_scale[t];
-    T *y = (T *)a.y + (int64_t)t * a.y_ld;
+    const float scale = a.x_scale[t];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int n = n0 + wn + i * 16 + q * 4;
-      if (aligned && n + 3 < a.outputs) {
-        typedef T pack __attribute__((ext_vector_type(4)));
-        pack v;
+    for (int i = 0; i < I; ++i) put_four<T>(a, acc[i][j], scale, t, n0 + wn + i * 16 + q * 4, aligned);
+  }
+}
+
+// Few tokens: a workgroup has 16 TI channels and all tokens (16 TJ of them at most), its
+// waves every WAVES-th 64 bytes of the inputs; operands go to registers, AHEAD of the
+// wave's shares at once.
+template <typename T, int TI, int TJ, int WAVES, int AHEAD>
+__global__ void __launch_bounds__(64 * WAVES) few_kernel(Product a, const int32_t *status, bool aligned) {
+  __shared__ i32x4 sums[WAVES][TI * TJ][64];
+  const int failed = entry_status(status);
+  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, q = lane >> 4, l16 = lane & 15;
+  const int n0 = (int)blockIdx.x * 16 * TI;
+  const int8_t *w[TI], *x[TJ];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = finish<T>(a, acc[i][j][r], xs, n + r);
-        *(pack *)(y + n) = v;
-      } else {
+  for (int i = 0; i < TI; ++i) w[i] = a.w + (int64_t)min(n0 + i * 16 + l16, a.outputs - 1) * a.w_ld;
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (n + r < a.outputs) y[n + r] = finish<T>(a, acc[i][j][r], xs, n + r);
-      }
+  for (int j = 0; j < TJ; ++j) x[j] = a.x + (int64_t)min(j * 16 + l16, a.tokens - 1) * a.x_ld;
+  const int steps = (a.pieces + 3) / 4;          // of 64 bytes
+  i32x4 acc[TI][TJ];
+#pragma unroll
+  for (int i = 0; i < TI; ++i)
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+#pragma unroll 1
+  for (int s0 = wave; s0 < steps; s0 += WAVES * AHEAD) {
+    i32x4 wf[AHEAD][TI], xf[AHEAD][TJ];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      // what lies past the end is multiplied by x's zeros, or not at all
+      const int p = min(s0 + k * WAVES, steps - 1) * 4 + q;
+#pragma unroll
+      for (int i = 0; i < TI; ++i) wf[k][i] = *(const i32x4 *)(w[i] + (int64_t)min(p, a.pieces - 1) * 16);
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) xf[k][j] = *(const i32x4 *)(x[j] + (int64_t)p * 16);
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (s0 + k * WAVES < steps)
+#pragma unroll
+        for (int i = 0; i < TI; ++i)
+#pragma unroll
+          for (int j = 0; j < TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[k][i], xf[k][j], acc[i][j], 0, 0, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < TI; ++i)
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) sums[wave][i * TJ + j][lane] = acc[i][j];
+  if (__syncthreads_or(failed != 0)) return;
+  for (int k = wave; k < TI * TJ; k += WAVES) {
+    i32x4 s = sums[0][k][lane];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) s += sums[i][k][lane];
+    const int t = k % TJ * 16 + l16;
+    if (t < a.tokens) put_four<T>(a, s, a.x_scale[t], t, n0 + k / TJ * 16 + q * 4, aligned);
+  }
+}
+
+// One to four tokens, brought to 8 bits by every workgroup for itself, beside the loads of
+// its first weights: a launch less.  Rows of x stay in LDS.
+constexpr int kOwnTokens = 4, kOwnBytes = 16384, kOwnWaves = 4;
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(64 * kOwnWaves) own_kernel(Product a, const T *x, int64_t x_ld, int columns, const int32_t *status, bool aligned) {
+  constexpr int kAhead = 8, kThreads = 64 * kOwnWaves;
+  __shared__ __attribute__((aligned(16))) int8_t rows[kOwnBytes];
+  __shared__ i32x4 sums[kOwnWaves][64];
+  __shared__ unsigned int most[kOwnTokens][kOwnWaves];
+  __shared__ float scales[kOwnTokens];
+  const int failed = entry_status(status);
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, q = lane >> 4, l16 = lane & 15;
+  const int n0 = (int)blockIdx.x * 16, steps = (a.pieces + 3) / 4, bytes = steps * 64;
+  const int8_t *w = a.w + (int64_t)min(n0 + l16, a.outputs - 1) * a.w_ld;
+  i32x4 wf[kAhead];
+  auto fetch = [&](int s0) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      wf[k] = *(const i32x4 *)(w + (int64_t)min(min(s0 + k * kOwnWaves, steps - 1) * 4 + q, a.pieces - 1) * 16);
+  };
+  fetch(wave);
+  for (int t = 0; t < a.tokens; ++t) {
+    unsigned int top = 0;
+    for (int c = tid * 8; c < columns; c += kThreads * 8) {
+      float v[8];
+      load_eight<T, WIDE>(x + t * x_ld + c, columns - c, v);
+      top = top_of(v, top);
+    }
+    top = wave_top(top);
+    if (lane == 0) most[t][wave] = top;
+  }
+  if (__syncthreads_or(failed != 0)) return;
+  for (int t = 0; t < a.tokens; ++t) {
+    bool none;
+    const float scale = quant_scale(max(max(most[t][0], most[t][1]), max(most[t][2], most[t][3])), none);
+    if (tid == 0) scales[t] = scale;
+    for (int c = tid * 8; c < bytes; c += kThreads * 8) {
+      float v[8];
+      load_eight<T, WIDE>(x + t * x_ld + c, columns - c, v);
+      *(u32x2 *)&rows[t * bytes + c] = quant_eight(v, scale, none);
     }
   }
+  __syncthreads();
+  const int8_t *xs = rows + min(l16, a.tokens - 1) * bytes;
+  i32x4 acc = {0, 0, 0, 0};
+#pragma unroll 1
+  for (int s0 = wave; s0 < steps; s0 += kOwnWaves * kAhead) {
+    if (s0 != wave) fetch(s0);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (s0 + k * kOwnWaves < steps)
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[k], *(const i32x4 *)(xs + (s0 + k * kOwnWaves) * 64 + q * 16), acc, 0, 0, 0);
+  }
+  sums[wave][lane] = acc;
+  __syncthreads();
+  if (wave == 0 && l16 < a.tokens)
+    put_four<T>(a, (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]), scales[l16], l16, n0 + q * 4, aligned);
 }
 
 // ---------------------------------------------------------------------------
 // The call
 // ---------------------------------------------------------------------------
-// The workspace: tokens in 8 bits, in rows of a multiple of 16 bytes, and their scales.
-static int64_t row_bytes(int32_t inputs) { return ((int64_t)inputs + 15) / 16 * 16; }
+// The workspace: tokens in 8 bits, in rows of whole stages, and their scales.
+static int64_t row_bytes(int32_t inputs) { return ((int64_t)inputs + kDepth - 1) / kDepth * kDepth; }
 static size_t linear_bytes(int64_t tokens, int32_t inputs) {
   return align_up((size_t)(tokens * row_bytes(inputs)), 256) + align_up((size_t)tokens * 4, 256);
 }
@@ -205,12 +417,47 @@ static bool bad_linear_size(int32_t tokens, int32_t outputs, int32_t inputs) {
   return tokens < 0 || outputs < 1 || inputs < 1 || inputs > kMaxInputs;
 }
 
+template <typename T, int TN, int TT, int WN, int WT, int BUFFERS>
+int launch_tiles(const Product &p, const int32_t *status, bool aligned, hipStream_t st) {
+  const int n_tiles = (p.outputs + TN - 1) / TN, t_tiles = (p.tokens + TT - 1) / TT;
+  product_kernel<T, TN, TT, WN, WT, BUFFERS>
+      <<<blocks_of_units((int64_t)n_tiles * t_tiles), 64 * WN * WT, 0, st>>>(p, status, aligned, n_tiles, t_tiles);
+  return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+}
+
+template <typename T, int TI, int TJ, int WAVES, int AHEAD>
+int launch_few(const Product &p, const int32_t *status, bool aligned, hipStream_t st) {
+  few_kernel<T, TI, TJ, WAVES, AHEAD><<<(unsigned)((p.outputs + 16 * TI - 1) / (16 * TI)), 64 * WAVES, 0, st>>>(p, status, aligned);
+  return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+}
+
+template <typename T> int launch_product(const Product &p, const int32_t *status, bool aligned, hipStream_t st) {
+  if (p.tokens <= 64) {
+    const bool many = (p.outputs + 15) / 16 >= 512;
+    if (p.tokens <= 16) return many ? launch_few<T, 1, 1, 4, 8>(p, status, aligned, st) : launch_few<T, 1, 1, 8, 8>(p, status, aligned, st);
+    if (p.tokens <= 32) return many ? launch_few<T, 2, 2, 8, 4>(p, status, aligned, st) : launch_few<T, 1, 2, 8, 4>(p, status, aligned, st);
+    return many ? launch_few<T, 2, 4, 8, 4>(p, status, aligned, st) : launch_few<T, 1, 4, 8, 4>(p, status, aligned, st);
+  }
+  auto tiles = [&](int64_t n, int64_t t) { return (p.outputs + n - 1) / n * ((p.tokens + t - 1) / t); };
+  if (tiles(256, 256) >= 192) return launch_tiles<T, 256, 256, 4, 4, 4>(p, status, aligned, st);
+  if (tiles(128, 128) >= 192) return launch_tiles<T, 128, 128, 2, 2, 4>(p, status, aligned, st);
+  return launch_tiles<T, 64, 64, 2, 2, 8>(p, status, aligned, st);
+}
+
 template <typename T> int launch_linear(const cortex_linear_i8_t &a, int32_t *status, void *ws, void *stream) {
   const hipStream_t st = (hipStream_t)stream;
   const int64_t row = row_bytes(a.inputs);
-  Product p = {(const int8_t *)a.x, a.w, a.x_ld, a.w_ld, a.y_ld, a.x_scale, a.w_scale, a.bias, a.y, a.tokens, a.outputs, (int32_t)(row / 16)};
+  Product p = {(const int8_t *)a.x, a.w, a.x_ld, a.w_ld, a.y_ld, a.x_scale, a.w_scale, a.bias, a.y, a.tokens, a.outputs, (a.inputs + 15) / 16};
   int8_t *rows = (int8_t *)ws;
   float *scales = (float *)(rows + align_up((size_t)(a.tokens * row), 256));
+  const bool aligned = a.y_ld % 4 == 0 && ((uintptr_t)a.y & (4 * sizeof(T) - 1)) == 0;
+  if (!a.x_scale && a.tokens <= kOwnTokens && a.tokens * row <= kOwnBytes) {
+    const unsigned grid = (unsigned)((a.outputs + 15) / 16);
+    const T *x = (const T *)a.x;
+    if (eights<T>(x, a.x_ld, a.inputs)) own_kernel<T, true><<<grid, 64 * kOwnWaves, 0, st>>>(p, x, a.x_ld, a.inputs, status, aligned);
+    else own_kernel<T, false><<<grid, 64 * kOwnWaves, 0, st>>>(p, x, a.x_ld, a.inputs, status, aligned);
+    return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+  }
   if (!a.x_scale) {
     const cortex_quant_i8_t q = {a.dtype, a.tokens, a.inputs, a.x, a.x_ld, rows, row, scales};
     const int rc = launch_quant<T>(q, status, (int)row, stream);
@@ -218,15 +465,13 @@ template <typename T> int launch_linear(const cortex_linear_i8_t &a, int32_t *st
     p.x = rows;
     p.x_ld = row;
     p.x_scale = scales;
-  } else if (a.inputs % 16 || a.x_ld % 16 || !aligned16(a.x)) {
+  } else if (a.inputs % kDepth || a.x_ld % 16 || a.x_ld > kMaxRow || !aligned16(a.x)) {
     pad_kernel<<<(unsigned)a.tokens, 256, 0, st>>>((const int8_t *)a.x, a.x_ld, a.inputs, rows, row, status);
     if (hipGetLastError() != hipSuccess) return CORTEX_E_HIP;
     p.x = rows;
     p.x_ld = row;
   }
-  const bool aligned = a.y_ld % 4 == 0 && ((uintptr_t)a.y & (4 * sizeof(T) - 1)) == 0;
-  product_kernel<T><<<dim3((a.outputs + kTile - 1) / kTile, (a.tokens + kTile - 1) / kTile), 256, 0, st>>>(p, status, aligned);
-  return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+  return launch_product<T>(p, status, aligned, st);
 }
 
 }  // namespace cortex
@@ -246,15 +491,16 @@ extern "C" int cortex_quant_i8(const cortex_quant_i8_t *a, int32_t *status, void
 }
 
 extern "C" size_t cortex_linear_i8_workspace_bytes(int32_t tokens, int32_t outputs, int32_t inputs) {
-  return bad_linear_size(tokens, outputs, inputs) ? 0 : linear_bytes(tokens, inputs) + 16;
+  if (bad_linear_size(tokens, outputs, inputs)) return 0;
+  return tokens ? linear_bytes(tokens, inputs) : 256;
 }
 
 extern "C" int cortex_linear_i8(const cortex_linear_i8_t *a, int32_t *status, void *ws, size_t ws_bytes, void *stream) {
   if (!a || !status) return CORTEX_E_INVAL;
   if (a->dtype != CORTEX_F32 && a->dtype != CORTEX_BF16) return CORTEX_E_INVAL;
-  // tiles of tokens are counted in 16 bits
-  if (bad_linear_size(a->tokens, a->outputs, a->inputs) || a->tokens > 65535 * kTile) return CORTEX_E_INVAL;
-  if (a->x_ld < a->inputs || a->y_ld < a->outputs || a->w_ld < row_bytes(a->inputs) || a->w_ld % 16) return CORTEX_E_INVAL;
+  // bringing tokens to 8 bits takes a workgroup of 256 each, and a grid has less than 2^32 threads
+  if (bad_linear_size(a->tokens, a->outputs, a->inputs) || a->tokens >= 1 << 24) return CORTEX_E_INVAL;
+  if (a->x_ld < a->inputs || a->y_ld < a->outputs || a->w_ld < a->inputs || a->w_ld % 16 || a->w_ld > kMaxRow) return CORTEX_E_INVAL;
   if (a->tokens == 0) return CORTEX_OK;
   if (!a->x || !a->w || !a->w_scale || !a->y || !aligned16(a->w)) return CORTEX_E_INVAL;
   if (!ws || !aligned16(ws)) return CORTEX_E_INVAL;

@@ -55,9 +55,9 @@ template <int LANES> __device__ __forceinline__ float lanes_sum(float v) {
 
 // Rows at 16-byte boundaries; LANES lanes a head.  A wave takes the rows (a
 // token's heads, queries then keys) from `first` on, `rows` of them.
-template <typename T, int LANES>
+template <typename T, int LANES, bool INTERLEAVED>
 __global__ void __launch_bounds__(64 * kNormWaves) norm_wide_kernel(cortex_qk_norm_t a, int32_t *status, int splits) {
-  constexpr int V = 16 / (int)sizeof(T);
+  constexpr int V = 16 / (int)sizeof(T), kRound = 64 / LANES, UNROLL = 2;
   __shared__ float turn[kNormWaves][2][kMaxHeadDim / 2];
   if (entry_status(status) != 0) return;
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(64 * kNormWaves) norm_wide_kernel(cortex_qk_no
   const bool works = part * 2 * V < P;
   // the lane's two pieces
   int lo = part * 2 * V, hi = lo + V;
-  if (!a.interleaved && lo < R) {
+  if (!INTERLEAVED && lo < R) {
     lo = part * V;
     hi = R / 2 + lo;
   }
@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(64 * kNormWaves) norm_wide_kernel(cortex_qk_no
     if (turns)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const int at = a.interleaved ? lo / 2 + i : lo + i;
+        const int at = INTERLEAVED ? lo / 2 + i : lo + i;
         if (at < R / 2) {
           c[i] = turn[wave][0][at];
           s[i] = turn[wave][1][at];
@@ -98,47 +98,61 @@ __global__ void __launch_bounds__(64 * kNormWaves) norm_wide_kernel(cortex_qk_no
       }
   }
   const int each = (total + splits - 1) / splits, first = (int)(task % splits) * each, last = min(first + each, total);
-  for (int r = first + group; r < last; r += 64 / LANES) {
-    const NormRow<T> row = norm_row<T>(a, t, r);
-    float x[2 * V];
-    {
-      float u[V], w[V];
-      Pack<T, V>::load(row.in + lo, u);
-      Pack<T, V>::load(row.in + hi, w);
+  // Heads of q, then of k, each with their weights in registers; UNROLL rounds' loads are
+  // made at once.
+  auto run = [&](const T *in, T *out, const float *weight, int from, int to) {
+    if (from >= to) return;
+    float g[2 * V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        x[i] = u[i];
-        x[V + i] = w[i];
+    for (int i = 0; i < V; ++i) {
+      g[i] = weight ? weight[lo + i] : 1.0f;
+      g[V + i] = weight ? weight[hi + i] : 1.0f;
+    }
+    for (int r0 = from + group; r0 - group < to; r0 += kRound * UNROLL) {
+      typedef T pack __attribute__((ext_vector_type(V)));
+      pack u[UNROLL], w[UNROLL];
+#pragma unroll
+      for (int k = 0; k < UNROLL; ++k) {
+        const T *p = in + (int64_t)min(r0 + k * kRound, to - 1) * P;
+        u[k] = *(const pack *)(p + lo);
+        w[k] = *(const pack *)(p + hi);
+      }
+#pragma unroll
+      for (int k = 0; k < UNROLL; ++k) {
+        float x[2 * V], squares = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          x[i] = to_float<T>(u[k][i]);
+          x[V + i] = to_float<T>(w[k][i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) squares = __builtin_fmaf(x[i], x[i], squares);
+        const float m = norm_scale(a, lanes_sum<LANES>(works ? squares : 0.0f));
+#pragma unroll
+        for (int i = 0; i < 2 * V; ++i) x[i] *= m * g[i];
+        float y[2][V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const float f = INTERLEAVED ? x[2 * i] : x[i], h = INTERLEAVED ? x[2 * i + 1] : x[V + i];
+          const float d = f * c[i] - h * s[i], e = h * c[i] + f * s[i];
+          if (INTERLEAVED) {
+            y[2 * i / V][2 * i % V] = d;
+            y[2 * i / V][2 * i % V + 1] = e;
+          } else {
+            y[0][i] = d;
+            y[1][i] = e;
+          }
+        }
+        const int r = r0 + k * kRound;
+        if (works && r < to) {
+          Pack<T, V>::store(out + (int64_t)r * P + lo, y[0]);
+          Pack<T, V>::store(out + (int64_t)r * P + hi, y[1]);
+        }
       }
     }
-    float squares = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 2 * V; ++i) squares = __builtin_fmaf(x[i], x[i], squares);
-    const float m = norm_scale(a, lanes_sum<LANES>(works ? squares : 0.0f));
-#pragma unroll
-    for (int i = 0; i < 2 * V; ++i) {
-      x[i] *= m;
-      if (row.weight) x[i] *= row.weight[(i < V ? lo : hi - V) + i];
-    }
-    float y[2][V];
-    if (a.interleaved) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        y[2 * i / V][2 * i % V] = x[2 * i] * c[i] - x[2 * i + 1] * s[i];
-        y[2 * i / V][2 * i % V + 1] = x[2 * i + 1] * c[i] + x[2 * i] * s[i];
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        y[0][i] = x[i] * c[i] - x[V + i] * s[i];
-        y[1][i] = x[V + i] * c[i] + x[i] * s[i];
-      }
-    }
-    if (works) {
-      Pack<T, V>::store(row.out + lo, y[0]);
-      Pack<T, V>::store(row.out + hi, y[1]);
-    }
-  }
+  };
+  run((const T *)a.q + t * a.q_ld, (T *)a.q_out + t * a.q_out_ld, a.q_weight, first, min(last, a.heads));
+  run((const T *)a.k + t * a.k_ld, (T *)a.k_out + t * a.k_out_ld, a.k_weight, max(first - a.heads, 0), last - a.heads);
 }
 
 // Any alignment and any even sizes: a wave a head, pairs by lane.
@@ -185,8 +199,10 @@ __global__ void __launch_bounds__(64 * kNormWaves) norm_pair_kernel(cortex_qk_no
 
 template <typename T, int LANES> int launch_wide(const cortex_qk_norm_t &a, int32_t *status, int splits, void *stream) {
   const int64_t tasks = (int64_t)a.num_tokens * splits;
-  norm_wide_kernel<T, LANES><<<(unsigned)((tasks + kNormWaves - 1) / kNormWaves), 64 * kNormWaves, 0, (hipStream_t)stream>>>(
-      a, status, splits);
+  const unsigned grid = (unsigned)((tasks + kNormWaves - 1) / kNormWaves);
+  const hipStream_t st = (hipStream_t)stream;
+  if (a.interleaved) norm_wide_kernel<T, LANES, true><<<grid, 64 * kNormWaves, 0, st>>>(a, status, splits);
+  else norm_wide_kernel<T, LANES, false><<<grid, 64 * kNormWaves, 0, st>>>(a, status, splits);
   return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
 }
 

@@ -194,15 +194,6 @@ __device__ __forceinline__ bf16x8v join8(s16x4 a, s16x4 b) {
   return __builtin_bit_cast(bf16x8v, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Workgroups go to the eight XCDs in turn.  Each XCD takes a run of neighbouring
-// units (slot by slot, a slot's heads together), so that the heads of a group find
-// its B and C in the L2 that they share.
-__device__ __forceinline__ int64_t unit_of_block(int64_t units) {
-  const int64_t per = (units + 7) / 8;
-  return (int64_t)(blockIdx.x % 8) * per + blockIdx.x / 8;
-}
-inline unsigned blocks_of_units(int64_t units) { return (unsigned)((units + 7) / 8 * 8); }
-
 // PART as for the channel scan: 0 whole sequences, 1 a segment's state from
 // zero, 2 outputs from the state that enters it.
 template <int N, int PART, bool WIDE>

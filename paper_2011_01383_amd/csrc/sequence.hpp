@@ -201,6 +201,14 @@ struct SegmentScratch {
   float *steps;      // [slots, channels or heads]: its sum of dt
 };
 
+// Workgroups go to the eight XCDs in turn.  Each XCD takes a run of neighbouring
+// units, so that those which read the same rows find them in the L2 that they share.
+__device__ __forceinline__ int64_t unit_of_block(int64_t units) {
+  const int64_t per = (units + 7) / 8;
+  return (int64_t)(blockIdx.x % 8) * per + blockIdx.x / 8;
+}
+inline unsigned blocks_of_units(int64_t units) { return (unsigned)((units + 7) / 8 * 8); }
+
 inline bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
 // Grids count tiles of channels in 16 bits.

@@ -124,7 +124,7 @@ def linear_args(**kw):
 @pytest.mark.parametrize("bad", [
     dict(dtype=2), dict(tokens=-1), dict(inputs=0), dict(inputs=131072, x_ld=131072, w_ld=131072), dict(outputs=0), dict(x=None),
     dict(w=None), dict(w_scale=None), dict(y=None), dict(x_ld=39), dict(w_ld=40), dict(w_ld=56), dict(w_ld=32), dict(y_ld=7),
-    dict(w=P8 + 8), dict(tokens=1 << 30)])
+    dict(w=P8 + 8), dict(w_ld=(1 << 24) + 16), dict(tokens=1 << 24)])
 def test_linear_refuses(lib, bad):
     assert lib.cortex_linear_i8(ctypes.byref(linear_args(**bad)), P8, P8, 1 << 50, None) == C.CORTEX_E_INVAL
 
