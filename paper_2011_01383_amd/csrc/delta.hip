@@ -118,11 +118,12 @@ void launch_walk(const cortex_delta_t &a, int32_t *status, const ChunkMap *maps,
 template <typename T, int K, bool WIDE> int launch_chunks_of(const cortex_delta_t &a, int32_t *status, ChunkMap *maps, void *stream) {
   const hipStream_t st = (hipStream_t)stream;
   const int64_t chunks = chunk_slots(a.num_tokens, a.num_seqs, kChunk) * a.heads;
-  chunk_maps_kernel<T, K, WIDE><<<blocks_of_units(chunks), kChunkThreads, 0, st>>>(a, status, maps, chunks);
-  if (!launched()) return CORTEX_E_HIP;
   const int64_t units = (int64_t)a.num_seqs * a.heads * (a.value_dim / 16);
-  if (units <= 1024) chunk_chain_kernel<T, K, WIDE><<<blocks_of_units(units), 2 * kChunkThreads, 0, st>>>(a, status, maps, units);
-  else if (sizeof(T) == 2 && a.value_dim % 32 == 0) launch_walk<T, K, sizeof(T) == 2 ? 2 : 1, WIDE>(a, status, maps, st);
+  const bool few = units <= 1024;
+  if (few) chunk_maps_kernel<T, K, false, WIDE><<<blocks_of_units(chunks), kChunkThreads, 0, st>>>(a, status, maps, chunks);
+  else chunk_maps_kernel<T, K, true, WIDE><<<blocks_of_units(chunks), kChunkThreads, 0, st>>>(a, status, maps, chunks);
+  if (!launched()) return CORTEX_E_HIP;
+  if (few) chunk_chain_kernel<T, K, WIDE><<<blocks_of_units(units), kChainThreads, 0, st>>>(a, status, maps, units);
   else launch_walk<T, K, 1, WIDE>(a, status, maps, st);
   return launched() ? CORTEX_OK : CORTEX_E_HIP;
 }

@@ -31,21 +31,26 @@ namespace cortex {
 constexpr int kChunk = 64;
 constexpr int kChunkWaves = 4;                   // 16 tokens each
 constexpr int kChunkThreads = 64 * kChunkWaves;
+constexpr int kChainThreads = 2 * kChunkThreads + 64;
 
-// What the first launch leaves for a chunk and head.  Operand pieces of T and P: rows
+// What the first launch leaves for a chunk and head.  Operand pieces of T: rows
 // 16 w .. + 15, 32 tokens m = 0 .. w / 2; a lane's eight values in each of three planes.
 constexpr int kMapPieces = 6;
 // (For w < 2 there is no m = 1: its number names the wave's one piece.)
 __device__ __forceinline__ constexpr int map_piece(int w, int m) { return w < 2 ? w : 2 * w - 2 + m; }
+// Tiles of P: rows 16 w .. + 15 by tokens 16 c .. + 15, c <= w; a lane has tokens 4 q .. + 3 of row lane & 15.
+constexpr int kMapTiles = 10;
+__device__ __forceinline__ constexpr int map_tile(int w, int c) { return w * (w + 1) / 2 + c; }
+enum { kBeta, kGrow, kWeight, kRest, kGates };
 struct alignas(16) ChunkMap {
   u32x4v T[kMapPieces][3][64];
-  u32x4v P[kMapPieces][3][64];
-  float beta[kChunk];      // 0 past the sequence's end
-  float grow[kChunk];      // exp(c_i)
-  float weight[kChunk];    // exp(c_63 - c_i)
-  float decay;             // exp(c_63)
-  int first;               // first token that loses the whole head (not finite), or kChunk
-  int pad[62];
+  union {
+    f32x4 P[kMapTiles][64];
+    u32x4v pieces[kMapPieces][3][64];            // of P, as T's
+  };
+  // beta_i (0 past the sequence's end); exp(c_i); exp(c_63 - c_i); then exp(c_63) and the first token
+  // that loses the whole head (not finite), or kChunk.
+  float gates[kGates][kChunk];
 };
 static_assert(sizeof(ChunkMap) % 256 == 0, "maps start at 256 bytes");
 
@@ -139,17 +144,20 @@ __device__ __forceinline__ f32x4 mul_block(f32x4 a, f32x4 b, f32x4 c) {
   return c;
 }
 
-// T and P of a chunk and head.  A wave has 16 rows of both; the products k . k and
-// q . k are computed with the earlier token as the result's row, so a lane ends with four
-// earlier tokens of its own row, which is how P is handed on.  T's blocks of 16 on the
-// diagonal are inverted by substitution, a lane a column, then joined in two
-// rounds: the corner below two inverses T1, T2 is - T2 L21 T1 (float32 matrix units).
-template <typename T, int K, bool WIDE>
-__global__ void __launch_bounds__(kChunkThreads, 2) chunk_maps_kernel(cortex_delta_t a, int32_t *status, ChunkMap *maps, int64_t units) {
+// T, P and the gates of a chunk and head.  A wave has 16 rows; the products k . k and q . k are computed with
+// the earlier token as the result's row, so a lane ends with four earlier tokens of its own row.
+// T's blocks of 16 on the diagonal are inverted by substitution, a lane a column, then
+// joined in two rounds: the corner below two inverses T1, T2 is - T2 L21 T1 (float32 matrix
+// units).  A block of T takes the place of L's once that is used up.
+template <typename T, int K, bool PIECES, bool WIDE>
+__global__ void __launch_bounds__(kChunkThreads, 4) chunk_maps_kernel(cortex_delta_t a, int32_t *status, ChunkMap *maps, int64_t units) {
   constexpr int KP = kKeyPlanes<T>, M = K / 32;
+  typedef Rows<K> K_;
   __shared__ struct {
-    alignas(16) float L[kChunk * kMatrixRow];
-    alignas(16) float inverse[kChunk * kMatrixRow];
+    union {
+      alignas(16) float L[kChunk * kMatrixRow];
+      alignas(16) unsigned short keys[KP][kChunk * K_::kStride];
+    };
     alignas(16) float cum[kChunk], low[kChunk], beta[kChunk];
     int first;
   } lds;
@@ -164,53 +172,51 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_maps_kernel(cortex_del
   if (tid == 0) lds.first = kChunk;
   if (__syncthreads_or(failed != 0)) return;
   ChunkMap &map = maps[(int64_t)slot * a.heads + head];
-  const int last = ch.end - 1 - ch.begin;
+  const int last = ch.end - 1 - ch.begin, i = w * 16 + l16;
 
   const T *ks = (const T *)a.k + (int64_t)ch.begin * a.k_ld + g * K + q * 8;
   const T *qs = (const T *)a.q + (int64_t)ch.begin * a.q_ld + g * K + q * 8;
-  const int64_t own = min(w * 16 + l16, last);
   bf16x8v kf[M][KP], qf[M][KP];
   {
-    Eight<T> kr[M], qr[M];
+    Eight<T> raw[M], qr[M];
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-      kr[m].template load<WIDE>(ks + own * a.k_ld + m * 32);
-      qr[m].template load<WIDE>(qs + own * a.q_ld + m * 32);
+      raw[m].template load<WIDE>(ks + (int64_t)min(i, last) * a.k_ld + m * 32);
+      qr[m].template load<WIDE>(qs + (int64_t)min(i, last) * a.q_ld + m * 32);
+    }
+    if (w == 0) {
+      const int64_t t = ch.begin + min(lane, last);
+      float e = 0.0f;
+      if (a.A) {
+        const float v = to_float<T>(((const T *)a.dt)[t * a.dt_ld + head]) + (a.dt_bias ? a.dt_bias[head] : 0.0f);
+        e = (a.softplus ? softplus(v) : v) * decay_rate(a.A[head]);
+      }
+      const float b = to_float<T>(((const T *)a.b)[t * a.b_ld + head]);
+      float beta = a.sigmoid ? sigmoid(b) : b;
+      // An exponent is held to -256, which leaves nothing of the state, so that no sum is infinite.
+      float held = e < -256.0f ? -256.0f : e;
+      if (lane > last) beta = held = 0.0f;
+      if (!finite(beta) || !finite(held)) {
+        atomicMin(&lds.first, lane);
+        beta = held = 0.0f;
+      }
+      float low, after_low;
+      const float up = exact_lane_sums(held, low);
+      const float down = exact_lane_sums(__shfl_xor(held, 63), after_low);      // from token 63 - lane on
+      const float after = __shfl_up(down, 1);
+      lds.cum[lane] = up;
+      lds.low[lane] = low;
+      lds.beta[lane] = beta;
+      map.gates[kBeta][lane] = beta;
+      map.gates[kGrow][lane] = fast_exp2(up);
+      map.gates[kWeight][63 - lane] = fast_exp2(lane == 0 ? 0.0f : after);
+      if (lane == 63) map.gates[kRest][0] = fast_exp2(down);
     }
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-      kr[m].planes(kf[m]);
+      raw[m].planes(kf[m]);
       qr[m].planes(qf[m]);
     }
-  }
-  if (w == 0) {
-    const int64_t t = ch.begin + min(lane, last);
-    const bool live = lane <= last;
-    float e = 0.0f;
-    if (a.A) {
-      const float raw = to_float<T>(((const T *)a.dt)[t * a.dt_ld + head]) + (a.dt_bias ? a.dt_bias[head] : 0.0f);
-      e = (a.softplus ? softplus(raw) : raw) * decay_rate(a.A[head]);
-    }
-    const float b = to_float<T>(((const T *)a.b)[t * a.b_ld + head]);
-    float beta = a.sigmoid ? sigmoid(b) : b;
-    // An exponent is held to -256, which leaves nothing of the state, so that no sum is infinite.
-    float held = e < -256.0f ? -256.0f : e;
-    if (!live) beta = held = 0.0f;
-    if (!finite(beta) || !finite(held)) {
-      atomicMin(&lds.first, lane);
-      beta = held = 0.0f;
-    }
-    float low, after_low;
-    const float up = exact_lane_sums(held, low);
-    const float down = exact_lane_sums(__shfl_xor(held, 63), after_low);      // from token 63 - lane on
-    const float after = __shfl_up(down, 1);
-    lds.cum[lane] = up;
-    lds.low[lane] = low;
-    lds.beta[lane] = beta;
-    map.beta[lane] = beta;
-    map.grow[lane] = fast_exp2(up);
-    map.weight[63 - lane] = fast_exp2(lane == 0 ? 0.0f : after);
-    if (lane == 63) map.decay = fast_exp2(down);
   }
   // a key that is not finite
   {
@@ -219,60 +225,71 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_maps_kernel(cortex_del
     for (int m = 0; m < M; ++m) {
       const u32x4v bits = __builtin_bit_cast(u32x4v, kf[m][0]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) odd |= (((bits[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0;
+      for (int r = 0; r < 4; ++r) odd |= (((bits[r] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0;
     }
-    if (odd && w * 16 + l16 <= last) atomicMin(&lds.first, w * 16 + l16);
+    if (odd && i <= last) atomicMin(&lds.first, i);
   }
+#pragma unroll
+  for (int m = 0; m < M; ++m)
+#pragma unroll
+    for (int p = 0; p < KP; ++p) *(u32x4v *)&lds.keys[p][K_::at(i, m * 32 + q * 8)] = __builtin_bit_cast(u32x4v, kf[m][p]);
   __syncthreads();
-  const int i = w * 16 + l16;
-  const float ci = lds.cum[i], li = lds.low[i], bi = lds.beta[i];
-  float pv[2][4];
+  f32x4 l[kChunkWaves], s[kChunkWaves];
 #pragma unroll
   for (int c = 0; c < kChunkWaves; ++c) {
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    l[c] = s[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (c <= w) {
-      Parts kp, qp;
-      const int64_t row = min(c * 16 + l16, last);
+      Parts kk, qk;
 #pragma unroll
       for (int m = 0; m < M; ++m) {
-        Eight<T> raw;
         bf16x8v f[KP];
-        raw.template load<WIDE>(ks + row * a.k_ld + m * 32);
-        raw.planes(f);
-        kp.add(f, kf[m]);
-        qp.add(f, qf[m]);
+#pragma unroll
+        for (int p = 0; p < KP; ++p) f[p] = lds8(&lds.keys[p][K_::at(c * 16 + l16, m * 32 + q * 8)]);
+        kk.add(f, kf[m]);
+        qk.add(f, qf[m]);
       }
-      const f32x4 kk = kp.sum(), qk = qp.sum();
+      l[c] = kk.sum();
+      s[c] = qk.sum();
+    }
+  }
+  const float ci = lds.cum[i], li = lds.low[i], bi = lds.beta[i];
+  __syncthreads();                               // the keys are read: L takes their place
+#pragma unroll
+  for (int c = 0; c < kChunkWaves; ++c)
+    if (c <= w) {
       const int j0 = c * 16 + q * 4;
       const f32x4 cj = *(const f32x4 *)&lds.cum[j0], lj = *(const f32x4 *)&lds.low[j0];
-      f32x4 l;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
 #pragma clang fp reassociate(off)
         const float e = fast_exp2((ci - cj[r]) + (li - lj[r]));
-        l[r] = j0 + r < i ? bi * e * kk[r] : 0.0f;
-        v[r] = j0 + r <= i ? a.scale * e * qk[r] : 0.0f;
-        if (!finite(l[r])) {
+        l[c][r] = j0 + r < i ? bi * e * l[c][r] : 0.0f;
+        s[c][r] = j0 + r <= i ? a.scale * e * s[c][r] : 0.0f;
+        if (!finite(l[c][r])) {
           atomicMin(&lds.first, i);
-          l[r] = 0.0f;
+          l[c][r] = 0.0f;
         }
       }
-      *(f32x4 *)&lds.L[i * kMatrixRow + j0] = l;
+      *(f32x4 *)&lds.L[i * kMatrixRow + j0] = l[c];
+      if (!PIECES) map.P[map_tile(w, c)][lane] = s[c];
     }
+  if (PIECES)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) pv[c % 2][r] = v[r];
-    if (c % 2 == 1 && c / 2 <= w / 2) {
-      float e[8] = {pv[0][0], pv[0][1], pv[0][2], pv[0][3], pv[1][0], pv[1][1], pv[1][2], pv[1][3]};
-      bf16x8v p[3];
-      planes8(e, p);
+    for (int m = 0; m < 2; ++m)
+      if (m <= w / 2) {
+        float e[8] = {s[2 * m][0], s[2 * m][1], s[2 * m][2], s[2 * m][3], s[2 * m + 1][0], s[2 * m + 1][1], s[2 * m + 1][2], s[2 * m + 1][3]};
+        bf16x8v p[3];
+        planes8(e, p);
 #pragma unroll
-      for (int n = 0; n < 3; ++n) map.P[map_piece(w, c / 2)][n][lane] = __builtin_bit_cast(u32x4v, p[n]);
-    }
-  }
+        for (int n = 0; n < 3; ++n) map.pieces[map_piece(w, m)][n][lane] = __builtin_bit_cast(u32x4v, p[n]);
+      }
   // The wave's own block on the diagonal: its rows were written by the wave itself.
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  auto wave_fence = [] {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  wave_fence();
   {
     float x[16];
 #pragma unroll
@@ -280,30 +297,36 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_maps_kernel(cortex_del
       x[r] = r == l16 ? 1.0f : 0.0f;
 #pragma unroll
       for (int s = 0; s < r; ++s) x[r] = __builtin_fmaf(-lds.L[(w * 16 + r) * kMatrixRow + w * 16 + s], x[s], x[r]);
-      if (r / 4 == q) lds.inverse[(w * 16 + r) * kMatrixRow + w * 16 + l16] = x[r];
     }
+    wave_fence();
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (r / 4 == q) lds.L[(w * 16 + r) * kMatrixRow + w * 16 + l16] = x[r];
   }
   __syncthreads();
   const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
   auto put_block = [&](int rb, int cb, f32x4 v) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) lds.inverse[(rb * 16 + q * 4 + r) * kMatrixRow + cb * 16 + l16] = -v[r];
+    for (int r = 0; r < 4; ++r) lds.L[(rb * 16 + q * 4 + r) * kMatrixRow + cb * 16 + l16] = -v[r];
   };
   if (w < 2) {
     const int b = 2 * w;
-    const f32x4 x = mul_block(block_left(lds.L, b + 1, b, l16, q), block_right(lds.inverse, b, b, l16, q), zero);
-    put_block(b + 1, b, mul_block(block_left(lds.inverse, b + 1, b + 1, l16, q), x, zero));
+    const f32x4 x = mul_block(block_left(lds.L, b + 1, b, l16, q), block_right(lds.L, b, b, l16, q), zero);
+    const f32x4 y = mul_block(block_left(lds.L, b + 1, b + 1, l16, q), x, zero);
+    wave_fence();
+    put_block(b + 1, b, y);
   }
   __syncthreads();
   {
     const int rb = 2 + w / 2, cb = w % 2;
     auto corner = [&](int s) {
-      f32x4 y = zero;
-      for (int c = cb; c < 2; ++c) y = mul_block(block_left(lds.L, s, c, l16, q), block_right(lds.inverse, c, cb, l16, q), y);
+      f32x4 y = mul_block(block_left(lds.L, s, 1, l16, q), block_right(lds.L, 1, cb, l16, q), zero);
+      if (cb == 0) y = mul_block(block_left(lds.L, s, 0, l16, q), block_right(lds.L, 0, 0, l16, q), y);
       return y;
     };
-    f32x4 y = mul_block(block_left(lds.inverse, rb, 2, l16, q), corner(2), zero);
-    if (rb == 3) y = mul_block(block_left(lds.inverse, 3, 3, l16, q), corner(3), y);
+    f32x4 y = mul_block(block_left(lds.L, rb, 2, l16, q), corner(2), zero);
+    if (rb == 3) y = mul_block(block_left(lds.L, 3, 3, l16, q), corner(3), y);
+    __syncthreads();                             // L's blocks there are read
     put_block(rb, cb, y);
   }
   __syncthreads();
@@ -314,7 +337,7 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_maps_kernel(cortex_del
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       f32x4 v = zero;
-      if (2 * m + s <= w) v = *(const f32x4 *)&lds.inverse[i * kMatrixRow + m * 32 + s * 16 + q * 4];
+      if (2 * m + s <= w) v = *(const f32x4 *)&lds.L[i * kMatrixRow + m * 32 + s * 16 + q * 4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) e[4 * s + r] = v[r];
     }
@@ -323,7 +346,7 @@ __global__ void __launch_bounds__(kChunkThreads, 2) chunk_maps_kernel(cortex_del
 #pragma unroll
     for (int n = 0; n < 3; ++n) map.T[map_piece(w, m)][n][lane] = __builtin_bit_cast(u32x4v, p[n]);
   }
-  if (tid == 0) map.first = lds.first;
+  if (tid == 0) map.gates[kRest][1] = __builtin_bit_cast(float, lds.first);
 }
 
 // Products of planes, the largest part last: which plane of a and of b.
@@ -353,19 +376,32 @@ __device__ __forceinline__ void drop_odd(f32x4 (&v)[4], int q, int &first) {
   first = min(first, __shfl_xor(first, 32));
 }
 
+// Rows of K elements in LDS, one after another, as copies straight from memory leave them; their
+// 16-byte pieces are exchanged so that the rows and pieces that the hardware serves together lie in
+// different banks (see Rows).
+template <int K> struct Packed {
+  static constexpr int kPieces = K / 8;
+  static __device__ __forceinline__ int place(int row, int piece) {
+    return piece ^ (kPieces == 16 ? row & 15 : kPieces == 8 ? row >> 1 & 7 : -(row >> 2) & 3);
+  }
+  static __device__ __forceinline__ int at(int row, int e) { return row * K + place(row, e >> 3) * 8 + (e & 7); }
+};
+
 template <typename T, int K> struct ChunkLds {
   static constexpr int KP = kKeyPlanes<T>;
-  typedef Rows<K> K_;
-  alignas(16) unsigned short keys[KP][kChunk * K_::kStride];
-  alignas(16) unsigned short queries[KP][kChunk * K_::kStride];
-  alignas(16) float beta[kChunk], grow[kChunk], weight[kChunk];
+  typedef Packed<K> K_;
+  alignas(1024) unsigned short keys[KP][kChunk * K];
+  alignas(1024) unsigned short queries[KP][kChunk * K];
+  alignas(1024) u32x4v inverse[kMapPieces][3][64];
+  alignas(1024) u32x4v scores[kMapPieces][3][64];
+  alignas(1024) float gates[kGates][kChunk];
 };
 
 // A wave has 16 NT columns of the state (value channels) for all tokens and keys of its head, so
 // what one product leaves is the next one's operand in the same lane and nothing goes
-// between waves; a workgroup's waves share the keys and queries in LDS.
+// between waves; keys, queries, T and P are shared in LDS.
 template <typename T, int K, int NT, bool WIDE>
-__global__ void __launch_bounds__(kChunkThreads) chunk_walk_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps, int64_t units) {
+__global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 : 1) chunk_walk_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps, int64_t units) {
   typedef ChunkLds<T, K> Lds;
   constexpr int KP = Lds::KP, M = K / 32;
   constexpr int kItems = kChunk * (K / 8) / kChunkThreads;     // eights of keys that a thread brings in
@@ -373,13 +409,15 @@ __global__ void __launch_bounds__(kChunkThreads) chunk_walk_kernel(cortex_delta_
   const int failed = entry_status(status);
   const int64_t unit = unit_of_block(units);
   if (unit >= units) return;
-  const int tid = (int)threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, l16 = lane & 15;
-  const int V = a.value_dim, wide = 16 * NT * kChunkWaves, slices = (V + wide - 1) / wide, per = a.heads * slices;
-  const int seq = (int)(unit / per), rest = (int)(unit % per), head = rest / slices;
-  const int v0 = rest % slices * wide + w * 16 * NT;
+  const int tid = (int)threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, l16 = lane & 15;
+  // a head's sequences are neighbours: an XCD's run of units has long and short ones
+  const int V = a.value_dim, wide = 16 * NT * kChunkWaves, slices = (V + wide - 1) / wide;
+  const int slice = (int)(unit % slices), seq = (int)(unit / slices % a.num_seqs), head = (int)(unit / slices / a.num_seqs);
+  const int v0 = slice * wide + w * 16 * NT;
   const bool works = v0 < V;
   const int g = head / (a.heads / a.key_heads);
-  const int begin = a.seq_offsets[seq], end = a.seq_offsets[seq + 1];
+  // (the same in every lane, and the compiler is told so)
+  const int begin = __builtin_amdgcn_readfirstlane(a.seq_offsets[seq]), end = __builtin_amdgcn_readfirstlane(a.seq_offsets[seq + 1]);
   if (begin < 0 || end < begin || end > a.num_tokens) return;
   int pool = -1;
   if (a.state_in || a.state_out) {
@@ -402,61 +440,67 @@ __global__ void __launch_bounds__(kChunkThreads) chunk_walk_kernel(cortex_delta_
   const T *ks = (const T *)a.k + g * K, *qs = (const T *)a.q + g * K;
   const T *vs = (const T *)a.v + (int64_t)head * V + col;
   T *ys = (T *)a.y + (int64_t)head * V + col;
-  Eight<T> kr[kItems], qr[kItems];
-  // Rows past the sequence's end repeat its last.
-  auto load_rows = [&](int64_t t0) {
-    const int last = (int)min((int64_t)kChunk, end - t0) - 1;
-    const T *k0 = ks + t0 * a.k_ld, *q0 = qs + t0 * a.q_ld;
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const int id = i * kChunkThreads + tid;
-      const uint32_t row = min(id / (K / 8), last), o = id % (K / 8) * 8;
-      kr[i].template load<WIDE>(k0 + (row * (uint32_t)a.k_ld + o));
-      qr[i].template load<WIDE>(q0 + (row * (uint32_t)a.q_ld + o));
-    }
-  };
-  if (begin < end) load_rows(begin);
 #pragma unroll 1
-  for (int64_t t0 = begin; t0 < end; t0 += kChunk, map += a.heads) {
-    const int last = (int)min((int64_t)kChunk, end - t0) - 1;
+  for (int t0 = begin; t0 < end; t0 += kChunk, map += a.heads) {
+    const int last = min(kChunk, end - t0) - 1;
     __syncthreads();                             // the last chunk's rows are read
+    // T, P and gates, then keys and queries (bf16 in whole 16-byte pieces: straight into LDS).  Rows past
+    // the sequence's end repeat its last; places in a chunk are 32 bits (the host admits no longer rows).
+    constexpr int kCopies = kMapPieces * 3 * 2;
+    static_assert(kCopies % kChunkWaves == 0 && sizeof(ChunkMap) == (kCopies + 1) * 1024, "copies of 1 KB, the gates' last");
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const int id = i * kChunkThreads + tid, at = Lds::K_::at(id / (K / 8), id % (K / 8) * 8);
-      bf16x8v kf[KP], qf[KP];
-      kr[i].planes(kf);
-      qr[i].planes(qf);
+    for (int i = 0; i < kCopies / kChunkWaves; ++i) {
+      const int c = w * (kCopies / kChunkWaves) + i;
+      copy_to_lds(map, (uint32_t)(c * 1024 + lane * 16), lds_place(lds.inverse) + (uint32_t)c * 1024);
+    }
+    if (w == 0) copy_to_lds(map, (uint32_t)(kCopies * 1024 + lane * 16), lds_place(lds.gates));
+    const T *k0 = ks + (int64_t)t0 * a.k_ld, *q0 = qs + (int64_t)t0 * a.q_ld;
+    if constexpr (KP == 1 && WIDE) {
+      constexpr int kRows = 512 / K;             // of a copy
 #pragma unroll
-      for (int p = 0; p < KP; ++p) {
-        *(u32x4v *)&lds.keys[p][at] = __builtin_bit_cast(u32x4v, kf[p]);
-        *(u32x4v *)&lds.queries[p][at] = __builtin_bit_cast(u32x4v, qf[p]);
+      for (int i = 0; i < kChunk / kRows / kChunkWaves; ++i) {
+        const int first = (w * (kChunk / kRows / kChunkWaves) + i) * kRows, row = first + lane / (K / 8);
+        const uint32_t e = (uint32_t)Lds::K_::place(row, lane % (K / 8)) * 8, r = (uint32_t)min(row, last);
+        copy_to_lds(k0, (r * (uint32_t)a.k_ld + e) * 2, lds_place(lds.keys) + (uint32_t)(first * K * 2));
+        copy_to_lds(q0, (r * (uint32_t)a.q_ld + e) * 2, lds_place(lds.queries) + (uint32_t)(first * K * 2));
+      }
+    } else {
+      Eight<T> kr[kItems], qr[kItems];
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) {
+        const int id = i * kChunkThreads + tid;
+        const uint32_t row = min(id / (K / 8), last), o = id % (K / 8) * 8;
+        kr[i].template load<WIDE>(k0 + (row * (uint32_t)a.k_ld + o));
+        qr[i].template load<WIDE>(q0 + (row * (uint32_t)a.q_ld + o));
+      }
+#pragma unroll
+      for (int i = 0; i < kItems; ++i) {
+        const int id = i * kChunkThreads + tid, at = Lds::K_::at(id / (K / 8), id % (K / 8) * 8);
+        bf16x8v kf[KP], qf[KP];
+        kr[i].planes(kf);
+        qr[i].planes(qf);
+#pragma unroll
+        for (int p = 0; p < KP; ++p) {
+          *(u32x4v *)&lds.keys[p][at] = __builtin_bit_cast(u32x4v, kf[p]);
+          *(u32x4v *)&lds.queries[p][at] = __builtin_bit_cast(u32x4v, qf[p]);
+        }
       }
     }
-    if (tid < kChunk) {
-      lds.beta[tid] = map->beta[tid];
-      lds.grow[tid] = map->grow[tid];
-      lds.weight[tid] = map->weight[tid];
-    }
-    u32x4v tr[kMapPieces][3];
-#pragma unroll
-    for (int i = 0; i < kMapPieces; ++i)
-#pragma unroll
-      for (int p = 0; p < 3; ++p) tr[i][p] = map->T[i][p][lane];
     T v[4][4][NT];
-    const T *vt = vs + t0 * a.v_ld;
+    const T *vt = vs + (int64_t)t0 * a.v_ld;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int n = 0; n < NT; ++n) v[t][r][n] = vt[(uint32_t)min(t * 16 + q * 4 + r, last) * (uint32_t)a.v_ld + n];
-    const float decay = map->decay;
+    copies_done<0>();
+    __syncthreads();                             // keys, queries, T, P and gates are there
+    if (!works) continue;
+    const float decay = lds.gates[kRest][0];
     int first[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) first[n] = map->first;
-    load_rows(t0 + kChunk < end ? t0 + kChunk : t0);
-    __syncthreads();                             // keys, queries and gates are there
-    if (!works) continue;
+    for (int n = 0; n < NT; ++n) first[n] = __builtin_bit_cast(int, lds.gates[kRest][1]);
     f32x4 kS[NT][4], y[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -464,7 +508,7 @@ __global__ void __launch_bounds__(kChunkThreads) chunk_walk_kernel(cortex_delta_
       for (int t = 0; t < 4; ++t) kS[n][t] = y[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-      bf16x8v sp[NT][3], kf[4][KP], qf[4][KP];
+      bf16x8v sp[NT][3];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         float e[8];
@@ -475,36 +519,54 @@ __global__ void __launch_bounds__(kChunkThreads) chunk_walk_kernel(cortex_delta_
         }
         planes8(e, sp[n]);
       }
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int p = 0; p < KP; ++p) {
-          const int at = Lds::K_::at(t * 16 + l16, m * 32 + q * 8);
-          kf[t][p] = lds8(&lds.keys[p][at]);
-          qf[t][p] = lds8(&lds.queries[p][at]);
-        }
       typedef PlanePairs<KP, 3> Pairs;
-#pragma unroll
-      for (int i = 0; i < Pairs::kCount; ++i)
+      auto by_state = [&](const unsigned short (&rows)[KP][kChunk * K], f32x4 (&to)[NT][4]) {
+        bf16x8v f[4][KP];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            kS[n][t] = mfma_bf16x32(kf[t][Pairs::left(i)], sp[n][Pairs::right(i)], kS[n][t]);
-            y[n][t] = mfma_bf16x32(qf[t][Pairs::left(i)], sp[n][Pairs::right(i)], y[n][t]);
-          }
+          for (int p = 0; p < KP; ++p) f[t][p] = lds8(&rows[p][Lds::K_::at(t * 16 + l16, m * 32 + q * 8)]);
+#pragma unroll
+        for (int i = 0; i < Pairs::kCount; ++i)
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) to[n][t] = mfma_bf16x32(f[t][Pairs::left(i)], sp[n][Pairs::right(i)], to[n][t]);
+      };
+      by_state(lds.keys, kS);
+      by_state(lds.queries, y);
     }
     typedef PlanePairs<3, 3> Pairs;
-    bf16x8v rp[NT][2][3], up[NT][2][3], wp[NT][2][3];
     auto to_planes = [](const f32x4 &lo, const f32x4 &hi, bf16x8v (&p)[3]) {
       float e[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
       planes8(e, p);
     };
+    // c += pieces of T or P by the planes of 64 tokens
+    auto by_map = [&](const u32x4v (&map)[kMapPieces][3][64], const bf16x8v (&p)[NT][2][3], f32x4 (&to)[NT][4]) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int t = 2 * m; t < 4; t += 2) {
+          bf16x8v f[2][3];
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < 3; ++i) f[s][i] = __builtin_bit_cast(bf16x8v, map[map_piece(t + s, m)][i][lane]);
+#pragma unroll
+          for (int i = 0; i < Pairs::kCount; ++i)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+              for (int n = 0; n < NT; ++n) to[n][t + s] = mfma_bf16x32(f[s][Pairs::left(i)], p[n][m][Pairs::right(i)], to[n][t + s]);
+        }
+    };
+    f32x4 u[NT][4];
+    bf16x8v planes[NT][2][3];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const f32x4 beta = *(const f32x4 *)&lds.beta[t * 16 + q * 4], grow = *(const f32x4 *)&lds.grow[t * 16 + q * 4];
+        const f32x4 beta = *(const f32x4 *)&lds.gates[kBeta][t * 16 + q * 4], grow = *(const f32x4 *)&lds.gates[kGrow][t * 16 + q * 4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float x = beta[r] * (to_float<T>(v[t][r][n]) - grow[r] * kS[n][t][r]);
@@ -514,37 +576,24 @@ __global__ void __launch_bounds__(kChunkThreads) chunk_walk_kernel(cortex_delta_
       }
       drop_odd(kS[n], q, first[n]);
 #pragma unroll
-      for (int m = 0; m < 2; ++m) to_planes(kS[n][2 * m], kS[n][2 * m + 1], rp[n][m]);
-    }
-    f32x4 u[NT][4];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
+      for (int m = 0; m < 2; ++m) to_planes(kS[n][2 * m], kS[n][2 * m + 1], planes[n][m]);
 #pragma unroll
       for (int t = 0; t < 4; ++t) u[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int i = 0; i < Pairs::kCount; ++i)
-#pragma unroll
-        for (int t = 2 * m; t < 4; ++t)
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-            u[n][t] = mfma_bf16x32(__builtin_bit_cast(bf16x8v, tr[map_piece(t, m)][Pairs::left(i)]), rp[n][m][Pairs::right(i)], u[n][t]);
-#pragma unroll
-    for (int i = 0; i < kMapPieces; ++i)
-#pragma unroll
-      for (int p = 0; p < 3; ++p) tr[i][p] = map->P[i][p][lane];
+    }
+    by_map(lds.inverse, planes, u);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       drop_odd(u[n], q, first[n]);
-      f32x4 weighted[4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) weighted[t] = u[n][t] * *(const f32x4 *)&lds.weight[t * 16 + q * 4];
+      for (int m = 0; m < 2; ++m) to_planes(u[n][2 * m], u[n][2 * m + 1], planes[n][m]);
+    }
+    by_map(lds.scores, planes, y);
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        to_planes(u[n][2 * m], u[n][2 * m + 1], up[n][m]);
-        to_planes(weighted[2 * m], weighted[2 * m + 1], wp[n][m]);
-      }
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) u[n][t] *= *(const f32x4 *)&lds.gates[kWeight][t * 16 + q * 4];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) to_planes(u[n][2 * m], u[n][2 * m + 1], planes[n][m]);
     }
 #pragma unroll
     for (int m = 0; m < M; ++m) {
@@ -570,18 +619,9 @@ __global__ void __launch_bounds__(kChunkThreads) chunk_walk_kernel(cortex_delta_
           for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
-              S[n][2 * m + s] = mfma_bf16x32(kt[s][h][KeyPairs::left(i)], wp[n][h][KeyPairs::right(i)], S[n][2 * m + s]);
+              S[n][2 * m + s] = mfma_bf16x32(kt[s][h][KeyPairs::left(i)], planes[n][h][KeyPairs::right(i)], S[n][2 * m + s]);
     }
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int i = 0; i < Pairs::kCount; ++i)
-#pragma unroll
-        for (int t = 2 * m; t < 4; ++t)
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-            y[n][t] = mfma_bf16x32(__builtin_bit_cast(bf16x8v, tr[map_piece(t, m)][Pairs::left(i)]), up[n][m][Pairs::right(i)], y[n][t]);
-    T *yt = ys + t0 * a.y_ld;
+    T *yt = ys + (int64_t)t0 * a.y_ld;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
       if (__any(first[n] < kChunk)) {
@@ -626,16 +666,21 @@ template <typename T, int K> struct ChainLds {
   alignas(16) u32x4v S[3][M][64];
   alignas(16) u32x4v R[3][2][64];
   alignas(16) u32x4v W[3][2][64];                // exp(c_63 - c_j) u_j
-  alignas(16) f32x4 U[4][64];
+  alignas(16) f32x4 U[2][4][64];
+  alignas(16) f32x4 V[2][4][64];
   alignas(16) unsigned short keys[KP][kChunk * K_::kStride];
+  alignas(1024) u32x4v inverse[2][kMapPieces][3][64];
+  alignas(1024) f32x4 scores[2][kMapTiles][64];
+  alignas(16) float gates[2][kGates][kChunk];
   int first[2][16];
 };
 
 // The same for few columns: eight waves share 16 of them, so that the chain from one state to
 // the next is short.  Four waves of 16 tokens each form it: keys by state, R; U; the
-// next state, an LDS exchange and a barrier between; four more form the outputs beside them.
+// next state, with an LDS exchange and a barrier between.  Four more bring in values and gates and form the
+// outputs beside them, those of a chunk while the next one's R is made.  One more brings T and P into LDS.
 template <typename T, int K, bool WIDE>
-__global__ void __launch_bounds__(2 * kChunkThreads) chunk_chain_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps, int64_t units) {
+__global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps, int64_t units) {
   typedef ChainLds<T, K> Lds;
   constexpr int KP = Lds::KP, M = Lds::M;
   constexpr int ST = K == 128 ? 2 : 1;           // tiles of 16 state entries of a wave
@@ -644,11 +689,13 @@ __global__ void __launch_bounds__(2 * kChunkThreads) chunk_chain_kernel(cortex_d
   const int64_t unit = unit_of_block(units);
   if (unit >= units) return;
   const int tid = (int)threadIdx.x, lane = tid & 63, q = lane >> 4, l16 = lane & 15;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), w = wave & 3;
-  const int V = a.value_dim, slices = V / 16, per = a.heads * slices;
-  const int seq = (int)(unit / per), rest = (int)(unit % per), head = rest / slices, v0 = rest % slices * 16;
+  // the tokens of a wave; the products of T and of P grow with them, so that a SIMD's two waves have five tiles together
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), w = wave < kChunkWaves ? wave : kChunkWaves - 1 - wave % kChunkWaves;
+  const int V = a.value_dim, slices = V / 16, v0 = (int)(unit % slices) * 16;
+  const int seq = (int)(unit / slices % a.num_seqs), head = (int)(unit / slices / a.num_seqs);
   const int g = head / (a.heads / a.key_heads);
-  const int begin = a.seq_offsets[seq], end = a.seq_offsets[seq + 1];
+  // (the same in every lane, and the compiler is told so)
+  const int begin = __builtin_amdgcn_readfirstlane(a.seq_offsets[seq]), end = __builtin_amdgcn_readfirstlane(a.seq_offsets[seq + 1]);
   if (begin < 0 || end < begin || end > a.num_tokens) return;
   int pool = -1;
   if (a.state_in || a.state_out) {
@@ -656,81 +703,124 @@ __global__ void __launch_bounds__(2 * kChunkThreads) chunk_chain_kernel(cortex_d
     if (pool < -1) return;
   }
   if (__syncthreads_or(failed != 0)) return;
-  const ChunkMap *map = maps + ((int64_t)(begin / kChunk) + seq) * a.heads + head;
+  const ChunkMap *const first_map = maps + ((int64_t)(begin / kChunk) + seq) * a.heads + head;
   // What a chunk needs is loaded as soon as the last chunk's is used up, without a condition, so
   // that nothing waits for it: the last chunk repeats its own.  Rows past the sequence's end
   // repeat its last.  Places in a chunk are 32 bits (the host admits no longer rows).
-  u32x4v piece[2][3];
-  auto load_pieces = [&](const u32x4v (&of)[kMapPieces][3][64]) {
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int p = 0; p < 3; ++p) piece[m][p] = of[map_piece(w, m)][p][lane];
-  };
   Eight<T> raw[M];
   uint32_t own = 0;
   auto load_own = [&](const T *rows) {
 #pragma unroll
     for (int m = 0; m < M; ++m) raw[m].template load<WIDE>(rows + own + m * 32);
   };
-  int b = 0;
-  if (wave >= kChunkWaves) {
-    const T *qs = (const T *)a.q + g * K + q * 8;
-    T *ys = (T *)a.y + (int64_t)head * V + v0 + l16;
-    uint32_t y_at[4];
+  auto last_of = [&](int t0) { return min(kChunk, end - t0) - 1; };
+  auto after = [&](int t0) { return t0 + kChunk < end ? t0 + kChunk : t0; };
+  if (wave == 2 * kChunkWaves) {
+    // T and P of the next chunk go straight into LDS, 1 KB at a time
+    static_assert(offsetof(ChunkMap, P) == kMapPieces * 3 * 1024, "P follows T");
+    auto bring = [&](const ChunkMap *map, int b) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) y_at[r] = (uint32_t)(w * 16 + q * 4 + r) * (uint32_t)a.y_ld;
-    f32x4 grow = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (begin < end) {
-      own = (uint32_t)min(w * 16 + l16, min(kChunk, end - begin) - 1) * (uint32_t)a.q_ld;
-      load_own(qs + (int64_t)begin * a.q_ld);
-      load_pieces(map->P);
-      grow = *(const f32x4 *)&map->grow[w * 16 + q * 4];
-    }
-#pragma unroll 1
-    for (int64_t t0 = begin; t0 < end; t0 += kChunk, b ^= 1) {
-      const int last = (int)min((int64_t)kChunk, end - t0) - 1;
-      const bool more = t0 + kChunk < end;
-      const int64_t next = more ? t0 + kChunk : t0;
-      if (more) map += a.heads;
-      __syncthreads();                           // the state is there
-      Parts qp;
-#pragma unroll
-      for (int m = 0; m < M; ++m) {
-        bf16x8v f[KP], s[3];
-        raw[m].planes(f);
-#pragma unroll
-        for (int p = 0; p < 3; ++p) s[p] = __builtin_bit_cast(bf16x8v, lds.S[p][m][lane]);
-        qp.add(f, s);
+      for (int i = 0; i < kMapPieces * 3 + kMapTiles; ++i)
+        copy_to_lds(map, (uint32_t)(i * 1024 + lane * 16),
+                    i < kMapPieces * 3 ? lds_place(lds.inverse[b]) + i * 1024 : lds_place(lds.scores[b]) + (i - kMapPieces * 3) * 1024);
+    };
+    const ChunkMap *map = first_map;
+    int b = 0;
+    if (begin < end) bring(map, 0);
+    for (int t0 = begin; t0 < end; t0 += kChunk, b ^= 1) {
+      copies_done<0>();
+      __syncthreads();
+      __syncthreads();                           // the outputs of the last chunk, which read the other buffer, are formed
+      if (t0 + kChunk < end) {
+        map += a.heads;
+        bring(map, b ^ 1);
       }
-      f32x4 y = qp.sum() * (grow * a.scale);
-      if (end - next < kChunk) own = (uint32_t)min(w * 16 + l16, (int)(end - next) - 1) * (uint32_t)a.q_ld;
-      load_own(qs + next * a.q_ld);
-      grow = *(const f32x4 *)&map->grow[w * 16 + q * 4];
-      __syncthreads();                           // R is there
-      __syncthreads();                           // U is there
-      Parts yp;
+      __syncthreads();
+    }
+    return;
+  }
+  if (wave >= kChunkWaves) {
+    if (begin >= end) return;
+    const T *qs = (const T *)a.q + g * K + q * 8, *vs = (const T *)a.v + (int64_t)head * V + v0 + l16;
+    T *ys = (T *)a.y + (int64_t)head * V + v0 + l16;
+    T v[4];
+    float gate;
+    auto load_values = [&](int t0, const ChunkMap *of) {
+      const T *vt = vs + (int64_t)t0 * a.v_ld;
+      const int last = last_of(t0);
 #pragma unroll
-      for (int m = 0; m < 2; ++m)
-        if (m <= w / 2) {
-          const f32x4 lo = lds.U[2 * m][lane], hi = lds.U[2 * m + 1][lane];
-          float e[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-          bf16x8v p3[3], s[3];
-          planes8(e, s);
+      for (int r = 0; r < 4; ++r) v[r] = vt[(uint32_t)min(w * 16 + q * 4 + r, last) * (uint32_t)a.v_ld];
+      gate = of->gates[w][lane];
+    };
+    auto load_queries = [&](int t0) {
+      own = (uint32_t)min(w * 16 + l16, last_of(t0)) * (uint32_t)a.q_ld;
+      load_own(qs + (int64_t)t0 * a.q_ld);
+    };
+    auto put_values = [&](int b) {
+      lds.V[b][w][lane] = f32x4{to_float<T>(v[0]), to_float<T>(v[1]), to_float<T>(v[2]), to_float<T>(v[3])};
+      lds.gates[b][w][lane] = gate;
+      if (w == kRest) {
+        const int first = __builtin_bit_cast(int, __shfl(gate, 1));
+        if (lane < 16) lds.first[b][lane] = first;
+      }
+    };
+    const ChunkMap *map = first_map;
+    // the first chunk's values and gates; then the second's are on their way
+    load_values(begin, map);
+    load_queries(begin);
+    put_values(0);
+    int coming = after(begin);
+    if (coming != begin) map += a.heads;
+    load_values(coming, map);
+    f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+    // y of the chunk from t0 on, of buffer b, once its updates are there: P by U in float32 on both
+    // sides as they stand, k = 4 q + step of each 16 tokens.
+    auto finish = [&](int b) {
+      f32x4 yp[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
-          for (int p = 0; p < 3; ++p) p3[p] = __builtin_bit_cast(bf16x8v, piece[m][p]);
-          yp.add(p3, s);
-        }
-      y += yp.sum();
-      load_pieces(map->P);
-      const int from = lds.first[b][l16];
-      T *yt = ys + t0 * a.y_ld;
+      for (int c = 0; c < kChunkWaves; ++c)
+        if (c <= w) yp[c % 2] = mul_block(lds.scores[b][map_tile(w, c)][lane], lds.U[b][c][lane], yp[c % 2]);
+      y += yp[0] + yp[1];
+    };
+    auto store = [&](int t0, int b) {
+      const int from = lds.first[b][l16], last = last_of(t0);
+      T *yt = ys + (int64_t)t0 * a.y_ld;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int i = w * 16 + q * 4 + r;
-        if (i <= last) yt[y_at[r]] = from_float<T>(i < from ? y[r] : __builtin_nanf(""));
+        if (i <= last) yt[(uint32_t)i * (uint32_t)a.y_ld] = from_float<T>(i < from ? y[r] : __builtin_nanf(""));
       }
+    };
+    int t0 = begin, b = 0;
+#pragma unroll 1
+    for (;; b ^= 1) {
+      __syncthreads();                           // the state, values and gates are there
+      if (t0 != begin) finish(b ^ 1);
+      __syncthreads();                           // R and the keys are there
+      if (t0 != begin) store(t0 - kChunk, b ^ 1);
+      // beside U; the next state comes after it
+      Parts qp;
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        bf16x8v qf[KP], s[3];
+        raw[m].planes(qf);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) s[p] = __builtin_bit_cast(bf16x8v, lds.S[p][m][lane]);
+        qp.add(qf, s);
+      }
+      y = qp.sum() * (*(const f32x4 *)&lds.gates[b][kGrow][w * 16 + q * 4] * a.scale);
+      const int next = after(t0);
+      load_queries(next);
+      __syncthreads();                           // U is there
+      put_values(b ^ 1);
+      coming = after(next);
+      if (coming != next) map += a.heads;
+      load_values(coming, map);
+      if (next == t0) break;
+      t0 = next;
     }
+    finish(b);
+    store(t0, b);
     return;
   }
   __builtin_amdgcn_s_setprio(2);                 // the outputs have time until the next state
@@ -748,38 +838,13 @@ __global__ void __launch_bounds__(2 * kChunkThreads) chunk_chain_kernel(cortex_d
   for (int s = 0; s < ST; ++s)
     S[s] = a.state_in && pool >= 0 && holds ? *(const f32x4 *)(a.state_in + state_at + s * 4) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   put_state();
-  const T *ks = (const T *)a.k + g * K + q * 8, *vs = (const T *)a.v + (int64_t)head * V + v0 + l16;
-  T v[4];
-  uint32_t v_at[4] = {};
-  struct Gates {
-    f32x4 beta, grow, weight;
-    float decay;
-    int first;
-  } gates, coming = {};
-  auto place_rows = [&](int last) {
-    own = (uint32_t)min(w * 16 + l16, last) * (uint32_t)a.k_ld;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) v_at[r] = (uint32_t)min(w * 16 + q * 4 + r, last) * (uint32_t)a.v_ld;
-  };
-  auto load_rows = [&](int64_t t0) {
-    load_own(ks + t0 * a.k_ld);
-    const T *vt = vs + t0 * a.v_ld;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = vt[v_at[r]];
-  };
-  auto load_gates = [&]() {
-    coming.beta = *(const f32x4 *)&map->beta[w * 16 + q * 4];
-    coming.grow = *(const f32x4 *)&map->grow[w * 16 + q * 4];
-    coming.weight = *(const f32x4 *)&map->weight[w * 16 + q * 4];
-    coming.decay = map->decay;
-    coming.first = map->first;
-  };
+  const T *ks = (const T *)a.k + g * K + q * 8;
   // Values of the lane's tokens that are not finite become 0: their products with the zeros above
   // the diagonal would carry them to earlier tokens.  The first is noted.
-  auto drop = [&](f32x4 &x) {
+  auto drop = [&](f32x4 &x, int b) {
 #pragma clang fp reassociate(off)
     const float none = (x[0] * 0.0f + x[1] * 0.0f) + (x[2] * 0.0f + x[3] * 0.0f);
-    if (none == 0.0f) return;
+    if (!__any(none != 0.0f)) return;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
       if (!finite(x[r])) {
@@ -788,21 +853,15 @@ __global__ void __launch_bounds__(2 * kChunkThreads) chunk_chain_kernel(cortex_d
       }
   };
   if (begin < end) {
-    load_gates();
-    place_rows(min(kChunk, end - begin) - 1);
-    load_rows(begin);
-    load_pieces(map->T);
+    own = (uint32_t)min(w * 16 + l16, last_of(begin)) * (uint32_t)a.k_ld;
+    load_own(ks + (int64_t)begin * a.k_ld);
   }
+  int b = 0;
 #pragma unroll 1
-  for (int64_t t0 = begin; t0 < end; t0 += kChunk, b ^= 1) {
-    const int last = (int)min((int64_t)kChunk, end - t0) - 1;
-    const bool more = t0 + kChunk < end;
-    const int64_t next = more ? t0 + kChunk : t0;
-    if (more) map += a.heads;
-    gates = coming;
-    load_gates();
-    if (tid < 16) lds.first[b][tid] = gates.first;
-    __syncthreads();                             // the state is there; the last chunk's keys are read
+  for (int t0 = begin; t0 < end; t0 += kChunk, b ^= 1) {
+    const int last = last_of(t0);
+    const int next = after(t0);
+    __syncthreads();                             // the state, values and gates are there; the last chunk's keys are read
     bf16x8v kf[M][KP];
 #pragma unroll
     for (int m = 0; m < M; ++m) raw[m].planes(kf[m]);
@@ -819,16 +878,15 @@ __global__ void __launch_bounds__(2 * kChunkThreads) chunk_chain_kernel(cortex_d
 #pragma unroll
       for (int p = 0; p < KP; ++p)
         *(u32x4v *)&lds.keys[p][Lds::K_::at(w * 16 + l16, m * 32 + q * 8)] = __builtin_bit_cast(u32x4v, kf[m][p]);
-    f32x4 x = kp.sum();
+    const f32x4 beta = *(const f32x4 *)&lds.gates[b][kBeta][w * 16 + q * 4], grow = *(const f32x4 *)&lds.gates[b][kGrow][w * 16 + q * 4];
+    f32x4 x = beta * (lds.V[b][w][lane] - grow * kp.sum());
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      x[r] = gates.beta[r] * (to_float<T>(v[r]) - gates.grow[r] * x[r]);
+    for (int r = 0; r < 4; ++r)
       if (w * 16 + q * 4 + r > last) x[r] = 0.0f;
-    }
-    drop(x);
+    drop(x, b);
     put_planes4(&lds.R[0][w / 2][0], 2 * 64, lane, w % 2, x);
-    if (end - next < kChunk) place_rows((int)(end - next) - 1);
-    load_rows(next);
+    own = (uint32_t)min(w * 16 + l16, last_of(next)) * (uint32_t)a.k_ld;
+    load_own(ks + (int64_t)next * a.k_ld);
     __syncthreads();                             // R and the keys are there
     Parts up;
 #pragma unroll
@@ -837,7 +895,7 @@ __global__ void __launch_bounds__(2 * kChunkThreads) chunk_chain_kernel(cortex_d
         bf16x8v t[3], s[3];
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
-          t[p] = __builtin_bit_cast(bf16x8v, piece[m][p]);
+          t[p] = __builtin_bit_cast(bf16x8v, lds.inverse[b][map_piece(w, m)][p][lane]);
           s[p] = __builtin_bit_cast(bf16x8v, lds.R[p][m][lane]);
         }
         up.add(t, s);
@@ -854,13 +912,13 @@ __global__ void __launch_bounds__(2 * kChunkThreads) chunk_chain_kernel(cortex_d
           for (int p = 0; p < KP; ++p) kt[s][m][p] = join8(lds_columns(&lds.keys[p][at]), lds_columns(&lds.keys[p][to]));
         }
     f32x4 u = up.sum();
-    drop(u);
-    put_planes4(&lds.W[0][w / 2][0], 2 * 64, lane, w % 2, u * gates.weight);
-    lds.U[w][lane] = u;
-    load_pieces(map->T);
+    drop(u, b);
+    put_planes4(&lds.W[0][w / 2][0], 2 * 64, lane, w % 2, u * *(const f32x4 *)&lds.gates[b][kWeight][w * 16 + q * 4]);
+    lds.U[b][w][lane] = u;
     __syncthreads();                             // U is there
     if (holds) {
       const bool gone = lds.first[b][l16] < kChunk;
+      const float decay = lds.gates[b][kRest][0];
       Parts sp[ST];
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
@@ -872,7 +930,7 @@ __global__ void __launch_bounds__(2 * kChunkThreads) chunk_chain_kernel(cortex_d
       }
 #pragma unroll
       for (int s = 0; s < ST; ++s) {
-        S[s] = S[s] * gates.decay + sp[s].sum();
+        S[s] = S[s] * decay + sp[s].sum();
         if (gone) S[s] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
       }
     }

@@ -191,13 +191,6 @@ template <typename T> __device__ __forceinline__ void put_four(const Product &a,
 // the next piece) lie in different banks.
 __device__ __forceinline__ int piece_place(int row, int piece) { return piece ^ (-(row >> 2) & 3); }
 
-// 16 bytes a lane straight into LDS, lane after lane from `to` on.  The compiler does not
-// see the load: the caller waits for it (copies_done) before the barrier.
-__device__ __forceinline__ void copy_to_lds(const int8_t *base, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
-}
-template <int N> __device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory"); }
-
 // Tiles of TN channels and TT tokens by WN x WT waves; BUFFERS stages of kDepth bytes in
 // LDS, all but one of them on their way while one is multiplied.  XCDs take runs of
 // neighbouring tiles, four tiles of tokens by as many of channels as there are.
@@ -215,7 +208,7 @@ __global__ void __launch_bounds__(64 * WN * WT) product_kernel(Product a, const 
   const int n0 = rest / tall * TN, t0 = (band * 4 + rest % tall) * TT;
   const int wn = wave % WN * (TN / WN), wt = wave / WN * (TT / WT);
   const int8_t *ws = a.w + (int64_t)n0 * a.w_ld, *xs = a.x + (int64_t)t0 * a.x_ld;
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t *)lds;
+  const uint32_t lds0 = lds_place(lds);
   // The lane's piece of each copy; a copy is of w or of x alone.
   uint32_t offset[kCopies];
   int piece[kCopies];

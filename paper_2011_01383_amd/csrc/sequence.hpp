@@ -38,6 +38,22 @@ template <typename T> struct Pack<T, 1> {
   static __device__ __forceinline__ void store(T *p, const float (&v)[1]) { *p = from_float<T>(v[0]); }
 };
 
+// 16 bytes a lane straight into LDS, lane after lane from `to` on.  The compiler does not
+// see the load: the caller waits for it (copies_done) before the barrier.
+// `base` and `to` are the same in every lane.
+__device__ __forceinline__ void copy_to_lds(const void *base, uint32_t offset, uint32_t to) {
+  const uint64_t at = (uint64_t)base;
+  const uint64_t uniform = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 |
+                           (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(offset),
+               "s"(uniform)
+               : "memory", "m0");
+}
+template <int N> __device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory"); }
+__device__ __forceinline__ uint32_t lds_place(const void *p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
+}
+
 // The status as earlier launches left it, through the caches: these kernels have
 // many waves, and none of them waits for another launch's word.
 __device__ __forceinline__ int entry_status(const int32_t *status) {
