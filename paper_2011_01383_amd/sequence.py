@@ -11,7 +11,10 @@ mask keeps every text one.  The finished trees go to a tree cell in one call.
 runs it with random weights.  The recurrences, convolutions and the choice of the
 next token are the library's kernels (``cortex_conv_*``, ``cortex_scan_*``,
 ``cortex_logits_process``, ``cortex_tree_infer``); the projections between them are
-plain matrix products of the framework that also supplies the memory.
+plain matrix products of the framework that also supplies the memory.  Layers of
+the kind ``delta`` have the gated delta rule as their recurrence (``cortex_delta_*``,
+with ``cortex_qk_norm`` before and behind it) and projections in 8 bits
+(``cortex_linear_i8``).
 """
 from __future__ import annotations
 
@@ -77,21 +80,99 @@ class _Layer:
         return x + y @ self.w_out
 
 
+class _Weights8:
+    """A projection's weights in 8 bits, a scale per output channel."""
+
+    def __init__(self, w: torch.Tensor, status: torch.Tensor):
+        N, K = w.shape
+        self.q = torch.zeros(N, (K + 15) // 16 * 16, dtype=torch.int8, device=w.device)[:, :K]     # rows start at 16 bytes
+        self.scale = torch.empty(N, device=w.device)
+        C.check(C.cortex_quant_i8(w, self.q, self.scale, status=status), "cortex_quant_i8")
+
+    def __call__(self, x: torch.Tensor, status: torch.Tensor) -> torch.Tensor:
+        T, (N, K) = x.shape[0], self.q.shape
+        y = torch.empty(T, N, dtype=x.dtype, device=x.device)
+        ws = C.workspace(C.cortex_linear_i8_workspace_bytes(T, N, K), x.device)
+        C.check(C.cortex_linear_i8(x, self.q, self.scale, y, status=status, ws=ws), "cortex_linear_i8")
+        return y
+
+
+class _DeltaLayer:
+    """Projection, convolution of queries, keys and values, queries and keys of norm 1, delta
+    rule, a norm per head with its gate, projection back.  Heads of 64 by 64, two to a key head."""
+
+    K = V = 64
+
+    def __init__(self, g, width: int, channels: int, rows: int, dtype, device, status, W: int = 4):
+        def normal(n, k):
+            return _Weights8((torch.randn(n, k, generator=g) / k ** 0.5).to(device), status)
+
+        self.D, self.H = channels, channels // self.V
+        self.G = max(1, self.H // 2)
+        self.H -= self.H % self.G
+        D, H, G, K = self.D, self.H, self.G, self.K
+        if H * self.V != D:
+            raise ValueError("%d channels are no whole number of heads of %d" % (D, self.V))
+        self.conv_channels = 2 * G * K + D
+        self.w_in, self.w_out = normal(D + self.conv_channels + 2 * H, width), normal(width, D)
+        self.conv_w = (torch.randn(self.conv_channels, W, generator=g) / W ** 0.5).to(device)
+        self.conv_b = torch.zeros(self.conv_channels, device=device)
+        size = 0.001 * 100.0 ** torch.rand(H, generator=g)
+        self.dt_bias = torch.log(torch.expm1(size)).to(device)
+        self.A = -(1 + 15 * torch.rand(H, generator=g)).to(device)
+        self.weight = torch.ones(self.V, device=device)
+        self.conv_state = torch.zeros(rows, W - 1, self.conv_channels, dtype=dtype, device=device)
+        self.state = torch.zeros(rows, D, K, device=device)
+
+    def __call__(self, x, slots, status, offsets=None):
+        """As ``_Layer``."""
+        D, H, G, K, V, T = self.D, self.H, self.G, self.K, self.V, x.shape[0]
+        u = self.w_in(x, status)
+        z, c, b, dt = u.split([D, self.conv_channels, H, H], 1)
+        m = torch.empty_like(c, memory_format=torch.contiguous_format)
+        states = dict(state_in=self.conv_state, state_out=self.conv_state, state_index=slots, status=status)
+        if offsets is None:
+            C.check(C.cortex_conv_step(c, self.conv_w, m, bias=self.conv_b, **states), "cortex_conv_step")
+        else:
+            C.check(C.cortex_conv_forward(c, self.conv_w, offsets, m, bias=self.conv_b, **states), "cortex_conv_forward")
+        q, k, v = m[:, :G * K].unflatten(1, (G, K)), m[:, G * K:2 * G * K].unflatten(1, (G, K)), m[:, 2 * G * K:].unflatten(1, (H, V))
+        C.check(C.cortex_qk_norm(q, q, k=k, k_out=k, norm=C.CORTEX_NORM_L2, status=status), "cortex_qk_norm")
+        y = torch.empty(T, H, V, dtype=x.dtype, device=x.device)
+        kw = dict(dt=dt, A=self.A, dt_bias=self.dt_bias, scale=K ** -0.5, state_in=self.state, state_out=self.state,
+                  state_index=slots, status=status)
+        if offsets is None:
+            C.check(C.cortex_delta_step(q, k, v, b, y, **kw), "cortex_delta_step")
+        else:
+            ws = C.workspace(C.cortex_delta_workspace_bytes(T, offsets.numel() - 1, H, K, V), x.device)
+            C.check(C.cortex_delta_forward(q, k, v, b, offsets, y, ws=ws, **kw), "cortex_delta_forward")
+        C.check(C.cortex_qk_norm(y, y, norm=C.CORTEX_NORM_RMS, q_weight=self.weight, status=status), "cortex_qk_norm")
+        return x + self.w_out(y.flatten(1) * torch.nn.functional.silu(z), status)
+
+
 class SequenceModel:
-    """Embedding, layers (decays per channel and per head in turn), output weights.
+    """Embedding, layers (of ``kinds`` in turn: decays per channel, per head, or the delta rule), output weights.
 
     ``rows`` sequences can run at once; each has a row of every state pool."""
 
     def __init__(self, vocab: int, width: int = 256, layers: int = 2, rows: int = 64, dtype=torch.float32, device="cuda",
-                 seed: int = 0):
+                 seed: int = 0, kinds=("channel", "head")):
+        for kind in kinds:
+            if kind not in ("channel", "head", "delta"):
+                raise ValueError("a layer is of kind channel, head or delta, got %r" % (kind,))
         C.load()
         g = torch.Generator().manual_seed(seed)
         self.vocab, self.device, self.rows = vocab, device, rows
         self.embedding = torch.randn(vocab, width, generator=g).to(device, dtype)
-        self.layers = [_Layer(g, width, 2 * width, 64 if k % 2 else 16, 2 * width // 64 if k % 2 else 0, rows, dtype, device)
-                       for k in range(layers)]
-        self.w_out = (torch.randn(width, vocab, generator=g) / width ** 0.5).to(device, dtype)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
+
+        def layer(kind):
+            if kind == "delta":
+                return _DeltaLayer(g, width, 2 * width, rows, dtype, device, self.status)
+            head = kind == "head"
+            return _Layer(g, width, 2 * width, 64 if head else 16, 2 * width // 64 if head else 0, rows, dtype, device)
+
+        self.layers = [layer(kinds[k % len(kinds)]) for k in range(layers)]
+        self.w_out = (torch.randn(width, vocab, generator=g) / width ** 0.5).to(device, dtype)
 
     def _run(self, tokens, slots, offsets=None):
         x = self.embedding[tokens.long()]
@@ -243,6 +324,9 @@ def main() -> None:
     U, b = 0.05 * (2 * torch.rand(2, 5, H, H, generator=g) - 1), 0.05 * (2 * torch.rand(5, H, generator=g) - 1)
     h, _, lin = read_trees(trees, vectors, U.cuda(), b.cuda())
     print("tree cell: %d nodes, %d levels, |h| %.4f" % (lin.N, int(lin.num_levels.item()), float(h.norm())))
+    trees, _ = write_trees(SequenceModel(vocab, dtype=torch.bfloat16, kinds=("delta",)), prompts, most=31, repetition=1.1,
+                           frequency=0.5, opening=6.0)
+    print("by the delta rule: %s tokens" % ", ".join(str(len(t)) for t in trees))
 
 
 if __name__ == "__main__":
