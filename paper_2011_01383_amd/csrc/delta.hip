@@ -115,16 +115,64 @@ void launch_walk(const cortex_delta_t &a, int32_t *status, const ChunkMap *maps,
   chunk_walk_kernel<T, K, NT, WIDE><<<blocks_of_units(units), kChunkThreads, 0, st>>>(a, status, maps, units);
 }
 
+// Workgroups that a launch of segments may have, and so the rows of 16 that they leave.
+constexpr int64_t kMaxSegmentTiles = 2048;
+
+// Tokens of a segment, 0 for whole sequences.  By the time of a chunk in one launch of
+// workgroups (one a CU): 2 us with outputs, 1.5 without, 1.5 for joining two segments and 12 for the two
+// launches more.  The host knows no lengths: sequences are taken as equally long.  24,576 tokens of one head
+// of 128 by 128 take 159 us in segments and 717 whole, 8,192 tokens of 2 heads 130 and 248, of 8
+// heads 192 and 252, 2,048 tokens of 4 heads of 64 by 64 47 and 61.
+static int segment_tokens(int64_t T, int64_t S, int64_t heads, int64_t K, int64_t V) {
+  const int64_t columns = heads * V / 16, maps = heads * (V + K) / 16;
+  auto rounds = [](int64_t workgroups) { return (double)((workgroups + 255) / 256); };
+  double best = 0.8 * 2.0 * rounds(S * columns) * (double)((T / S + kChunk - 1) / kChunk);
+  int Q = 0;
+  for (int64_t chunks = 4; chunks <= 512; chunks *= 2) {
+    if (chunk_slots(T, S, (int)chunks * kChunk) * maps > kMaxSegmentTiles) continue;
+    const int64_t each = (T / S + chunks * kChunk - 1) / (chunks * kChunk), segments = S * each;
+    const double time = (double)chunks * (1.5 * rounds((segments - S) * maps) + 2.0 * rounds(segments * columns)) + 1.5 * (double)each + 12.0;
+    if (time < best) {
+      best = time;
+      Q = (int)chunks * kChunk;
+    }
+  }
+  return Q;
+}
+
+// The workspace: what the first launch leaves for every chunk and head, and the segments' states.
+static size_t map_bytes(int64_t T, int64_t S, int64_t heads) { return (size_t)(chunk_slots(T, S, kChunk) * heads) * sizeof(ChunkMap); }
+static size_t segment_bytes(int64_t K) { return (size_t)(kMaxSegmentTiles * 16 * K) * sizeof(float); }
+
 template <typename T, int K, bool WIDE> int launch_chunks_of(const cortex_delta_t &a, int32_t *status, ChunkMap *maps, void *stream) {
   const hipStream_t st = (hipStream_t)stream;
   const int64_t chunks = chunk_slots(a.num_tokens, a.num_seqs, kChunk) * a.heads;
   const int64_t units = (int64_t)a.num_seqs * a.heads * (a.value_dim / 16);
-  const bool few = units <= 1024;
+  // Eight waves to 16 columns while there are fewer than four workgroups of them a CU, else a wave each:
+  // 512 columns' units 400 us against 515 (8,192 tokens of 2 prompts, 32 heads of 128 by 128), 768 units 223
+  // against 279 (12,000 tokens of 6, 16 heads of 64 by 128), 1,024 units 370 against 348 (8,192 of 4),
+  // 2,048 units 362 against 270 (of 8).
+  const bool few = units < 1024;
   if (few) chunk_maps_kernel<T, K, false, WIDE><<<blocks_of_units(chunks), kChunkThreads, 0, st>>>(a, status, maps, chunks);
   else chunk_maps_kernel<T, K, true, WIDE><<<blocks_of_units(chunks), kChunkThreads, 0, st>>>(a, status, maps, chunks);
   if (!launched()) return CORTEX_E_HIP;
-  if (few) chunk_chain_kernel<T, K, WIDE><<<blocks_of_units(units), kChainThreads, 0, st>>>(a, status, maps, units);
-  else launch_walk<T, K, 1, WIDE>(a, status, maps, st);
+  if (!few) {
+    launch_walk<T, K, 1, WIDE>(a, status, maps, st);
+    return launched() ? CORTEX_OK : CORTEX_E_HIP;
+  }
+  const int Q = segment_tokens(a.num_tokens, a.num_seqs, a.heads, K, a.value_dim);
+  if (!Q) {
+    chunk_chain_kernel<T, K, 0, WIDE><<<blocks_of_units(units), kChainThreads, 0, st>>>(a, status, maps, nullptr, 0, units);
+    return launched() ? CORTEX_OK : CORTEX_E_HIP;
+  }
+  float *segments = (float *)((char *)maps + map_bytes(a.num_tokens, a.num_seqs, a.heads));
+  const int64_t slots = chunk_slots(a.num_tokens, a.num_seqs, Q) * a.heads;
+  const int64_t tiles = slots * ((a.value_dim + K) / 16), columns = slots * (a.value_dim / 16);
+  chunk_chain_kernel<T, K, 1, WIDE><<<blocks_of_units(tiles), kChainThreads, 0, st>>>(a, status, maps, segments, Q, tiles);
+  if (!launched()) return CORTEX_E_HIP;
+  enter_segments_kernel<K><<<(unsigned)units, kChunkThreads, 0, st>>>(a, status, segments, Q);
+  if (!launched()) return CORTEX_E_HIP;
+  chunk_chain_kernel<T, K, 2, WIDE><<<blocks_of_units(columns), kChainThreads, 0, st>>>(a, status, maps, segments, Q, columns);
   return launched() ? CORTEX_OK : CORTEX_E_HIP;
 }
 
@@ -149,8 +197,6 @@ template <typename T> int launch_step(const cortex_delta_t &a, int32_t *status, 
     default: return launch_step_of<T, 128>(a, status, stream);
   }
 }
-
-static size_t delta_bytes(int64_t T, int64_t S, int64_t heads) { return (size_t)(chunk_slots(T, S, kChunk) * heads) * sizeof(ChunkMap); }
 
 static bool bad_delta_size(int32_t heads, int32_t key_heads, int32_t K, int32_t V) {
   if (heads < 1 || key_heads < 1 || heads % key_heads) return true;
@@ -186,8 +232,7 @@ using namespace cortex;
 extern "C" size_t cortex_delta_workspace_bytes(int32_t num_tokens, int32_t num_seqs, int32_t heads, int32_t key_dim,
                                                int32_t value_dim) {
   if (num_tokens < 0 || num_seqs < 0 || bad_delta_size(heads, 1, key_dim, value_dim)) return 0;
-  const size_t bytes = delta_bytes(num_tokens, num_seqs, heads);
-  return bytes ? bytes : 256;
+  return map_bytes(num_tokens, num_seqs, heads) + segment_bytes(key_dim);
 }
 
 extern "C" int cortex_delta_forward(const cortex_delta_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream) {
@@ -197,7 +242,7 @@ extern "C" int cortex_delta_forward(const cortex_delta_t *args, int32_t *d_statu
   // a workgroup a chunk and head, and a grid has less than 2^32 threads
   if (chunk_slots(args->num_tokens, args->num_seqs, kChunk) * args->heads >= (int64_t)1 << 24) return CORTEX_E_INVAL;
   if (!d_ws || !aligned16(d_ws)) return CORTEX_E_INVAL;
-  if (ws_bytes < delta_bytes(args->num_tokens, args->num_seqs, args->heads)) return CORTEX_E_WORKSPACE;
+  if (ws_bytes < map_bytes(args->num_tokens, args->num_seqs, args->heads) + segment_bytes(args->key_dim)) return CORTEX_E_WORKSPACE;
   return args->dtype == CORTEX_BF16 ? launch_forward<bf16_t>(*args, d_status, d_ws, stream)
                                     : launch_forward<float>(*args, d_status, d_ws, stream);
 }

@@ -679,8 +679,14 @@ template <typename T, int K> struct ChainLds {
 // the next is short.  Four waves of 16 tokens each form it: keys by state, R; U; the
 // next state, with an LDS exchange and a barrier between.  Four more bring in values and gates and form the
 // outputs beside them, those of a chunk while the next one's R is made.  One more brings T and P into LDS.
-template <typename T, int K, bool WIDE>
-__global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps, int64_t units) {
+//
+// PART 0: whole sequences.  Where even these are few, a sequence is cut into segments of Q tokens: what
+// a segment does to the state that enters it is S M + N, and part 1 finds N (from a zero state) and M
+// (from the unit rows, without values) as columns of their own, V + K of them; enter_segments_kernel
+// joins them; part 2 forms the outputs from the state that enters.
+template <typename T, int K, int PART, bool WIDE>
+__global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps, float *segments, int Q,
+                                                                    int64_t units) {
   typedef ChainLds<T, K> Lds;
   constexpr int KP = Lds::KP, M = Lds::M;
   constexpr int ST = K == 128 ? 2 : 1;           // tiles of 16 state entries of a wave
@@ -691,19 +697,38 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
   const int tid = (int)threadIdx.x, lane = tid & 63, q = lane >> 4, l16 = lane & 15;
   // the tokens of a wave; the products of T and of P grow with them, so that a SIMD's two waves have five tiles together
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), w = wave < kChunkWaves ? wave : kChunkWaves - 1 - wave % kChunkWaves;
-  const int V = a.value_dim, slices = V / 16, v0 = (int)(unit % slices) * 16;
-  const int seq = (int)(unit / slices % a.num_seqs), head = (int)(unit / slices / a.num_seqs);
+  const int V = a.value_dim, rows = PART == 0 ? V : V + K, slices = (PART == 1 ? rows : V) / 16, v0 = (int)(unit % slices) * 16;
+  const int slots = PART == 0 ? a.num_seqs : (int)chunk_slots(a.num_tokens, a.num_seqs, Q);
+  const int slot = (int)(unit / slices % slots), head = (int)(unit / slices / slots);
+  const bool values = PART != 1 || v0 < V;       // else unit rows
   const int g = head / (a.heads / a.key_heads);
+  int seq = slot, begin, end, first, last_token;
+  if constexpr (PART == 0) {
+    first = begin = a.seq_offsets[seq];
+    last_token = end = a.seq_offsets[seq + 1];
+    if (begin < 0 || end < begin || end > a.num_tokens) return;
+  } else {
+    const Chunk c = find_chunk(a.seq_offsets, a.num_seqs, a.num_tokens, Q, slot);
+    if (c.seq < 0) return;
+    seq = c.seq;
+    begin = c.begin;
+    end = c.end;
+    first = c.first;
+    last_token = c.last;
+    if (PART == 1 && end == last_token) return;  // nothing follows it
+  }
   // (the same in every lane, and the compiler is told so)
-  const int begin = __builtin_amdgcn_readfirstlane(a.seq_offsets[seq]), end = __builtin_amdgcn_readfirstlane(a.seq_offsets[seq + 1]);
-  if (begin < 0 || end < begin || end > a.num_tokens) return;
+  begin = __builtin_amdgcn_readfirstlane(begin);
+  end = __builtin_amdgcn_readfirstlane(end);
+  first = __builtin_amdgcn_readfirstlane(first);
+  seq = __builtin_amdgcn_readfirstlane(seq);
   int pool = -1;
-  if (a.state_in || a.state_out) {
+  if (PART != 1 && (a.state_in || a.state_out)) {
     pool = state_row(a.state_index, seq, a.state_rows, status);
     if (pool < -1) return;
   }
   if (__syncthreads_or(failed != 0)) return;
-  const ChunkMap *const first_map = maps + ((int64_t)(begin / kChunk) + seq) * a.heads + head;
+  const ChunkMap *const first_map = maps + ((int64_t)(first / kChunk) + seq + (begin - first) / kChunk) * a.heads + head;
   // What a chunk needs is loaded as soon as the last chunk's is used up, without a condition, so
   // that nothing waits for it: the last chunk repeats its own.  Rows past the sequence's end
   // repeat its last.  Places in a chunk are 32 bits (the host admits no longer rows).
@@ -720,7 +745,7 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
     static_assert(offsetof(ChunkMap, P) == kMapPieces * 3 * 1024, "P follows T");
     auto bring = [&](const ChunkMap *map, int b) {
 #pragma unroll
-      for (int i = 0; i < kMapPieces * 3 + kMapTiles; ++i)
+      for (int i = 0; i < kMapPieces * 3 + (PART == 1 ? 0 : kMapTiles); ++i)
         copy_to_lds(map, (uint32_t)(i * 1024 + lane * 16),
                     i < kMapPieces * 3 ? lds_place(lds.inverse[b]) + i * 1024 : lds_place(lds.scores[b]) + (i - kMapPieces * 3) * 1024);
     };
@@ -741,7 +766,7 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
   }
   if (wave >= kChunkWaves) {
     if (begin >= end) return;
-    const T *qs = (const T *)a.q + g * K + q * 8, *vs = (const T *)a.v + (int64_t)head * V + v0 + l16;
+    const T *qs = (const T *)a.q + g * K + q * 8, *vs = (const T *)a.v + (int64_t)head * V + (values ? v0 : 0) + l16;
     T *ys = (T *)a.y + (int64_t)head * V + v0 + l16;
     T v[4];
     float gate;
@@ -749,7 +774,7 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
       const T *vt = vs + (int64_t)t0 * a.v_ld;
       const int last = last_of(t0);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = vt[(uint32_t)min(w * 16 + q * 4 + r, last) * (uint32_t)a.v_ld];
+      for (int r = 0; r < 4; ++r) v[r] = values ? vt[(uint32_t)min(w * 16 + q * 4 + r, last) * (uint32_t)a.v_ld] : (T)0.0f;
       gate = of->gates[w][lane];
     };
     auto load_queries = [&](int t0) {
@@ -767,7 +792,7 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
     const ChunkMap *map = first_map;
     // the first chunk's values and gates; then the second's are on their way
     load_values(begin, map);
-    load_queries(begin);
+    if (PART != 1) load_queries(begin);
     put_values(0);
     int coming = after(begin);
     if (coming != begin) map += a.heads;
@@ -795,22 +820,24 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
 #pragma unroll 1
     for (;; b ^= 1) {
       __syncthreads();                           // the state, values and gates are there
-      if (t0 != begin) finish(b ^ 1);
+      if (PART != 1 && t0 != begin) finish(b ^ 1);
       __syncthreads();                           // R and the keys are there
-      if (t0 != begin) store(t0 - kChunk, b ^ 1);
-      // beside U; the next state comes after it
-      Parts qp;
-#pragma unroll
-      for (int m = 0; m < M; ++m) {
-        bf16x8v qf[KP], s[3];
-        raw[m].planes(qf);
-#pragma unroll
-        for (int p = 0; p < 3; ++p) s[p] = __builtin_bit_cast(bf16x8v, lds.S[p][m][lane]);
-        qp.add(qf, s);
-      }
-      y = qp.sum() * (*(const f32x4 *)&lds.gates[b][kGrow][w * 16 + q * 4] * a.scale);
+      if (PART != 1 && t0 != begin) store(t0 - kChunk, b ^ 1);
       const int next = after(t0);
-      load_queries(next);
+      if constexpr (PART != 1) {
+        // beside U; the next state comes after it
+        Parts qp;
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          bf16x8v qf[KP], s[3];
+          raw[m].planes(qf);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) s[p] = __builtin_bit_cast(bf16x8v, lds.S[p][m][lane]);
+          qp.add(qf, s);
+        }
+        y = qp.sum() * (*(const f32x4 *)&lds.gates[b][kGrow][w * 16 + q * 4] * a.scale);
+        load_queries(next);
+      }
       __syncthreads();                           // U is there
       put_values(b ^ 1);
       coming = after(next);
@@ -819,15 +846,19 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
       if (next == t0) break;
       t0 = next;
     }
-    finish(b);
-    store(t0, b);
+    if (PART != 1) {
+      finish(b);
+      store(t0, b);
+    }
     return;
   }
   __builtin_amdgcn_s_setprio(2);                 // the outputs have time until the next state
   // the wave's part of the state: 32 entries m, its halves of four in eight from `half` on
   const int sm = K == 128 ? w : K == 64 ? w / 2 : 0, half = K == 128 ? 0 : K == 64 ? w % 2 : w;
   const bool holds = K > 32 || w < 2;
-  const int64_t state_at = (((int64_t)pool * a.heads + head) * V + v0 + l16) * K + sm * 32 + q * 8 + half * 4;
+  const int entry = sm * 32 + q * 8 + half * 4;  // and four further on for the second tile
+  const int64_t state_at = (((int64_t)pool * a.heads + head) * V + v0 + l16) * K + entry;
+  float *const segment = PART == 0 ? nullptr : segments + (((int64_t)slot * a.heads + head) * rows + v0 + l16) * K + entry;
   f32x4 S[ST];
   auto put_state = [&]() {
     if (!holds) return;
@@ -836,7 +867,14 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
   };
 #pragma unroll
   for (int s = 0; s < ST; ++s)
-    S[s] = a.state_in && pool >= 0 && holds ? *(const f32x4 *)(a.state_in + state_at + s * 4) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  {
+    S[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (PART == 0 && a.state_in && pool >= 0 && holds) S[s] = *(const f32x4 *)(a.state_in + state_at + s * 4);
+    if (PART == 2 && holds) S[s] = *(const f32x4 *)(segment + s * 4);
+    if (PART == 1 && !values)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) S[s][r] = v0 - V + l16 == entry + s * 4 + r ? 1.0f : 0.0f;
+  }
   put_state();
   const T *ks = (const T *)a.k + g * K + q * 8;
   // Values of the lane's tokens that are not finite become 0: their products with the zeros above
@@ -914,7 +952,7 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
     f32x4 u = up.sum();
     drop(u, b);
     put_planes4(&lds.W[0][w / 2][0], 2 * 64, lane, w % 2, u * *(const f32x4 *)&lds.gates[b][kWeight][w * 16 + q * 4]);
-    lds.U[b][w][lane] = u;
+    if (PART != 1) lds.U[b][w][lane] = u;
     __syncthreads();                             // U is there
     if (holds) {
       const bool gone = lds.first[b][l16] < kChunk;
@@ -936,9 +974,84 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
     }
     put_state();
   }
-  if (a.state_out && pool >= 0 && holds)
+  float *const to = PART == 1 ? segment : a.state_out && pool >= 0 && end == last_token ? a.state_out + state_at : nullptr;
+  if (to && holds)
 #pragma unroll
-    for (int s = 0; s < ST; ++s) *(f32x4 *)(a.state_out + state_at + s * 4) = S[s];
+    for (int s = 0; s < ST; ++s) *(f32x4 *)(to + s * 4) = S[s];
+}
+
+// The states that enter a sequence's segments, in the place of what they add: s <- s M + N.  A workgroup
+// takes 16 rows of a head's state; a wave K / 4 of their entries (float32 matrix units, k = 4 q + step of each
+// 16 on both sides), M's loads for the next segment on their way.
+template <int K>
+__global__ void __launch_bounds__(kChunkThreads) enter_segments_kernel(cortex_delta_t a, int32_t *status, float *segments, int Q) {
+  constexpr int kRow = K + 4, kTiles = K < 64 ? 1 : K / 64, kBlocks = K / 16;
+  __shared__ __attribute__((aligned(16))) float lds[2][16 * kRow];
+  const int failed = entry_status(status);
+  const int tid = (int)threadIdx.x, lane = tid & 63, w = tid >> 6, q = lane >> 4, l16 = lane & 15;
+  const int V = a.value_dim, v0 = (int)blockIdx.x % (V / 16) * 16, head = (int)blockIdx.x / (V / 16) % a.heads;
+  const int seq = (int)blockIdx.x / (V / 16) / a.heads;
+  const int begin = a.seq_offsets[seq], end = a.seq_offsets[seq + 1];
+  if (begin < 0 || end < begin || end > a.num_tokens) return;
+  int pool = -1;
+  if (a.state_in || a.state_out) {
+    pool = state_row(a.state_index, seq, a.state_rows, status);
+    if (pool < -1) return;
+  }
+  if (__syncthreads_or(failed != 0)) return;
+  const bool works = w * kTiles * 16 < K;
+  const int k0 = works ? w * kTiles * 16 : 0;    // the wave's entries
+  const int64_t stride = (int64_t)a.heads * (V + K) * K;
+  float *at = segments + ((int64_t)(begin / Q + seq) * a.heads + head) * (V + K) * K;
+  // a lane has rows 4 q .. + 3 of entry l16 of each tile
+  f32x4 s[kTiles];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      s[t][r] = a.state_in && pool >= 0 ? a.state_in[(((int64_t)pool * a.heads + head) * V + v0 + q * 4 + r) * K + k0 + t * 16 + l16] : 0.0f;
+  float m[kTiles][kBlocks][4];
+  f32x4 add[kTiles];
+  auto load = [&]() {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[t][b][i] = at[(int64_t)(V + b * 16 + q * 4 + i) * K + k0 + t * 16 + l16];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) add[t][r] = at[(int64_t)(v0 + q * 4 + r) * K + k0 + t * 16 + l16];
+    }
+  };
+  int64_t t0 = begin;
+  int b = 0;
+#pragma unroll 1
+  for (;; b ^= 1) {
+    const bool more = t0 + Q < end;
+    if (more && works) load();
+    if (works)
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          at[(int64_t)(v0 + q * 4 + r) * K + k0 + t * 16 + l16] = s[t][r];
+          lds[b][(q * 4 + r) * kRow + k0 + t * 16 + l16] = s[t][r];
+        }
+    if (!more) return;
+    __syncthreads();
+    if (works) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) s[t] = add[t];
+#pragma unroll
+      for (int c = 0; c < kBlocks; ++c) {
+        const f32x4 left = *(const f32x4 *)&lds[b][l16 * kRow + c * 16 + q * 4];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) s[t] = mul_block(left, f32x4{m[t][c][0], m[t][c][1], m[t][c][2], m[t][c][3]}, s[t]);
+      }
+    }
+    at += stride;
+    t0 += Q;
+  }
 }
 
 }  // namespace cortex

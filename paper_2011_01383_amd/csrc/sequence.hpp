@@ -153,7 +153,7 @@ struct Chunk {
   int slot0;          // the sequence's first slot
 };
 
-inline int64_t chunk_slots(int64_t T, int64_t S, int Q) { return T / Q + S; }
+__host__ __device__ inline int64_t chunk_slots(int64_t T, int64_t S, int Q) { return T / Q + S; }
 
 // The largest i in [0, S) with off[i] / Q + i <= slot, by a search that splits
 // the range 64 ways a round, one offset per lane (one round up to 64 sequences).

@@ -231,3 +231,44 @@ def test_many_prompts(H, G, K, V, dtype):
     p = Delta(11, [int(n) for n in r.integers(0, 100, S)], H, G, K, V, dtype, index=r.permutation(S).tolist())
     y, out = run(p)
     p.check(y, out, "many prompts")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,K,V,lens", [(1, 1, 32, 16, [1500]), (2, 1, 64, 48, [700, 0, 1, 900]), (1, 1, 128, 128, [1300]), (3, 3, 64, 64, [256, 257, 511]),
+                                          (4, 2, 128, 32, [640, 0])])
+def test_few_columns_and_long_prompts(H, G, K, V, lens, dtype):
+    """Prompts cut into segments: their states come from the segments before, in the pool's rows or from zero."""
+    need_gpu()
+    say("delta long prompts", H, G, K, V, lens, dtype)
+    S = len(lens)
+    p = Delta(12, lens, H, G, K, V, dtype, index=[S - i for i in range(S)], rows=S + 1, slow=0.05)
+    y, out = run(p)
+    new = p.check(y, out, "long prompts")
+    got = host(out)
+    for row in set(range(S + 1)) - set(new):
+        assert np.array_equal(got[row], np.full_like(got[row], 7.0))
+    y, _ = run(Delta(12, lens, H, G, K, V, dtype, state=False, slow=0.05), with_state=False)
+    Delta(12, lens, H, G, K, V, dtype, state=False, slow=0.05).check(y, None, "long prompts without states")
+
+
+@pytest.mark.parametrize("where", ["v", "k", "state"])
+def test_what_is_not_finite_in_a_long_prompt(where):
+    need_gpu()
+    say("delta long prompts, not finite", where)
+    p = Delta(13, [1200, 90], 2, 1, 64, 32)
+    clean, end = (host(v) for v in run(p))
+    hit = np.zeros(clean.shape, dtype=bool)
+    hit_end = np.zeros(end.shape, dtype=bool).reshape(2, 2, 32, 64)
+    if where == "v":
+        p.v[600, 1, 5] = np.nan
+        hit[600:1200, 1, 5] = hit_end[0, 1, 5] = True
+    elif where == "k":
+        p.k[600, 0, 9] = np.inf
+        hit[600:1200] = hit_end[0] = True
+    else:
+        p.state[0, 32 + 5, 3] = np.inf
+        hit[:1200, 1, 5] = hit_end[0, 1, 5] = True
+    got, got_end = (host(v) for v in run(p))
+    hit_end = hit_end.reshape(end.shape)
+    assert np.array_equal(got[~hit], clean[~hit]) and np.array_equal(got_end[~hit_end], end[~hit_end])
+    assert not np.isfinite(got[hit]).any() and not np.isfinite(got_end[hit_end].reshape(-1, 64)).all(1).any()
