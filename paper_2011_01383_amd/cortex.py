@@ -724,24 +724,42 @@ def cortex_logits_process(logits: torch.Tensor, *, out=None, token=None, lse=Non
                                         _stream(stream))
 
 
-def _on_current_device(names: str, *tensors) -> None:
-    """The launch goes to the current device, whose memory these have to be."""
+def _all_here(specs, names: str, *tensors) -> None:
+    """_need_all over `specs`, and that these and `tensors` (views, named in `names`) are in the
+    memory of the current device, to which the launch goes."""
     device = tensors[0].get_device()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            break
-    else:
-        if device >= 0 and device == torch.cuda.current_device():
-            return                      # nothing to refuse: the usual call
+    if device >= 0:
+        for t in tensors:
+            if t is not None and t.get_device() != device:
+                break
+        else:
+            for t, _, dtype, min_numel, optional in specs:
+                if t is None:
+                    if not optional:
+                        break
+                elif not (type(t) is torch.Tensor and (dtype is None or t.dtype is dtype) and t.is_contiguous()
+                          and t.numel() >= min_numel and t.get_device() == device):
+                    break
+            else:
+                if device == torch._C._cuda_getDevice():
+                    return              # nothing to refuse: the usual call
+    _need_all(specs)
     _on_device(names, *tensors)
     current = torch.cuda.current_device()
-    for name, t in zip(names.split(), tensors):
+    for name, t in [*zip(names.split(), tensors), *((s[1], s[0]) for s in specs)]:
         if t is not None and t.get_device() != current:
             raise ValueError("%s must be on the current device (%d), got %d" % (name, current, t.get_device()))
 
 
 def _head_rows(t, name: str, dtype, T: int, like=None):
     """A [T, heads, elements] tensor: heads, elements and its row stride."""
+    if type(t) is torch.Tensor and t.dtype is dtype:
+        shape = t.shape
+        if len(shape) == 3:
+            rows, H, P = shape
+            ld, between, inner = t.stride()
+            if rows == T and inner == 1 and between == P and ld >= H * P and (like is None or like == (H, P)):
+                return H, P, ld         # the usual rows
     H, P, ld = _group_rows(t, name, dtype, T)
     if like is not None and (H, P) != like:
         raise ValueError("%s must be [%d, %d, %d], got %s" % (name, T, like[0], like[1], list(t.shape)))
@@ -749,6 +767,8 @@ def _head_rows(t, name: str, dtype, T: int, like=None):
 
 
 def _number(v, name: str) -> float:
+    if type(v) is float:
+        return v
     if isinstance(v, torch.Tensor) or isinstance(v, str):
         raise ValueError("%s must be a number, got %s" % (name, type(v).__name__))
     return float(v)
@@ -780,9 +800,8 @@ def _delta(step: bool, q, k, v, b, offsets, y, dt, A, dt_bias, softplus, sigmoid
         S = offsets.numel() - 1
         specs = [(offsets, "offsets", i32, S + 1, False), (ws, "ws", None, 1, False)]
     rows, state = _state_specs(state_in, state_out, state_index, S, f32, (H * V, K))
-    _need_all(specs + state + [(A, "A", f32, H, True), (dt_bias, "dt_bias", f32, H, True), (status, "status", i32, 1, False)])
-    _on_current_device("q k v b dt y offsets ws A dt_bias state_in state_out state_index status", q, k, v, b, dt, y, offsets, ws,
-                       A, dt_bias, state_in, state_out, state_index, status)
+    _all_here(specs + state + [(A, "A", f32, H, True), (dt_bias, "dt_bias", f32, H, True), (status, "status", i32, 1, False)],
+              "q k v b dt y", q, k, v, b, dt, y)
     args = _pack_delta(_DTYPES[typ], S, T, H, G, K, V, 1 if softplus else 0, 1 if sigmoid else 0, rows,
                        scale, _at(offsets), _at(state_index), q.data_ptr(), k.data_ptr(), v.data_ptr(),
                        b.data_ptr(), _at(dt), q_ld, k_ld, v_ld, b_ld, dt_ld, _at(A), _at(dt_bias), _at(state_in),
@@ -826,8 +845,9 @@ def cortex_qk_norm(q: torch.Tensor, q_out: torch.Tensor, *, k=None, k_out=None, 
     _, _, qo_ld = _head_rows(q_out, "q_out", typ, T, (H, P))
     G = k_ld = ko_ld = R = 0
     if k is not None:
-        G, _, k_ld = _head_rows(k, "k", typ, T)
-        _head_rows(k, "k", typ, T, (G, P))
+        G, K, k_ld = _head_rows(k, "k", typ, T)
+        if K != P:
+            raise ValueError("k must be [%d, heads, %d], got %s" % (T, P, list(k.shape)))
         _, _, ko_ld = _head_rows(k_out, "k_out", typ, T, (G, P))
     elif k_out is not None or k_weight is not None:
         raise ValueError("k is required with k_out and k_weight")
@@ -837,11 +857,9 @@ def cortex_qk_norm(q: torch.Tensor, q_out: torch.Tensor, *, k=None, k_out=None, 
         R = 2 * freqs.numel()
     elif positions is not None:
         raise ValueError("freqs is required with positions")
-    _need_all([(q_weight, "q_weight", f32, P, True), (k_weight, "k_weight", f32, P, True),
+    _all_here([(q_weight, "q_weight", f32, P, True), (k_weight, "k_weight", f32, P, True),
                (positions, "positions", torch.int32, T, freqs is None), (freqs, "freqs", f32, 0, True),
-               (status, "status", torch.int32, 1, False)])
-    _on_current_device("q q_out k k_out q_weight k_weight positions freqs status", q, q_out, k, k_out, q_weight, k_weight,
-                       positions, freqs, status)
+               (status, "status", torch.int32, 1, False)], "q q_out k k_out", q, q_out, k, k_out)
     args = _pack_qk_norm(_DTYPES[typ], T, H, G, P, R, 1 if interleaved else 0, norm, eps, q.data_ptr(), _at(k),
                          q_ld, k_ld, _at(q_weight), _at(k_weight), _at(positions), _at(freqs), q_out.data_ptr(), _at(k_out),
                          qo_ld, ko_ld)
@@ -853,8 +871,7 @@ def cortex_quant_i8(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, *, st
     """x [rows, columns] to q (int8) of the same shape and scale [rows]."""
     rows, cols = _shape2(x, "x")
     x_ld, q_ld = _rows(x, "x", x.dtype, rows, cols), _rows(q, "q", torch.int8, rows, cols)
-    _need_all([(scale, "scale", torch.float32, rows, False), (status, "status", torch.int32, 1, False)])
-    _on_current_device("x q scale status", x, q, scale, status)
+    _all_here([(scale, "scale", torch.float32, rows, False), (status, "status", torch.int32, 1, False)], "x q", x, q)
     args = _pack_quant(_DTYPES[x.dtype], rows, cols, x.data_ptr(), x_ld, q.data_ptr(), q_ld, scale.data_ptr())
     return load().cortex_quant_i8(args, status.data_ptr(), _stream(stream))
 
@@ -878,11 +895,10 @@ def cortex_linear_i8(x: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor, y:
     x_ld, y_ld = _rows(x, "x", y.dtype if x_scale is None else i8, T, K), _rows(y, "y", y.dtype, T, N)
     if w_ld % 16 or w.data_ptr() % 16:
         raise ValueError("w must have rows that start at 16-byte boundaries")
-    if N > 0 and w.storage_offset() + (N - 1) * w_ld + (K + 15) // 16 * 16 > w.untyped_storage().nbytes():
+    if K % 16 and N > 0 and w.storage_offset() + (N - 1) * w_ld + (K + 15) // 16 * 16 > w.untyped_storage().nbytes():
         raise ValueError("w must hold whole pieces of 16 bytes, its last row too")
-    _need_all([(w_scale, "w_scale", f32, N, False), (x_scale, "x_scale", f32, T, True), (bias, "bias", f32, N, True),
-               (status, "status", torch.int32, 1, False), (ws, "ws", None, 1, False)])
-    _on_current_device("x w w_scale y x_scale bias status ws", x, w, w_scale, y, x_scale, bias, status, ws)
+    _all_here([(w_scale, "w_scale", f32, N, False), (x_scale, "x_scale", f32, T, True), (bias, "bias", f32, N, True),
+               (status, "status", torch.int32, 1, False), (ws, "ws", None, 1, False)], "x w y", x, w, y)
     args = _pack_linear(_DTYPES[y.dtype], T, K, N, x.data_ptr(), x_ld, _at(x_scale), w.data_ptr(), w_ld, w_scale.data_ptr(),
                         _at(bias), y.data_ptr(), y_ld)
     return load().cortex_linear_i8(args, status.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream))

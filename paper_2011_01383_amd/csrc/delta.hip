@@ -112,7 +112,7 @@ template <typename T, int K, int NT, bool WIDE>
 void launch_walk(const cortex_delta_t &a, int32_t *status, const ChunkMap *maps, hipStream_t st) {
   constexpr int kColumns = 16 * NT * kChunkWaves;
   const int64_t units = (int64_t)a.num_seqs * a.heads * ((a.value_dim + kColumns - 1) / kColumns);
-  chunk_walk_kernel<T, K, NT, WIDE><<<blocks_of_units(units), kChunkThreads, 0, st>>>(a, status, maps, units);
+  chunk_walk_kernel<T, K, NT, WIDE><<<(unsigned)units, kChunkThreads, 0, st>>>(a, status, maps);
 }
 
 // Workgroups that a launch of segments may have, and so the rows of 16 that they leave.
@@ -162,17 +162,17 @@ template <typename T, int K, bool WIDE> int launch_chunks_of(const cortex_delta_
   }
   const int Q = segment_tokens(a.num_tokens, a.num_seqs, a.heads, K, a.value_dim);
   if (!Q) {
-    chunk_chain_kernel<T, K, 0, WIDE><<<blocks_of_units(units), kChainThreads, 0, st>>>(a, status, maps, nullptr, 0, units);
+    chunk_chain_kernel<T, K, 0, WIDE><<<(unsigned)units, kChainThreads, 0, st>>>(a, status, maps, nullptr, 0);
     return launched() ? CORTEX_OK : CORTEX_E_HIP;
   }
   float *segments = (float *)((char *)maps + map_bytes(a.num_tokens, a.num_seqs, a.heads));
   const int64_t slots = chunk_slots(a.num_tokens, a.num_seqs, Q) * a.heads;
   const int64_t tiles = slots * ((a.value_dim + K) / 16), columns = slots * (a.value_dim / 16);
-  chunk_chain_kernel<T, K, 1, WIDE><<<blocks_of_units(tiles), kChainThreads, 0, st>>>(a, status, maps, segments, Q, tiles);
+  chunk_chain_kernel<T, K, 1, WIDE><<<(unsigned)tiles, kChainThreads, 0, st>>>(a, status, maps, segments, Q);
   if (!launched()) return CORTEX_E_HIP;
   enter_segments_kernel<K><<<(unsigned)units, kChunkThreads, 0, st>>>(a, status, segments, Q);
   if (!launched()) return CORTEX_E_HIP;
-  chunk_chain_kernel<T, K, 2, WIDE><<<blocks_of_units(columns), kChainThreads, 0, st>>>(a, status, maps, segments, Q, columns);
+  chunk_chain_kernel<T, K, 2, WIDE><<<(unsigned)columns, kChainThreads, 0, st>>>(a, status, maps, segments, Q);
   return launched() ? CORTEX_OK : CORTEX_E_HIP;
 }
 

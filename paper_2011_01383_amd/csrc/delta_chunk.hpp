@@ -349,6 +349,25 @@ __global__ void __launch_bounds__(kChunkThreads, 4) chunk_maps_kernel(cortex_del
   if (tid == 0) map.gates[kRest][1] = __builtin_bit_cast(float, lds.first);
 }
 
+// The sequence of a workgroup and its columns' place.  The longest sequences come first (up to 64 of them: a
+// lane each), so that the last workgroups to start are short; workgroups go to the eight XCDs in turn, and
+// neighbouring columns, which read the same keys, to one of them.
+__device__ __forceinline__ int nth_longest(const int32_t *off, int S, int n) {
+  if (S > 64) return n;
+  const int lane = (int)threadIdx.x & 63;
+  const int length = lane < S ? off[lane + 1] - off[lane] : -1;
+  int rank = 0;
+  for (int j = 0; j < S; ++j) {
+    const int other = __builtin_amdgcn_readlane(length, j);
+    rank += other > length || (other == length && j < lane);
+  }
+  return __builtin_ctzll(__ballot(lane < S && rank == n));
+}
+__device__ __forceinline__ int column_of(int64_t unit, int columns) {
+  const int c = (int)(unit % columns);
+  return columns % 8 == 0 ? c % 8 * (columns / 8) + c / 8 : c;
+}
+
 // Products of planes, the largest part last: which plane of a and of b.
 template <int A, int B> struct PlanePairs {
   static constexpr int kCount = A == 1 ? B : 6;
@@ -401,19 +420,17 @@ template <typename T, int K> struct ChunkLds {
 // what one product leaves is the next one's operand in the same lane and nothing goes
 // between waves; keys, queries, T and P are shared in LDS.
 template <typename T, int K, int NT, bool WIDE>
-__global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 : 1) chunk_walk_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps, int64_t units) {
+__global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 : 1) chunk_walk_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps) {
   typedef ChunkLds<T, K> Lds;
   constexpr int KP = Lds::KP, M = K / 32;
   constexpr int kItems = kChunk * (K / 8) / kChunkThreads;     // eights of keys that a thread brings in
   __shared__ Lds lds;
   const int failed = entry_status(status);
-  const int64_t unit = unit_of_block(units);
-  if (unit >= units) return;
+  const int64_t unit = blockIdx.x;
   const int tid = (int)threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, l16 = lane & 15;
-  // a head's sequences are neighbours: an XCD's run of units has long and short ones
-  const int V = a.value_dim, wide = 16 * NT * kChunkWaves, slices = (V + wide - 1) / wide;
-  const int slice = (int)(unit % slices), seq = (int)(unit / slices % a.num_seqs), head = (int)(unit / slices / a.num_seqs);
-  const int v0 = slice * wide + w * 16 * NT;
+  const int V = a.value_dim, wide = 16 * NT * kChunkWaves, slices = (V + wide - 1) / wide, columns = a.heads * slices;
+  const int seq = nth_longest(a.seq_offsets, a.num_seqs, (int)(unit / columns)), column = column_of(unit, columns), head = column / slices;
+  const int v0 = column % slices * wide + w * 16 * NT;
   const bool works = v0 < V;
   const int g = head / (a.heads / a.key_heads);
   // (the same in every lane, and the compiler is told so)
@@ -440,14 +457,15 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
   const T *ks = (const T *)a.k + g * K, *qs = (const T *)a.q + g * K;
   const T *vs = (const T *)a.v + (int64_t)head * V + col;
   T *ys = (T *)a.y + (int64_t)head * V + col;
-#pragma unroll 1
-  for (int t0 = begin; t0 < end; t0 += kChunk, map += a.heads) {
+  // T, P, gates and queries of the next chunk are on their way while the state is updated, straight into LDS; its
+  // keys meanwhile in registers, since the update reads this chunk's.  Rows past the sequence's end repeat its
+  // last; places in a chunk are 32 bits (the host admits no longer rows).
+  constexpr bool kStraight = KP == 1 && WIDE;    // bf16 in whole 16-byte pieces
+  constexpr int kCopies = kMapPieces * 3 * 2, kRows = 512 / K;
+  static_assert(kCopies % kChunkWaves == 0 && sizeof(ChunkMap) == (kCopies + 1) * 1024, "copies of 1 KB, the gates' last");
+  Eight<T> kr[kItems], qr[kStraight ? 1 : kItems];
+  auto bring = [&](int t0, const ChunkMap *map) {
     const int last = min(kChunk, end - t0) - 1;
-    __syncthreads();                             // the last chunk's rows are read
-    // T, P and gates, then keys and queries (bf16 in whole 16-byte pieces: straight into LDS).  Rows past
-    // the sequence's end repeat its last; places in a chunk are 32 bits (the host admits no longer rows).
-    constexpr int kCopies = kMapPieces * 3 * 2;
-    static_assert(kCopies % kChunkWaves == 0 && sizeof(ChunkMap) == (kCopies + 1) * 1024, "copies of 1 KB, the gates' last");
 #pragma unroll
     for (int i = 0; i < kCopies / kChunkWaves; ++i) {
       const int c = w * (kCopies / kChunkWaves) + i;
@@ -455,35 +473,37 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
     }
     if (w == 0) copy_to_lds(map, (uint32_t)(kCopies * 1024 + lane * 16), lds_place(lds.gates));
     const T *k0 = ks + (int64_t)t0 * a.k_ld, *q0 = qs + (int64_t)t0 * a.q_ld;
-    if constexpr (KP == 1 && WIDE) {
-      constexpr int kRows = 512 / K;             // of a copy
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const int id = i * kChunkThreads + tid;
+      const uint32_t row = min(id / (K / 8), last), o = id % (K / 8) * 8;
+      kr[i].template load<WIDE>(k0 + (row * (uint32_t)a.k_ld + o));
+      if constexpr (!kStraight) qr[i].template load<WIDE>(q0 + (row * (uint32_t)a.q_ld + o));
+    }
+    if constexpr (kStraight)
 #pragma unroll
       for (int i = 0; i < kChunk / kRows / kChunkWaves; ++i) {
         const int first = (w * (kChunk / kRows / kChunkWaves) + i) * kRows, row = first + lane / (K / 8);
         const uint32_t e = (uint32_t)Lds::K_::place(row, lane % (K / 8)) * 8, r = (uint32_t)min(row, last);
-        copy_to_lds(k0, (r * (uint32_t)a.k_ld + e) * 2, lds_place(lds.keys) + (uint32_t)(first * K * 2));
         copy_to_lds(q0, (r * (uint32_t)a.q_ld + e) * 2, lds_place(lds.queries) + (uint32_t)(first * K * 2));
       }
-    } else {
-      Eight<T> kr[kItems], qr[kItems];
+  };
+  if (begin < end) bring(begin, map);
+#pragma unroll 1
+  for (int t0 = begin; t0 < end; t0 += kChunk) {
+    const int last = min(kChunk, end - t0) - 1;
+    __syncthreads();                             // the last chunk's keys are read
 #pragma unroll
-      for (int i = 0; i < kItems; ++i) {
-        const int id = i * kChunkThreads + tid;
-        const uint32_t row = min(id / (K / 8), last), o = id % (K / 8) * 8;
-        kr[i].template load<WIDE>(k0 + (row * (uint32_t)a.k_ld + o));
-        qr[i].template load<WIDE>(q0 + (row * (uint32_t)a.q_ld + o));
-      }
+    for (int i = 0; i < kItems; ++i) {
+      const int id = i * kChunkThreads + tid, at = Lds::K_::at(id / (K / 8), id % (K / 8) * 8);
+      bf16x8v f[KP];
+      kr[i].planes(f);
 #pragma unroll
-      for (int i = 0; i < kItems; ++i) {
-        const int id = i * kChunkThreads + tid, at = Lds::K_::at(id / (K / 8), id % (K / 8) * 8);
-        bf16x8v kf[KP], qf[KP];
-        kr[i].planes(kf);
-        qr[i].planes(qf);
+      for (int p = 0; p < KP; ++p) *(u32x4v *)&lds.keys[p][at] = __builtin_bit_cast(u32x4v, f[p]);
+      if constexpr (!kStraight) {
+        qr[i].planes(f);
 #pragma unroll
-        for (int p = 0; p < KP; ++p) {
-          *(u32x4v *)&lds.keys[p][at] = __builtin_bit_cast(u32x4v, kf[p]);
-          *(u32x4v *)&lds.queries[p][at] = __builtin_bit_cast(u32x4v, qf[p]);
-        }
+        for (int p = 0; p < KP; ++p) *(u32x4v *)&lds.queries[p][at] = __builtin_bit_cast(u32x4v, f[p]);
       }
     }
     T v[4][4][NT];
@@ -496,7 +516,6 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
         for (int n = 0; n < NT; ++n) v[t][r][n] = vt[(uint32_t)min(t * 16 + q * 4 + r, last) * (uint32_t)a.v_ld + n];
     copies_done<0>();
     __syncthreads();                             // keys, queries, T, P and gates are there
-    if (!works) continue;
     const float decay = lds.gates[kRest][0];
     int first[NT];
 #pragma unroll
@@ -595,6 +614,11 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
 #pragma unroll
       for (int m = 0; m < 2; ++m) to_planes(u[n][2 * m], u[n][2 * m + 1], planes[n][m]);
     }
+    __syncthreads();                             // all but the keys is read
+    if (t0 + kChunk < end) {
+      map += a.heads;
+      bring(t0 + kChunk, map);
+    }
 #pragma unroll
     for (int m = 0; m < M; ++m) {
       bf16x8v kt[2][2][KP];
@@ -638,7 +662,7 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        if (t * 16 + q * 4 + r <= last)
+        if (works && t * 16 + q * 4 + r <= last)
 #pragma unroll
           for (int n = 0; n < NT; ++n) yt[(uint32_t)(t * 16 + q * 4 + r) * (uint32_t)a.y_ld + n] = from_float<T>(y[n][t][r]);
   }
@@ -685,21 +709,19 @@ template <typename T, int K> struct ChainLds {
 // (from the unit rows, without values) as columns of their own, V + K of them; enter_segments_kernel
 // joins them; part 2 forms the outputs from the state that enters.
 template <typename T, int K, int PART, bool WIDE>
-__global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps, float *segments, int Q,
-                                                                    int64_t units) {
+__global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps, float *segments, int Q) {
   typedef ChainLds<T, K> Lds;
   constexpr int KP = Lds::KP, M = Lds::M;
   constexpr int ST = K == 128 ? 2 : 1;           // tiles of 16 state entries of a wave
   __shared__ Lds lds;
   const int failed = entry_status(status);
-  const int64_t unit = unit_of_block(units);
-  if (unit >= units) return;
+  const int64_t unit = blockIdx.x;
   const int tid = (int)threadIdx.x, lane = tid & 63, q = lane >> 4, l16 = lane & 15;
   // the tokens of a wave; the products of T and of P grow with them, so that a SIMD's two waves have five tiles together
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), w = wave < kChunkWaves ? wave : kChunkWaves - 1 - wave % kChunkWaves;
-  const int V = a.value_dim, rows = PART == 0 ? V : V + K, slices = (PART == 1 ? rows : V) / 16, v0 = (int)(unit % slices) * 16;
-  const int slots = PART == 0 ? a.num_seqs : (int)chunk_slots(a.num_tokens, a.num_seqs, Q);
-  const int slot = (int)(unit / slices % slots), head = (int)(unit / slices / slots);
+  const int V = a.value_dim, rows = PART == 0 ? V : V + K, slices = (PART == 1 ? rows : V) / 16, columns = a.heads * slices;
+  const int place = (int)(unit / columns), slot = PART == 0 ? nth_longest(a.seq_offsets, a.num_seqs, place) : place;
+  const int column = column_of(unit, columns), head = column / slices, v0 = column % slices * 16;
   const bool values = PART != 1 || v0 < V;       // else unit rows
   const int g = head / (a.heads / a.key_heads);
   int seq = slot, begin, end, first, last_token;
