@@ -140,18 +140,19 @@ static int segment_tokens(int64_t T, int64_t S, int64_t heads, int64_t K, int64_
   return Q;
 }
 
-// The workspace: what the first launch leaves for every chunk and head, and the segments' states.
+// The workspace: what the first launch leaves for every chunk and head, the segments' states, and a line that is
+// written and never read.
 static size_t map_bytes(int64_t T, int64_t S, int64_t heads) { return (size_t)(chunk_slots(T, S, kChunk) * heads) * sizeof(ChunkMap); }
-static size_t segment_bytes(int64_t K) { return (size_t)(kMaxSegmentTiles * 16 * K) * sizeof(float); }
+static size_t segment_bytes(int64_t K) { return (size_t)(kMaxSegmentTiles * 16 * K) * sizeof(float) + 256; }
 
 template <typename T, int K, bool WIDE> int launch_chunks_of(const cortex_delta_t &a, int32_t *status, ChunkMap *maps, void *stream) {
   const hipStream_t st = (hipStream_t)stream;
   const int64_t chunks = chunk_slots(a.num_tokens, a.num_seqs, kChunk) * a.heads;
   const int64_t units = (int64_t)a.num_seqs * a.heads * (a.value_dim / 16);
-  // Eight waves to 16 columns while there are fewer than four workgroups of them a CU, else a wave each:
-  // 512 columns' units 400 us against 515 (8,192 tokens of 2 prompts, 32 heads of 128 by 128), 768 units 223
-  // against 279 (12,000 tokens of 6, 16 heads of 64 by 128), 1,024 units 370 against 348 (8,192 of 4),
-  // 2,048 units 362 against 270 (of 8).
+  // Eight waves to 16 columns while there are fewer than four workgroups of them a CU, else a wave each: at 512
+  // units 324 us against 486 (8,192 tokens of 2 prompts, 32 heads of 128 by 128), at 768 189 against 255 (12,000 tokens
+  // of 6, 16 heads of 64 by 128), at 1,024 319 against 325 (8,192 of 4) and 48 against 36 (4,096 of 32, 8 heads of
+  // 64 by 64), at 2,048 339 against 234 (8,192 of 8).
   const bool few = units < 1024;
   if (few) chunk_maps_kernel<T, K, false, WIDE><<<blocks_of_units(chunks), kChunkThreads, 0, st>>>(a, status, maps, chunks);
   else chunk_maps_kernel<T, K, true, WIDE><<<blocks_of_units(chunks), kChunkThreads, 0, st>>>(a, status, maps, chunks);
@@ -161,18 +162,19 @@ template <typename T, int K, bool WIDE> int launch_chunks_of(const cortex_delta_
     return launched() ? CORTEX_OK : CORTEX_E_HIP;
   }
   const int Q = segment_tokens(a.num_tokens, a.num_seqs, a.heads, K, a.value_dim);
+  float *segments = (float *)((char *)maps + map_bytes(a.num_tokens, a.num_seqs, a.heads));
+  float *nowhere = segments + kMaxSegmentTiles * 16 * K;
   if (!Q) {
-    chunk_chain_kernel<T, K, 0, WIDE><<<(unsigned)units, kChainThreads, 0, st>>>(a, status, maps, nullptr, 0);
+    chunk_chain_kernel<T, K, 0, WIDE><<<(unsigned)units, kChainThreads, 0, st>>>(a, status, maps, segments, nowhere, 0);
     return launched() ? CORTEX_OK : CORTEX_E_HIP;
   }
-  float *segments = (float *)((char *)maps + map_bytes(a.num_tokens, a.num_seqs, a.heads));
   const int64_t slots = chunk_slots(a.num_tokens, a.num_seqs, Q) * a.heads;
   const int64_t tiles = slots * ((a.value_dim + K) / 16), columns = slots * (a.value_dim / 16);
-  chunk_chain_kernel<T, K, 1, WIDE><<<(unsigned)tiles, kChainThreads, 0, st>>>(a, status, maps, segments, Q);
+  chunk_chain_kernel<T, K, 1, WIDE><<<(unsigned)tiles, kChainThreads, 0, st>>>(a, status, maps, segments, nowhere, Q);
   if (!launched()) return CORTEX_E_HIP;
   enter_segments_kernel<K><<<(unsigned)units, kChunkThreads, 0, st>>>(a, status, segments, Q);
   if (!launched()) return CORTEX_E_HIP;
-  chunk_chain_kernel<T, K, 2, WIDE><<<(unsigned)columns, kChainThreads, 0, st>>>(a, status, maps, segments, Q);
+  chunk_chain_kernel<T, K, 2, WIDE><<<(unsigned)columns, kChainThreads, 0, st>>>(a, status, maps, segments, nowhere, Q);
   return launched() ? CORTEX_OK : CORTEX_E_HIP;
 }
 

@@ -492,6 +492,7 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
 #pragma unroll 1
   for (int t0 = begin; t0 < end; t0 += kChunk) {
     const int last = min(kChunk, end - t0) - 1;
+    copies_done<0>();
     __syncthreads();                             // the last chunk's keys are read
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
@@ -514,7 +515,6 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int n = 0; n < NT; ++n) v[t][r][n] = vt[(uint32_t)min(t * 16 + q * 4 + r, last) * (uint32_t)a.v_ld + n];
-    copies_done<0>();
     __syncthreads();                             // keys, queries, T, P and gates are there
     const float decay = lds.gates[kRest][0];
     int first[NT];
@@ -614,6 +614,23 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
 #pragma unroll
       for (int m = 0; m < 2; ++m) to_planes(u[n][2 * m], u[n][2 * m + 1], planes[n][m]);
     }
+    // y, before the copies that the next chunk waits for
+    T *yt = ys + (int64_t)t0 * a.y_ld;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+      if (__any(first[n] < kChunk))
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (t * 16 + q * 4 + r >= first[n]) y[n][t][r] = __builtin_nanf("");
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (works && t * 16 + q * 4 + r <= last)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) yt[(uint32_t)(t * 16 + q * 4 + r) * (uint32_t)a.y_ld + n] = from_float<T>(y[n][t][r]);
     __syncthreads();                             // all but the keys is read
     if (t0 + kChunk < end) {
       map += a.heads;
@@ -645,26 +662,11 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
             for (int n = 0; n < NT; ++n)
               S[n][2 * m + s] = mfma_bf16x32(kt[s][h][KeyPairs::left(i)], planes[n][h][KeyPairs::right(i)], S[n][2 * m + s]);
     }
-    T *yt = ys + (int64_t)t0 * a.y_ld;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
-      if (__any(first[n] < kChunk)) {
+      if (first[n] < kChunk)
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (t * 16 + q * 4 + r >= first[n]) y[n][t][r] = __builtin_nanf("");
-        if (first[n] < kChunk)
-#pragma unroll
-          for (int s = 0; s < 2 * M; ++s) S[n][s] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
-      }
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (works && t * 16 + q * 4 + r <= last)
-#pragma unroll
-          for (int n = 0; n < NT; ++n) yt[(uint32_t)(t * 16 + q * 4 + r) * (uint32_t)a.y_ld + n] = from_float<T>(y[n][t][r]);
+        for (int s = 0; s < 2 * M; ++s) S[n][s] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
   }
   if (a.state_out && pool >= 0 && works)
 #pragma unroll
@@ -709,7 +711,7 @@ template <typename T, int K> struct ChainLds {
 // (from the unit rows, without values) as columns of their own, V + K of them; enter_segments_kernel
 // joins them; part 2 forms the outputs from the state that enters.
 template <typename T, int K, int PART, bool WIDE>
-__global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps, float *segments, int Q) {
+__global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps, float *segments, float *nowhere, int Q) {
   typedef ChainLds<T, K> Lds;
   constexpr int KP = Lds::KP, M = Lds::M;
   constexpr int ST = K == 128 ? 2 : 1;           // tiles of 16 state entries of a wave
@@ -832,10 +834,13 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
     auto store = [&](int t0, int b) {
       const int from = lds.first[b][l16], last = last_of(t0);
       T *yt = ys + (int64_t)t0 * a.y_ld;
+      // Without a condition, so that the wait for a later load does not take the stores with it (they may not have
+      // been made): rows past the end go where nothing is read.
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int i = w * 16 + q * 4 + r;
-        if (i <= last) yt[(uint32_t)i * (uint32_t)a.y_ld] = from_float<T>(i < from ? y[r] : __builtin_nanf(""));
+        T *const p = i <= last ? yt + (uint32_t)i * (uint32_t)a.y_ld : (T *)nowhere + lane;
+        *p = from_float<T>(i < from ? y[r] : __builtin_nanf(""));
       }
     };
     int t0 = begin, b = 0;
