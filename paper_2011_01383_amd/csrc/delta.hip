@@ -108,11 +108,11 @@ template <typename T, int K> int launch_step_of(const cortex_delta_t &a, int32_t
   return launched() ? CORTEX_OK : CORTEX_E_HIP;
 }
 
-template <typename T, int K, int NT, bool WIDE>
+template <typename T, int K, bool WIDE>
 void launch_walk(const cortex_delta_t &a, int32_t *status, const ChunkMap *maps, hipStream_t st) {
-  constexpr int kColumns = 16 * NT * kChunkWaves;
+  constexpr int kColumns = 16 * kChunkWaves;
   const int64_t units = (int64_t)a.num_seqs * a.heads * ((a.value_dim + kColumns - 1) / kColumns);
-  chunk_walk_kernel<T, K, NT, WIDE><<<(unsigned)units, kChunkThreads, 0, st>>>(a, status, maps);
+  chunk_walk_kernel<T, K, WIDE><<<(unsigned)units, kChunkThreads, 0, st>>>(a, status, maps);
 }
 
 // Workgroups that a launch of segments may have, and so the rows of 16 that they leave.
@@ -158,7 +158,7 @@ template <typename T, int K, bool WIDE> int launch_chunks_of(const cortex_delta_
   else chunk_maps_kernel<T, K, true, WIDE><<<blocks_of_units(chunks), kChunkThreads, 0, st>>>(a, status, maps, chunks);
   if (!launched()) return CORTEX_E_HIP;
   if (!few) {
-    launch_walk<T, K, 1, WIDE>(a, status, maps, st);
+    launch_walk<T, K, WIDE>(a, status, maps, st);
     return launched() ? CORTEX_OK : CORTEX_E_HIP;
   }
   const int Q = segment_tokens(a.num_tokens, a.num_seqs, a.heads, K, a.value_dim);

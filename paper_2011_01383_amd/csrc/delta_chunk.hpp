@@ -9,8 +9,9 @@
 //   y_i = scale exp(c_i) S q_i + sum_{j <= i} P_ij u_j
 //   S'  = exp(c_63) S + sum_j exp(c_63 - c_j) u_j k_j^T
 // T and P depend on keys, queries and gates only: one launch makes them for all chunks
-// at once (chunk_maps_kernel), and a second walks the chunks of a sequence, a workgroup 16 NT
-// rows of one head's state (chunk_walk_kernel).
+// at once (chunk_maps_kernel), and a second walks the chunks of a sequence: with a wave to 16
+// rows of a head's state where there are many (chunk_walk_kernel), a workgroup where there are few
+// (chunk_chain_kernel).
 //
 // Precision.  bf16 queries and keys enter the matrix units as they are, float32 ones and
 // all that is computed on the way (T, P, R, U, the state) as three bf16 planes, eight bits
@@ -416,11 +417,11 @@ template <typename T, int K> struct ChunkLds {
   alignas(1024) float gates[kGates][kChunk];
 };
 
-// A wave has 16 NT columns of the state (value channels) for all tokens and keys of its head, so
+// A wave has 16 columns of the state (value channels) for all tokens and keys of its head, so
 // what one product leaves is the next one's operand in the same lane and nothing goes
 // between waves; keys, queries, T and P are shared in LDS.
-template <typename T, int K, int NT, bool WIDE>
-__global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 : 1) chunk_walk_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps) {
+template <typename T, int K, bool WIDE>
+__global__ void __launch_bounds__(kChunkThreads, sizeof(T) == 2 ? 2 : 1) chunk_walk_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps) {
   typedef ChunkLds<T, K> Lds;
   constexpr int KP = Lds::KP, M = K / 32;
   constexpr int kItems = kChunk * (K / 8) / kChunkThreads;     // eights of keys that a thread brings in
@@ -428,9 +429,9 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
   const int failed = entry_status(status);
   const int64_t unit = blockIdx.x;
   const int tid = (int)threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, l16 = lane & 15;
-  const int V = a.value_dim, wide = 16 * NT * kChunkWaves, slices = (V + wide - 1) / wide, columns = a.heads * slices;
+  const int V = a.value_dim, wide = 16 * kChunkWaves, slices = (V + wide - 1) / wide, columns = a.heads * slices;
   const int seq = nth_longest(a.seq_offsets, a.num_seqs, (int)(unit / columns)), column = column_of(unit, columns), head = column / slices;
-  const int v0 = column % slices * wide + w * 16 * NT;
+  const int v0 = column % slices * wide + w * 16;
   const bool works = v0 < V;
   const int g = head / (a.heads / a.key_heads);
   // (the same in every lane, and the compiler is told so)
@@ -442,15 +443,13 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
     if (pool < -1) return;
   }
   if (__syncthreads_or(failed != 0)) return;
-  // columns NT l16 .. + NT - 1; of the state's tile 2 m + s the lane has entries 32 m + 8 q + 4 s .. + 3
-  const int col = works ? v0 + l16 * NT : 0;
+  // column l16; of the state's tile 2 m + s the lane has entries 32 m + 8 q + 4 s .. + 3
+  const int col = works ? v0 + l16 : 0;
   const int64_t state_at = (((int64_t)pool * a.heads + head) * V + col) * K + q * 8;
-  f32x4 S[NT][2 * M];
+  f32x4 S[2 * M];
 #pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int s = 0; s < 2 * M; ++s)
-      S[n][s] = a.state_in && pool >= 0 && works ? *(const f32x4 *)(a.state_in + state_at + n * K + s / 2 * 32 + s % 2 * 4)
+  for (int s = 0; s < 2 * M; ++s)
+      S[s] = a.state_in && pool >= 0 && works ? *(const f32x4 *)(a.state_in + state_at + s / 2 * 32 + s % 2 * 4)
                                                  : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
   const ChunkMap *map = maps + ((int64_t)(begin / kChunk) + seq) * a.heads + head;
@@ -507,39 +506,28 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
         for (int p = 0; p < KP; ++p) *(u32x4v *)&lds.queries[p][at] = __builtin_bit_cast(u32x4v, f[p]);
       }
     }
-    T v[4][4][NT];
+    T v[4][4];
     const T *vt = vs + (int64_t)t0 * a.v_ld;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) v[t][r][n] = vt[(uint32_t)min(t * 16 + q * 4 + r, last) * (uint32_t)a.v_ld + n];
+      for (int r = 0; r < 4; ++r) v[t][r] = vt[(uint32_t)min(t * 16 + q * 4 + r, last) * (uint32_t)a.v_ld];
     __syncthreads();                             // keys, queries, T, P and gates are there
     const float decay = lds.gates[kRest][0];
-    int first[NT];
+    int first = __builtin_bit_cast(int, lds.gates[kRest][1]);
+    auto to_planes = [](const f32x4 &lo, const f32x4 &hi, bf16x8v (&p)[3]) {
+      float e[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      planes8(e, p);
+    };
+    f32x4 kS[4], y[4];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) first[n] = __builtin_bit_cast(int, lds.gates[kRest][1]);
-    f32x4 kS[NT][4], y[NT][4];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) kS[n][t] = y[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int t = 0; t < 4; ++t) kS[t] = y[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-      bf16x8v sp[NT][3];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float e[8];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          e[r] = S[n][2 * m][r];
-          e[4 + r] = S[n][2 * m + 1][r];
-        }
-        planes8(e, sp[n]);
-      }
+      bf16x8v sp[3];
+      to_planes(S[2 * m], S[2 * m + 1], sp);
       typedef PlanePairs<KP, 3> Pairs;
-      auto by_state = [&](const unsigned short (&rows)[KP][kChunk * K], f32x4 (&to)[NT][4]) {
+      auto by_state = [&](const unsigned short (&rows)[KP][kChunk * K], f32x4 (&to)[4]) {
         bf16x8v f[4][KP];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -548,20 +536,14 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
 #pragma unroll
         for (int i = 0; i < Pairs::kCount; ++i)
 #pragma unroll
-          for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) to[n][t] = mfma_bf16x32(f[t][Pairs::left(i)], sp[n][Pairs::right(i)], to[n][t]);
+          for (int t = 0; t < 4; ++t) to[t] = mfma_bf16x32(f[t][Pairs::left(i)], sp[Pairs::right(i)], to[t]);
       };
       by_state(lds.keys, kS);
       by_state(lds.queries, y);
     }
     typedef PlanePairs<3, 3> Pairs;
-    auto to_planes = [](const f32x4 &lo, const f32x4 &hi, bf16x8v (&p)[3]) {
-      float e[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      planes8(e, p);
-    };
     // c += pieces of T or P by the planes of 64 tokens
-    auto by_map = [&](const u32x4v (&map)[kMapPieces][3][64], const bf16x8v (&p)[NT][2][3], f32x4 (&to)[NT][4]) {
+    auto by_map = [&](const u32x4v (&map)[kMapPieces][3][64], const bf16x8v (&p)[2][3], f32x4 (&to)[4]) {
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -574,63 +556,47 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
 #pragma unroll
           for (int i = 0; i < Pairs::kCount; ++i)
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-              for (int n = 0; n < NT; ++n) to[n][t + s] = mfma_bf16x32(f[s][Pairs::left(i)], p[n][m][Pairs::right(i)], to[n][t + s]);
+            for (int s = 0; s < 2; ++s) to[t + s] = mfma_bf16x32(f[s][Pairs::left(i)], p[m][Pairs::right(i)], to[t + s]);
         }
     };
-    f32x4 u[NT][4];
-    bf16x8v planes[NT][2][3];
+    f32x4 u[4];
+    bf16x8v planes[2][3];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int t = 0; t < 4; ++t) {
+      const f32x4 beta = *(const f32x4 *)&lds.gates[kBeta][t * 16 + q * 4], grow = *(const f32x4 *)&lds.gates[kGrow][t * 16 + q * 4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const f32x4 beta = *(const f32x4 *)&lds.gates[kBeta][t * 16 + q * 4], grow = *(const f32x4 *)&lds.gates[kGrow][t * 16 + q * 4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float x = beta[r] * (to_float<T>(v[t][r][n]) - grow[r] * kS[n][t][r]);
-          kS[n][t][r] = t * 16 + q * 4 + r <= last ? x : 0.0f;
-          y[n][t][r] *= a.scale * grow[r];
-        }
+      for (int r = 0; r < 4; ++r) {
+        const float x = beta[r] * (to_float<T>(v[t][r]) - grow[r] * kS[t][r]);
+        kS[t][r] = t * 16 + q * 4 + r <= last ? x : 0.0f;
+        y[t][r] *= a.scale * grow[r];
       }
-      drop_odd(kS[n], q, first[n]);
-#pragma unroll
-      for (int m = 0; m < 2; ++m) to_planes(kS[n][2 * m], kS[n][2 * m + 1], planes[n][m]);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) u[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      u[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
+    drop_odd(kS, q, first);
+#pragma unroll
+    for (int m = 0; m < 2; ++m) to_planes(kS[2 * m], kS[2 * m + 1], planes[m]);
     by_map(lds.inverse, planes, u);
+    drop_odd(u, q, first);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      drop_odd(u[n], q, first[n]);
-#pragma unroll
-      for (int m = 0; m < 2; ++m) to_planes(u[n][2 * m], u[n][2 * m + 1], planes[n][m]);
-    }
+    for (int m = 0; m < 2; ++m) to_planes(u[2 * m], u[2 * m + 1], planes[m]);
     by_map(lds.scores, planes, y);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int t = 0; t < 4; ++t) u[t] *= *(const f32x4 *)&lds.gates[kWeight][t * 16 + q * 4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) u[n][t] *= *(const f32x4 *)&lds.gates[kWeight][t * 16 + q * 4];
-#pragma unroll
-      for (int m = 0; m < 2; ++m) to_planes(u[n][2 * m], u[n][2 * m + 1], planes[n][m]);
-    }
+    for (int m = 0; m < 2; ++m) to_planes(u[2 * m], u[2 * m + 1], planes[m]);
     // y, before the copies that the next chunk waits for
     T *yt = ys + (int64_t)t0 * a.y_ld;
+    if (__any(first < kChunk))
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-      if (__any(first[n] < kChunk))
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (t * 16 + q * 4 + r >= first[n]) y[n][t][r] = __builtin_nanf("");
+        for (int r = 0; r < 4; ++r)
+          if (t * 16 + q * 4 + r >= first) y[t][r] = __builtin_nanf("");
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        if (works && t * 16 + q * 4 + r <= last)
-#pragma unroll
-          for (int n = 0; n < NT; ++n) yt[(uint32_t)(t * 16 + q * 4 + r) * (uint32_t)a.y_ld + n] = from_float<T>(y[n][t][r]);
+        if (works && t * 16 + q * 4 + r <= last) yt[(uint32_t)(t * 16 + q * 4 + r) * (uint32_t)a.y_ld] = from_float<T>(y[t][r]);
     __syncthreads();                             // all but the keys is read
     if (t0 + kChunk < end) {
       map += a.heads;
@@ -641,8 +607,7 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
       bf16x8v kt[2][2][KP];
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) S[n][2 * m + s] *= decay;
+        S[2 * m + s] *= decay;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int at = Lds::K_::at(h * 32 + q * 4 + l16 / 4, m * 32 + l16 % 4 * 8 + s * 4);
@@ -658,21 +623,15 @@ __global__ void __launch_bounds__(kChunkThreads, NT == 1 && sizeof(T) == 2 ? 2 :
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-              S[n][2 * m + s] = mfma_bf16x32(kt[s][h][KeyPairs::left(i)], planes[n][h][KeyPairs::right(i)], S[n][2 * m + s]);
+            S[2 * m + s] = mfma_bf16x32(kt[s][h][KeyPairs::left(i)], planes[h][KeyPairs::right(i)], S[2 * m + s]);
     }
+    if (first < kChunk)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-      if (first[n] < kChunk)
-#pragma unroll
-        for (int s = 0; s < 2 * M; ++s) S[n][s] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
+      for (int s = 0; s < 2 * M; ++s) S[s] = f32x4{__builtin_nanf(""), __builtin_nanf(""), __builtin_nanf(""), __builtin_nanf("")};
   }
   if (a.state_out && pool >= 0 && works)
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int s = 0; s < 2 * M; ++s) *(f32x4 *)(a.state_out + state_at + n * K + s / 2 * 32 + s % 2 * 4) = S[n][s];
+    for (int s = 0; s < 2 * M; ++s) *(f32x4 *)(a.state_out + state_at + s / 2 * 32 + s % 2 * 4) = S[s];
 }
 
 // Four values of one column as the lane's half of an operand, three planes.
