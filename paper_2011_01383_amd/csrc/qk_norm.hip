@@ -57,7 +57,7 @@ template <int LANES> __device__ __forceinline__ float lanes_sum(float v) {
 // token's heads, queries then keys) from `first` on, `rows` of them.
 template <typename T, int LANES, bool INTERLEAVED>
 __global__ void __launch_bounds__(64 * kNormWaves) norm_wide_kernel(cortex_qk_norm_t a, int32_t *status, int splits) {
-  constexpr int V = 16 / (int)sizeof(T), kRound = 64 / LANES, UNROLL = 2;
+  constexpr int V = 16 / (int)sizeof(T), kRound = 64 / LANES;
   __shared__ float turn[kNormWaves][2][kMaxHeadDim / 2];
   if (entry_status(status) != 0) return;
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
@@ -98,8 +98,7 @@ __global__ void __launch_bounds__(64 * kNormWaves) norm_wide_kernel(cortex_qk_no
       }
   }
   const int each = (total + splits - 1) / splits, first = (int)(task % splits) * each, last = min(first + each, total);
-  // Heads of q, then of k, each with their weights in registers; UNROLL rounds' loads are
-  // made at once.
+  // Heads of q, then of k, each with their weights in registers.
   auto run = [&](const T *in, T *out, const float *weight, int from, int to) {
     if (from >= to) return;
     float g[2 * V];
@@ -108,46 +107,31 @@ __global__ void __launch_bounds__(64 * kNormWaves) norm_wide_kernel(cortex_qk_no
       g[i] = weight ? weight[lo + i] : 1.0f;
       g[V + i] = weight ? weight[hi + i] : 1.0f;
     }
-    for (int r0 = from + group; r0 - group < to; r0 += kRound * UNROLL) {
-      typedef T pack __attribute__((ext_vector_type(V)));
-      pack u[UNROLL], w[UNROLL];
+    for (int r = from + group; r - group < to; r += kRound) {
+      const T *p = in + (int64_t)min(r, to - 1) * P;
+      float x[2][V], squares = 0.0f;
+      Pack<T, V>::load(p + lo, x[0]);
+      Pack<T, V>::load(p + hi, x[1]);
 #pragma unroll
-      for (int k = 0; k < UNROLL; ++k) {
-        const T *p = in + (int64_t)min(r0 + k * kRound, to - 1) * P;
-        u[k] = *(const pack *)(p + lo);
-        w[k] = *(const pack *)(p + hi);
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < V; ++i) squares = __builtin_fmaf(x[h][i], x[h][i], squares);
+      const float m = norm_scale(a, lanes_sum<LANES>(works ? squares : 0.0f));
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[h][i] *= m * g[h * V + i];
+      float y[2][V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float *d = INTERLEAVED ? &y[2 * i / V][2 * i % V] : &y[0][i], *e = INTERLEAVED ? &y[2 * i / V][2 * i % V + 1] : &y[1][i];
+        const float f = INTERLEAVED ? x[2 * i / V][2 * i % V] : x[0][i], k = INTERLEAVED ? x[2 * i / V][2 * i % V + 1] : x[1][i];
+        *d = f * c[i] - k * s[i];
+        *e = k * c[i] + f * s[i];
       }
-#pragma unroll
-      for (int k = 0; k < UNROLL; ++k) {
-        float x[2 * V], squares = 0.0f;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          x[i] = to_float<T>(u[k][i]);
-          x[V + i] = to_float<T>(w[k][i]);
-        }
-#pragma unroll
-        for (int i = 0; i < 2 * V; ++i) squares = __builtin_fmaf(x[i], x[i], squares);
-        const float m = norm_scale(a, lanes_sum<LANES>(works ? squares : 0.0f));
-#pragma unroll
-        for (int i = 0; i < 2 * V; ++i) x[i] *= m * g[i];
-        float y[2][V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float f = INTERLEAVED ? x[2 * i] : x[i], h = INTERLEAVED ? x[2 * i + 1] : x[V + i];
-          const float d = f * c[i] - h * s[i], e = h * c[i] + f * s[i];
-          if (INTERLEAVED) {
-            y[2 * i / V][2 * i % V] = d;
-            y[2 * i / V][2 * i % V + 1] = e;
-          } else {
-            y[0][i] = d;
-            y[1][i] = e;
-          }
-        }
-        const int r = r0 + k * kRound;
-        if (works && r < to) {
-          Pack<T, V>::store(out + (int64_t)r * P + lo, y[0]);
-          Pack<T, V>::store(out + (int64_t)r * P + hi, y[1]);
-        }
+      if (works && r < to) {
+        Pack<T, V>::store(out + (int64_t)r * P + lo, y[0]);
+        Pack<T, V>::store(out + (int64_t)r * P + hi, y[1]);
       }
     }
   };
@@ -212,17 +196,21 @@ template <typename T> int launch_norm(const cortex_qk_norm_t &a, int32_t *status
   const bool wide = a.head_dim % (2 * V) == 0 && (a.interleaved || a.rotary_dim % (2 * V) == 0) && rows16(a.q, a.q_ld) &&
                     rows16(a.q_out, a.q_out_ld) && (!a.key_heads || (rows16(a.k, a.k_ld) && rows16(a.k_out, a.k_out_ld)));
   const int total = a.heads + a.key_heads;
-  if (!wide) {
-    const int64_t tasks = (int64_t)a.num_tokens * total;
+  const int64_t tasks = (int64_t)a.num_tokens * total;
+  // A wave a head while there are at most four a SIMD: 1 token of 40 heads of 128 2.9 us against 4.0, 100 tokens 3.8
+  // against 4.4, but 200 tokens 5.2 against 4.6 and 8,192 126 against 43.
+  if (!wide || tasks <= 4096) {
     norm_pair_kernel<T><<<(unsigned)((tasks + kNormWaves - 1) / kNormWaves), 64 * kNormWaves, 0, (hipStream_t)stream>>>(a, status);
     return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
   }
   int lanes = 1;
   while (lanes * 2 * V < a.head_dim) lanes *= 2;
-  // A token's heads go to several waves while there are fewer than four a SIMD (1,024).
+  // A token's heads go to several waves as long as that leaves at most two a SIMD (1,024 of them): 512 tokens of 72
+  // heads of 256 13.5 us with 4 waves each, 15.7 with 8, 18.8 with one; 8,192 of 40 heads of 128 43 with one, 65 with
+  // ten.  Loads of two heads at once changed nothing (43.3, 15.6).
   const int at_once = 64 / lanes, most = (total + at_once - 1) / at_once;
-  const int64_t want = (4096 + a.num_tokens - 1) / a.num_tokens;
-  const int splits = (int)(want < most ? want : most);
+  const int64_t want = 2048 / a.num_tokens;
+  const int splits = (int)(want < 1 ? 1 : want < most ? want : most);
   switch (lanes) {
     case 1: return launch_wide<T, 1>(a, status, splits, stream);
     case 2: return launch_wide<T, 2>(a, status, splits, stream);

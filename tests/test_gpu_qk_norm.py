@@ -159,3 +159,54 @@ def test_an_earlier_error_leaves_outputs():
         C.check(C.cortex_qk_norm(q[:, :, :P].contiguous(), out, status=status))
         torch.cuda.synchronize()
         assert (out == 5.0).all() and int(status.item()) == C.CORTEX_ST_CYCLE
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("norm", sorted(NORMS))
+@pytest.mark.parametrize("P,R", [(128, 128), (128, 32), (64, 64), (64, 0), (32, 32), (256, 128), (80, 48), (96, 96), (512, 512), (16, 16),
+                                 (512, 16), (256, 6), (66, 10)])
+def test_heads_of_many_rows(P, R, norm, interleaved, dtype):
+    """More rows than have a wave each."""
+    need_gpu()
+    say("norm many rows", P, R, norm, interleaved, dtype)
+    run(make(8, 823, 3, 2, P, R, dtype), norm, interleaved)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H,G", [(64, 65, 0), (101, 40, 8), (513, 9, 1), (1025, 17, 5), (4099, 1, 0), (4500, 4, 4)])
+def test_sizes_of_many_rows(T, H, G, dtype):
+    need_gpu()
+    say("norm sizes of many rows", T, H, G, dtype)
+    run(make(9, T, H, G, 64, 64, dtype), "rms", False)
+    run(make(9, T, H, G, 32, 16, dtype), "l2", True, left=8, in_place=True)
+
+
+def test_special_values_in_many_rows():
+    """As in few: zeros, NaN, infinities, positions to the ends of their type, an earlier error, a graph."""
+    need_gpu()
+    say("norm special values in many rows")
+    p = make(10, 4200, 1, 1, 64, 64, "f32", far=2 ** 31 - 1)
+    p["at"][:4] = [2 ** 31 - 1, -2 ** 31, 0, -1]
+    run(p, "none", True, weights=False)
+    q = dev(p["q"].reshape(4200, -1)).reshape(4200, 1, 64)
+    q[1] = 0.0
+    q[2, 0, 5], q[3, 0, 7] = float("nan"), float("inf")
+    out, status = torch.full_like(q, 5.0), torch.full((1,), C.CORTEX_ST_CYCLE, dtype=torch.int32, device="cuda")
+    kw = dict(norm=C.CORTEX_NORM_L2, positions=dev(p["at"], torch.int32), freqs=dev(p["freqs"]), status=status)
+    C.check(C.cortex_qk_norm(q, out, **kw))
+    torch.cuda.synchronize()
+    assert (out == 5.0).all() and int(status.item()) == C.CORTEX_ST_CYCLE
+    status.zero_()
+    C.check(C.cortex_qk_norm(q, out, **kw))
+    torch.cuda.synchronize()
+    assert (out[1] == 0).all() and torch.isnan(out[2]).all() and torch.isnan(out[3]).any()
+    assert torch.isfinite(out[0]).all() and torch.isfinite(out[4:]).all()
+    graph, again = torch.cuda.CUDAGraph(), torch.empty_like(q)
+    with torch.cuda.graph(graph):
+        C.check(C.cortex_qk_norm(q, again, **kw))
+    for _ in range(3):
+        again.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(again[4:], out[4:]) and torch.equal(again[:2], out[:2])
