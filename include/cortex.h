@@ -532,7 +532,10 @@ typedef struct {
 } cortex_delta_t;
 
 /* Workspace bytes of cortex_delta_forward for batches of up to num_tokens tokens in
- * up to num_seqs sequences (0 if invalid); it need not be zeroed. */
+ * up to num_seqs sequences (0 if invalid); it need not be zeroed.  It holds 37,888 for
+ * each of floor(T / 64) + S chunks and every head, and 4 to 16 MiB for segments.  Chunks times
+ * heads are at most 2^23, or cortex_delta_forward returns CORTEX_E_INVAL; a caller that
+ * serves longer prompts does them in parts, each from the state that the last one left. */
 size_t cortex_delta_workspace_bytes(int32_t num_tokens, int32_t num_seqs, int32_t heads, int32_t key_dim,
                                     int32_t value_dim);
 int cortex_delta_forward(const cortex_delta_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream);
@@ -605,7 +608,8 @@ int cortex_quant_i8(const cortex_quant_i8_t *args, int32_t *d_status, void *stre
  * then rounded to float32, multiplied by the two scales in turn and added to the bias,
  * each rounded on its own, and rounded to dtype.  Rows of w start at 16-byte
  * boundaries and lie w_ld bytes apart, a multiple of 16 up to 2^24; what their last 16
- * bytes hold past the inputs does not matter, but is read.
+ * bytes hold past the inputs does not matter, but is read.  N is at most 2^26, T less than
+ * 2^24 and T N at most 2^37.
  */
 typedef struct {
   int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: y, and x without x_scale */

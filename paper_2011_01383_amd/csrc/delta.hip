@@ -242,7 +242,7 @@ extern "C" int cortex_delta_forward(const cortex_delta_t *args, int32_t *d_statu
   if (rc != CORTEX_OK) return rc;
   if (args->num_seqs == 0) return CORTEX_OK;
   // a workgroup a chunk and head, and a grid has less than 2^32 threads
-  if (chunk_slots(args->num_tokens, args->num_seqs, kChunk) * args->heads >= (int64_t)1 << 24) return CORTEX_E_INVAL;
+  if (chunk_slots(args->num_tokens, args->num_seqs, kChunk) * args->heads > (int64_t)1 << 23) return CORTEX_E_INVAL;
   if (!d_ws || !aligned16(d_ws)) return CORTEX_E_INVAL;
   if (ws_bytes < map_bytes(args->num_tokens, args->num_seqs, args->heads) + segment_bytes(args->key_dim)) return CORTEX_E_WORKSPACE;
   return args->dtype == CORTEX_BF16 ? launch_forward<bf16_t>(*args, d_status, d_ws, stream)

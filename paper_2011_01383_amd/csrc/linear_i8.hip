@@ -11,6 +11,9 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int64_t kMaxRow = 1 << 24;              // 255 rows of bytes stay below 2^32
 constexpr int32_t kMaxInputs = 131071;           // 128 * 128 of each stay below 2^31
+// Of each call's grid, which has less than 2^32 threads: 512 to 16 channels of few tokens, 1,024 to a tile of 256 by 256.
+constexpr int32_t kMaxOutputs = 1 << 26;
+constexpr int64_t kMaxResults = (int64_t)1 << 37;
 
 // ---------------------------------------------------------------------------
 // Rows to 8 bits
@@ -407,7 +410,8 @@ static size_t linear_bytes(int64_t tokens, int32_t inputs) {
 }
 
 static bool bad_linear_size(int32_t tokens, int32_t outputs, int32_t inputs) {
-  return tokens < 0 || outputs < 1 || inputs < 1 || inputs > kMaxInputs;
+  return tokens < 0 || outputs < 1 || outputs > kMaxOutputs || (int64_t)tokens * outputs > kMaxResults || inputs < 1 ||
+         inputs > kMaxInputs;
 }
 
 template <typename T, int TN, int TT, int WN, int WT, int BUFFERS>

@@ -79,6 +79,13 @@ def test_delta_of_more_than_a_grid_holds(lib):
     assert lib.cortex_delta_forward(ctypes.byref(a), P8, P8, 1 << 62, None) == C.CORTEX_E_INVAL
 
 
+def test_delta_of_more_chunks_than_a_grid_holds(lib):
+    for T, S, heads in ((1 << 29, 1, 1), (64, 1 << 23, 1), ((1 << 29) // 32, 1, 32)):
+        a = delta_args(num_seqs=S, num_tokens=T, heads=heads, key_heads=1, value_dim=16, state_rows=S, q_ld=1 << 12, k_ld=1 << 12,
+                       v_ld=1 << 12, y_ld=1 << 12, b_ld=1 << 12, dt_ld=1 << 12)
+        assert lib.cortex_delta_forward(ctypes.byref(a), P8, P8, 1 << 62, None) == C.CORTEX_E_INVAL
+
+
 def norm_args(**kw):
     a = dict(dtype=0, num_tokens=2, heads=4, key_heads=2, head_dim=64, rotary_dim=32, interleaved=0, norm=1, eps=1e-6, q=P8, k=P8,
              q_ld=256, k_ld=128, q_weight=None, k_weight=None, positions=P8, freqs=P8, q_out=P8, k_out=P8, q_out_ld=256,
@@ -127,6 +134,14 @@ def linear_args(**kw):
     dict(w=P8 + 8), dict(w_ld=(1 << 24) + 16), dict(tokens=1 << 24)])
 def test_linear_refuses(lib, bad):
     assert lib.cortex_linear_i8(ctypes.byref(linear_args(**bad)), P8, P8, 1 << 50, None) == C.CORTEX_E_INVAL
+
+
+@pytest.mark.parametrize("size", [(1, (1 << 26) + 16), (1 << 12, (1 << 25) + 16), ((1 << 24) - 1, 1 << 14)])
+def test_linear_of_more_than_a_grid_holds(lib, size):
+    tokens, outputs = size
+    a = linear_args(tokens=tokens, outputs=outputs, y_ld=outputs)
+    assert lib.cortex_linear_i8(ctypes.byref(a), P8, P8, 1 << 62, None) == C.CORTEX_E_INVAL
+    assert lib.cortex_linear_i8_workspace_bytes(tokens, outputs, 40) == 0
 
 
 def test_linear_workspace(lib):
