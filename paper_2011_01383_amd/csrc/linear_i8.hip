@@ -129,7 +129,6 @@ template <typename T, bool WIDE> int launch_quant_rows(const cortex_quant_i8_t &
   const hipStream_t st = (hipStream_t)stream;
   if (filled <= 2048) quant_kernel<T, WIDE, 1><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a, status, filled);
   else if (filled <= 4096) quant_kernel<T, WIDE, 2><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a, status, filled);
-  else if (filled <= 8192) quant_kernel<T, WIDE, 4><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a, status, filled);
   else quant_kernel<T, WIDE, 0><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a, status, filled);
   return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
 }
@@ -341,19 +340,18 @@ __global__ void __launch_bounds__(64 * WAVES) few_kernel(Product a, const int32_
   }
 }
 
-// One to four tokens, brought to 8 bits by every workgroup for itself, beside the loads of
-// its first weights: a launch less.  Rows of x stay in LDS.
-constexpr int kOwnTokens = 4, kOwnBytes = 16384, kOwnWaves = 4;
+// One token, brought to 8 bits by every workgroup for itself, beside the loads of its first
+// weights: a launch less.  The row stays in LDS.
+constexpr int kOwnBytes = 16384, kOwnWaves = 4;
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(64 * kOwnWaves) own_kernel(Product a, const T *x, int64_t x_ld, int columns, const int32_t *status, bool aligned) {
+__global__ void __launch_bounds__(64 * kOwnWaves) own_kernel(Product a, const T *x, int columns, const int32_t *status, bool aligned) {
   constexpr int kAhead = 8, kThreads = 64 * kOwnWaves;
-  __shared__ __attribute__((aligned(16))) int8_t rows[kOwnBytes];
+  __shared__ __attribute__((aligned(16))) int8_t row[kOwnBytes];
   __shared__ i32x4 sums[kOwnWaves][64];
-  __shared__ unsigned int most[kOwnTokens][kOwnWaves];
-  __shared__ float scales[kOwnTokens];
+  __shared__ unsigned int most[kOwnWaves];
   const int failed = entry_status(status);
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, q = lane >> 4, l16 = lane & 15;
-  const int n0 = (int)blockIdx.x * 16, steps = (a.pieces + 3) / 4, bytes = steps * 64;
+  const int n0 = (int)blockIdx.x * 16, steps = (a.pieces + 3) / 4;
   const int8_t *w = a.w + (int64_t)min(n0 + l16, a.outputs - 1) * a.w_ld;
   i32x4 wf[kAhead];
   auto fetch = [&](int s0) {
@@ -362,29 +360,23 @@ __global__ void __launch_bounds__(64 * kOwnWaves) own_kernel(Product a, const T 
       wf[k] = *(const i32x4 *)(w + (int64_t)min(min(s0 + k * kOwnWaves, steps - 1) * 4 + q, a.pieces - 1) * 16);
   };
   fetch(wave);
-  for (int t = 0; t < a.tokens; ++t) {
-    unsigned int top = 0;
-    for (int c = tid * 8; c < columns; c += kThreads * 8) {
-      float v[8];
-      load_eight<T, WIDE>(x + t * x_ld + c, columns - c, v);
-      top = top_of(v, top);
-    }
-    top = wave_top(top);
-    if (lane == 0) most[t][wave] = top;
+  unsigned int top = 0;
+  for (int c = tid * 8; c < columns; c += kThreads * 8) {
+    float v[8];
+    load_eight<T, WIDE>(x + c, columns - c, v);
+    top = top_of(v, top);
   }
+  top = wave_top(top);
+  if (lane == 0) most[wave] = top;
   if (__syncthreads_or(failed != 0)) return;
-  for (int t = 0; t < a.tokens; ++t) {
-    bool none;
-    const float scale = quant_scale(max(max(most[t][0], most[t][1]), max(most[t][2], most[t][3])), none);
-    if (tid == 0) scales[t] = scale;
-    for (int c = tid * 8; c < bytes; c += kThreads * 8) {
-      float v[8];
-      load_eight<T, WIDE>(x + t * x_ld + c, columns - c, v);
-      *(u32x2 *)&rows[t * bytes + c] = quant_eight(v, scale, none);
-    }
+  bool none;
+  const float scale = quant_scale(max(max(most[0], most[1]), max(most[2], most[3])), none);
+  for (int c = tid * 8; c < steps * 64; c += kThreads * 8) {
+    float v[8];
+    load_eight<T, WIDE>(x + c, columns - c, v);
+    *(u32x2 *)&row[c] = quant_eight(v, scale, none);
   }
   __syncthreads();
-  const int8_t *xs = rows + min(l16, a.tokens - 1) * bytes;
   i32x4 acc = {0, 0, 0, 0};
 #pragma unroll 1
   for (int s0 = wave; s0 < steps; s0 += kOwnWaves * kAhead) {
@@ -392,12 +384,12 @@ __global__ void __launch_bounds__(64 * kOwnWaves) own_kernel(Product a, const T 
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
       if (s0 + k * kOwnWaves < steps)
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[k], *(const i32x4 *)(xs + (s0 + k * kOwnWaves) * 64 + q * 16), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[k], *(const i32x4 *)(row + (s0 + k * kOwnWaves) * 64 + q * 16), acc, 0, 0, 0);
   }
   sums[wave][lane] = acc;
   __syncthreads();
-  if (wave == 0 && l16 < a.tokens)
-    put_four<T>(a, (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]), scales[l16], l16, n0 + q * 4, aligned);
+  if (wave == 0 && l16 == 0)
+    put_four<T>(a, (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]), scale, 0, n0 + q * 4, aligned);
 }
 
 // ---------------------------------------------------------------------------
@@ -430,8 +422,8 @@ int launch_few(const Product &p, const int32_t *status, bool aligned, hipStream_
 
 template <typename T> int launch_product(const Product &p, const int32_t *status, bool aligned, hipStream_t st) {
   if (p.tokens <= 64) {
+    if (p.tokens <= 16) return launch_few<T, 1, 1, 4, 8>(p, status, aligned, st);
     const bool many = (p.outputs + 15) / 16 >= 512;
-    if (p.tokens <= 16) return many ? launch_few<T, 1, 1, 4, 8>(p, status, aligned, st) : launch_few<T, 1, 1, 8, 8>(p, status, aligned, st);
     if (p.tokens <= 32) return many ? launch_few<T, 2, 2, 8, 4>(p, status, aligned, st) : launch_few<T, 1, 2, 8, 4>(p, status, aligned, st);
     return many ? launch_few<T, 2, 4, 8, 4>(p, status, aligned, st) : launch_few<T, 1, 4, 8, 4>(p, status, aligned, st);
   }
@@ -448,11 +440,11 @@ template <typename T> int launch_linear(const cortex_linear_i8_t &a, int32_t *st
   int8_t *rows = (int8_t *)ws;
   float *scales = (float *)(rows + align_up((size_t)(a.tokens * row), 256));
   const bool aligned = a.y_ld % 4 == 0 && ((uintptr_t)a.y & (4 * sizeof(T) - 1)) == 0;
-  if (!a.x_scale && a.tokens <= kOwnTokens && a.tokens * row <= kOwnBytes) {
+  if (!a.x_scale && a.tokens == 1 && row <= kOwnBytes) {
     const unsigned grid = (unsigned)((a.outputs + 15) / 16);
     const T *x = (const T *)a.x;
-    if (eights<T>(x, a.x_ld, a.inputs)) own_kernel<T, true><<<grid, 64 * kOwnWaves, 0, st>>>(p, x, a.x_ld, a.inputs, status, aligned);
-    else own_kernel<T, false><<<grid, 64 * kOwnWaves, 0, st>>>(p, x, a.x_ld, a.inputs, status, aligned);
+    if (eights<T>(x, a.x_ld, a.inputs)) own_kernel<T, true><<<grid, 64 * kOwnWaves, 0, st>>>(p, x, a.inputs, status, aligned);
+    else own_kernel<T, false><<<grid, 64 * kOwnWaves, 0, st>>>(p, x, a.inputs, status, aligned);
     return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
   }
   if (!a.x_scale) {

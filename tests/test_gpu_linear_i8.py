@@ -190,3 +190,41 @@ def test_an_earlier_error_leaves_outputs(T):
     C.check(C.cortex_quant_i8(x, q, scale, status=status))
     torch.cuda.synchronize()
     assert (y == 5.0).all() and (q == 3).all() and (scale == 5.0).all() and int(status.item()) == C.CORTEX_ST_CYCLE
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("T,K,N", [(1, 16384, 40), (1, 16385, 40), (2, 16385, 17), (4, 8200, 50), (9, 100, 8203), (24, 100, 8203),
+                                   (32, 1000, 8177), (50, 200, 8190), (64, 70, 8176)])
+def test_few_tokens_of_many_channels_and_inputs(T, K, N, given, dtype):
+    need_gpu()
+    say("linear few tokens", T, K, N, given, dtype)
+    product(T, K, N, dtype, given)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("left", [0, 1, 2, 3, 4, 16])
+def test_one_token(left, dtype):
+    need_gpu()
+    say("linear one token", left, dtype)
+    for K in (15, 16, 208, 2048, 2050, 4100):
+        product(1, K, 139, dtype, left=left)
+
+
+def test_one_token_of_special_values():
+    """A NaN or an infinity makes the outputs NaN, a row of zeros leaves the bias, an earlier error everything."""
+    need_gpu()
+    say("linear one token of special values")
+    w, ws = torch.ones(20, 48, dtype=torch.int8, device="cuda")[:, :40], C.workspace(C.cortex_linear_i8_workspace_bytes(1, 20, 40))
+    one, bias, status = torch.ones(20, device="cuda"), torch.arange(20.0, device="cuda"), status_word()
+    for bad in (float("nan"), float("inf"), 0.0):
+        x, y = torch.zeros(1, 40, device="cuda"), torch.full((1, 20), 5.0, device="cuda")
+        x[0, 3] = bad
+        C.check(C.cortex_linear_i8(x, w, one, y, bias=bias, status=status, ws=ws))
+        torch.cuda.synchronize()
+        assert torch.equal(y[0], bias) if bad == 0.0 else torch.isnan(y).all()
+    status.fill_(C.CORTEX_ST_CYCLE)
+    y = torch.full((1, 20), 5.0, device="cuda")
+    C.check(C.cortex_linear_i8(torch.zeros(1, 40, device="cuda"), w, one, y, bias=bias, status=status, ws=ws))
+    torch.cuda.synchronize()
+    assert (y == 5.0).all() and int(status.item()) == C.CORTEX_ST_CYCLE
