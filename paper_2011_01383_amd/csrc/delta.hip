@@ -4,7 +4,8 @@
 //
 // Rows of a head's state (one per value channel) share nothing but k, q, a and
 // beta.  Eight lanes hold a row, four entries of each 32 a lane, so that a row's
-// loads and stores are whole 128-byte pieces; a wave holds sixteen rows.
+// loads and stores are whole 128-byte pieces; a wave holds sixteen rows.  The states' bytes bound it:
+// 64 rows of 32 heads of 128 by 128 are 268 MB, 46 us (5.8 TB/s: some stay in the last-level cache), one row 5 us.
 #include "delta_chunk.hpp"
 
 namespace cortex {

@@ -1,6 +1,7 @@
 // Norms of queries and keys per head, their weights and their rotation, in one pass.
 //
-// Every element is read once and written once: the bytes bound it.  A rotation
+// Every element is read once and written once: the bytes bound it (8,192 tokens of 40 heads of 128 bf16, 168 MB: 33 us, 5.1
+// TB/s, what a large copy reaches).  A rotation
 // pairs elements R / 2 apart or neighbours, so a lane takes two pieces of 16 bytes
 // whose pairs are all its own, and a head's lanes (a power of two of them, some
 // without work where the head is none) only have to add their squares.  A wave
