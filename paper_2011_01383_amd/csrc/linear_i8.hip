@@ -169,26 +169,39 @@ struct Product {
   int32_t tokens, outputs, pieces;
 };
 
-template <typename T> __device__ __forceinline__ T finish(const Product &a, int acc, float xs, int n) {
+// Scales and biases of four neighbouring channels from n on.
+struct Four {
+  float scale[4], bias[4];
+  __device__ __forceinline__ void load(const Product &a, int n) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int at = min(n + r, a.outputs - 1);
+      scale[r] = a.w_scale[at];
+      bias[r] = a.bias ? a.bias[at] : 0.0f;
+    }
+  }
+};
+
+template <typename T> __device__ __forceinline__ T finish(const Product &a, int acc, float xs, float ws, float bias) {
 #pragma clang fp contract(off)
-  float v = (float)acc * xs * a.w_scale[n];
-  if (a.bias) v += a.bias[n];
+  float v = (float)acc * xs * ws;
+  if (a.bias) v += bias;
   return from_float<T>(v);
 }
 
 // Four neighbouring channels of one token.
-template <typename T> __device__ __forceinline__ void put_four(const Product &a, i32x4 acc, float xs, int t, int n, bool aligned) {
+template <typename T> __device__ __forceinline__ void put_four(const Product &a, i32x4 acc, float xs, const Four &f, int t, int n, bool aligned) {
   T *y = (T *)a.y + (int64_t)t * a.y_ld;
   if (aligned && n + 3 < a.outputs) {
     typedef T pack __attribute__((ext_vector_type(4)));
     pack v;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = finish<T>(a, acc[r], xs, n + r);
+    for (int r = 0; r < 4; ++r) v[r] = finish<T>(a, acc[r], xs, f.scale[r], f.bias[r]);
     *(pack *)(y + n) = v;
   } else {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      if (n + r < a.outputs) y[n + r] = finish<T>(a, acc[r], xs, n + r);
+      if (n + r < a.outputs) y[n + r] = finish<T>(a, acc[r], xs, f.scale[r], f.bias[r]);
   }
 }
 
@@ -246,6 +259,17 @@ __global__ void __launch_bounds__(64 * WN * WT) product_kernel(Product a, const 
   for (int i = 0; i < I; ++i)
 #pragma unroll
     for (int j = 0; j < J; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  // Scales and biases come first where registers admit it: the last stage does not wait for them then.
+  constexpr bool kEarly = I * J <= 4;
+  Four four[I];
+  float xscale[J];
+  auto scales = [&]() {
+#pragma unroll
+    for (int i = 0; i < I; ++i) four[i].load(a, n0 + wn + i * 16 + q * 4);
+#pragma unroll
+    for (int j = 0; j < J; ++j) xscale[j] = a.x_scale[min(t0 + wt + j * 16 + l16, a.tokens - 1)];
+  };
+  if constexpr (kEarly) scales();
 #pragma unroll
   for (int b = 0; b < BUFFERS - 1; ++b) copy(b, b);
   i32x4 wf[2][I], xf[2][J];
@@ -284,13 +308,13 @@ __global__ void __launch_bounds__(64 * WN * WT) product_kernel(Product a, const 
     if (step + 1 < steps) multiply(step + 1, wf[1], xf[1], wf[0], xf[0]);
   }
   copies_done<0>();                              // LDS is given back only when nothing is on its way to it
+  if constexpr (!kEarly) scales();
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     const int t = t0 + wt + j * 16 + l16;
     if (t >= a.tokens) continue;
-    const float scale = a.x_scale[t];
 #pragma unroll
-    for (int i = 0; i < I; ++i) put_four<T>(a, acc[i][j], scale, t, n0 + wn + i * 16 + q * 4, aligned);
+    for (int i = 0; i < I; ++i) put_four<T>(a, acc[i][j], xscale[j], four[i], t, n0 + wn + i * 16 + q * 4, aligned);
   }
 }
 
@@ -310,6 +334,12 @@ __global__ void __launch_bounds__(64 * WAVES) few_kernel(Product a, const int32_
 #pragma unroll
   for (int j = 0; j < TJ; ++j) x[j] = a.x + (int64_t)min(j * 16 + l16, a.tokens - 1) * a.x_ld;
   const int steps = (a.pieces + 3) / 4;          // of 64 bytes
+  // the wave's tile of the results, and what it is multiplied by
+  static_assert(TI * TJ <= WAVES, "a tile a wave");
+  const int t = wave % TJ * 16 + l16, n = n0 + wave / TJ * 16 + q * 4;
+  Four four;
+  four.load(a, n);
+  const float xscale = a.x_scale[min(t, a.tokens - 1)];
   i32x4 acc[TI][TJ];
 #pragma unroll
   for (int i = 0; i < TI; ++i)
@@ -340,13 +370,11 @@ __global__ void __launch_bounds__(64 * WAVES) few_kernel(Product a, const int32_
 #pragma unroll
     for (int j = 0; j < TJ; ++j) sums[wave][i * TJ + j][lane] = acc[i][j];
   if (__syncthreads_or(failed != 0)) return;
-  for (int k = wave; k < TI * TJ; k += WAVES) {
-    i32x4 s = sums[0][k][lane];
+  if (wave >= TI * TJ || t >= a.tokens) return;
+  i32x4 s = sums[0][wave][lane];
 #pragma unroll
-    for (int i = 1; i < WAVES; ++i) s += sums[i][k][lane];
-    const int t = k % TJ * 16 + l16;
-    if (t < a.tokens) put_four<T>(a, s, a.x_scale[t], t, n0 + k / TJ * 16 + q * 4, aligned);
-  }
+  for (int i = 1; i < WAVES; ++i) s += sums[i][wave][lane];
+  put_four<T>(a, s, xscale, four, t, n, aligned);
 }
 
 // One token, brought to 8 bits by every workgroup for itself, beside the loads of its first
@@ -368,22 +396,39 @@ __global__ void __launch_bounds__(64 * kOwnWaves) own_kernel(Product a, const T 
     for (int k = 0; k < kAhead; ++k)
       wf[k] = *(const i32x4 *)(w + (int64_t)min(min(s0 + k * kOwnWaves, steps - 1) * 4 + q, a.pieces - 1) * 16);
   };
+  // Most of the row stays in registers until its scale is known.
+  constexpr int kKeep = 2;
+  float v[kKeep][8];
+#pragma unroll
+  for (int k = 0; k < kKeep; ++k) {
+    const int c = (k * kThreads + tid) * 8;
+    load_eight<T, WIDE>(x + c, columns - c, v[k]);
+  }
   fetch(wave);
+  Four four;
+  four.load(a, n0 + q * 4);
   unsigned int top = 0;
-  for (int c = tid * 8; c < columns; c += kThreads * 8) {
-    float v[8];
-    load_eight<T, WIDE>(x + c, columns - c, v);
-    top = top_of(v, top);
+#pragma unroll
+  for (int k = 0; k < kKeep; ++k) top = top_of(v[k], top);
+  for (int c = (kKeep * kThreads + tid) * 8; c < columns; c += kThreads * 8) {
+    float u[8];
+    load_eight<T, WIDE>(x + c, columns - c, u);
+    top = top_of(u, top);
   }
   top = wave_top(top);
   if (lane == 0) most[wave] = top;
   if (__syncthreads_or(failed != 0)) return;
   bool none;
   const float scale = quant_scale(max(max(most[0], most[1]), max(most[2], most[3])), none);
-  for (int c = tid * 8; c < steps * 64; c += kThreads * 8) {
-    float v[8];
-    load_eight<T, WIDE>(x + c, columns - c, v);
-    *(u32x2 *)&row[c] = quant_eight(v, scale, none);
+#pragma unroll
+  for (int k = 0; k < kKeep; ++k) {
+    const int c = (k * kThreads + tid) * 8;
+    if (c < steps * 64) *(u32x2 *)&row[c] = quant_eight(v[k], scale, none);
+  }
+  for (int c = (kKeep * kThreads + tid) * 8; c < steps * 64; c += kThreads * 8) {
+    float u[8];
+    load_eight<T, WIDE>(x + c, columns - c, u);
+    *(u32x2 *)&row[c] = quant_eight(u, scale, none);
   }
   __syncthreads();
   i32x4 acc = {0, 0, 0, 0};
@@ -398,7 +443,7 @@ __global__ void __launch_bounds__(64 * kOwnWaves) own_kernel(Product a, const T 
   sums[wave][lane] = acc;
   __syncthreads();
   if (wave == 0 && l16 == 0)
-    put_four<T>(a, (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]), scale, 0, n0 + q * 4, aligned);
+    put_four<T>(a, (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]), scale, four, 0, n0 + q * 4, aligned);
 }
 
 // ---------------------------------------------------------------------------
