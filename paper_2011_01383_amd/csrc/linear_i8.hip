@@ -8,6 +8,7 @@
 namespace cortex {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int64_t kMaxRow = 1 << 24;              // 255 rows of bytes stay below 2^32
@@ -221,7 +222,11 @@ template <typename T, int TN, int TT, int WN, int WT, int BUFFERS>
 __global__ void __launch_bounds__(64 * WN * WT) product_kernel(Product a, const int32_t *status, bool aligned, int n_tiles, int t_tiles) {
   constexpr int kWaves = WN * WT, I = TN / WN / 16, J = TT / WT / 16, kStage = (TN + TT) * kDepth;
   constexpr int kCopies = (TN + TT) / 16 / kWaves;         // of 16 rows each, per wave and stage
+  // Scales and biases come first: the last stage does not wait for them then.  They stay in registers
+  // where there are some, else in LDS.
+  constexpr bool kEarly = kWaves <= 4;
   __shared__ __attribute__((aligned(1024))) int8_t lds[BUFFERS * kStage];
+  __shared__ __attribute__((aligned(16))) float late[kEarly ? 1 : 2 * TN + TT];
   const int64_t total = (int64_t)n_tiles * t_tiles, tile = unit_of_block(total);
   if (tile >= total) return;
   if (__syncthreads_or(entry_status(status) != 0)) return;
@@ -259,17 +264,20 @@ __global__ void __launch_bounds__(64 * WN * WT) product_kernel(Product a, const 
   for (int i = 0; i < I; ++i)
 #pragma unroll
     for (int j = 0; j < J; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-  // Scales and biases come first where registers admit it: the last stage does not wait for them then.
-  constexpr bool kEarly = I * J <= 4;
   Four four[I];
   float xscale[J];
-  auto scales = [&]() {
+  if constexpr (kEarly) {
 #pragma unroll
     for (int i = 0; i < I; ++i) four[i].load(a, n0 + wn + i * 16 + q * 4);
 #pragma unroll
     for (int j = 0; j < J; ++j) xscale[j] = a.x_scale[min(t0 + wt + j * 16 + l16, a.tokens - 1)];
-  };
-  if constexpr (kEarly) scales();
+  } else {
+    static_assert(2 * TN + TT <= 64 * kWaves, "a thread each");
+    const int c = (int)threadIdx.x;
+    if (c < TN) late[c] = a.w_scale[min(n0 + c, a.outputs - 1)];
+    else if (c < 2 * TN) late[c] = a.bias ? a.bias[min(n0 + c - TN, a.outputs - 1)] : 0.0f;
+    else if (c < 2 * TN + TT) late[c] = a.x_scale[min(t0 + c - 2 * TN, a.tokens - 1)];
+  }
 #pragma unroll
   for (int b = 0; b < BUFFERS - 1; ++b) copy(b, b);
   i32x4 wf[2][I], xf[2][J];
@@ -308,7 +316,19 @@ __global__ void __launch_bounds__(64 * WN * WT) product_kernel(Product a, const 
     if (step + 1 < steps) multiply(step + 1, wf[1], xf[1], wf[0], xf[0]);
   }
   copies_done<0>();                              // LDS is given back only when nothing is on its way to it
-  if constexpr (!kEarly) scales();
+  if constexpr (!kEarly) {
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      const f32x4 s = *(const f32x4 *)&late[wn + i * 16 + q * 4], b = *(const f32x4 *)&late[TN + wn + i * 16 + q * 4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        four[i].scale[r] = s[r];
+        four[i].bias[r] = b[r];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j) xscale[j] = late[2 * TN + wt + j * 16 + l16];
+  }
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     const int t = t0 + wt + j * 16 + l16;
