@@ -20,22 +20,20 @@ constexpr int64_t kMaxResults = (int64_t)1 << 37;
 // ---------------------------------------------------------------------------
 // Rows to 8 bits
 // ---------------------------------------------------------------------------
-constexpr int kQuantThreads = 256;
-
-// One value: x / scale rounded to a whole number.  A scale in the denormals may
-// leave the quotient above 127.
-__device__ __forceinline__ int quant_value(float x, float scale) {
-  const float v = __builtin_rintf(x / scale);
-  return (int)__builtin_fminf(__builtin_fmaxf(v, -127.0f), 127.0f);
-}
-
-// The scale of a row whose largest |x| has these bits, and whether its values are all 0.
-__device__ __forceinline__ float quant_scale(unsigned int top, bool &none) {
-  const bool odd = top >= 0x7f800000u;           // infinities and NaN are the largest
-  const float scale = odd ? __builtin_nanf("") : __builtin_bit_cast(float, top) / 127.0f;
-  none = odd || scale == 0.0f;
-  return scale;
-}
+// The scale of a row whose largest |x| has the bits of `top`.
+struct RowScale {
+  float scale;
+  bool none;                                     // its values are all 0
+  float lift, lifted, inverse;                   // 2^64 for small rows, else 1; scale times it; the reciprocal of that
+  __device__ __forceinline__ explicit RowScale(unsigned int top) {
+    const bool odd = top >= 0x7f800000u;         // infinities and NaN are the largest
+    scale = odd ? __builtin_nanf("") : __builtin_bit_cast(float, top) / 127.0f;
+    none = odd || scale == 0.0f;
+    lift = scale < 0x1p-64f ? 0x1p64f : 1.0f;
+    lifted = scale * lift;
+    inverse = 1.0f / lifted;
+  }
+};
 
 // Eight elements; `n` of them are there, the others 0.
 template <typename T, bool WIDE> __device__ __forceinline__ void load_eight(const T *x, int n, float (&v)[8]) {
@@ -52,11 +50,28 @@ template <typename T, bool WIDE> __device__ __forceinline__ void load_eight(cons
   }
 }
 
-__device__ __forceinline__ u32x2 quant_eight(const float (&v)[8], float scale, bool none) {
-  unsigned int b[2] = {0, 0};
+// x / scale rounded to a whole number.  With the reciprocal rounded correctly, a quotient off by less than a step becomes
+// the correctly rounded one by one step of q + (x - q scale) / scale, whose remainder is exact (Markstein 1990); q = x / scale as
+// a product may be off by two, so there are two such steps.  Small rows are lifted by a power of two, which changes no
+// quotient, so that remainders do not underflow; a scale in the denormals may leave a quotient above 127.  The sum with 1.5 2^23
+// rounds to whole numbers, which then are its low bits.  Divisions took most of the time: 8,192 rows of 4,096 28 us.
+__device__ __forceinline__ u32x2 quant_eight(const float (&v)[8], const RowScale &s) {
+#pragma clang fp contract(off) reassociate(off)
+  unsigned int b[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) b[i / 4] |= (none ? 0u : (unsigned int)quant_value(v[i], scale) & 255u) << (8 * (i % 4));
-  return u32x2{b[0], b[1]};
+  for (int i = 0; i < 8; ++i) {
+    const float x = v[i] * s.lift;
+    float q = x * s.inverse;
+    q = __builtin_fmaf(__builtin_fmaf(-q, s.lifted, x), s.inverse, q);
+    q = __builtin_fmaf(__builtin_fmaf(-q, s.lifted, x), s.inverse, q);
+    b[i] = __builtin_bit_cast(unsigned int, __builtin_amdgcn_fmed3f(q, -127.0f, 127.0f) + 12582912.0f);
+  }
+  u32x2 r;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    r[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[4 * i + 3], b[4 * i + 2], 0x0c0c0400u),
+                                 __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400u), 0x05040100u);
+  return s.none ? u32x2{0u, 0u} : r;
 }
 
 // |x| as whole numbers keep their order.
@@ -71,29 +86,28 @@ __device__ __forceinline__ unsigned int wave_top(unsigned int top) {
   return top;
 }
 
-// A workgroup a row, which it keeps in registers where it has at most 8 * 256 * KEEP
-// columns, and reads again (from the caches) otherwise.  `filled`: columns of q that are written, zeros past
-// the row's own.  WIDE: rows of x and q in whole eights at their alignment.  The bytes bound it: 8,192 rows of 4,096
-// bf16 take 28 us, 3.6 TB/s.
-template <typename T, bool WIDE, int KEEP>
-__global__ void __launch_bounds__(kQuantThreads) quant_kernel(cortex_quant_i8_t a, int32_t *status, int filled) {
-  __shared__ unsigned int most[kQuantThreads / 64];
+// A workgroup of THREADS a row, which it keeps in registers (KEPT: 16 elements a thread), or, where it has more columns, reads
+// again from the caches.  `filled`: columns of q that are written, zeros past the row's own.  WIDE: rows of x and q in
+// whole eights at their alignment.  The bytes bound it: 8,192 rows of 4,096 bf16 take 22 us, 4.6 TB/s.
+template <typename T, bool WIDE, int THREADS, bool KEPT>
+__global__ void __launch_bounds__(THREADS) quant_kernel(cortex_quant_i8_t a, int32_t *status, int filled) {
+  constexpr int kWaves = THREADS / 64, kStride = THREADS * 8, kKeep = KEPT ? 2 : 1;
+  __shared__ unsigned int most[kWaves];
   if (__syncthreads_or(entry_status(status) != 0)) return;
-  constexpr int kStride = kQuantThreads * 8;
   const int tid = (int)threadIdx.x;
   const int64_t r = blockIdx.x;
   const T *x = (const T *)a.x + r * a.x_ld;
   int8_t *q = a.q + r * a.q_ld;
-  float v[KEEP > 0 ? KEEP : 1][8];
+  float v[kKeep][8];
   unsigned int top = 0;
-  if constexpr (KEEP > 0) {
+  if constexpr (KEPT) {
 #pragma unroll
-    for (int k = 0; k < KEEP; ++k) {
+    for (int k = 0; k < kKeep; ++k) {
       const int c = tid * 8 + k * kStride;
       load_eight<T, WIDE>(x + c, a.columns - c, v[k]);
     }
 #pragma unroll
-    for (int k = 0; k < KEEP; ++k) top = top_of(v[k], top);
+    for (int k = 0; k < kKeep; ++k) top = top_of(v[k], top);
   } else {
     for (int c = tid * 8; c < a.columns; c += kStride) {
       load_eight<T, WIDE>(x + c, a.columns - c, v[0]);
@@ -103,11 +117,12 @@ __global__ void __launch_bounds__(kQuantThreads) quant_kernel(cortex_quant_i8_t 
   top = wave_top(top);
   if ((tid & 63) == 0) most[tid >> 6] = top;
   __syncthreads();
-  bool none;
-  const float scale = quant_scale(max(max(most[0], most[1]), max(most[2], most[3])), none);
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = max(top, most[w]);
+  const RowScale s(__builtin_amdgcn_readfirstlane(top));
   auto put = [&](int c, const float (&u)[8]) {
     if (c >= filled) return;
-    const u32x2 b = quant_eight(u, scale, none);
+    const u32x2 b = quant_eight(u, s);
     if (WIDE) {
       *(u32x2 *)(q + c) = b;
     } else {
@@ -116,25 +131,31 @@ __global__ void __launch_bounds__(kQuantThreads) quant_kernel(cortex_quant_i8_t 
         if (c + i < filled) q[c + i] = (int8_t)(b[i / 4] >> (8 * (i % 4)));
     }
   };
-  if constexpr (KEEP > 0) {
+  if constexpr (KEPT) {
 #pragma unroll
-    for (int k = 0; k < KEEP; ++k) put(tid * 8 + k * kStride, v[k]);
+    for (int k = 0; k < kKeep; ++k) put(tid * 8 + k * kStride, v[k]);
   } else {
     for (int c = tid * 8; c < filled; c += kStride) {
       load_eight<T, WIDE>(x + c, a.columns - c, v[0]);
       put(c, v[0]);
     }
   }
-  if (tid == 0) a.scale[r] = scale;
+  if (tid == 0) a.scale[r] = s.scale;
+}
+
+template <typename T, bool WIDE, int THREADS, bool KEPT> void launch_quant_of(const cortex_quant_i8_t &a, int32_t *status, int filled, hipStream_t st) {
+  quant_kernel<T, WIDE, THREADS, KEPT><<<(unsigned)a.rows, THREADS, 0, st>>>(a, status, filled);
 }
 
 template <typename T, bool WIDE> int launch_quant_rows(const cortex_quant_i8_t &a, int32_t *status, int filled, void *stream) {
   const hipStream_t st = (hipStream_t)stream;
-  // Kept or read again: 1,000 columns 21.9 us and 22.8 (with a product over 64 channels of 8,192 rows), 2,048 28.1 and 28.3, 4,096
-  // 44.5 and 46.9, 8,192 90.5 and 84.9.
-  if (filled <= 2048) quant_kernel<T, WIDE, 1><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a, status, filled);
-  else if (filled <= 4096) quant_kernel<T, WIDE, 2><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a, status, filled);
-  else quant_kernel<T, WIDE, 0><<<(unsigned)a.rows, kQuantThreads, 0, st>>>(a, status, filled);
+  // As few waves as hold a row: 8,192 rows of 1,000 (with a product over 64 channels) by one wave 13.8 us, two 19, four 22.6; of 2,048
+  // by two 20.5, four 29.7; of 4,096 by four 34.3, two (32 elements a thread) 37.1.  8,192 columns kept by
+  // four waves 90, read again 85.
+  if (filled <= 1024) launch_quant_of<T, WIDE, 64, true>(a, status, filled, st);
+  else if (filled <= 2048) launch_quant_of<T, WIDE, 128, true>(a, status, filled, st);
+  else if (filled <= 4096) launch_quant_of<T, WIDE, 256, true>(a, status, filled, st);
+  else launch_quant_of<T, WIDE, 256, false>(a, status, filled, st);
   return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
 }
 
@@ -438,17 +459,16 @@ __global__ void __launch_bounds__(64 * kOwnWaves) own_kernel(Product a, const T 
   top = wave_top(top);
   if (lane == 0) most[wave] = top;
   if (__syncthreads_or(failed != 0)) return;
-  bool none;
-  const float scale = quant_scale(max(max(most[0], most[1]), max(most[2], most[3])), none);
+  const RowScale s(__builtin_amdgcn_readfirstlane(max(max(most[0], most[1]), max(most[2], most[3]))));
 #pragma unroll
   for (int k = 0; k < kKeep; ++k) {
     const int c = (k * kThreads + tid) * 8;
-    if (c < steps * 64) *(u32x2 *)&row[c] = quant_eight(v[k], scale, none);
+    if (c < steps * 64) *(u32x2 *)&row[c] = quant_eight(v[k], s);
   }
   for (int c = (kKeep * kThreads + tid) * 8; c < steps * 64; c += kThreads * 8) {
     float u[8];
     load_eight<T, WIDE>(x + c, columns - c, u);
-    *(u32x2 *)&row[c] = quant_eight(u, scale, none);
+    *(u32x2 *)&row[c] = quant_eight(u, s);
   }
   __syncthreads();
   i32x4 acc = {0, 0, 0, 0};
@@ -463,7 +483,7 @@ __global__ void __launch_bounds__(64 * kOwnWaves) own_kernel(Product a, const T 
   sums[wave][lane] = acc;
   __syncthreads();
   if (wave == 0 && l16 == 0)
-    put_four<T>(a, (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]), scale, four, 0, n0 + q * 4, aligned);
+    put_four<T>(a, (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]), s.scale, four, 0, n0 + q * 4, aligned);
 }
 
 // ---------------------------------------------------------------------------

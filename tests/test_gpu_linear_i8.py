@@ -228,3 +228,23 @@ def test_one_token_of_special_values():
     C.check(C.cortex_linear_i8(torch.zeros(1, 40, device="cuda"), w, one, y, bias=bias, status=status, ws=ws))
     torch.cuda.synchronize()
     assert (y == 5.0).all() and int(status.item()) == C.CORTEX_ST_CYCLE
+
+
+@pytest.mark.parametrize("cols", [1000, 2048, 5000])
+def test_quant_near_halves(cols):
+    """Quotients within a few steps of n + 1/2, where a quotient off by one step would be another whole number; scales
+    over the whole range of the type."""
+    need_gpu()
+    say("quant near halves", cols)
+    r = np.random.default_rng(cols)
+    tops = (2.0 ** r.uniform(-145, 127, 400) * (1 + r.random(400))).astype(np.float32)
+    scale = tops / np.float32(127)
+    x = (r.integers(-127, 127, (400, cols)) + 0.5).astype(np.float32) * scale[:, None]
+    x = (x.view(np.int32) + r.integers(-2, 3, x.shape).astype(np.int32)).view(np.float32)
+    x = np.where(np.abs(x) <= tops[:, None], x, np.float32(0))
+    x[:, 7] = tops
+    q, s, status = torch.empty(400, cols, dtype=torch.int8, device="cuda"), torch.empty(400, device="cuda"), status_word()
+    C.check(C.cortex_quant_i8(dev(x), q, s, status=status))
+    torch.cuda.synchronize()
+    want, ws = O.quant_rows(x)
+    assert np.array_equal(s.cpu().numpy(), ws) and np.array_equal(q.cpu().numpy(), want)
