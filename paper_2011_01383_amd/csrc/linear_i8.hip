@@ -88,7 +88,7 @@ __device__ __forceinline__ unsigned int wave_top(unsigned int top) {
 
 // A workgroup of THREADS a row, which it keeps in registers (KEPT: 16 elements a thread), or, where it has more columns, reads
 // again from the caches.  `filled`: columns of q that are written, zeros past the row's own.  WIDE: rows of x and q in
-// whole eights at their alignment.  The bytes bound it: 8,192 rows of 4,096 bf16 take 22 us, 4.6 TB/s.
+// whole eights at their alignment.  The bytes bound it: 8,192 rows of 4,096 bf16 take 21 us, 4.7 TB/s.
 template <typename T, bool WIDE, int THREADS, bool KEPT>
 __global__ void __launch_bounds__(THREADS) quant_kernel(cortex_quant_i8_t a, int32_t *status, int filled) {
   constexpr int kWaves = THREADS / 64, kStride = THREADS * 8, kKeep = KEPT ? 2 : 1;
@@ -236,9 +236,10 @@ __device__ __forceinline__ int piece_place(int row, int piece) { return piece ^ 
 // LDS, all but one of them on their way while one is multiplied.  XCDs take runs of
 // neighbouring tiles, four tiles of tokens by as many of channels as there are.
 //
-// 8,192 tokens, 4,096 inputs, 8,192 channels in tiles of 256 by 256: 270 us, 2.0e15 operations a second, the matrix units
-// busy half of it, no conflicts in LDS.  Sixteen waves of 64 by 64 (4 a SIMD) and four buffers; in its place eight waves 331,
-// four of 128 by 128 470, three buffers 329, two of 128 bytes 317, tiles of 128 by 128 391, all with the rows' 28.
+// 8,192 tokens, 4,096 inputs, 8,192 channels in tiles of 256 by 256: 255 us, 2.15e15 operations a second, the matrix units
+// busy 55% of it, no conflicts in LDS.  Sixteen waves of 64 by 64 (4 a SIMD) and four buffers; in its place eight waves 331,
+// four of 128 by 128 470, three buffers 329, two of 128 bytes 317, tiles of 128 by 128 391, all with the rows' 28, of a
+// form that took 303 in all.
 template <typename T, int TN, int TT, int WN, int WT, int BUFFERS>
 __global__ void __launch_bounds__(64 * WN * WT) product_kernel(Product a, const int32_t *status, bool aligned, int n_tiles, int t_tiles) {
   constexpr int kWaves = WN * WT, I = TN / WN / 16, J = TT / WT / 16, kStage = (TN + TT) * kDepth;
@@ -362,7 +363,7 @@ __global__ void __launch_bounds__(64 * WN * WT) product_kernel(Product a, const 
 // Few tokens: a workgroup has 16 TI channels and all tokens (16 TJ of them at most), its
 // waves every WAVES-th 64 bytes of the inputs; operands go to registers, AHEAD of the
 // wave's shares at once.  The weights' bytes bound it, and the latency of one workgroup: 64 tokens, 2,048 inputs, 8,192
-// channels (16.8 MB) take 10 us.
+// channels (16.8 MB) take 9.5 us.
 template <typename T, int TI, int TJ, int WAVES, int AHEAD>
 __global__ void __launch_bounds__(64 * WAVES) few_kernel(Product a, const int32_t *status, bool aligned) {
   __shared__ i32x4 sums[WAVES][TI * TJ][64];
@@ -419,7 +420,7 @@ __global__ void __launch_bounds__(64 * WAVES) few_kernel(Product a, const int32_
 }
 
 // One token, brought to 8 bits by every workgroup for itself, beside the loads of its first
-// weights: a launch less.  The row stays in LDS.  4,096 inputs by 8,192 channels 10 us, 3.4 TB/s of weights.
+// weights: a launch less.  The row stays in LDS.  4,096 inputs by 8,192 channels 9.2 us, 3.6 TB/s of weights.
 constexpr int kOwnBytes = 16384, kOwnWaves = 4;
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(64 * kOwnWaves) own_kernel(Product a, const T *x, int columns, const int32_t *status, bool aligned) {
