@@ -381,6 +381,20 @@ template <int A, int B> struct PlanePairs {
   static __device__ __forceinline__ constexpr int right(int i) { return A == 1 ? B - 1 - i : i == 0 ? 2 : i == 1 ? 1 : i == 2 ? 0 : i == 3 ? 1 : 0; }
 };
 
+// Four consecutive elements of a row of outputs; whole where rows are aligned to four.
+template <typename T> __device__ __forceinline__ bool packed_rows(const void *p, int64_t ld) {
+  return ld % 4 == 0 && ((uintptr_t)p & (4 * sizeof(T) - 1)) == 0;
+}
+template <typename T> __device__ __forceinline__ void store_four(T *p, const f32x4 &y, bool packed) {
+  const float v[4] = {y[0], y[1], y[2], y[3]};
+  if (packed) {
+    Pack<T, 4>::store(p, v);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[r] = from_float<T>(v[r]);
+  }
+}
+
 // The first of the tokens 16 tile + 4 q + r whose value is not finite; those values become 0: their
 // products with the zeros above the diagonal would carry them to earlier tokens.
 __device__ __forceinline__ void drop_odd(f32x4 (&v)[4], int q, int &first) {
@@ -464,7 +478,8 @@ __global__ void __launch_bounds__(kChunkThreads, sizeof(T) == 2 ? 2 : 1) chunk_w
   const ChunkMap *map = maps + ((int64_t)(begin / kChunk) + seq) * a.heads + head;
   const T *ks = (const T *)a.k + g * K, *qs = (const T *)a.q + g * K;
   const T *vs = (const T *)a.v + (int64_t)head * V + col;
-  T *ys = (T *)a.y + (int64_t)head * V + col;
+  T *ys = (T *)a.y + (int64_t)head * V + (works ? v0 + q * 4 : 0);
+  const bool packed = packed_rows<T>(a.y, a.y_ld);
   // T, P, gates and queries of the next chunk are on their way while the state is updated, straight into LDS; its
   // keys meanwhile in registers, since the update reads this chunk's.  Rows past the sequence's end repeat its
   // last; places in a chunk are 32 bits (the host admits no longer rows).
@@ -536,7 +551,7 @@ __global__ void __launch_bounds__(kChunkThreads, sizeof(T) == 2 ? 2 : 1) chunk_w
       bf16x8v sp[3];
       to_planes(S[2 * m], S[2 * m + 1], sp);
       typedef PlanePairs<KP, 3> Pairs;
-      auto by_state = [&](const unsigned short (&rows)[KP][kChunk * K], f32x4 (&to)[4]) {
+      auto by_state = [&](const unsigned short (&rows)[KP][kChunk * K], f32x4 (&to)[4], auto turned) {
         bf16x8v f[4][KP];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -545,14 +560,15 @@ __global__ void __launch_bounds__(kChunkThreads, sizeof(T) == 2 ? 2 : 1) chunk_w
 #pragma unroll
         for (int i = 0; i < Pairs::kCount; ++i)
 #pragma unroll
-          for (int t = 0; t < 4; ++t) to[t] = mfma_bf16x32(f[t][Pairs::left(i)], sp[Pairs::right(i)], to[t]);
+          for (int t = 0; t < 4; ++t)
+            to[t] = turned ? mfma_bf16x32(sp[Pairs::right(i)], f[t][Pairs::left(i)], to[t]) : mfma_bf16x32(f[t][Pairs::left(i)], sp[Pairs::right(i)], to[t]);
       };
-      by_state(lds.keys, kS);
-      by_state(lds.queries, y);
+      by_state(lds.keys, kS, std::false_type());
+      by_state(lds.queries, y, std::true_type());
     }
     typedef PlanePairs<3, 3> Pairs;
-    // c += pieces of T or P by the planes of 64 tokens
-    auto by_map = [&](const u32x4v (&map)[kMapPieces][3][64], const bf16x8v (&p)[2][3], f32x4 (&to)[4]) {
+    // c += pieces of T or P by the planes of 64 tokens; turned, a token is the result's column
+    auto by_map = [&](const u32x4v (&map)[kMapPieces][3][64], const bf16x8v (&p)[2][3], f32x4 (&to)[4], auto turned) {
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -565,7 +581,9 @@ __global__ void __launch_bounds__(kChunkThreads, sizeof(T) == 2 ? 2 : 1) chunk_w
 #pragma unroll
           for (int i = 0; i < Pairs::kCount; ++i)
 #pragma unroll
-            for (int s = 0; s < 2; ++s) to[t + s] = mfma_bf16x32(f[s][Pairs::left(i)], p[m][Pairs::right(i)], to[t + s]);
+            for (int s = 0; s < 2; ++s)
+              to[t + s] = turned ? mfma_bf16x32(p[m][Pairs::right(i)], f[s][Pairs::left(i)], to[t + s])
+                                 : mfma_bf16x32(f[s][Pairs::left(i)], p[m][Pairs::right(i)], to[t + s]);
         }
     };
     f32x4 u[4];
@@ -577,35 +595,35 @@ __global__ void __launch_bounds__(kChunkThreads, sizeof(T) == 2 ? 2 : 1) chunk_w
       for (int r = 0; r < 4; ++r) {
         const float x = beta[r] * (to_float<T>(v[t][r]) - grow[r] * kS[t][r]);
         kS[t][r] = t * 16 + q * 4 + r <= last ? x : 0.0f;
-        y[t][r] *= a.scale * grow[r];
       }
+      y[t] *= a.scale * lds.gates[kGrow][t * 16 + l16];
       u[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
     drop_odd(kS, q, first);
 #pragma unroll
     for (int m = 0; m < 2; ++m) to_planes(kS[2 * m], kS[2 * m + 1], planes[m]);
-    by_map(lds.inverse, planes, u);
+    by_map(lds.inverse, planes, u, std::false_type());
     drop_odd(u, q, first);
 #pragma unroll
     for (int m = 0; m < 2; ++m) to_planes(u[2 * m], u[2 * m + 1], planes[m]);
-    by_map(lds.scores, planes, y);
+    by_map(lds.scores, planes, y, std::true_type());
 #pragma unroll
     for (int t = 0; t < 4; ++t) u[t] *= *(const f32x4 *)&lds.gates[kWeight][t * 16 + q * 4];
 #pragma unroll
     for (int m = 0; m < 2; ++m) to_planes(u[2 * m], u[2 * m + 1], planes[m]);
-    // y, before the copies that the next chunk waits for
+    // y, before the copies that the next chunk waits for: four columns of a token a lane
     T *yt = ys + (int64_t)t0 * a.y_ld;
     if (__any(first < kChunk))
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int r = 0; r < 4; ++r) {
+        const int from = __shfl(first, q * 4 + r);
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (t * 16 + q * 4 + r >= first) y[t][r] = __builtin_nanf("");
+        for (int t = 0; t < 4; ++t)
+          if (t * 16 + l16 >= from) y[t][r] = __builtin_nanf("");
+      }
 #pragma unroll
     for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (works && t * 16 + q * 4 + r <= last) yt[(uint32_t)(t * 16 + q * 4 + r) * (uint32_t)a.y_ld] = from_float<T>(y[t][r]);
+      if (works && t * 16 + l16 <= last) store_four<T>(yt + (uint32_t)(t * 16 + l16) * (uint32_t)a.y_ld, y[t], packed);
     __syncthreads();                             // all but the keys is read
     if (t0 + kChunk < end) {
       map += a.heads;
@@ -666,7 +684,7 @@ template <typename T, int K> struct ChainLds {
   alignas(1024) u32x4v inverse[2][kMapPieces][3][64];
   alignas(1024) f32x4 scores[2][kMapTiles][64];
   alignas(16) float gates[2][kGates][kChunk];
-  int first[2][16];
+  alignas(16) int first[2][16];
 };
 
 // The same for few columns: eight waves share 16 of them, so that the chain from one state to
@@ -759,7 +777,8 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
   if (wave >= kChunkWaves) {
     if (begin >= end) return;
     const T *qs = (const T *)a.q + g * K + q * 8, *vs = (const T *)a.v + (int64_t)head * V + (values ? v0 : 0) + l16;
-    T *ys = (T *)a.y + (int64_t)head * V + v0 + l16;
+    T *ys = (T *)a.y + (int64_t)head * V + v0 + q * 4;
+    const bool packed = packed_rows<T>(a.y, a.y_ld);
     T v[4];
     float gate;
     auto load_values = [&](int t0, const ChunkMap *of) {
@@ -791,25 +810,25 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
     load_values(coming, map);
     f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
     // y of the chunk from t0 on, of buffer b, once its updates are there: P by U in float32 on both
-    // sides as they stand, k = 4 q + step of each 16 tokens.
+    // sides as they stand, k = 4 q + step of each 16 tokens.  A lane ends with four columns of a token.
     auto finish = [&](int b) {
       f32x4 yp[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
       for (int c = 0; c < kChunkWaves; ++c)
-        if (c <= w) yp[c % 2] = mul_block(lds.scores[b][map_tile(w, c)][lane], lds.U[b][c][lane], yp[c % 2]);
+        if (c <= w) yp[c % 2] = mul_block(lds.U[b][c][lane], lds.scores[b][map_tile(w, c)][lane], yp[c % 2]);
       y += yp[0] + yp[1];
     };
     auto store = [&](int t0, int b) {
-      const int from = lds.first[b][l16], last = last_of(t0);
-      T *yt = ys + (int64_t)t0 * a.y_ld;
+      typedef int i32x4 __attribute__((ext_vector_type(4)));
+      const i32x4 from = *(const i32x4 *)&lds.first[b][q * 4];
+      const int i = w * 16 + l16;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (i >= from[r]) y[r] = __builtin_nanf("");
       // Without a condition, so that the wait for a later load does not take the stores with it (they may not have
       // been made): rows past the end go where nothing is read.
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int i = w * 16 + q * 4 + r;
-        T *const p = i <= last ? yt + (uint32_t)i * (uint32_t)a.y_ld : (T *)nowhere + lane;
-        *p = from_float<T>(i < from ? y[r] : __builtin_nanf(""));
-      }
+      T *const p = i <= last_of(t0) ? ys + (int64_t)t0 * a.y_ld + (uint32_t)i * (uint32_t)a.y_ld : (T *)nowhere + l16 * 4;
+      store_four<T>(p, y, packed);
     };
     int t0 = begin, b = 0;
 #pragma unroll 1
@@ -828,9 +847,9 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
           raw[m].planes(qf);
 #pragma unroll
           for (int p = 0; p < 3; ++p) s[p] = __builtin_bit_cast(bf16x8v, lds.S[p][m][lane]);
-          qp.add(qf, s);
+          qp.add(s, qf);
         }
-        y = qp.sum() * (*(const f32x4 *)&lds.gates[b][kGrow][w * 16 + q * 4] * a.scale);
+        y = qp.sum() * (lds.gates[b][kGrow][w * 16 + l16] * a.scale);
         load_queries(next);
       }
       __syncthreads();                           // U is there
