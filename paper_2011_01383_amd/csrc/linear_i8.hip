@@ -509,9 +509,15 @@ int launch_tiles(const Product &p, const int32_t *status, bool aligned, hipStrea
   return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
 }
 
-template <typename T, int TI, int TJ, int WAVES, int AHEAD>
+template <typename T, int TI, int TJ, int WAVES>
 int launch_few(const Product &p, const int32_t *status, bool aligned, hipStream_t st) {
-  few_kernel<T, TI, TJ, WAVES, AHEAD><<<(unsigned)((p.outputs + 16 * TI - 1) / (16 * TI)), 64 * WAVES, 0, st>>>(p, status, aligned);
+  const unsigned grid = (unsigned)((p.outputs + 16 * TI - 1) / (16 * TI));
+  // No more loads at once than a wave has shares, or it loads the last one again: 10,000 channels of 500 inputs, 64
+  // tokens 9.2 us and 14.9, 7 tokens 7.0 and 10.0.
+  const int each = ((p.pieces + 3) / 4 + WAVES - 1) / WAVES;
+  if (each <= 1) few_kernel<T, TI, TJ, WAVES, 1><<<grid, 64 * WAVES, 0, st>>>(p, status, aligned);
+  else if (each <= 2) few_kernel<T, TI, TJ, WAVES, 2><<<grid, 64 * WAVES, 0, st>>>(p, status, aligned);
+  else few_kernel<T, TI, TJ, WAVES, 4><<<grid, 64 * WAVES, 0, st>>>(p, status, aligned);
   return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
 }
 
@@ -519,13 +525,14 @@ template <typename T> int launch_product(const Product &p, const int32_t *status
   // Up to 64 tokens against tiles of 64 by 64, over 2,048 inputs: 16 tokens of 1,024 channels 9.3 us and 11.4, 64 of 8,192
   // 13.4 and 14.2.
   if (p.tokens <= 64) {
-    // Four waves against eight: 8 tokens of 2,048 channels 7.2 us and 8.6, of 16,384 12.8 and 19.7.
-    if (p.tokens <= 16) return launch_few<T, 1, 1, 4, 8>(p, status, aligned, st);
-    // 32 channels a workgroup where that leaves one a CU, else 16: 24 tokens of 4,096 channels 10.0 us and 8.4, of 8,192 10.7
-    // and 11.9; 64 tokens of 4,096 12.8 and 11.5, of 8,192 13.3 and 16.4.
+    // Four, eight and sixteen waves: 7 tokens, 2,695 channels of 8,140 inputs, 19.5 us, 17.5 and 17.6, 10,000 of 500 6.8, 7.0
+    // and 7.9.
+    if (p.tokens <= 16) return launch_few<T, 1, 1, 8>(p, status, aligned, st);
+    // 32 channels a workgroup where that leaves one a CU, else 16 (2,048 inputs): 24 tokens of 4,096 channels 10.0 us and 8.4, of
+    // 8,192 10.7 and 11.9; 64 tokens of 4,096 12.8 and 11.5, of 8,192 13.3 and 16.4.
     const bool many = (p.outputs + 15) / 16 >= 512;
-    if (p.tokens <= 32) return many ? launch_few<T, 2, 2, 8, 4>(p, status, aligned, st) : launch_few<T, 1, 2, 8, 4>(p, status, aligned, st);
-    return many ? launch_few<T, 2, 4, 8, 4>(p, status, aligned, st) : launch_few<T, 1, 4, 8, 4>(p, status, aligned, st);
+    if (p.tokens <= 32) return many ? launch_few<T, 2, 2, 8>(p, status, aligned, st) : launch_few<T, 1, 2, 8>(p, status, aligned, st);
+    return many ? launch_few<T, 2, 4, 8>(p, status, aligned, st) : launch_few<T, 1, 4, 8>(p, status, aligned, st);
   }
   // The largest tiles that keep three of four CUs at work, over 2,048 inputs in tiles of 256, 128 and 64: 128 tokens of
   // 2,048 channels 35.9, 25.6 and 13.0 us, 1,024 of 2,048 43.8, 28.9 and 20.0, 1,024 of 8,192 48.2, 42.9 and 57.1, 2,048 of

@@ -248,3 +248,12 @@ def test_quant_near_halves(cols):
     torch.cuda.synchronize()
     want, ws = O.quant_rows(x)
     assert np.array_equal(s.cpu().numpy(), ws) and np.array_equal(q.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("T,N", [(5, 50), (20, 50), (60, 50), (20, 8200), (60, 8200)])
+def test_few_tokens_of_every_number_of_shares(T, N):
+    """Inputs of one, two and more 64-byte shares for each of eight waves, and of fewer than waves."""
+    need_gpu()
+    say("linear shares", T, N)
+    for K in (64, 65, 512, 513, 1024, 1025, 2048, 2100):
+        product(T, K, N, "bf16", given=K % 2 == 1)
