@@ -589,7 +589,7 @@ int cortex_qk_norm(const cortex_qk_norm_t *args, int32_t *d_status, void *stream
  */
 typedef struct {
   int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: x */
-  int32_t rows;
+  int32_t rows;               /* less than 2^22 */
   int32_t columns;            /* at most 131,071 */
   const void *x;              /* [rows, columns], row stride x_ld */
   int64_t x_ld;
@@ -609,7 +609,7 @@ int cortex_quant_i8(const cortex_quant_i8_t *args, int32_t *d_status, void *stre
  * each rounded on its own, and rounded to dtype.  Rows of w start at 16-byte
  * boundaries and lie w_ld bytes apart, a multiple of 16 up to 2^24; what their last 16
  * bytes hold past the inputs does not matter, but is read.  N is at most 2^26, T less than
- * 2^24 and T N at most 2^37.
+ * 2^22 and T N at most 2^37.
  */
 typedef struct {
   int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: y, and x without x_scale */

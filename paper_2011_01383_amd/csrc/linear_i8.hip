@@ -13,7 +13,9 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int64_t kMaxRow = 1 << 24;              // 255 rows of bytes stay below 2^32
 constexpr int32_t kMaxInputs = 131071;           // 128 * 128 of each stay below 2^31
-// Of each call's grid, which has less than 2^32 threads: 512 to 16 channels of few tokens, 1,024 to a tile of 256 by 256.
+// A grid has less than 2^32 threads: up to 1,024 to a row that is brought to 8 bits, 512 to 16 channels of few tokens, 1,024 to a
+// tile of 256 by 256.
+constexpr int32_t kMaxRows = 1 << 22;
 constexpr int32_t kMaxOutputs = 1 << 26;
 constexpr int64_t kMaxResults = (int64_t)1 << 37;
 
@@ -150,12 +152,15 @@ template <typename T, bool WIDE, int THREADS, bool KEPT> void launch_quant_of(co
 template <typename T, bool WIDE> int launch_quant_rows(const cortex_quant_i8_t &a, int32_t *status, int filled, void *stream) {
   const hipStream_t st = (hipStream_t)stream;
   // As few waves as hold a row: 8,192 rows of 1,000 (with a product over 64 channels) by one wave 13.8 us, two 19, four 22.6; of 2,048
-  // by two 20.5, four 29.7; of 4,096 by four 34.3, two (32 elements a thread) 37.1.  8,192 columns kept by
-  // four waves 90, read again 85.
+  // by two 20.5, four 29.7; of 4,096 by four 34.3, two (32 elements a thread) 37.1; of 8,192
+  // by eight 73, read again by four 76 (float32 93 and 118); 7 rows of 6,098 10.6 and 13.2; 1,024 float32 rows of 16,384 by sixteen 51,
+  // read again by four 58.
   if (filled <= 1024) launch_quant_of<T, WIDE, 64, true>(a, status, filled, st);
   else if (filled <= 2048) launch_quant_of<T, WIDE, 128, true>(a, status, filled, st);
   else if (filled <= 4096) launch_quant_of<T, WIDE, 256, true>(a, status, filled, st);
-  else launch_quant_of<T, WIDE, 256, false>(a, status, filled, st);
+  else if (filled <= 8192) launch_quant_of<T, WIDE, 512, true>(a, status, filled, st);
+  else if (filled <= 16384) launch_quant_of<T, WIDE, 1024, true>(a, status, filled, st);
+  else launch_quant_of<T, WIDE, 1024, false>(a, status, filled, st);
   return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
 }
 
@@ -582,8 +587,7 @@ using namespace cortex;
 extern "C" int cortex_quant_i8(const cortex_quant_i8_t *a, int32_t *status, void *stream) {
   if (!a || !status) return CORTEX_E_INVAL;
   if (a->dtype != CORTEX_F32 && a->dtype != CORTEX_BF16) return CORTEX_E_INVAL;
-  // a workgroup of 256 a row, and a grid has less than 2^32 threads
-  if (a->rows < 0 || a->rows >= 1 << 24 || a->columns < 1 || a->columns > kMaxInputs) return CORTEX_E_INVAL;
+  if (a->rows < 0 || a->rows >= kMaxRows || a->columns < 1 || a->columns > kMaxInputs) return CORTEX_E_INVAL;
   if (a->x_ld < a->columns || a->q_ld < a->columns) return CORTEX_E_INVAL;
   if (a->rows == 0) return CORTEX_OK;
   if (!a->x || !a->q || !a->scale) return CORTEX_E_INVAL;
@@ -599,8 +603,7 @@ extern "C" size_t cortex_linear_i8_workspace_bytes(int32_t tokens, int32_t outpu
 extern "C" int cortex_linear_i8(const cortex_linear_i8_t *a, int32_t *status, void *ws, size_t ws_bytes, void *stream) {
   if (!a || !status) return CORTEX_E_INVAL;
   if (a->dtype != CORTEX_F32 && a->dtype != CORTEX_BF16) return CORTEX_E_INVAL;
-  // bringing tokens to 8 bits takes a workgroup of 256 each, and a grid has less than 2^32 threads
-  if (bad_linear_size(a->tokens, a->outputs, a->inputs) || a->tokens >= 1 << 24) return CORTEX_E_INVAL;
+  if (bad_linear_size(a->tokens, a->outputs, a->inputs) || a->tokens >= kMaxRows) return CORTEX_E_INVAL;
   if (a->x_ld < a->inputs || a->y_ld < a->outputs || a->w_ld < a->inputs || a->w_ld % 16 || a->w_ld > kMaxRow) return CORTEX_E_INVAL;
   if (a->tokens == 0) return CORTEX_OK;
   if (!a->x || !a->w || !a->w_scale || !a->y || !aligned16(a->w)) return CORTEX_E_INVAL;

@@ -115,7 +115,7 @@ def quant_args(**kw):
     return C.cortex_quant_i8_t(**a)
 
 
-@pytest.mark.parametrize("bad", [dict(dtype=2), dict(rows=-1), dict(rows=1 << 24), dict(columns=0),
+@pytest.mark.parametrize("bad", [dict(dtype=2), dict(rows=-1), dict(rows=1 << 24), dict(rows=1 << 22), dict(columns=0),
                                  dict(columns=131072, x_ld=131072, q_ld=131072), dict(x=None), dict(q=None), dict(scale=None),
                                  dict(x_ld=7), dict(q_ld=7)])
 def test_quant_refuses(lib, bad):
@@ -131,7 +131,7 @@ def linear_args(**kw):
 @pytest.mark.parametrize("bad", [
     dict(dtype=2), dict(tokens=-1), dict(inputs=0), dict(inputs=131072, x_ld=131072, w_ld=131072), dict(outputs=0), dict(x=None),
     dict(w=None), dict(w_scale=None), dict(y=None), dict(x_ld=39), dict(w_ld=40), dict(w_ld=56), dict(w_ld=32), dict(y_ld=7),
-    dict(w=P8 + 8), dict(w_ld=(1 << 24) + 16), dict(tokens=1 << 24)])
+    dict(w=P8 + 8), dict(w_ld=(1 << 24) + 16), dict(tokens=1 << 24), dict(tokens=1 << 22)])
 def test_linear_refuses(lib, bad):
     assert lib.cortex_linear_i8(ctypes.byref(linear_args(**bad)), P8, P8, 1 << 50, None) == C.CORTEX_E_INVAL
 

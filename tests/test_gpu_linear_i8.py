@@ -257,3 +257,11 @@ def test_few_tokens_of_every_number_of_shares(T, N):
     say("linear shares", T, N)
     for K in (64, 65, 512, 513, 1024, 1025, 2048, 2100):
         product(T, K, N, "bf16", given=K % 2 == 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("left", [0, 1, 8])
+@pytest.mark.parametrize("rows,cols", [(7, 1024), (3, 1025), (7, 2049), (5, 4096), (3, 4097), (5, 8192), (3, 8193), (3, 16384), (2, 16385),
+                                       (300, 6098)])
+def test_quant_of_every_number_of_waves(rows, cols, left, dtype):
+    test_quant(rows, cols, left, dtype)
