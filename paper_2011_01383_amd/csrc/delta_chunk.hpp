@@ -441,7 +441,7 @@ template <typename T, int K> struct ChunkLds {
 // between waves; keys, queries, T and P are shared in LDS.
 //
 // 8,192 tokens of 16 prompts, 32 heads of 128 by 128: 157 us.  The matrix units are busy 35% of it, the vector units (planes of S,
-// R and U) 43%, two workgroups a CU, which is what 251 registers and 80 KB of LDS admit.  32 columns a wave halve the reads
+// R and U) 42%, two workgroups a CU, which is what 222 registers and 71 KB of LDS admit.  32 columns a wave halve the reads
 // of LDS but leave one workgroup a CU: 382 us against 260 of an earlier form.
 template <typename T, int K, bool WIDE>
 __global__ void __launch_bounds__(kChunkThreads, sizeof(T) == 2 ? 2 : 1) chunk_walk_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps) {
@@ -696,6 +696,11 @@ template <typename T, int K> struct ChainLds {
 // a segment does to the state that enters it is S M + N, and part 1 finds N (from a zero state) and M
 // (from the unit rows, without values) as columns of their own, V + K of them; enter_segments_kernel
 // joins them; part 2 forms the outputs from the state that enters.
+//
+// The latency of a chunk bounds it: 2 us at 128 by 128, 1.5 of them the chain's three exchanges (32,768 tokens of 32 heads, a
+// workgroup a CU: 1,140 us for 512 chunks; matrix units busy 23%, LDS 34%).  Without the outputs' stores it took 0.3 us a chunk
+// less, which is why a lane stores four columns at once (1,222 us in all before, 1,171 since); values loaded so as well changed
+// nothing.
 template <typename T, int K, int PART, bool WIDE>
 __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta_t a, int32_t *status, const ChunkMap *maps, float *segments, float *nowhere, int Q) {
   typedef ChainLds<T, K> Lds;
@@ -996,7 +1001,7 @@ __global__ void __launch_bounds__(kChainThreads) chunk_chain_kernel(cortex_delta
 
 // The states that enter a sequence's segments, in the place of what they add: s <- s M + N.  A workgroup
 // takes 16 rows of a head's state; a wave K / 4 of their entries (float32 matrix units, k = 4 q + step of each
-// 16 on both sides), M's loads for the next segment on their way.
+// 16 on both sides), M's loads for the next segment on their way.  About 1.5 us a segment, its loads' latency.
 template <int K>
 __global__ void __launch_bounds__(kChunkThreads) enter_segments_kernel(cortex_delta_t a, int32_t *status, float *segments, int Q) {
   constexpr int kRow = K + 4, kTiles = K < 64 ? 1 : K / 64, kBlocks = K / 16;
