@@ -839,6 +839,8 @@ def cortex_qk_norm(q: torch.Tensor, q_out: torch.Tensor, *, k=None, k_out=None, 
     """q, q_out [T, H, P]; k, k_out [T, key heads, P]; weights [P]; positions [T]; freqs [R / 2]."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3 or q.dtype not in _DTYPES:
         raise ValueError("q must be a [T, H, P] torch.Tensor of torch.float32 or torch.bfloat16")
+    if not isinstance(norm, int):
+        raise ValueError("norm must be one of CORTEX_NORM_*, got %r" % (norm,))
     eps = _number(eps, "eps")
     T, typ, f32 = q.shape[0], q.dtype, torch.float32
     H, P, q_ld = _head_rows(q, "q", typ, T)

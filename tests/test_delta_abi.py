@@ -187,7 +187,8 @@ def test_binding_refuses_norm():
                      (dict(k_out=Z(3, 2, 32)), "k is required"), (dict(positions=Z(3, dtype=I32)), "freqs is required"),
                      (dict(freqs=Z(8)), "positions is required"), (dict(freqs=Z(8), positions=Z(2, dtype=I32)), "positions holds 2"),
                      (dict(freqs=Z(8), positions=Z(3)), "positions must be torch.int32"), (dict(q_weight=Z(31)), "q_weight holds 31"),
-                     (dict(freqs=[1.0], positions=Z(3, dtype=I32)), "freqs must be a torch.Tensor"), (dict(status=None), "status is required")):
+                     (dict(freqs=[1.0], positions=Z(3, dtype=I32)), "freqs must be a torch.Tensor"), (dict(norm="rms"), "norm must be one of"),
+                     (dict(status=None), "status is required")):
         with pytest.raises(ValueError, match=what):
             C.cortex_qk_norm(**{**good, **kw})
 

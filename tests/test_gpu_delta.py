@@ -272,3 +272,71 @@ def test_what_is_not_finite_in_a_long_prompt(where):
     hit_end = hit_end.reshape(end.shape)
     assert np.array_equal(got[~hit], clean[~hit]) and np.array_equal(got_end[~hit_end], end[~hit_end])
     assert not np.isfinite(got[hit]).any() and not np.isfinite(got_end[hit_end].reshape(-1, 64)).all(1).any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("left", [1, 2, 4, 8, 16])
+def test_strides_and_alignments_of_many_prompts(left, dtype):
+    need_gpu()
+    say("delta strides of many prompts", left, dtype)
+    p = Delta(14, [5, 70, 0, 1] * 32, 4, 1, 64, 48, dtype, left=left)
+    y, out = run(p)
+    p.check(y, out, "strides of many prompts")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("where", ["v", "k", "q", "b", "dt", "state"])
+def test_what_is_not_finite_in_many_prompts(where, bad, dtype):
+    """As in few: in every third of 66 prompts, at another token of each."""
+    need_gpu()
+    say("delta many prompts, not finite", where, bad, dtype)
+    S, n, V, K = 66, 130, 64, 32
+    p = Delta(15, [n] * S, 4, 2, K, V, dtype)
+    clean, end = (host(v) for v in run(p))
+    hit = np.zeros(clean.shape, dtype=bool)
+    hit_end = np.zeros(end.shape, dtype=bool).reshape(S, 4, V, K)
+    for s in range(0, S, 3):
+        first, last, head, row = n * s, n * s + n, 2 + s % 2, s % V
+        t = first + (s * 7) % n
+        if where == "v":
+            p.v[t, head, row] = bad
+            hit[t:last, head, row] = hit_end[s, head, row] = True
+        elif where == "k":
+            p.k[t, 1, 9] = bad
+            hit[t:last, 2:] = hit_end[s, 2:] = True
+        elif where == "q":
+            p.q[t, 1, 9] = bad
+            hit[t, 2:] = True
+        elif where == "state":
+            p.state[s, head * V + row, 3] = bad
+            hit[first:last, head, row] = hit_end[s, head, row] = True
+        else:
+            (p.b if where == "b" else p.dt)[t, head] = bad
+            hit[t:last, head] = hit_end[s, head] = True
+    got, got_end = (host(v) for v in run(p))
+    hit_end = hit_end.reshape(end.shape)
+    assert np.array_equal(got[~hit], clean[~hit]) and np.array_equal(got_end[~hit_end], end[~hit_end])
+    # an infinite share is one or none, an infinite step forgets the state: finite either way
+    if not (where in ("b", "dt") and np.isinf(bad)):
+        assert not np.isfinite(got[hit]).any() and not np.isfinite(got_end[hit_end].reshape(-1, K)).all(1).any()
+
+
+@pytest.mark.parametrize("many", [False, True])
+def test_two_streams_at_once(many):
+    """Two batches on two streams, each with its own workspace, over and over: what each gives alone."""
+    need_gpu()
+    say("delta two streams", many)
+    ps = [Delta(16 + i, [30, 200, 65] * (24 if many else 1), 4, 2, 64, 64) for i in range(2)]
+    alone = [tuple(t.clone() for t in run(p)) for p in ps]
+    ends = [torch.empty_like(out) for _, out in alone]
+    streams = [torch.cuda.Stream() for _ in ps]
+    for p in ps:
+        p.d["y"].zero_()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for p, end, stream in zip(ps, ends, streams):
+            C.check(p.call(False, state_out=end, stream=stream))
+    torch.cuda.synchronize()
+    for p, end, (y, out) in zip(ps, ends, alone):
+        assert torch.equal(p.d["y"], y) and torch.equal(end, out) and int(p.d["status"].item()) == 0
