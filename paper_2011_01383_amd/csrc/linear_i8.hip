@@ -425,23 +425,23 @@ __global__ void __launch_bounds__(64 * WAVES) few_kernel(Product a, const int32_
 }
 
 // One token, brought to 8 bits by every workgroup for itself, beside the loads of its first
-// weights: a launch less.  The row stays in LDS.  4,096 inputs by 8,192 channels 9.2 us, 3.6 TB/s of weights.
-constexpr int kOwnBytes = 16384, kOwnWaves = 4;
-template <typename T, bool WIDE>
-__global__ void __launch_bounds__(64 * kOwnWaves) own_kernel(Product a, const T *x, int columns, const int32_t *status, bool aligned) {
-  constexpr int kAhead = 8, kThreads = 64 * kOwnWaves;
+// weights: a launch less.  The row stays in LDS.  4,096 inputs by 8,192 channels 9.4 us, 3.6 TB/s of weights.
+constexpr int kOwnBytes = 16384;
+template <typename T, bool WIDE, int WAVES, int AHEAD>
+__global__ void __launch_bounds__(64 * WAVES) own_kernel(Product a, const T *x, int columns, const int32_t *status, bool aligned) {
+  constexpr int kThreads = 64 * WAVES;
   __shared__ __attribute__((aligned(16))) int8_t row[kOwnBytes];
-  __shared__ i32x4 sums[kOwnWaves][64];
-  __shared__ unsigned int most[kOwnWaves];
+  __shared__ i32x4 sums[WAVES][64];
+  __shared__ unsigned int most[WAVES];
   const int failed = entry_status(status);
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, q = lane >> 4, l16 = lane & 15;
   const int n0 = (int)blockIdx.x * 16, steps = (a.pieces + 3) / 4;
   const int8_t *w = a.w + (int64_t)min(n0 + l16, a.outputs - 1) * a.w_ld;
-  i32x4 wf[kAhead];
+  i32x4 wf[AHEAD];
   auto fetch = [&](int s0) {
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-      wf[k] = *(const i32x4 *)(w + (int64_t)min(min(s0 + k * kOwnWaves, steps - 1) * 4 + q, a.pieces - 1) * 16);
+    for (int k = 0; k < AHEAD; ++k)
+      wf[k] = *(const i32x4 *)(w + (int64_t)min(min(s0 + k * WAVES, steps - 1) * 4 + q, a.pieces - 1) * 16);
   };
   // Most of the row stays in registers until its scale is known.
   constexpr int kKeep = 2;
@@ -465,7 +465,9 @@ __global__ void __launch_bounds__(64 * kOwnWaves) own_kernel(Product a, const T 
   top = wave_top(top);
   if (lane == 0) most[wave] = top;
   if (__syncthreads_or(failed != 0)) return;
-  const RowScale s(__builtin_amdgcn_readfirstlane(max(max(most[0], most[1]), max(most[2], most[3]))));
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) top = max(top, most[i]);
+  const RowScale s(__builtin_amdgcn_readfirstlane(top));
 #pragma unroll
   for (int k = 0; k < kKeep; ++k) {
     const int c = (k * kThreads + tid) * 8;
@@ -479,17 +481,19 @@ __global__ void __launch_bounds__(64 * kOwnWaves) own_kernel(Product a, const T 
   __syncthreads();
   i32x4 acc = {0, 0, 0, 0};
 #pragma unroll 1
-  for (int s0 = wave; s0 < steps; s0 += kOwnWaves * kAhead) {
+  for (int s0 = wave; s0 < steps; s0 += WAVES * AHEAD) {
     if (s0 != wave) fetch(s0);
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-      if (s0 + k * kOwnWaves < steps)
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[k], *(const i32x4 *)(row + (s0 + k * kOwnWaves) * 64 + q * 16), acc, 0, 0, 0);
+    for (int k = 0; k < AHEAD; ++k)
+      if (s0 + k * WAVES < steps)
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[k], *(const i32x4 *)(row + (s0 + k * WAVES) * 64 + q * 16), acc, 0, 0, 0);
   }
   sums[wave][lane] = acc;
   __syncthreads();
-  if (wave == 0 && l16 == 0)
-    put_four<T>(a, (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]), s.scale, four, 0, n0 + q * 4, aligned);
+  if (wave != 0 || l16 != 0) return;
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) acc += sums[i][lane];
+  put_four<T>(a, acc, s.scale, four, 0, n0 + q * 4, aligned);
 }
 
 // ---------------------------------------------------------------------------
@@ -548,6 +552,20 @@ template <typename T> int launch_product(const Product &p, const int32_t *status
   return launch_tiles<T, 64, 64, 2, 2, 8>(p, status, aligned, st);
 }
 
+template <typename T, bool WIDE> int launch_own(const Product &p, int inputs, const int32_t *status, bool aligned, hipStream_t st) {
+  const unsigned grid = (unsigned)((p.outputs + 15) / 16);
+  const T *x = (const T *)p.x;
+  const int shares = (p.pieces + 3) / 4;
+  // Eight waves where that leaves each eight shares of the weights, all loaded at once, else four, and no more loads than shares: 8,192
+  // channels of 4,096 inputs by eight waves 9.4 us, by four 10.1, 4,096 of 8,192 10.0 and 12.7, but 8,192 of 2,048 7.6 and 6.6;
+  // 10,000 of 500 by two loads at once 5.4 and by eight 6.9.
+  if (shares >= 64) own_kernel<T, WIDE, 8, 8><<<grid, 512, 0, st>>>(p, x, inputs, status, aligned);
+  else if (shares > 16) own_kernel<T, WIDE, 4, 8><<<grid, 256, 0, st>>>(p, x, inputs, status, aligned);
+  else if (shares > 8) own_kernel<T, WIDE, 4, 4><<<grid, 256, 0, st>>>(p, x, inputs, status, aligned);
+  else own_kernel<T, WIDE, 4, 2><<<grid, 256, 0, st>>>(p, x, inputs, status, aligned);
+  return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+}
+
 template <typename T> int launch_linear(const cortex_linear_i8_t &a, int32_t *status, void *ws, void *stream) {
   const hipStream_t st = (hipStream_t)stream;
   const int64_t row = row_bytes(a.inputs);
@@ -558,11 +576,8 @@ template <typename T> int launch_linear(const cortex_linear_i8_t &a, int32_t *st
   // One token in one launch against two: 1,000 channels of 2,048 inputs 5.0 us and 7.6, 8,192 of 4,096 12.4 and 13.9, 32,000
   // of 4,096 34.5 and 37.3; two tokens, 8,192 of 4,096, 14.3 and 14.3, four, 32,000 of 4,096, 49 and 39.
   if (!a.x_scale && a.tokens == 1 && row <= kOwnBytes) {
-    const unsigned grid = (unsigned)((a.outputs + 15) / 16);
-    const T *x = (const T *)a.x;
-    if (eights<T>(x, a.x_ld, a.inputs)) own_kernel<T, true><<<grid, 64 * kOwnWaves, 0, st>>>(p, x, a.inputs, status, aligned);
-    else own_kernel<T, false><<<grid, 64 * kOwnWaves, 0, st>>>(p, x, a.inputs, status, aligned);
-    return hipGetLastError() == hipSuccess ? CORTEX_OK : CORTEX_E_HIP;
+    return eights<T>(a.x, a.x_ld, a.inputs) ? launch_own<T, true>(p, a.inputs, status, aligned, st)
+                                            : launch_own<T, false>(p, a.inputs, status, aligned, st);
   }
   if (!a.x_scale) {
     const cortex_quant_i8_t q = {a.dtype, a.tokens, a.inputs, a.x, a.x_ld, rows, row, scales};

@@ -265,3 +265,12 @@ def test_few_tokens_of_every_number_of_shares(T, N):
                                        (300, 6098)])
 def test_quant_of_every_number_of_waves(rows, cols, left, dtype):
     test_quant(rows, cols, left, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [1, 50, 1000])
+def test_one_token_of_every_number_of_shares(N, dtype):
+    need_gpu()
+    say("linear one token, shares", N, dtype)
+    for K in (1, 63, 64, 512, 513, 1024, 1025, 4032, 4033, 4096, 4100, 8192, 8193, 16384):
+        product(1, K, N, dtype)
