@@ -554,6 +554,8 @@ int cortex_delta_step(const cortex_delta_t *args, int32_t *d_status, void *strea
  * rounded once.  Prompts and single tokens alike: rows are tokens.  P is even, at
  * most 512; R is even, at most P, 0 for no rotation (positions and freqs are then not
  * read).  Without keys key_heads is 0.  Outputs may be the inputs themselves.
+ * An infinity or NaN reaches the rest of its head through the norm, the other element
+ * of its pair through the rotation, and no other element.
  */
 #define CORTEX_NORM_NONE 0
 #define CORTEX_NORM_RMS 1

@@ -127,8 +127,10 @@ __global__ void __launch_bounds__(64 * kNormWaves) norm_wide_kernel(cortex_qk_no
       for (int i = 0; i < V; ++i) {
         float *d = INTERLEAVED ? &y[2 * i / V][2 * i % V] : &y[0][i], *e = INTERLEAVED ? &y[2 * i / V][2 * i % V + 1] : &y[1][i];
         const float f = INTERLEAVED ? x[2 * i / V][2 * i % V] : x[0][i], k = INTERLEAVED ? x[2 * i / V][2 * i % V + 1] : x[1][i];
-        *d = f * c[i] - k * s[i];
-        *e = k * c[i] + f * s[i];
+        // what is not rotated is left alone: a sine of 0 would carry an infinity or NaN to the other
+        const bool turned = turns && (!INTERLEAVED || lo / 2 + i < R / 2);
+        *d = turned ? f * c[i] - k * s[i] : f;
+        *e = turned ? k * c[i] + f * s[i] : k;
       }
       if (works && r < to) {
         Pack<T, V>::store(out + (int64_t)r * P + lo, y[0]);
@@ -175,10 +177,15 @@ __global__ void __launch_bounds__(64 * kNormWaves) norm_pair_kernel(cortex_qk_no
       u *= row.weight[at[n]];
       v *= row.weight[to[n]];
     }
-    float c = 1.0f, s = 0.0f;
-    if (pair < R / 2) angle(a.positions[t], a.freqs[pair], c, s);
-    row.out[at[n]] = from_float<T>(u * c - v * s);
-    row.out[to[n]] = from_float<T>(v * c + u * s);
+    if (pair < R / 2) {
+      float c, s;
+      angle(a.positions[t], a.freqs[pair], c, s);
+      const float turned = u * c - v * s;
+      v = v * c + u * s;
+      u = turned;
+    }
+    row.out[at[n]] = from_float<T>(u);
+    row.out[to[n]] = from_float<T>(v);
   }
 }
 

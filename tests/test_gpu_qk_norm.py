@@ -210,3 +210,53 @@ def test_special_values_in_many_rows():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(again[4:], out[4:]) and torch.equal(again[:2], out[:2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("P,R", [(64, 0), (64, 16), (128, 96), (32, 32), (66, 10), (80, 40)])
+def test_what_is_not_finite_without_a_norm_stays_with_its_element(P, R, bad, interleaved, dtype):
+    """An element outside the rotation reaches its own output, one inside that of its pair too, in few rows and in many."""
+    need_gpu()
+    say("norm none, not finite", P, R, bad, interleaved, dtype)
+    for T in (6, 1400):
+        p = make(11, T, 2, 1, P, R, dtype)
+        kw = dict(norm=C.CORTEX_NORM_NONE, interleaved=interleaved, q_weight=dev(p["qw"]), status=torch.zeros(1, dtype=torch.int32, device="cuda"))
+        if R:
+            kw.update(positions=dev(p["at"], torch.int32), freqs=dev(p["freqs"]))
+        k = heads(p["k"], p["t"])
+        q, hit = heads(p["q"], p["t"]), np.zeros((T, 2, P), dtype=bool)
+        clean, k_clean = torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
+        C.check(C.cortex_qk_norm(q, clean, k=k, k_out=k_clean, **kw))
+        for t in range(min(T, P)):               # every place of a head, in another token each
+            q[t, t % 2, t] = bad
+            hit[t, t % 2, t] = True
+            if t < R:
+                hit[t, t % 2, t ^ 1 if interleaved else (t + R // 2) % R] = True
+        got, k_got = torch.empty_like(clean), torch.empty_like(k_clean)
+        C.check(C.cortex_qk_norm(q, got, k=k, k_out=k_got, **kw))
+        torch.cuda.synchronize()
+        assert torch.equal(k_got, k_clean)
+        assert np.array_equal(host(got)[~hit], host(clean)[~hit]) and not np.isfinite(host(got)[hit]).any()
+        for t in range(R, min(T, P)):
+            assert np.array_equal(host(got)[t, t % 2, t], bad, equal_nan=True)
+
+
+@pytest.mark.parametrize("norm", ["rms", "l2"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("P,R", [(64, 0), (128, 32), (66, 10)])
+def test_an_infinity_in_a_norm_leaves_zeros_beside_it(P, R, interleaved, norm):
+    """x / infinity is 0 but for the infinite element itself, which has no value."""
+    need_gpu()
+    say("norm of an infinity", P, R, interleaved, norm)
+    for T in (6, 4200):
+        p = make(12, T, 1, 0, P, R, "f32")
+        q = heads(p["q"], p["t"])
+        q[:6, 0, P - 3] = float("inf")
+        kw = dict(positions=dev(p["at"], torch.int32), freqs=dev(p["freqs"])) if R else {}
+        out = torch.empty_like(q)
+        C.check(C.cortex_qk_norm(q, out, norm=NORMS[norm], interleaved=interleaved, status=torch.zeros(1, dtype=torch.int32, device="cuda"), **kw))
+        torch.cuda.synchronize()
+        rest = [i for i in range(P) if i != P - 3]
+        assert torch.isnan(out[:6, 0, P - 3]).all() and (out[:6, 0, rest] == 0).all() and torch.isfinite(out[6:]).all()
