@@ -729,6 +729,12 @@ int64_t cortex_get_knob(int32_t knob);
 /* Workgroups the last launch of each kind used (for reports; host-side). */
 int32_t cortex_last_grid(int32_t which /* 0 = linearize, 1 = forward */);
 
+/* How cortex_delta_forward walks such a batch (for reports; host-side): the tokens of
+ * the segments that it cuts prompts into, 0 where it takes sequences whole (and for
+ * sizes that it refuses).  It goes by the mean length; results agree to rounding. */
+int32_t cortex_delta_segment_tokens(int32_t num_tokens, int32_t num_seqs, int32_t heads, int32_t key_dim,
+                                    int32_t value_dim);
+
 /* Matrix-core throughput probe, for reporting achieved rates beside a sustained
  * (measured) peak as well as the nominal one.  cortex_probe_mfma enqueues one
  * workgroup of 8 waves per compute unit on `stream`; every wave runs `iters`

@@ -73,6 +73,7 @@ EXPORTED = [
     "cortex_conv_forward", "cortex_conv_step", "cortex_scan_workspace_bytes", "cortex_scan_forward",
     "cortex_scan_step", "cortex_logits_workspace_bytes", "cortex_logits_process",
     "cortex_delta_workspace_bytes", "cortex_delta_forward", "cortex_delta_step", "cortex_qk_norm",
+    "cortex_delta_segment_tokens",
     "cortex_quant_i8", "cortex_linear_i8_workspace_bytes", "cortex_linear_i8",
 ]
 
@@ -225,6 +226,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.cortex_logits_process.restype = ctypes.c_int
     lib.cortex_delta_workspace_bytes.argtypes = [I32, I32, I32, I32, I32]
     lib.cortex_delta_workspace_bytes.restype = SZ
+    lib.cortex_delta_segment_tokens.argtypes = [I32, I32, I32, I32, I32]
+    lib.cortex_delta_segment_tokens.restype = I32
     lib.cortex_delta_forward.argtypes = [P, P, P, SZ, P]
     lib.cortex_delta_forward.restype = ctypes.c_int
     lib.cortex_delta_step.argtypes = [P, P, P]
@@ -814,6 +817,10 @@ def _delta(step: bool, q, k, v, b, offsets, y, dt, A, dt_bias, softplus, sigmoid
 
 def cortex_delta_workspace_bytes(T: int, S: int, H: int, K: int, V: int) -> int:
     return load().cortex_delta_workspace_bytes(T, S, H, K, V)
+
+
+def cortex_delta_segment_tokens(T: int, S: int, H: int, K: int, V: int) -> int:
+    return load().cortex_delta_segment_tokens(T, S, H, K, V)
 
 
 def cortex_delta_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, b: torch.Tensor, offsets: torch.Tensor,

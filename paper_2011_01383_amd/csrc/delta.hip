@@ -121,17 +121,19 @@ constexpr int64_t kMaxSegmentTiles = 2048;
 
 // Tokens of a segment, 0 for whole sequences.  By the time of a chunk in one launch of
 // workgroups (one a CU): 2 us with outputs, 1.5 without, 1.5 for joining two segments and 12 for the two
-// launches more.  The host knows no lengths: sequences are taken as equally long.  24,576 tokens of one head
+// launches more.  The host knows no lengths: sequences are taken as equally long, of one token at least.  24,576 tokens of one head
 // of 128 by 128 take 159 us in segments and 717 whole, 8,192 tokens of 2 heads 130 and 248, of 8
 // heads 192 and 252, 2,048 tokens of 4 heads of 64 by 64 47 and 61.
 static int segment_tokens(int64_t T, int64_t S, int64_t heads, int64_t K, int64_t V) {
   const int64_t columns = heads * V / 16, maps = heads * (V + K) / 16;
   auto rounds = [](int64_t workgroups) { return (double)((workgroups + 255) / 256); };
-  double best = 0.8 * 2.0 * rounds(S * columns) * (double)((T / S + kChunk - 1) / kChunk);
+  const int64_t length = T > S ? (T + S - 1) / S : 1;
+  double best = 0.8 * 2.0 * rounds(S * columns) * (double)((length + kChunk - 1) / kChunk);
   int Q = 0;
   for (int64_t chunks = 4; chunks <= 512; chunks *= 2) {
     if (chunk_slots(T, S, (int)chunks * kChunk) * maps > kMaxSegmentTiles) continue;
-    const int64_t each = (T / S + chunks * kChunk - 1) / (chunks * kChunk), segments = S * each;
+    const int64_t each = (length + chunks * kChunk - 1) / (chunks * kChunk), segments = S * each;
+    if (each < 2) break;                         // nothing is cut
     const double time = (double)chunks * (1.5 * rounds((segments - S) * maps) + 2.0 * rounds(segments * columns)) + 1.5 * (double)each + 12.0;
     if (time < best) {
       best = time;
@@ -146,15 +148,17 @@ static int segment_tokens(int64_t T, int64_t S, int64_t heads, int64_t K, int64_
 static size_t map_bytes(int64_t T, int64_t S, int64_t heads) { return (size_t)(chunk_slots(T, S, kChunk) * heads) * sizeof(ChunkMap); }
 static size_t segment_bytes(int64_t K) { return (size_t)(kMaxSegmentTiles * 16 * K) * sizeof(float) + 256; }
 
+// Eight waves to 16 columns while there are fewer than four workgroups of them a CU, else a wave each: at 512
+// units 324 us against 486 (8,192 tokens of 2 prompts, 32 heads of 128 by 128), at 768 189 against 255 (12,000 tokens
+// of 6, 16 heads of 64 by 128), at 1,024 319 against 325 (8,192 of 4) and 48 against 36 (4,096 of 32, 8 heads of
+// 64 by 64), at 2,048 339 against 234 (8,192 of 8).
+static bool few_columns(int64_t S, int64_t heads, int64_t V) { return S * heads * (V / 16) < 1024; }
+
 template <typename T, int K, bool WIDE> int launch_chunks_of(const cortex_delta_t &a, int32_t *status, ChunkMap *maps, void *stream) {
   const hipStream_t st = (hipStream_t)stream;
   const int64_t chunks = chunk_slots(a.num_tokens, a.num_seqs, kChunk) * a.heads;
   const int64_t units = (int64_t)a.num_seqs * a.heads * (a.value_dim / 16);
-  // Eight waves to 16 columns while there are fewer than four workgroups of them a CU, else a wave each: at 512
-  // units 324 us against 486 (8,192 tokens of 2 prompts, 32 heads of 128 by 128), at 768 189 against 255 (12,000 tokens
-  // of 6, 16 heads of 64 by 128), at 1,024 319 against 325 (8,192 of 4) and 48 against 36 (4,096 of 32, 8 heads of
-  // 64 by 64), at 2,048 339 against 234 (8,192 of 8).
-  const bool few = units < 1024;
+  const bool few = few_columns(a.num_seqs, a.heads, a.value_dim);
   if (few) chunk_maps_kernel<T, K, false, WIDE><<<blocks_of_units(chunks), kChunkThreads, 0, st>>>(a, status, maps, chunks);
   else chunk_maps_kernel<T, K, true, WIDE><<<blocks_of_units(chunks), kChunkThreads, 0, st>>>(a, status, maps, chunks);
   if (!launched()) return CORTEX_E_HIP;
@@ -236,6 +240,11 @@ extern "C" size_t cortex_delta_workspace_bytes(int32_t num_tokens, int32_t num_s
                                                int32_t value_dim) {
   if (num_tokens < 0 || num_seqs < 0 || bad_delta_size(heads, 1, key_dim, value_dim)) return 0;
   return map_bytes(num_tokens, num_seqs, heads) + segment_bytes(key_dim);
+}
+
+extern "C" int32_t cortex_delta_segment_tokens(int32_t num_tokens, int32_t num_seqs, int32_t heads, int32_t key_dim, int32_t value_dim) {
+  if (num_tokens < 0 || num_seqs < 1 || bad_delta_size(heads, 1, key_dim, value_dim)) return 0;
+  return few_columns(num_seqs, heads, value_dim) ? segment_tokens(num_tokens, num_seqs, heads, key_dim, value_dim) : 0;
 }
 
 extern "C" int cortex_delta_forward(const cortex_delta_t *args, int32_t *d_status, void *d_ws, size_t ws_bytes, void *stream) {

@@ -207,3 +207,22 @@ def test_binding_refuses_linear():
                      (dict(q=Z(3, 41, dtype=I8)), "q must be")):
         with pytest.raises(ValueError, match=what):
             C.cortex_quant_i8(**{**dict(x=Z(3, 40), q=Z(3, 40, dtype=I8), scale=Z(3), status=STATUS), **kw})
+
+
+@pytest.mark.parametrize("T,S,H,K,V", [(0, 1, 1, 128, 128), (0, 9, 8, 128, 128), (1, 2, 1, 32, 16), (7, 8, 8, 128, 128), (30, 40, 4, 64, 64),
+                                       (3, 10, 6, 128, 128), (1, 15, 10, 64, 32), (63, 64, 1, 32, 16), (64, 64, 1, 32, 16), (1, 1, 1, 128, 128)])
+def test_delta_takes_short_prompts_whole(lib, T, S, H, K, V):
+    """Two launches, also where sequences have less than a token each."""
+    assert lib.cortex_delta_segment_tokens(T, S, H, K, V) == 0
+
+
+@pytest.mark.parametrize("T,S,H,K,V", [(24576, 1, 1, 128, 128), (8192, 1, 2, 128, 128), (8192, 1, 8, 128, 128), (2048, 1, 4, 64, 64)])
+def test_delta_cuts_long_prompts_of_few_columns(lib, T, S, H, K, V):
+    Q = lib.cortex_delta_segment_tokens(T, S, H, K, V)
+    assert 0 < Q < T and Q % 64 == 0
+
+
+@pytest.mark.parametrize("size", [(-1, 1, 4, 64, 32), (9999, 0, 4, 64, 32), (9999, 1, 0, 64, 32), (9999, 1, 4, 100, 32), (9999, 1, 4, 64, 20),
+                                  (1 << 20, 128, 64, 64, 64)])
+def test_delta_cuts_nothing_of_sizes_that_it_refuses_or_of_many_columns(lib, size):
+    assert lib.cortex_delta_segment_tokens(*size) == 0

@@ -340,3 +340,16 @@ def test_two_streams_at_once(many):
     torch.cuda.synchronize()
     for p, end, (y, out) in zip(ps, ends, alone):
         assert torch.equal(p.d["y"], y) and torch.equal(end, out) and int(p.d["status"].item()) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,K,V,lens", [(8, 4, 128, 128, [1, 0, 1, 2, 0, 1, 1, 1]), (4, 4, 64, 64, [0, 1, 1, 0, 2, 0, 1, 1] * 5),
+                                          (6, 2, 32, 32, [0, 0, 0, 3, 0]), (2, 1, 128, 16, [0, 0])])
+def test_fewer_tokens_than_prompts(H, G, K, V, lens, dtype):
+    need_gpu()
+    say("delta fewer tokens than prompts", H, G, K, V, lens, dtype)
+    S = len(lens)
+    assert C.cortex_delta_segment_tokens(sum(lens), S, H, K, V) == 0
+    p = Delta(17, lens, H, G, K, V, dtype, index=[S - 1 - i for i in range(S)])
+    y, out = run(p)
+    p.check(y, out, "fewer tokens than prompts")
