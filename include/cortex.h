@@ -497,11 +497,14 @@ int cortex_logits_process(const cortex_logits_t *args, int32_t *d_status, void *
  * dt_bias are then not read).  Keys of norm at most 1 (cortex_qk_norm) and beta in
  * [0, 1] keep states bounded; larger ones, and steps dt A > 0, may let them grow past
  * the float range, where the prompt form may give infinities or NaN earlier than the
- * token form.  After an infinite or NaN key, update share or step size a head's
- * outputs and state are no longer finite, after an infinite or NaN value or state entry
- * those of its row of the state; which of infinity and NaN they are is not said.  No
- * earlier token is touched, in either form.  Other sizes return CORTEX_E_INVAL, and
- * so do states that do not start at a 16-byte boundary.
+ * token form.  After a key, a beta or an exponent dt A that is NaN or infinite a head's
+ * outputs and state are no longer finite, but an exponent of minus infinity is a decay of 0,
+ * which forgets a finite state: so with the functions that are asked for a b of plus or minus
+ * infinity is a beta of 1 or 0, a dt_raw of minus infinity a decay of 1 and one of plus infinity,
+ * with A below 0, a decay of 0.  After an infinite or NaN value or state entry its row of the
+ * state and that row's outputs are no longer finite, whatever the decay.  Which of infinity and NaN
+ * they are is not said.  No earlier token is touched, in either form.  Other sizes return
+ * CORTEX_E_INVAL, and so do states that do not start at a 16-byte boundary.
  */
 typedef struct {
   int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: q, k, v, b, dt, y */

@@ -353,3 +353,56 @@ def test_fewer_tokens_than_prompts(H, G, K, V, lens, dtype):
     p = Delta(17, lens, H, G, K, V, dtype, index=[S - 1 - i for i in range(S)])
     y, out = run(p)
     p.check(y, out, "fewer tokens than prompts")
+
+
+def gates_at(p, name, value, places):
+    """b or dt of every sequence's tokens at `places` (where it has them), another head each."""
+    for s in range(p.S):
+        for n, t in enumerate(places):
+            if t < p.lens[s]:
+                getattr(p, name)[p.offsets[s] + t, (s + n) % p.H] = value
+
+
+FORMS = {"few": ([200, 64, 1, 65], 4, 2, 64, 32), "many": ([130, 0, 3, 64] * 17, 4, 2, 32, 64), "segments": ([1700, 1900], 3, 3, 64, 64),
+         "tokens": ([1] * 9, 4, 2, 64, 32)}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("form", sorted(FORMS))
+@pytest.mark.parametrize("name,value", [("b", np.inf), ("b", -np.inf), ("dt", np.inf), ("dt", -np.inf)])
+def test_infinite_gates_are_none_or_whole(name, value, form, dtype):
+    """A share of 0 or 1, a decay of 0 or 1: both forms give what the definition does."""
+    need_gpu()
+    say("delta infinite gates", name, value, form, dtype)
+    lens, H, G, K, V = FORMS[form]
+    assert (C.cortex_delta_segment_tokens(sum(lens), len(lens), H, K, V) > 0) == (form == "segments")
+    p = Delta(18, lens, H, G, K, V, dtype, slow=0.2)
+    gates_at(p, name, value, [0, 2, 17, 62, 63, 64, 128, 199, 700])
+    y, out = run(p, form == "tokens")
+    p.check(y, out, "infinite gates")
+
+
+@pytest.mark.parametrize("form", sorted(FORMS))
+@pytest.mark.parametrize("name,value,kw,A", [("b", np.inf, dict(sig=False), None), ("b", np.nan, dict(), None), ("dt", np.nan, dict(), None),
+                                             ("dt", -np.inf, dict(soft=False), None), ("dt", np.inf, dict(), 0.0), ("dt", np.inf, dict(), 0.5)])
+def test_gates_that_lose_a_head(name, value, kw, A, form):
+    """A share or an exponent that is no finite number after the functions asked for."""
+    need_gpu()
+    say("delta gates that lose a head", name, value, kw, A, form)
+    lens, H, G, K, V = FORMS[form]
+    p = Delta(19, lens, H, G, K, V, "f32", slow=0.2, **kw)
+    if A is not None:
+        p.dt[:] = -8.0                           # a step of 3e-4, so that a growing state stays small
+        p.dt_bias[:] = 0.0
+        p.A[H - 1] = A
+    clean, end = (host(v) for v in run(p, form == "tokens"))
+    hit, hit_end = np.zeros(clean.shape, dtype=bool), np.zeros((p.S, H, V * K), dtype=bool)
+    for s in range(0, p.S, 2):
+        if lens[s]:
+            t = p.offsets[s] + min(lens[s] - 1, 77)
+            getattr(p, name)[t, H - 1] = value
+            hit[t:p.offsets[s + 1], H - 1] = hit_end[s, H - 1] = True
+    hit_end = hit_end.reshape(end.shape)
+    got, got_end = (host(v) for v in run(p, form == "tokens"))
+    assert np.array_equal(got[~hit], clean[~hit]) and np.array_equal(got_end[~hit_end], end[~hit_end])
+    assert not np.isfinite(got[hit]).any() and not np.isfinite(got_end[hit_end]).any()
