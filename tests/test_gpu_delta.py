@@ -406,3 +406,156 @@ def test_gates_that_lose_a_head(name, value, kw, A, form):
     got, got_end = (host(v) for v in run(p, form == "tokens"))
     assert np.array_equal(got[~hit], clean[~hit]) and np.array_equal(got_end[~hit_end], end[~hit_end])
     assert not np.isfinite(got[hit]).any() and not np.isfinite(got_end[hit_end]).any()
+
+
+# Shapes that are cut into segments: of one and several heads, key groups, sequences, empty and short ones among them.
+SEGMENTS = [(1, 1, 128, 128, [2100]), (3, 3, 64, 64, [1700, 1900]), (2, 2, 64, 32, [2900, 90]), (2, 1, 128, 48, [2600, 0, 2800]),
+            (1, 1, 32, 256, [4200, 1]), (2, 1, 32, 16, [0, 6500, 64]), (1, 1, 64, 112, [256, 4000, 257])]
+
+
+def in_segments(p):
+    """The tokens of a segment of p's batch; some sequence has several."""
+    Q = C.cortex_delta_segment_tokens(p.T, p.S, p.H, p.K, p.V)
+    assert Q > 0 and max(p.lens) > Q, (Q, p.lens)
+    return Q
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,K,V,lens", SEGMENTS)
+def test_segments(H, G, K, V, lens, dtype):
+    """States from the segments before, in the pool's rows, in place and not, without a row and without states."""
+    need_gpu()
+    say("delta segments", H, G, K, V, lens, dtype)
+    S = len(lens)
+    for n, in_place in enumerate((False, True)):
+        index = [S + 1 - i for i in range(S)]
+        if S > 1:
+            index[n] = -1
+        p = Delta(20, lens, H, G, K, V, dtype, index=index, rows=S + 2, slow=0.02)
+        in_segments(p)
+        y, out = run(p, in_place=in_place)
+        new = p.check(y, out, "segments")
+        got = host(out)
+        for row in set(range(S + 2)) - set(new):
+            assert np.array_equal(got[row], p.state[row] if in_place else np.full_like(got[row], 7.0))
+    p = Delta(21, lens, H, G, K, V, dtype, state=False, decay=False, lean=2.0)
+    y, _ = run(p, with_state=False)
+    p.check(y, None, "segments without states")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("left", [1, 2, 4, 8, 16])
+def test_segments_at_every_alignment(left, dtype):
+    need_gpu()
+    say("delta segments, alignments", left, dtype)
+    for H, G, K, V, lens in ((2, 1, 64, 32, [2301, 3, 3030]), (1, 1, 128, 16, [2100])):
+        p = Delta(22, lens, H, G, K, V, dtype, left=left, slow=0.05)
+        in_segments(p)
+        y, out = run(p)
+        p.check(y, out, "segments, alignments")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("where", ["v", "k", "q", "state"])
+def test_what_is_not_finite_in_segments(where, bad, dtype):
+    """It passes from a segment to all that follow, of its row of the state or its head, and to nothing else."""
+    need_gpu()
+    say("delta segments, not finite", where, bad, dtype)
+    H, G, K, V, lens = 4, 2, 64, 32, [2500, 0, 2900]
+    p = Delta(23, lens, H, G, K, V, dtype, slow=0.05)
+    Q = in_segments(p)
+    clean, end = (host(v) for v in run(p))
+    hit, hit_end = np.zeros(clean.shape, dtype=bool), np.zeros((3, H, V, K), dtype=bool)
+    for s, t in ((0, Q + 77), (2, 3)):           # in a second segment and in a first one
+        t, last, head, row = p.offsets[s] + t, p.offsets[s + 1], 2 + s // 2, 5 + s
+        if where == "v":
+            p.v[t, head, row] = bad
+            hit[t:last, head, row] = hit_end[s, head, row] = True
+        elif where == "k":
+            p.k[t, 1, 9] = bad
+            hit[t:last, 2:] = hit_end[s, 2:] = True
+        elif where == "q":
+            p.q[t, 1, 9] = bad
+            hit[t, 2:] = True
+        else:
+            p.state[s, head * V + row, 3] = bad
+            hit[p.offsets[s]:last, head, row] = hit_end[s, head, row] = True
+    got, got_end = (host(v) for v in run(p))
+    hit_end = hit_end.reshape(end.shape)
+    assert np.array_equal(got[~hit], clean[~hit]) and np.array_equal(got_end[~hit_end], end[~hit_end])
+    assert not np.isfinite(got[hit]).any() and not np.isfinite(got_end[hit_end].reshape(-1, K)).all(1).any()
+
+
+def test_segments_of_broken_batches():
+    need_gpu()
+    say("delta segments, broken batches")
+    for index, offsets, want in (([0, 3, 1], None, C.CORTEX_ST_INPUT_RANGE), ([0, -2, 1], None, C.CORTEX_ST_INPUT_RANGE),
+                                 (None, [0, 2600, 2500, 5400], C.CORTEX_ST_SEQ_OFFSETS), (None, [1, 2500, 2700, 5400], C.CORTEX_ST_SEQ_OFFSETS),
+                                 (None, [0, 2500, 2700, 5399], C.CORTEX_ST_SEQ_OFFSETS), (None, [0, -2500, 2700, 5400], C.CORTEX_ST_SEQ_OFFSETS),
+                                 (None, [0, 2500, 2700, 2 ** 31 - 1], C.CORTEX_ST_SEQ_OFFSETS)):
+        p = Delta(24, [2500, 200, 2700], 2, 1, 32, 16, index=index)
+        in_segments(p)
+        if offsets is not None:
+            p.offsets = np.array(offsets)
+        d = p.upload()
+        out = torch.full_like(d["state"], 7.0)
+        C.check(p.call(state_out=out))
+        torch.cuda.synchronize()
+        assert int(d["status"].item()) == want
+        d["y"].fill_(5.0)
+        out.fill_(7.0)
+        C.check(p.call(state_out=out))
+        torch.cuda.synchronize()
+        assert (host(d["y"]) == 5.0).all() and (host(out) == 7.0).all()
+
+
+def test_segments_on_two_streams_and_in_a_graph():
+    """The same bits from two batches at once, each with its own workspace, and from every replay."""
+    need_gpu()
+    say("delta segments, streams and graph")
+    ps = [Delta(25 + i, [1700, 1900], 3, 3, 64, 64, slow=0.05) for i in range(2)]
+    for p in ps:
+        in_segments(p)
+    alone = [tuple(t.clone() for t in run(p)) for p in ps]
+    ends = [torch.empty_like(out) for _, out in alone]
+    streams = [torch.cuda.Stream() for _ in ps]
+    for p in ps:
+        p.d["y"].zero_()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for p, end, stream in zip(ps, ends, streams):
+            C.check(p.call(state_out=end, stream=stream))
+    torch.cuda.synchronize()
+    for p, end, (y, out) in zip(ps, ends, alone):
+        assert torch.equal(p.d["y"], y) and torch.equal(end, out)
+    p, end, (y, out) = ps[0], ends[0], alone[0]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        C.check(p.call(state_out=end))
+    for _ in range(3):
+        p.d["y"].zero_()
+        end.zero_()
+        p.d["ws"].fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(p.d["y"], y) and torch.equal(end, out)
+    assert all(int(p.d["status"].item()) == 0 for p in ps)
+
+
+def test_a_prompt_in_segments_then_tokens_is_one_prompt():
+    need_gpu()
+    say("delta segments then tokens")
+    whole = Delta(27, [2120], 1, 1, 128, 64, "f32", slow=0.05)
+    d = whole.upload()
+    assert C.cortex_delta_segment_tokens(2100, 1, 1, 128, 64) > 0
+    state, y, kw = d["state"].clone(), d["y"], dict(A=d["A"], dt_bias=d["dt_bias"], scale=whole.scale, status=d["status"])
+    kw.update(state_in=state, state_out=state)
+    part = lambda name, i, j: d[name][i:j]
+    C.check(C.cortex_delta_forward(*(part(n, 0, 2100) for n in ("q", "k", "v", "b")), dev([0, 2100], torch.int32), y[:2100],
+                                   dt=part("dt", 0, 2100), ws=d["ws"], **kw))
+    for t in range(2100, 2120):
+        C.check(C.cortex_delta_step(*(part(n, t, t + 1) for n in ("q", "k", "v", "b")), y[t:t + 1], dt=part("dt", t, t + 1), **kw))
+    torch.cuda.synchronize()
+    assert int(d["status"].item()) == 0
+    whole.check(y, state, "segments then tokens")
