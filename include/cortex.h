@@ -493,7 +493,8 @@ int cortex_logits_process(const cortex_logits_t *args, int32_t *d_status, void *
  *   S <- S + u k^T
  *   y  = scale S q
  * K = 32, 64 or 128; V a multiple of 16 up to 256; any number of key heads that
- * divides the heads; heads V at most 262,144.  A NULL leaves the decay out (dt and
+ * divides the heads; heads V at most 262,144; sequences times heads times V / 16 less than
+ * 2^25; row strides at most 2^25 elements.  A NULL leaves the decay out (dt and
  * dt_bias are then not read).  Keys of norm at most 1 (cortex_qk_norm) and beta in
  * [0, 1] keep states bounded; larger ones, and steps dt A > 0, may let them grow past
  * the float range, where the prompt form may give infinities or NaN earlier than the
@@ -553,10 +554,13 @@ int cortex_delta_step(const cortex_delta_t *args, int32_t *d_status, void *strea
  *   x <- x * weight                                           (if given)
  *   (x[i], x[j]) <- (x[i] cos f - x[j] sin f, x[j] cos f + x[i] sin f)    f = position * freqs[i']
  * for the R / 2 pairs of the first R elements: i' = i, j = i + R / 2, or neighbours
- * (i = 2 i', j = 2 i' + 1).  Angles are formed in 64 bits.  All is float32 and
- * rounded once.  Prompts and single tokens alike: rows are tokens.  P is even, at
+ * (i = 2 i', j = 2 i' + 1).  Angles are formed and cut to half a turn in 64 bits, then
+ * rounded to float32; all else is float32, and outputs are rounded once.  So are the squares:
+ * a head whose sum of them passes the float range becomes zeros, and without eps one whose
+ * sum underflows is not finite.  Prompts and single tokens alike: rows are tokens.  P is even, at
  * most 512; R is even, at most P, 0 for no rotation (positions and freqs are then not
- * read).  Without keys key_heads is 0.  Outputs may be the inputs themselves.
+ * read).  Without keys key_heads is 0.  H and G are at most 65,536 each, T (H + G) less
+ * than 2^25.  Outputs may be the inputs themselves.
  * An infinity or NaN reaches the rest of its head through the norm, the other element
  * of its pair through the rotation, and no other element.
  */
@@ -589,8 +593,8 @@ int cortex_qk_norm(const cortex_qk_norm_t *args, int32_t *d_status, void *stream
 
 /*
  * Rows to 8 bits: scale[r] = max |x[r]| / 127, q[r, c] = x[r, c] / scale[r] rounded to
- * the nearest whole number (ties to even), each in float32; a row of zeros has a scale
- * of 0 and zeros.  A row that holds an infinity or NaN gets a NaN scale and zeros.
+ * the nearest whole number (ties to even), each in float32, and held to 127 on either side
+ * (which matters where the scale is a denormal); a row of zeros has a scale of 0 and zeros.  A row that holds an infinity or NaN gets a NaN scale and zeros.
  */
 typedef struct {
   int32_t dtype;              /* CORTEX_F32 or CORTEX_BF16: x */

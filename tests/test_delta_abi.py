@@ -226,3 +226,23 @@ def test_delta_cuts_long_prompts_of_few_columns(lib, T, S, H, K, V):
                                   (1 << 20, 128, 64, 64, 64)])
 def test_delta_cuts_nothing_of_sizes_that_it_refuses_or_of_many_columns(lib, size):
     assert lib.cortex_delta_segment_tokens(*size) == 0
+
+
+def test_delta_limits_of_the_header(lib):
+    """Sequences times heads times V / 16 and the strides, on either side: what is admitted asks for its workspace."""
+    size = dict(heads=2, key_heads=1, key_dim=32, q_ld=32, k_ld=32, b_ld=2, dt_ld=2)
+    for V, S in ((256, 1 << 20), (128, 1 << 21)):
+        for n, want in ((S - 1, C.CORTEX_E_WORKSPACE), (S, C.CORTEX_E_INVAL)):
+            a = delta_args(value_dim=V, v_ld=2 * V, y_ld=2 * V, num_seqs=n, num_tokens=n, state_rows=n, **size)
+            assert lib.cortex_delta_forward(ctypes.byref(a), P8, P8, 1 << 20, None) == want
+        assert lib.cortex_delta_step(ctypes.byref(a), P8, None) == C.CORTEX_E_INVAL
+    for name in ("q_ld", "k_ld", "v_ld", "y_ld", "b_ld", "dt_ld"):
+        for ld, want in ((1 << 25, C.CORTEX_E_WORKSPACE), ((1 << 25) + 1, C.CORTEX_E_INVAL)):
+            assert lib.cortex_delta_forward(ctypes.byref(delta_args(**{name: ld})), P8, P8, 0, None) == want
+
+
+@pytest.mark.parametrize("bad", [dict(heads=65537, q_ld=65537 * 64, q_out_ld=65537 * 64), dict(key_heads=65537, k_ld=65537 * 64, k_out_ld=65537 * 64),
+                                 dict(num_tokens=(1 << 25) // 8, key_heads=4, k_ld=256, k_out_ld=256),
+                                 dict(num_tokens=512, heads=32768, key_heads=32768, q_ld=1 << 21, k_ld=1 << 21, q_out_ld=1 << 21, k_out_ld=1 << 21)])
+def test_norm_limits_of_the_header(lib, bad):
+    assert lib.cortex_qk_norm(ctypes.byref(norm_args(**bad)), P8, None) == C.CORTEX_E_INVAL

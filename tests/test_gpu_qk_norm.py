@@ -260,3 +260,16 @@ def test_an_infinity_in_a_norm_leaves_zeros_beside_it(P, R, interleaved, norm):
         torch.cuda.synchronize()
         rest = [i for i in range(P) if i != P - 3]
         assert torch.isnan(out[:6, 0, P - 3]).all() and (out[:6, 0, rest] == 0).all() and torch.isfinite(out[6:]).all()
+
+
+@pytest.mark.parametrize("T", [5, 4200])
+def test_sums_of_squares_past_the_float_range(T):
+    need_gpu()
+    say("norm past the float range", T)
+    q, status = torch.randn(T, 1, 64, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    q[1], q[3] = 1e20, 1e-30
+    for norm in ("rms", "l2"):
+        out = torch.empty_like(q)
+        C.check(C.cortex_qk_norm(q, out, norm=NORMS[norm], eps=0.0, status=status))
+        torch.cuda.synchronize()
+        assert (out[1] == 0).all() and not torch.isfinite(out[3]).any() and torch.isfinite(out[[0, 2, 4]]).all()
