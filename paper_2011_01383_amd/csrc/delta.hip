@@ -122,8 +122,8 @@ constexpr int64_t kMaxSegmentTiles = 2048;
 // Tokens of a segment, 0 for whole sequences.  By the time of a chunk in one launch of
 // workgroups (one a CU): 2 us with outputs, 1.5 without, 1.5 for joining two segments and 12 for the two
 // launches more.  The host knows no lengths: sequences are taken as equally long, of one token at least.  24,576 tokens of one head
-// of 128 by 128 take 159 us in segments and 717 whole, 8,192 tokens of 2 heads 130 and 248, of 8
-// heads 192 and 252, 2,048 tokens of 4 heads of 64 by 64 47 and 61.
+// of 128 by 128 take 156 us in segments and 650 whole, 8,192 tokens of 2 heads 99 and 227, of 8
+// heads 197 and 238, 2,048 tokens of 4 heads of 64 by 64 38 and 58.
 static int segment_tokens(int64_t T, int64_t S, int64_t heads, int64_t K, int64_t V) {
   const int64_t columns = heads * V / 16, maps = heads * (V + K) / 16;
   auto rounds = [](int64_t workgroups) { return (double)((workgroups + 255) / 256); };
@@ -149,9 +149,9 @@ static size_t map_bytes(int64_t T, int64_t S, int64_t heads) { return (size_t)(c
 static size_t segment_bytes(int64_t K) { return (size_t)(kMaxSegmentTiles * 16 * K) * sizeof(float) + 256; }
 
 // Eight waves to 16 columns while there are fewer than four workgroups of them a CU, else a wave each: at 512
-// units 324 us against 486 (8,192 tokens of 2 prompts, 32 heads of 128 by 128), at 768 189 against 255 (12,000 tokens
-// of 6, 16 heads of 64 by 128), at 1,024 319 against 325 (8,192 of 4) and 48 against 36 (4,096 of 32, 8 heads of
-// 64 by 64), at 2,048 339 against 234 (8,192 of 8).
+// units 290 us against 462 (8,192 tokens of 2 prompts, 32 heads of 128 by 128), at 768 202 against 258 (12,000 tokens
+// of 6, 16 heads of 64 by 128), at 1,024 300 against 314 (8,192 of 4) and 46 against 35 (4,096 of 32, 8 heads of
+// 64 by 64), at 2,048 323 against 225 (8,192 of 8).
 static bool few_columns(int64_t S, int64_t heads, int64_t V) { return S * heads * (V / 16) < 1024; }
 
 template <typename T, int K, bool WIDE> int launch_chunks_of(const cortex_delta_t &a, int32_t *status, ChunkMap *maps, void *stream) {

@@ -241,8 +241,8 @@ __device__ __forceinline__ int piece_place(int row, int piece) { return piece ^ 
 // LDS, all but one of them on their way while one is multiplied.  XCDs take runs of
 // neighbouring tiles, four tiles of tokens by as many of channels as there are.
 //
-// 8,192 tokens, 4,096 inputs, 8,192 channels in tiles of 256 by 256: 255 us, 2.15e15 operations a second, the matrix units
-// busy 55% of it, no conflicts in LDS.  Sixteen waves of 64 by 64 (4 a SIMD) and four buffers; in its place eight waves 331,
+// 8,192 tokens, 4,096 inputs, 8,192 channels in tiles of 256 by 256: 258 us (252 to 262 in five runs), 2.13e15 operations a
+// second, the matrix units busy 55% of it, no conflicts in LDS.  Sixteen waves of 64 by 64 (4 a SIMD) and four buffers; in its place eight waves 331,
 // four of 128 by 128 470, three buffers 329, two of 128 bytes 317, tiles of 128 by 128 391, all with the rows' 28, of a
 // form that took 303 in all.
 template <typename T, int TN, int TT, int WN, int WT, int BUFFERS>
@@ -573,8 +573,9 @@ template <typename T> int launch_linear(const cortex_linear_i8_t &a, int32_t *st
   int8_t *rows = (int8_t *)ws;
   float *scales = (float *)(rows + align_up((size_t)(a.tokens * row), 256));
   const bool aligned = a.y_ld % 4 == 0 && ((uintptr_t)a.y & (4 * sizeof(T) - 1)) == 0;
-  // One token in one launch against two: 1,000 channels of 2,048 inputs 5.0 us and 7.6, 8,192 of 4,096 12.4 and 13.9, 32,000
-  // of 4,096 34.5 and 37.3; two tokens, 8,192 of 4,096, 14.3 and 14.3, four, 32,000 of 4,096, 49 and 39.
+  // One token in one launch against two: 300 channels of 300 inputs 3.8 us and 5.6, 1,000 of 2,048 4.1 and 6.5, 8,192 of 4,096
+  // 9.4 and 12.3, 32,000 of 4,096 30.5 and 34.2, 2,048 of 16,384 13.9 and 17.8.  More tokens were measured with an earlier form of
+  // that kernel only (one token of 8,192 channels 12.4 us): two, 8,192 of 4,096, 14.3 and 14.3, four, 32,000 of 4,096, 49 and 39.
   if (!a.x_scale && a.tokens == 1 && row <= kOwnBytes) {
     return eights<T>(a.x, a.x_ld, a.inputs) ? launch_own<T, true>(p, a.inputs, status, aligned, st)
                                             : launch_own<T, false>(p, a.inputs, status, aligned, st);
